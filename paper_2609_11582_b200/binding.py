@@ -38,6 +38,22 @@ class okq_ladder_cache(C.Structure):
                 ("v_norm", C.c_void_p), ("modality", C.c_void_p)]
 
 
+class okq_paged(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("batch", C.c_int32), ("n_kv_heads", C.c_int32), ("n_q_heads", C.c_int32),
+                ("page_tokens", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("dtype", C.c_int32),
+                ("codes", C.c_void_p), ("scales", C.c_void_p), ("raw", C.c_void_p), ("table", C.c_void_p), ("refs", C.c_void_p),
+                ("seq_len", C.c_void_p), ("status", C.c_void_p)]
+
+
+class okq_rope(C.Structure):
+    _fields_ = [("sections", C.c_int32 * 3), ("interleaved", C.c_int32), ("freq", C.c_void_p), ("positions", C.c_void_p)]
+
+
+class okq_rope_tensor(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("in_strides", C.c_int64 * 3), ("out_strides", C.c_int64 * 3),
+                ("heads", C.c_int32)]
+
+
 class OkqError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -132,6 +148,30 @@ def lib():
         L.okq_turboquant_encode.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         L.okq_turboquant_decode.restype = C.c_int
         L.okq_turboquant_decode.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+        paged, i32, ptr, rope = C.POINTER(okq_paged), C.c_int32, C.c_void_p, C.POINTER(okq_rope)
+        L.okq_paged_sizes.restype = C.c_int
+        L.okq_paged_sizes.argtypes = [paged, C.POINTER(C.c_size_t)]
+        L.okq_paged_workspace_bytes.restype = C.c_size_t
+        L.okq_paged_workspace_bytes.argtypes = [paged, i32, i32]
+        L.okq_rope_apply.restype = C.c_int
+        L.okq_rope_apply.argtypes = [rope, i32, i32, i32, C.POINTER(okq_rope_tensor), C.POINTER(okq_rope_tensor), i32, ptr]
+        L.okq_paged_append.restype = C.c_int
+        L.okq_paged_append.argtypes = [paged, i32, i32, ptr, C.POINTER(C.c_int64), ptr, C.POINTER(C.c_int64), i32, ptr, rope, ptr]
+        L.okq_paged_read.restype = C.c_int
+        L.okq_paged_read.argtypes = [paged, i32, i32, i32, i32, ptr, ptr, ptr]
+        L.okq_paged_attention.restype = C.c_int
+        L.okq_paged_attention.argtypes = [paged, i32, i32, ptr, C.POINTER(C.c_int64), i32, ptr, rope, C.c_float, ptr, C.c_size_t, ptr,
+                                          C.POINTER(C.c_int64), ptr]
+        L.okq_pages_reserve.restype = C.c_int
+        L.okq_pages_reserve.argtypes = [paged, ptr, ptr]
+        L.okq_pages_fork.restype = C.c_int
+        L.okq_pages_fork.argtypes = [paged, ptr, ptr, i32, ptr, C.c_size_t, ptr]
+        L.okq_pages_release.restype = C.c_int
+        L.okq_pages_release.argtypes = [paged, ptr, i32, ptr]
+        L.okq_pages_copy.restype = C.c_int
+        L.okq_pages_copy.argtypes = [paged, ptr, ptr, i32, ptr]
+        L.okq_pages_compact.restype = C.c_int
+        L.okq_pages_compact.argtypes = [paged, ptr, ptr, C.c_size_t, ptr]
         _lib = L
     return _lib
 
@@ -144,7 +184,10 @@ def exported_symbols():
             "okq_calib_workspace_bytes", "okq_calib_attention_weights", "okq_debug_calib_timeout", "okq_debug_calib_direct",
             "okq_calib_moments", "okq_calib_rotation",
             "okq_ladder_codebook", "okq_ladder_quantize_keys", "okq_ladder_quantize_values",
-            "okq_debug_ladder_timeout", "okq_ladder_decode_attention", "okq_turboquant_encode", "okq_turboquant_decode"]
+            "okq_debug_ladder_timeout", "okq_ladder_decode_attention", "okq_turboquant_encode", "okq_turboquant_decode",
+            "okq_paged_sizes", "okq_paged_workspace_bytes", "okq_rope_apply", "okq_paged_append", "okq_paged_read",
+            "okq_paged_attention", "okq_pages_reserve", "okq_pages_fork", "okq_pages_release", "okq_pages_copy",
+            "okq_pages_compact"]
 
 
 def _ptr(t) -> int:
@@ -450,3 +493,187 @@ def turboquant_decode(codes: torch.Tensor, norms: torch.Tensor, signs: torch.Ten
     _check(lib().okq_turboquant_decode(_ptr(codes), _ptr(norms), n, bits, _ptr(signs), _ptr(x_hat), _stream(stream)),
            "okq_turboquant_decode")
     return x_hat
+
+
+# ---------------------------------------------------------------- 8-bit paged cache and rotary positions (okq_paged.h)
+DTYPE_CODES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+_I64x3, _I64x4 = C.c_int64 * 3, C.c_int64 * 4
+
+
+def _here(*tensors):
+    """Refuses tensors that do not lie on the current device, where the call is going to run."""
+    dev = torch.cuda.current_device() if _device_index is None or not torch.cuda.is_initialized() else _device_index()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor lies on {t.device}, the call runs on cuda:{dev}")
+
+
+def paged_sizes(n_layers, batch, n_kv_heads, n_q_heads, n_pages, max_pages, page_tokens=64, dtype=torch.float16):
+    """Bytes of codes, scales, raw, table, refs, seq_len and status."""
+    shape = okq_paged(n_layers, batch, n_kv_heads, n_q_heads, page_tokens, n_pages, max_pages, DTYPE_CODES[dtype])
+    out = (C.c_size_t * 7)()
+    _check(lib().okq_paged_sizes(C.byref(shape), out), "okq_paged_sizes")
+    return list(out)
+
+
+class PagedCache:
+    """Device buffers of an 8-bit paged cache plus the C struct that describes them.  `buffers`: a dict with codes, scales, raw,
+    table, refs and seq_len of the caller's own (shapes as in okq_paged.h); without it an empty cache is made."""
+
+    def __init__(self, n_layers, batch, n_kv_heads, n_q_heads, n_pages=None, max_pages=None, page_tokens=64, dtype=torch.float16,
+                 device="cuda", buffers=None):
+        if buffers is None:
+            paged_sizes(n_layers, batch, n_kv_heads, n_q_heads, n_pages, max_pages, page_tokens, dtype)   # refuses bad shapes
+            dev = torch.device(device)
+            buffers = {"codes": torch.zeros(n_layers, n_pages, n_kv_heads, 2, page_tokens, HEAD_DIM, dtype=torch.int8, device=dev),
+                       "scales": torch.zeros(n_layers, n_pages, n_kv_heads, 2, page_tokens // WINDOW, device=dev),
+                       "raw": torch.zeros(n_layers, batch, n_kv_heads, 2, WINDOW, HEAD_DIM, dtype=dtype, device=dev),
+                       "table": torch.full((batch, max_pages), -1, dtype=torch.int32, device=dev),
+                       "refs": torch.zeros(n_pages, dtype=torch.int32, device=dev),
+                       "seq_len": torch.zeros(n_layers, batch, dtype=torch.int32, device=dev)}
+        b = buffers
+        n_pages, max_pages = b["refs"].numel(), b["table"].shape[1]
+        want = {"codes": ((n_layers, n_pages, n_kv_heads, 2, page_tokens, HEAD_DIM), torch.int8),
+                "scales": ((n_layers, n_pages, n_kv_heads, 2, page_tokens // WINDOW), torch.float32),
+                "raw": ((n_layers, batch, n_kv_heads, 2, WINDOW, HEAD_DIM), dtype), "table": ((batch, max_pages), torch.int32),
+                "refs": ((n_pages,), torch.int32), "seq_len": ((n_layers, batch), torch.int32)}
+        for name, (shape, dt) in want.items():
+            assert tuple(b[name].shape) == shape and b[name].dtype == dt and b[name].is_contiguous(), name
+        self.codes, self.scales, self.raw, self.table, self.refs, self.seq_len = (b[n] for n in want)
+        self.n_layers, self.batch, self.n_kv_heads, self.n_q_heads = n_layers, batch, n_kv_heads, n_q_heads
+        self.n_pages, self.max_pages, self.page_tokens, self.dtype, self.device = n_pages, max_pages, page_tokens, dtype, self.codes.device
+        self.status = torch.zeros(4, dtype=torch.int32, device=self.device)
+        self.c = okq_paged(n_layers, batch, n_kv_heads, n_q_heads, page_tokens, n_pages, max_pages, DTYPE_CODES[dtype],
+                           *(t.data_ptr() for t in (self.codes, self.scales, self.raw, self.table, self.refs, self.seq_len, self.status)))
+        self.ref = C.byref(self.c)   # what the calls are handed, built once
+        _check(lib().okq_paged_sizes(self.ref, (C.c_size_t * 7)()), "PagedCache")
+
+    def device_status(self) -> int:
+        return int(self.status[0].item())
+
+
+def rope_frequencies(theta: float, pairs: int, device="cuda") -> torch.Tensor:
+    """float64 [pairs]: theta^(-c / pairs), the usual choice."""
+    return (float(theta) ** (-torch.arange(pairs, dtype=torch.float64) / pairs)).to(device)
+
+
+class Rope:
+    """Rotary positions of one call: positions int32 [3, batch, n], freq float64 [pairs] (contiguous, on the device; kept alive here)."""
+
+    def __init__(self, positions, freq, sections, interleaved=False):
+        assert positions.dtype == torch.int32 and positions.dim() == 3 and positions.shape[0] == 3 and positions.is_contiguous()
+        assert freq.dtype == torch.float64 and freq.numel() == sum(sections) and freq.is_contiguous()
+        self.positions, self.freq = positions, freq
+        self.batch, self.n = positions.shape[1], positions.shape[2]
+        self.c = okq_rope((C.c_int32 * 3)(*sections), 1 if interleaved else 0, freq.data_ptr(), positions.data_ptr())
+        self.ref = C.byref(self.c)
+
+
+def _rope_ref(rope, batch, n):
+    if rope is None:
+        return None
+    assert (rope.batch, rope.n) == (batch, n), "positions are [3, batch, n] of the call's own tokens"
+    return rope.ref
+
+
+def _rope_tensor(x, out):
+    assert x.dim() == 4 and x.shape == out.shape and x.dtype == out.dtype and x.shape[3] == HEAD_DIM
+    xs, os = x.stride(), out.stride()
+    assert xs[3] == 1 and os[3] == 1
+    return C.byref(okq_rope_tensor(x.data_ptr(), out.data_ptr(), xs[:3], os[:3], x.shape[1]))
+
+
+def rope_apply(rope: Rope, q, q_out, k=None, k_out=None, inverse=False, stream=None):
+    """Rotates q and k, [batch, heads, n, 128] of fp16, bf16 or fp32 (last dim contiguous, any other strides), into q_out and k_out
+    (which may be the inputs).  inverse=True is the transpose: gradients of the outputs in, gradients of the inputs out."""
+    _here(q, q_out, k, k_out, rope.positions, rope.freq)
+    batch, _, n, _ = q.shape
+    assert (rope.batch, rope.n) == (batch, n) and (k is None or (k.dtype == q.dtype and k.shape[0] == batch and k.shape[2] == n))
+    st = (_lib or lib()).okq_rope_apply(rope.ref, DTYPE_CODES[q.dtype], batch, n, _rope_tensor(q, q_out),
+                                        None if k is None else _rope_tensor(k, k_out), 1 if inverse else 0, _stream(stream))
+    if st != OK:
+        raise OkqError(st, "okq_rope_apply")
+
+
+def _rows(cache, x, layer_count, heads):
+    """Strides of a [layer_count, batch, heads, n, 128] tensor of the cache's dtype."""
+    s = x.stride()
+    assert x.dtype == cache.dtype and x.dim() == 5 and s[4] == 1
+    assert x.shape[0] == layer_count and x.shape[1] == cache.batch and x.shape[2] == heads and x.shape[4] == HEAD_DIM
+    return _I64x4(*s[:4])
+
+
+def paged_append(cache: PagedCache, layer: int, layer_count: int, k, v, new_len=None, rope=None, stream=None):
+    """k, v: [layer_count, batch, n_kv_heads, n_new, 128]; new_len: int32 [batch], new tokens of each sequence (all n_new without it);
+    rope: a Rope of [3, batch, n_new] positions that the keys are given first."""
+    _here(cache.codes, k, v, new_len, None if rope is None else rope.positions)
+    assert k.shape == v.shape and (new_len is None or (new_len.dtype == torch.int32 and new_len.is_contiguous()))
+    st = (_lib or lib()).okq_paged_append(cache.ref, layer, layer_count, k.data_ptr(), _rows(cache, k, layer_count, cache.n_kv_heads), v.data_ptr(),
+                                          _rows(cache, v, layer_count, cache.n_kv_heads), k.shape[3], _ptr(new_len),
+                                          _rope_ref(rope, cache.batch, k.shape[3]), _stream(stream))
+    if st != OK:
+        raise OkqError(st, "okq_paged_append")
+
+
+def paged_read(cache: PagedCache, layer: int, layer_count: int, begin: int, k_out, v_out, stream=None):
+    """Values of tokens [begin, begin + n) of every sequence into k_out, v_out: [layer_count, batch, n_kv_heads, n, 128], contiguous."""
+    _here(cache.codes, k_out, v_out)
+    assert k_out.shape == v_out.shape and k_out.is_contiguous() and v_out.is_contiguous() and k_out.dtype == v_out.dtype == cache.dtype
+    assert k_out.shape[:3] == (layer_count, cache.batch, cache.n_kv_heads) and k_out.shape[4] == HEAD_DIM
+    _check((_lib or lib()).okq_paged_read(cache.ref, layer, layer_count, begin, k_out.shape[3], k_out.data_ptr(), v_out.data_ptr(),
+                                          _stream(stream)), "okq_paged_read")
+
+
+def paged_workspace_bytes(cache: PagedCache, layer_count: int, n_new: int = 1) -> int:
+    return lib().okq_paged_workspace_bytes(cache.ref, layer_count, n_new)
+
+
+def paged_attention(cache: PagedCache, layer: int, layer_count: int, q, workspace, out, q_len=None, rope=None, sm_scale=None, stream=None):
+    """q, out: [layer_count, batch, n_q_heads, n_new, 128] of the cache's dtype (last dim contiguous); the queries are those of each
+    sequence's newest n_new (q_len[b] with q_len, int32 [batch]) tokens; rope: a Rope that the queries are given first."""
+    _here(cache.codes, q, workspace, out, q_len, None if rope is None else rope.positions)
+    assert q.shape == out.shape and (q_len is None or (q_len.dtype == torch.int32 and q_len.is_contiguous()))
+    st = (_lib or lib()).okq_paged_attention(cache.ref, layer, layer_count, q.data_ptr(), _rows(cache, q, layer_count, cache.n_q_heads), q.shape[3],
+                                             _ptr(q_len), _rope_ref(rope, cache.batch, q.shape[3]),
+                                             HEAD_DIM ** -0.5 if sm_scale is None else sm_scale, _ptr(workspace),
+                                             0 if workspace is None else workspace.nbytes, out.data_ptr(),
+                                             _rows(cache, out, layer_count, cache.n_q_heads), _stream(stream))
+    if st != OK:
+        raise OkqError(st, "okq_paged_attention")
+
+
+def _indices(x, n=None):
+    assert x.dtype == torch.int32 and x.is_contiguous() and (n is None or x.numel() == n)
+    return x.data_ptr()
+
+
+def pages_reserve(cache: PagedCache, tokens, stream=None):
+    """tokens: int32 [batch]; gives every sequence pages for at least so many tokens."""
+    _here(cache.codes, tokens)
+    _check(lib().okq_pages_reserve(cache.ref, _indices(tokens, cache.batch), _stream(stream)), "okq_pages_reserve")
+
+
+def pages_fork(cache: PagedCache, src, dst, workspace, stream=None):
+    """src, dst: int32 [count]; sequence dst[i], empty, becomes a copy of sequence src[i] that shares its full pages."""
+    _here(cache.codes, src, dst, workspace)
+    _check(lib().okq_pages_fork(cache.ref, _indices(src), _indices(dst, src.numel()), src.numel(), _ptr(workspace),
+                                0 if workspace is None else workspace.nbytes, _stream(stream)), "okq_pages_fork")
+
+
+def pages_release(cache: PagedCache, seqs, stream=None):
+    """seqs: int32 [count]; the sequences become empty, pages that no other shares become free."""
+    _here(cache.codes, seqs)
+    _check(lib().okq_pages_release(cache.ref, _indices(seqs), seqs.numel(), _stream(stream)), "okq_pages_release")
+
+
+def pages_copy(cache: PagedCache, src, dst, stream=None):
+    """src, dst: int32 [count] pages; codes and scales of src[i] go to dst[i]."""
+    _here(cache.codes, src, dst)
+    _check(lib().okq_pages_copy(cache.ref, _indices(src), _indices(dst, src.numel()), src.numel(), _stream(stream)), "okq_pages_copy")
+
+
+def pages_compact(cache: PagedCache, workspace, n_live=None, stream=None):
+    """Moves the pages in use to the front of the pool; n_live: int32 [1], receives their number."""
+    _here(cache.codes, workspace, n_live)
+    _check(lib().okq_pages_compact(cache.ref, 0 if n_live is None else _indices(n_live, 1), _ptr(workspace),
+                                   0 if workspace is None else workspace.nbytes, _stream(stream)), "okq_pages_compact")

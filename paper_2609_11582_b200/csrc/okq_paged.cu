@@ -1,0 +1,321 @@
+// The 8-bit paged cache: argument checks, append (quantising whole blocks of 32 tokens and one head), read-back.
+//
+// Append.  A block of keys or values is 32 x 128 numbers with one scale, so its codes are known when all of its tokens are: one
+// thread block per (32-token block, head, sequence) reads the tokens that are there (those of an unfinished block from the raw copies, the
+// new ones from the caller's tensor), takes the maximum and writes codes, scale and, for the block that stays unfinished, the raw
+// copies.  Requantising the unfinished block with every append costs at most 16 KB of reads per head and makes the cache
+// independent of how its tokens were dealt over calls; keeping the codes and only lowering their scale would round twice.
+#include "okq_paged.cuh"
+
+namespace okq {
+
+namespace {
+
+constexpr int NT = 256;
+
+// rows of one call's keys or values
+struct Rows {
+  const void* p;
+  int64_t s[4];
+  template <class T> __device__ const T* at(int l, int b, int h, int i) const {
+    return static_cast<const T*>(p) + l * s[0] + b * s[1] + h * s[2] + i * s[3];
+  }
+};
+
+// whether the sequence can take `m` tokens behind `len`: room in its row and a page for each (all threads of the block call it)
+__device__ __forceinline__ int pages_missing(const PagedView& c, int b, int len, int m, int tid, int nt) {
+  if (m == 0) return 0;
+  if (m > c.room() - len) return 1;
+  int bad = 0;
+  const int j0 = len >> c.page_shift, j1 = (len + m - 1) >> c.page_shift;
+  for (int j = j0 + tid; j <= j1; j += nt) bad |= c.page_of(b, j << c.page_shift) < 0;
+  return bad;
+}
+
+// rint(x / scale) of numbers no larger than 127.5 scale, the quotient rounded to fp32.  With the reciprocal r of the scale correctly
+// rounded, one residual step from x r gives the correctly rounded quotient (Markstein's theorem; the residual is exact), three
+// multiply-adds for a division; scales so small that the residual would be cut off are divided by.  1.5 * 2^23 + q rounds q to an
+// integer, whose low byte is the code.
+struct Quotient {
+  float scale, r;
+  int how;   // 0: codes 0 (a scale of zero or NaN), 1: residual step, 2: division
+  __device__ __forceinline__ uint32_t code(float x) const {
+    float q = 0.f;
+    if (how == 1) {
+      q = __fmul_rn(x, r);
+      q = __fmaf_rn(__fmaf_rn(-q, scale, x), r, q);
+    } else if (how == 2) {
+      q = fminf(fmaxf(__fdiv_rn(x, scale), -127.f), 127.f);   // (a subnormal scale may be too small by half of itself)
+    }
+    return __float_as_uint(__fadd_rn(q, 12582912.f));
+  }
+};
+
+__device__ __forceinline__ Quotient quotient_by(float scale) {
+  return Quotient{scale, __fdiv_rn(1.f, scale), !(scale > 0.f) ? 0 : scale >= 7.9e-31f ? 1 : 2};
+}
+
+template <class T>
+__global__ void __launch_bounds__(NT) k_paged_append(const PagedView c, int layer, const Rows k, const Rows v, int n_new, const int32_t* new_len,
+                                                     const RopeView rope, int n_blocks) {
+  depend_wait();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  long long u = blockIdx.x;
+  int blk = (int)(u % n_blocks);
+  u /= n_blocks;
+  const int h = (int)(u % c.n_kv);
+  u /= c.n_kv;
+  const int b = (int)(u % c.batch), li = (int)(u / c.batch), l = layer + li;
+  const int m = count_of(new_len, b, n_new), len = c.held(l, b), r = len % PB, end = len + m;
+  if (m == 0 || len - r + blk * PB >= end) return;
+  if (__syncthreads_or(pages_missing(c, b, len, m, tid, NT))) return;
+  // The raw tokens are read by the first block and replaced by the last, so one thread block does both, in that order.
+  const int last = (r + m - 1) / PB;
+  const bool follows = r > 0 && last > 0 && (r + m) % PB != 0;
+  if (follows && blk == last) return;
+
+  // thread: row t = tid / 8, two chunks of eight channels, keys and values (the chunks that a rotated pair of channels lies in, as
+  // okq_rope_apply deals them)
+  const int t = tid >> 3, j = tid & 7, nc = rope.half >> 3;
+  const bool turns = rope.freq && j < nc;
+  const int c0 = !rope.freq || j < nc ? 8 * j : 2 * rope.half + 16 * (j - nc);
+  const int c1 = !rope.freq ? c0 + 64 : j < nc ? c0 + rope.half : c0 + 8;
+  __shared__ unsigned top[2][NT / 32];
+  for (;; blk = last) {
+    const int first = len - r + blk * PB, rows = min(PB, end - first);
+    const int i = first + t - len;    // number among the new tokens, negative for raw ones
+    const bool there = t < rows;
+    Vec8<T> x[2][2];
+#pragma unroll
+    for (int side = 0; side < 2; side++) {
+      if (there) {
+        const T* src = i < 0 ? c.raw_of<T>(l, b, h, side) + (size_t)t * D : (side ? v : k).at<T>(li, b, h, i);
+        x[side][0] = *reinterpret_cast<const Vec8<T>*>(src + c0);
+        x[side][1] = *reinterpret_cast<const Vec8<T>*>(src + c1);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) x[side][0].v[e] = x[side][1].v[e] = from_f<T>(0.f);
+      }
+    }
+    if (turns && there && i >= 0) {
+      float cs[8], sn[8];
+      turns8(rope, rope.positions + (size_t)b * n_new + i, (size_t)c.batch * n_new, c0, cs, sn);
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        float a = to_f(x[0][0].v[e]), d = to_f(x[0][1].v[e]);
+        rotate_pair(a, d, cs[e], sn[e]);
+        x[0][0].v[e] = from_f<T>(a);
+        x[0][1].v[e] = from_f<T>(d);
+      }
+    }
+    // magnitudes as integers: their order is the numbers' own, with infinities and NaN at the top
+#pragma unroll
+    for (int side = 0; side < 2; side++) {
+      unsigned mx = 0;
+#pragma unroll
+      for (int e = 0; e < 16; e++) mx = max(mx, __float_as_uint(to_f(x[side][e >> 3].v[e & 7])) & 0x7fffffffu);
+      mx = __reduce_max_sync(0xffffffffu, mx);
+      if (lane == 0) top[side][warp] = mx;
+    }
+    __syncthreads();
+    const int page = c.page_of(b, first);
+#pragma unroll
+    for (int side = 0; side < 2; side++) {
+      unsigned mx = 0;
+#pragma unroll
+      for (int w = 0; w < NT / 32; w++) mx = max(mx, top[side][w]);
+      const float amax = __uint_as_float(mx);
+      float scale = __fdiv_rn(amax, 127.f);
+      if (mx >= 0x7f800000u) scale = __uint_as_float(0x7fc00000u);   // infinities, NaN
+      const Quotient by = quotient_by(scale);
+      const size_t row = c.code_row(l, page, h, side) + (first & (c.page - 1));
+      if (there) {
+        int8_t* dst = c.codes + (row + t) * D;
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+          uint32_t q[8];
+#pragma unroll
+          for (int e = 0; e < 8; e++) q[e] = by.code(to_f(x[side][half].v[e]));
+          uint2 w;
+          w.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+          w.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+          *reinterpret_cast<uint2*>(dst + (half ? c1 : c0)) = w;
+        }
+        if (rows < PB && i >= 0) {   // a block that stays unfinished
+          T* keep = c.raw_of<T>(l, b, h, side) + (size_t)t * D;
+          *reinterpret_cast<Vec8<T>*>(keep + c0) = x[side][0];
+          *reinterpret_cast<Vec8<T>*>(keep + c1) = x[side][1];
+        }
+      }
+      if (tid == side) c.scales[row / PB] = scale;
+    }
+    if (!follows || blk != 0) return;
+    __syncthreads();
+  }
+}
+
+// lengths after an append, and the status of sequences that could not take theirs; one warp per (layer, sequence)
+__global__ void __launch_bounds__(NT) k_paged_advance(const PagedView c, int layer, int layer_count, int n_new, const int32_t* new_len) {
+  depend_wait();
+  const int u = blockIdx.x * (NT / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (u >= layer_count * c.batch) return;
+  const int b = u % c.batch, l = layer + u / c.batch;
+  const int m = count_of(new_len, b, n_new), len = c.held(l, b);
+  const int bad = __any_sync(0xffffffffu, pages_missing(c, b, len, m, lane, 32));
+  if (lane) return;
+  if (bad) set_status(c.status, OKQ_ERR_CAPACITY);
+  else if (m) c.seq_len[(size_t)l * c.batch + b] = len + m;
+}
+
+template <class T>
+__global__ void __launch_bounds__(NT) k_paged_read(const PagedView c, int layer, int begin, int n, T* k_out, T* v_out, long long items) {
+  depend_wait();
+  const long long id = (long long)blockIdx.x * NT + threadIdx.x;
+  if (id >= items) return;
+  const int j = (int)(id & 7);                        // sixteen channels
+  long long u = id >> 3;
+  const int i = (int)(u % n);
+  u /= n;
+  const int h = (int)(u % c.n_kv);
+  u /= c.n_kv;
+  const int b = (int)(u % c.batch), li = (int)(u / c.batch), l = layer + li;
+  const int t = begin + i;
+  if (t >= c.held(l, b)) return;
+  const int page = c.page_of(b, t);
+  if (page < 0) { set_status(c.status, OKQ_ERR_INVALID_ARG); return; }
+#pragma unroll
+  for (int side = 0; side < 2; side++) {
+    const size_t row = c.code_row(l, page, h, side) + (t & (c.page - 1));
+    const float scale = c.scales[row / PB];
+    const int4 w = *reinterpret_cast<const int4*>(c.codes + row * D + 16 * j);
+    const int8_t* q = reinterpret_cast<const int8_t*>(&w);
+    T* out = (side ? v_out : k_out) + (size_t)(id >> 3) * D + 16 * j;
+#pragma unroll
+    for (int half = 0; half < 2; half++) {
+      Vec8<T> y;
+#pragma unroll
+      for (int e = 0; e < 8; e++) y.v[e] = from_f<T>((float)q[8 * half + e] * scale);
+      *reinterpret_cast<Vec8<T>*>(out + 8 * half) = y;
+    }
+  }
+}
+
+okq_status failed(cudaError_t e) {
+  set_last_cuda_error((int)e);
+  (void)cudaGetLastError();
+  return OKQ_ERR_CUDA;
+}
+
+template <class T>
+okq_status launch_append(const PagedView& c, int layer, int layer_count, const Rows& k, const Rows& v, int n_new, const int32_t* new_len,
+                         const RopeView& rope, cudaStream_t s) {
+  const int n_blocks = (PB - 1 + n_new + PB - 1) / PB;
+  const long long grid = (long long)layer_count * c.batch * c.n_kv * n_blocks;
+  if (grid > 0x7fffffffll) return OKQ_ERR_UNSUPPORTED;
+  cudaError_t e = launch_dependent(k_paged_append<T>, dim3((unsigned)grid), NT, 0, s, 1, c, layer, k, v, n_new, new_len, rope, n_blocks);
+  if (e != cudaSuccess) return failed(e);
+  const int warps = NT / 32;
+  e = launch_dependent(k_paged_advance, dim3((layer_count * c.batch + warps - 1) / warps), NT, 0, s, 1, c, layer, layer_count, n_new, new_len);
+  return e != cudaSuccess ? failed(e) : launch_status();
+}
+
+}  // namespace
+
+okq_status check_paged(const okq_paged* c, bool need_ptrs) {
+  if (!c) return OKQ_ERR_INVALID_ARG;
+  if (c->n_layers <= 0 || c->batch <= 0 || c->n_kv_heads <= 0 || c->n_q_heads <= 0 || c->n_pages <= 0 || c->max_pages <= 0) return OKQ_ERR_INVALID_ARG;
+  if (c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128 && c->page_tokens != 256) return OKQ_ERR_UNSUPPORTED;
+  if (c->dtype != OKQ_FP16 && c->dtype != OKQ_BF16) return OKQ_ERR_UNSUPPORTED;
+  if (c->n_q_heads % c->n_kv_heads != 0 || c->n_q_heads / c->n_kv_heads > OKQ_MAX_GROUP) return OKQ_ERR_UNSUPPORTED;
+  // token numbers, (layer, sequence, head) units and rows of the pool are 32-bit numbers in the kernels
+  if ((long long)c->max_pages * c->page_tokens > (1ll << 30)) return OKQ_ERR_UNSUPPORTED;
+  if ((double)c->n_layers * c->batch * c->n_kv_heads > 1 << 24) return OKQ_ERR_UNSUPPORTED;
+  if ((double)c->n_layers * c->n_pages * c->n_kv_heads * 2.0 * c->page_tokens > 2147483647.0) return OKQ_ERR_UNSUPPORTED;
+  if ((double)c->batch * c->max_pages > 2147483647.0) return OKQ_ERR_UNSUPPORTED;
+  if (need_ptrs) {
+    const void* p[7] = {c->codes, c->scales, c->raw, c->table, c->refs, c->seq_len, c->status};
+    for (const void* x : p)
+      if (!x) return OKQ_ERR_INVALID_ARG;
+    for (const void* x : p)
+      if (!aligned16(x)) return OKQ_ERR_ALIGNMENT;
+  }
+  return OKQ_OK;
+}
+
+okq_status check_paged_layers(const okq_paged* c, int32_t layer, int32_t layer_count) {
+  const okq_status st = check_paged(c, true);
+  if (st != OKQ_OK) return st;
+  return layer < 0 || layer_count <= 0 || layer > c->n_layers - layer_count ? OKQ_ERR_INVALID_ARG : OKQ_OK;
+}
+
+PagedView paged_view(const okq_paged* c) {
+  PagedView v;
+  v.n_layers = c->n_layers; v.batch = c->batch; v.n_kv = c->n_kv_heads; v.group = c->n_q_heads / c->n_kv_heads;
+  v.page = c->page_tokens;
+  v.page_shift = 5;
+  while ((1 << v.page_shift) < v.page) v.page_shift++;
+  v.n_pages = c->n_pages; v.max_pages = c->max_pages;
+  v.codes = c->codes; v.scales = c->scales; v.raw = c->raw;
+  v.table = c->table; v.refs = c->refs; v.seq_len = c->seq_len; v.status = c->status;
+  return v;
+}
+
+}  // namespace okq
+
+extern "C" {
+
+okq_status okq_paged_sizes(const okq_paged* c, size_t out[7]) {
+  const okq_status st = okq::check_paged(c, false);
+  if (st != OKQ_OK) return st;
+  if (!out) return OKQ_ERR_INVALID_ARG;
+  const size_t rows = (size_t)c->n_layers * c->n_pages * c->n_kv_heads * 2 * c->page_tokens;
+  out[0] = rows * OKQ_HEAD_DIM;
+  out[1] = rows / okq::PB * sizeof(float);
+  out[2] = (size_t)c->n_layers * c->batch * c->n_kv_heads * 2 * okq::PB * OKQ_HEAD_DIM * 2;
+  out[3] = (size_t)c->batch * c->max_pages * sizeof(int32_t);
+  out[4] = (size_t)c->n_pages * sizeof(int32_t);
+  out[5] = (size_t)c->n_layers * c->batch * sizeof(int32_t);
+  out[6] = 16;
+  return OKQ_OK;
+}
+
+okq_status okq_paged_append(const okq_paged* cache, int32_t layer, int32_t layer_count, const void* k, const int64_t ks[4], const void* v,
+                            const int64_t vs[4], int32_t n_new, const int32_t* new_len, const okq_rope* rope, void* stream) {
+  using namespace okq;
+  okq_status st = check_paged_layers(cache, layer, layer_count);
+  if (st != OKQ_OK) return st;
+  if (n_new < 0 || (n_new > 0 && (!k || !v)) || !ks || !vs) return OKQ_ERR_INVALID_ARG;
+  if (!aligned16(k) || !aligned16(v) || !strides_ok(ks, 4, 8) || !strides_ok(vs, 4, 8) || (reinterpret_cast<uintptr_t>(new_len) & 3))
+    return OKQ_ERR_ALIGNMENT;
+  if (n_new > (1 << 30)) return OKQ_ERR_UNSUPPORTED;
+  RopeView r;
+  if ((st = make_rope(rope, r)) != OKQ_OK) return st;
+  if (n_new == 0) return OKQ_OK;
+  const PagedView c = paged_view(cache);
+  Rows kr{k, {ks[0], ks[1], ks[2], ks[3]}}, vr{v, {vs[0], vs[1], vs[2], vs[3]}};
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return cache->dtype == OKQ_FP16 ? launch_append<__half>(c, layer, layer_count, kr, vr, n_new, new_len, r, s)
+                                  : launch_append<__nv_bfloat16>(c, layer, layer_count, kr, vr, n_new, new_len, r, s);
+}
+
+okq_status okq_paged_read(const okq_paged* cache, int32_t layer, int32_t layer_count, int32_t begin, int32_t n, void* k_out, void* v_out,
+                          void* stream) {
+  using namespace okq;
+  const okq_status st = check_paged_layers(cache, layer, layer_count);
+  if (st != OKQ_OK) return st;
+  if (begin < 0 || n < 0 || (n > 0 && (!k_out || !v_out)) || begin > INT32_MAX - n) return OKQ_ERR_INVALID_ARG;
+  if (!aligned16(k_out) || !aligned16(v_out)) return OKQ_ERR_ALIGNMENT;
+  if (n == 0) return OKQ_OK;
+  const PagedView c = paged_view(cache);
+  const long long items = (long long)layer_count * c.batch * c.n_kv * n * 8, grid = (items + NT - 1) / NT;
+  if (grid > 0x7fffffffll) return OKQ_ERR_UNSUPPORTED;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (cache->dtype == OKQ_FP16)
+    e = launch_dependent(k_paged_read<__half>, dim3((unsigned)grid), NT, 0, s, 1, c, layer, begin, n, static_cast<__half*>(k_out), static_cast<__half*>(v_out), items);
+  else
+    e = launch_dependent(k_paged_read<__nv_bfloat16>, dim3((unsigned)grid), NT, 0, s, 1, c, layer, begin, n, static_cast<__nv_bfloat16*>(k_out), static_cast<__nv_bfloat16*>(v_out), items);
+  return e != cudaSuccess ? failed(e) : launch_status();
+}
+
+}  // extern "C"
