@@ -2,23 +2,13 @@
 //
 // One warp per (layer, sequence, query head, query): it walks the tokens that its query sees with the running maximum and sum of the
 // softmax, four channels per lane.
-#include "okq_device.cuh"
-#include "okq_paged.cuh"
+#include "okq_paged_attn.cuh"
 
 namespace okq {
 
 namespace {
 
 constexpr int NT = 128;
-
-struct QRows {
-  const void* p;
-  int64_t s[4];
-};
-struct ORows {
-  void* p;
-  int64_t s[4];
-};
 
 template <class T>
 __global__ void __launch_bounds__(NT) k_paged_attention(const PagedView c, int layer, const QRows q, const ORows o, int n_new, const int32_t* q_len,
@@ -75,6 +65,13 @@ __global__ void __launch_bounds__(NT) k_paged_attention(const PagedView c, int l
   for (int e = 0; e < 4; e++) op[4 * lane + e] = from_f<T>(lost ? NAN : seen == 0 ? 0.f : acc[e] / sum);
 }
 
+// blocks of the attention kernel: one per SM, no more than there could be tiles
+int grid_of(const okq_paged* c, int layer_count, int n_new) {
+  const long long units = (long long)layer_count * c->batch * c->n_kv_heads;
+  const long long tiles = units * (((long long)c->max_pages * c->page_tokens + PT - 1) / PT), n = sm_count();
+  return (int)(tiles < n ? tiles : n);
+}
+
 okq_status failed(cudaError_t e) {
   set_last_cuda_error((int)e);
   (void)cudaGetLastError();
@@ -89,7 +86,9 @@ extern "C" {
 
 size_t okq_paged_workspace_bytes(const okq_paged* cache, int32_t layer_count, int32_t n_new) {
   if (okq::check_paged(cache, false) != OKQ_OK || layer_count <= 0 || layer_count > cache->n_layers || n_new < 0) return 0;
-  return (okq::pages_workspace(cache) + 255) & ~(size_t)255;
+  const size_t slots = (size_t)2 * okq::grid_of(cache, layer_count, n_new) * okq::DECODE_ROWS * (okq::D + 2) * sizeof(float);
+  const size_t pages = okq::pages_workspace(cache);
+  return ((slots > pages ? slots : pages) + 255) & ~(size_t)255;
 }
 
 okq_status okq_paged_attention(const okq_paged* cache, int32_t layer, int32_t layer_count, const void* q, const int64_t qs[4], int32_t n_new,
@@ -107,6 +106,12 @@ okq_status okq_paged_attention(const okq_paged* cache, int32_t layer, int32_t la
   if (n_new == 0) return OKQ_OK;
   if (!workspace || workspace_bytes < okq_paged_workspace_bytes(cache, layer_count, n_new)) return OKQ_ERR_WORKSPACE;
   const PagedView c = paged_view(cache);
+  if (c.group * n_new <= DECODE_ROWS) {
+    AttnArgs a{c, {q, {qs[0], qs[1], qs[2], qs[3]}}, {out, {os[0], os[1], os[2], os[3]}}, q_len, r, layer, layer_count, n_new,
+               sm_scale * 1.44269504088896340736f, static_cast<float*>(workspace)};
+    const cudaError_t e = launch_paged_decode(a, cache->dtype, grid_of(cache, layer_count, n_new), static_cast<cudaStream_t>(stream));
+    return e != cudaSuccess ? failed(e) : launch_status();
+  }
   const long long rows = (long long)layer_count * c.batch * c.n_kv * c.group * n_new, grid = (rows + NT / 32 - 1) / (NT / 32);
   if (grid > 0x7fffffffll) return OKQ_ERR_UNSUPPORTED;
   const QRows qr{q, {qs[0], qs[1], qs[2], qs[3]}};
