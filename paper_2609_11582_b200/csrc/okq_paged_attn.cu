@@ -86,7 +86,7 @@ extern "C" {
 
 size_t okq_paged_workspace_bytes(const okq_paged* cache, int32_t layer_count, int32_t n_new) {
   if (okq::check_paged(cache, false) != OKQ_OK || layer_count <= 0 || layer_count > cache->n_layers || n_new < 0) return 0;
-  const size_t slots = (size_t)2 * okq::grid_of(cache, layer_count, n_new) * okq::DECODE_ROWS * (okq::D + 2) * sizeof(float);
+  const size_t slots = okq::attn_workspace(okq::DECODE_PIPES * okq::grid_of(cache, layer_count, n_new), okq::DECODE_ROWS);
   const size_t pages = okq::pages_workspace(cache);
   return ((slots > pages ? slots : pages) + 255) & ~(size_t)255;
 }
@@ -108,8 +108,10 @@ okq_status okq_paged_attention(const okq_paged* cache, int32_t layer, int32_t la
   const PagedView c = paged_view(cache);
   if (c.group * n_new <= DECODE_ROWS) {
     AttnArgs a{c, {q, {qs[0], qs[1], qs[2], qs[3]}}, {out, {os[0], os[1], os[2], os[3]}}, q_len, r, layer, layer_count, n_new,
-               sm_scale * 1.44269504088896340736f, static_cast<float*>(workspace)};
-    const cudaError_t e = launch_paged_decode(a, cache->dtype, grid_of(cache, layer_count, n_new), static_cast<cudaStream_t>(stream));
+               sm_scale * 1.44269504088896340736f, static_cast<Head*>(workspace), nullptr};
+    const int grid = grid_of(cache, layer_count, n_new);
+    a.slots = reinterpret_cast<float*>(a.heads + DECODE_PIPES * grid);
+    const cudaError_t e = launch_paged_decode(a, cache->dtype, grid, static_cast<cudaStream_t>(stream));
     return e != cudaSuccess ? failed(e) : launch_status();
   }
   const long long rows = (long long)layer_count * c.batch * c.n_kv * c.group * n_new, grid = (rows + NT / 32 - 1) / (NT / 32);

@@ -1,10 +1,11 @@
 // What the two attention kernels over the 8-bit paged cache share: how the work is cut and numbered, partial results, the merge.
 //
 // An item is a (layer, sequence, KV head) with up to ROWS of its query rows (row = query * group + head of the group), a tile 128 of its
-// tokens.  Items follow one another in one long line of tiles; block c of the grid takes tiles [c * per, (c + 1) * per) of it,
-// whatever the lengths are, which only the device knows.  A piece is what a block holds of an item: all of it (the block writes the
-// output), or a part, whose unnormalised sums, maximum and normaliser go to one of the block's two slots (2 c for an item that began
-// in an earlier block, 2 c + 1 for one that goes on in a later one).  k_paged_merge puts parts together, in order.
+// tokens.  Items follow one another in one long line of tiles, which is cut into as many even ranges as there are pipelines on the GPU
+// (fewer where there are fewer tiles), whatever the lengths are, which only the device knows.  A piece is what a range holds of an
+// item: all of it (its pipeline writes the output), or a part, whose unnormalised sums, maximum and normaliser go to one of the
+// range's two slots (2 v for an item that began in an earlier range, 2 v + 1 for one that goes on in a later one).  k_paged_merge
+// puts parts together, in order.
 #pragma once
 #include "okq_device.cuh"
 #include "okq_paged.cuh"
@@ -30,7 +31,8 @@ struct AttnArgs {
   RopeView rope;
   int layer, layer_count, n_new;
   float scale2;     // softmax scale times log2(e)
-  float* slots;     // [2 * grid][ROWS * (128 + 2)]: sums, maxima, normalisers
+  struct Head* heads;   // [ranges]
+  float* slots;         // [2 * ranges][ROWS * (128 + 2)]: sums, maxima, normalisers
 };
 
 // tiles that an item reads: those up to the last token that its last row sees
@@ -78,15 +80,25 @@ template <int ROWS> struct Cursor {
   }
 };
 
-// All threads of a block find the whole line's length and the place of tile `want(total)`: cur, and the number of the first
-// tile of its item.  Threads hold consecutive ranges of pairs.
-struct FindSmem {
-  long long warp[32];
-  long long total, item0;
-  int place[4];
+// The line of `total` tiles in `ranges` parts: range v has tiles [start(v), start(v + 1)).
+struct Cuts {
+  long long total;
+  int ranges;        // of those, min(ranges, total) hold tiles
+  __device__ __forceinline__ int used() const { return total < ranges ? (int)total : ranges; }
+  __device__ __forceinline__ long long start(int v) const { return v >= used() ? total : (long long)v * total / used(); }
+  __device__ __forceinline__ int range_of(long long tile) const { return (int)(((tile + 1) * used() - 1) / total); }
 };
-template <int ROWS, int NT, class F>
-__device__ __forceinline__ void find_place(FindSmem& sm, const Work<ROWS>& w, F&& want, Cursor<ROWS>& cur, long long& target) {
+
+// All threads of a block find the line's length and where the first tiles of the block's ranges v0, v0 + step, .. lie.  Threads hold
+// consecutive pairs.
+template <int G> struct FindSmem {
+  long long warp[32];
+  long long total;
+  long long item0[G];   // first tile of the item that the range starts in
+  int place[G][4];
+};
+template <int ROWS, int NT, int G>
+__device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS>& w, int ranges, int v0, int step) {
   const int tid = threadIdx.x, lane = tid & 31, wp = tid >> 5;
   const int chunk = (w.pairs + NT - 1) / NT, p0 = min(w.pairs, tid * chunk), p1 = min(w.pairs, p0 + chunk);
   long long mine = 0;
@@ -102,16 +114,18 @@ __device__ __forceinline__ void find_place(FindSmem& sm, const Work<ROWS>& w, F&
     if (lane >= d) v += y;
   }
   if (lane == 31) sm.warp[wp] = v;
-  if (tid == 0) { sm.place[0] = w.pairs; sm.place[1] = sm.place[2] = sm.place[3] = 0; sm.item0 = 0; }
   __syncthreads();
   long long before = v - mine, total = 0;
+#pragma unroll
   for (int i = 0; i < NT / 32; i++) {
     if (i < wp) before += sm.warp[i];
     total += sm.warp[i];
   }
+  const Cuts cuts{total, ranges};
   if (tid == 0) sm.total = total;
-  target = want(total);
-  if (target >= before && target < before + mine) {
+  for (int g = 0; g < G && mine > 0; g++) {
+    const long long target = cuts.start(v0 + g * step);
+    if (target < before || target >= before + mine) continue;
     long long at = before;
     for (int p = p0; p < p1; p++) {
       int len, m;
@@ -122,18 +136,21 @@ __device__ __forceinline__ void find_place(FindSmem& sm, const Work<ROWS>& w, F&
       at += (long long)h * per_head;
       int rt = 0;
       while (target >= at + w.tiles(len, m, rt)) at += w.tiles(len, m, rt++);
-      sm.place[0] = p; sm.place[1] = h; sm.place[2] = rt; sm.place[3] = (int)(target - at);
-      sm.item0 = at;
+      sm.place[g][0] = p; sm.place[g][1] = h; sm.place[g][2] = rt; sm.place[g][3] = (int)(target - at);
+      sm.item0[g] = at;
       break;
     }
   }
   __syncthreads();
-  cur.pair = sm.place[0]; cur.h = sm.place[1]; cur.rt = sm.place[2]; cur.tile = sm.place[3];
-  cur.len = cur.m = cur.nt = 0;
-  if (cur.pair < w.pairs) cur.load(w);
+  return cuts;
 }
-
-__device__ __forceinline__ long long tiles_per_block(long long total, int grid) { return total <= 0 ? 1 : (total + grid - 1) / grid; }
+// the place found for range v0 + g * step; not to be called for a range without tiles
+template <int ROWS, int G> __device__ __forceinline__ Cursor<ROWS> place(const FindSmem<G>& sm, const Work<ROWS>& w, int g) {
+  Cursor<ROWS> c;
+  c.pair = sm.place[g][0]; c.h = sm.place[g][1]; c.rt = sm.place[g][2]; c.tile = sm.place[g][3];
+  c.load(w);
+  return c;
+}
 
 template <class T> __device__ __forceinline__ T* out_row(const AttnArgs& a, int pair, int h, int row) {
   const int li = pair / a.c.batch, b = pair % a.c.batch, g = a.c.group;
@@ -152,39 +169,79 @@ template <class T, int ROWS> __device__ __forceinline__ void write_empty(const A
   }
 }
 
-// Block i merges the item that the cut between blocks i and i + 1 of the attention kernel lies in, if it is that item's first cut.
-template <class T, int ROWS, int NT>
-__global__ void __launch_bounds__(NT) k_paged_merge(const AttnArgs a, int grid) {
-  __shared__ FindSmem fs;
+// What a range leaves for the merge: its last item goes on in the next `more` ranges (0: it does not).
+struct Head {
+  int more, pair, h, rt;
+};
+
+constexpr int MERGE_NT = 512, MERGE_ROWS = 8;
+
+// Block (v, y): rows [8 y, 8 y + 8) of the item that begins in range v and goes on behind it, if there is one.  A thread has four
+// channels of a row, and the parts of its half; factors of 32 parts at a time.  Bound by latency: the parts are a megabyte at most in
+// all; loads of eight parts are in flight per thread.
+template <class T, int ROWS>
+__global__ void __launch_bounds__(MERGE_NT) k_paged_merge(const AttnArgs a) {
+  constexpr int CH = 64;                       // parts whose factors are in shared memory
+  __shared__ float fac[MERGE_ROWS][CH], norm[MERGE_ROWS];
+  __shared__ float4 half_sum[MERGE_ROWS * D / 4];
   depend_wait();
-  const Work<ROWS> w(a);
-  Cursor<ROWS> cur;
-  long long g, per = 1;
-  find_place<ROWS, NT>(fs, w, [&](long long total) { per = tiles_per_block(total, grid); return ((long long)blockIdx.x + 1) * per; }, cur, g);
-  if (cur.pair >= w.pairs || cur.tile == 0) return;                 // behind the last tile, or between two items
-  const long long item0 = fs.item0;
-  const int first = (int)(item0 / per), last = (int)((item0 + cur.nt - 1) / per);
-  if (first != (int)blockIdx.x) return;
+  const int v = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const Head hd = a.heads[v];
+  if (hd.more == 0) return;
   constexpr size_t SLOT = (size_t)ROWS * (D + 2);
-  const int rows = min(ROWS, cur.m * w.group - cur.rt * ROWS);
-  for (int e = threadIdx.x; e < rows * D; e += NT) {
-    const int r = e / D, ch = e % D;
-    const float* s0 = a.slots + (size_t)(2 * first + 1) * SLOT;
-    float mx = s0[ROWS * D + r], l = s0[ROWS * D + ROWS + r], o = s0[e];
-    for (int c = first + 1; c <= last; c++) {
-      const float* s = a.slots + (size_t)(2 * c) * SLOT;
-      const float m2 = s[ROWS * D + r], l2 = s[ROWS * D + ROWS + r], o2 = s[e];
-      const float mn = fmaxf(mx, m2), at = mn == -INFINITY ? 0.f : mn, f1 = ex2(mx - at), f2 = ex2(m2 - at);
-      l = l * f1 + l2 * f2;
-      o = o * f1 + o2 * f2;
-      mx = mn;
+  const int n = hd.more + 1, row0 = MERGE_ROWS * blockIdx.y;
+  auto slot = [&](int k) { return a.slots + (size_t)(k == 0 ? 2 * v + 1 : 2 * (v + k)) * SLOT; };
+  const int r = (tid & 255) >> 5, part = tid >> 8;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float top = -INFINITY;
+  if (warp < MERGE_ROWS) {
+    for (int k = lane; k < n; k += 32) top = fmaxf(top, slot(k)[ROWS * D + row0 + warp]);
+#pragma unroll
+    for (int w = 16; w >= 1; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+    if (top == -INFINITY) top = 0.f;
+  }
+  float l = 0.f;
+  for (int k0 = 0; k0 < n; k0 += CH) {
+    const int kn = min(CH, n - k0);
+    __syncthreads();
+    if (warp < MERGE_ROWS)
+      for (int k = lane; k < kn; k += 32) {
+        const float* s = slot(k0 + k) + ROWS * D + row0 + warp;
+        const float f = ex2(s[0] - top);
+        fac[warp][k] = f;
+        l += s[ROWS] * f;
+      }
+    __syncthreads();
+#pragma unroll 8
+    for (int k = part; k < kn; k += 2) {
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(slot(k0 + k) + (size_t)(row0 + r) * D) + lane);
+      const float f = fac[r][k];
+      acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y); acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);
     }
-    out_row<T>(a, cur.pair, cur.h, cur.rt * ROWS + r)[ch] = from_f<T>(l == 0.f ? 0.f : o / l);
+  }
+  if (warp < MERGE_ROWS) {
+#pragma unroll
+    for (int w = 16; w >= 1; w >>= 1) l += __shfl_xor_sync(0xffffffffu, l, w);
+    if (lane == 0) norm[warp] = l;
+  }
+  if (part == 1) half_sum[tid & 255] = acc;
+  __syncthreads();
+  const Work<ROWS> w(a);
+  int len, m;
+  w.lens(hd.pair, len, m);
+  const int row = hd.rt * ROWS + row0 + r;
+  if (part == 0 && row < m * w.group) {
+    const float4 y = half_sum[tid & 255];
+    const float d = norm[r];
+    T o[4] = {from_f<T>(d == 0.f ? 0.f : (acc.x + y.x) / d), from_f<T>(d == 0.f ? 0.f : (acc.y + y.y) / d),
+              from_f<T>(d == 0.f ? 0.f : (acc.z + y.z) / d), from_f<T>(d == 0.f ? 0.f : (acc.w + y.w) / d)};
+    *reinterpret_cast<uint2*>(out_row<T>(a, hd.pair, hd.h, row) + 4 * lane) = *reinterpret_cast<const uint2*>(o);
   }
 }
 
-// launches (okq_paged_attn.cu, okq_paged_decode.cu)
+// okq_paged_decode.cu: up to DECODE_ROWS rows, DECODE_PIPES pipelines per block
+constexpr int DECODE_ROWS = 8, DECODE_PIPES = 3;
 cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int grid, cudaStream_t s);
-constexpr int DECODE_ROWS = 8;
+inline size_t attn_workspace(int ranges, int rows) { return (size_t)ranges * (sizeof(int) * 4 + 2 * (size_t)rows * (D + 2) * sizeof(float)); }
 
 }  // namespace okq
