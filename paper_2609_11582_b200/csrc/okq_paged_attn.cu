@@ -65,10 +65,15 @@ __global__ void __launch_bounds__(NT) k_paged_attention(const PagedView c, int l
   for (int e = 0; e < 4; e++) op[4 * lane + e] = from_f<T>(lost ? NAN : seen == 0 ? 0.f : acc[e] / sum);
 }
 
+// tiles that a call could have, were all sequences as long as their rows of the table
+long long most_tiles(const okq_paged* c, int layer_count, int n_new) {
+  const long long units = (long long)layer_count * c->batch * c->n_kv_heads, rows = (long long)n_new * (c->n_q_heads / c->n_kv_heads);
+  return units * ((rows + DECODE_ROWS - 1) / DECODE_ROWS) * (((long long)c->max_pages * c->page_tokens + PT - 1) / PT);
+}
+
 // blocks of the attention kernel: one per SM, no more than there could be tiles
 int grid_of(const okq_paged* c, int layer_count, int n_new) {
-  const long long units = (long long)layer_count * c->batch * c->n_kv_heads;
-  const long long tiles = units * (((long long)c->max_pages * c->page_tokens + PT - 1) / PT), n = sm_count();
+  const long long tiles = most_tiles(c, layer_count, n_new), n = sm_count();
   return (int)(tiles < n ? tiles : n);
 }
 
@@ -107,6 +112,7 @@ okq_status okq_paged_attention(const okq_paged* cache, int32_t layer, int32_t la
   if (!workspace || workspace_bytes < okq_paged_workspace_bytes(cache, layer_count, n_new)) return OKQ_ERR_WORKSPACE;
   const PagedView c = paged_view(cache);
   if (c.group * n_new <= DECODE_ROWS) {
+    if (most_tiles(cache, layer_count, n_new) > INT32_MAX) return OKQ_ERR_UNSUPPORTED;
     AttnArgs a{c, {q, {qs[0], qs[1], qs[2], qs[3]}}, {out, {os[0], os[1], os[2], os[3]}}, q_len, r, layer, layer_count, n_new,
                sm_scale * 1.44269504088896340736f, static_cast<Head*>(workspace), nullptr};
     const int grid = grid_of(cache, layer_count, n_new);

@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
   if (tid < G) {
     auto init = [](unsigned long long* b, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(smem_u32(b)), "r"(count)); };
     PipeSync& mine = sm.sync[tid];
-    for (int i = 0; i < NS; i++) init(&mine.full[i], 1);
+    for (int i = 0; i < NS; i++) init(&mine.full[i], 2);   // copies, scales
     init(&mine.s_full, 1);
     init(&mine.p_full, 4);
     init(&mine.o_full, 1);
@@ -191,8 +191,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
   const Work<R> work(a);
   const Cuts cuts = find_places<R, NT, G>(sm.find, work, G * gridDim.x, blockIdx.x, gridDim.x);
   const int v = blockIdx.x + g * gridDim.x;     // this pipeline's range
-  const long long g0 = cuts.start(v);
-  const int n_my = (int)(cuts.start(v + 1) - g0);
+  const int g0 = cuts.start(v), n_my = cuts.size(v);
+  const Heads<R> heads(work.pairs, c.n_kv, c.group, a.n_new, G * gridDim.x);
   Cursor<R> cur{};
   if (n_my > 0) cur = place<R, G>(sm.find, work, g);
 
@@ -239,10 +239,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         else in_nx = false;
       }
       const bool mine = lane >> 2 == k, there = mine && now.row >= 0;
-      if (mine) { sy.scale[s][lane & 3] = now.ks; sy.scale[s][4 + (lane & 3)] = now.vs; }
       const int blocks = __popc(__ballot_sync(0xffffffffu, there));
       const uint32_t bar = smem_u32(&sy.full[s]);
-      __syncwarp();   // the scales are written before the arrival
       if (lane == 0)
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(bar), "r"(blocks * 2 * PB * D) : "memory");
       __syncwarp();
@@ -254,6 +252,9 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
                        ::"r"(smem_u32(side ? pipe.v[s] : pipe.k[s]) + j * PB * D), "l"(reinterpret_cast<uint64_t>(&map)), "r"(0),
                          "r"(now.row + side * c.page), "r"(bar) : "memory");
       }
+      if (mine) { sy.scale[s][lane & 3] = now.ks; sy.scale[s][4 + (lane & 3)] = now.vs; }   // (may still be on their way: behind the copies)
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sy.full[s]);
       if (k == 4) scales();
     };
     int items = 0, armed = 0, scored = 0, done = 0;
@@ -302,14 +303,14 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       for (int i = max(0, armed - NS); i < armed; i++) mbar_drain(&sy.full[i % NS], (uint32_t)(i / NS) & 1u);
     if (scored >= 1 && !mbar_drain(&sy.s_full, (uint32_t)(scored - 1) & 1u)) sm.tmem_busy = 1;
     if (done >= 1 && !mbar_drain(&sy.o_full, (uint32_t)(done - 1) & 1u)) sm.tmem_busy = 1;
-    write_empty<T>(a, work, v, G * gridDim.x, lane);
+    write_empty<T>(a, work, heads, v, G * gridDim.x, lane);
   } else {
     // ------------------------------------------------------------------ workers (after a timeout they run on, waits failing at once)
     const uint32_t lanes = (uint32_t)(32 * role) << 16;
     const int ch = 32 * role + lane;
     float top[R], sum[R], qs[R], o[R];
     bool fresh = true, whole = cur.tile == 0, began = cur.tile != 0;   // the piece has its item's first tile; the item began in an earlier range
-    Head head{0, 0, 0, 0};
+    if (!heads.by_item && tid == g * 128) a.heads[v].more = 0;
     for (int i = 0; i < n_my; i++) {
       const int s = i % NS, b = i & 1;
       const int pair = cur.pair, h = cur.h, rt = cur.rt, tile = cur.tile, len = cur.len, m = cur.m, nt = cur.nt;
@@ -418,7 +419,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         asm volatile("bar.sync %0, 128;\n" ::"r"(1 + g) : "memory");
         const bool ends = cur.tile == 0, direct = whole && ends;
         float* slot = a.slots + (size_t)(2 * v + (began ? 0 : 1)) * SLOT;
-        if (!ends && !began) head = Head{cuts.range_of(g0 + i - tile + nt - 1) - v, pair, h, rt};
+        if (!began && (heads.by_item || !ends) && tid == g * 128)   // (the same thread as above)
+          a.heads[heads.at(v, c.n_kv, pair, h, rt)] = Head{ends ? 0 : cuts.range_of(g0 + i - tile + nt - 1) - v, v, pair, h, rt, {}};
 #pragma unroll
         for (int r = 0; r < R; r++) {
           float l = (sy.sum[0][r] + sy.sum[1][r]) + (sy.sum[2][r] + sy.sum[3][r]);
@@ -434,7 +436,6 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         began = false;
       }
     }
-    if (role == 0 && lane == 0) a.heads[v] = head;
   }
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
   __syncthreads();
@@ -453,7 +454,8 @@ template <class T> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map,
     attr_done(attr_mask, dev);
   }
   cudaError_t e = launch_dependent(k_paged_decode<T>, dim3(grid), NT, SMEM, s, 1, map, a, WAIT_LIMIT_CLOCKS);
-  if (e == cudaSuccess) e = launch_dependent(k_paged_merge<T, R>, dim3(G * grid), MERGE_NT, 0, s, 1, a);
+  const Heads<R> heads(a.layer_count * a.c.batch, a.c.n_kv, a.c.group, a.n_new, G * grid);
+  if (e == cudaSuccess) e = launch_dependent(k_paged_merge<T, R>, dim3(heads.count(G * grid), R), MERGE_NT, 0, s, 1, a);
   return e;
 }
 
