@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libokq.so")
 SOURCES = ["okq_host.cu", "okq_quant.cu", "okq_decode.cu", "okq_decode_mma.cu", "okq_decode_small.cu", "okq_decode_tc.cu", "okq_quant_tc.cu", "okq_calib.cu", "okq_calib_scores.cu", "okq_eigen.cu", "okq_ladder.cu", "okq_ladder_decode.cu",
-           "okq_rope.cu", "okq_paged.cu", "okq_paged_attn.cu", "okq_paged_decode.cu", "okq_pages.cu"]
+           "okq_rope.cu", "okq_paged.cu", "okq_paged_attn.cu", "okq_paged_decode.cu", "okq_paged_prompt.cu", "okq_pages.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "-Xcompiler", "-fPIC"]
 

@@ -9,6 +9,7 @@
 #pragma once
 #include "okq_device.cuh"
 #include "okq_paged.cuh"
+#include "okq_tc.cuh"
 
 namespace okq {
 
@@ -193,62 +194,107 @@ template <class T, int ROWS> __device__ __forceinline__ void write_empty(const A
   }
 }
 
-constexpr int MERGE_NT = 256, MERGE_WARPS = MERGE_NT / 32;
+constexpr int MERGE_NT = 256;
 
-// Block (x, y): row y of the item of head x, if it is in parts.  A warp has every eighth part, a lane four channels.  Bound by latency: a
-// megabyte of parts at most, the loads of seven parts in flight.
-template <class T, int ROWS>
+// Block (x, y): rows of the item of head x, if it is in parts.  WPR warps to a row (all eight where a handful of rows can be in hundreds
+// of parts, one where hundreds of rows are in a few), of which each has every WPR-th part, a lane four channels.  Bound by latency: a
+// few megabytes of parts at most; all of a part is loaded at once, seven parts in flight.
+template <class T, int ROWS, int WPR>
 __global__ void __launch_bounds__(MERGE_NT) k_paged_merge(const AttnArgs a) {
-  __shared__ float4 sums[MERGE_WARPS][32];
-  __shared__ float tops[MERGE_WARPS], norms[MERGE_WARPS];
+  constexpr int WARPS = MERGE_NT / 32;
+  __shared__ float4 sums[WARPS][32];
+  __shared__ float2 stat[WARPS];
   depend_wait();
-  const int r = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = blockIdx.y * (WARPS / WPR) + warp / WPR, first = warp % WPR;
   const Head hd = a.heads[blockIdx.x];
   if (hd.more == 0) return;
   constexpr size_t SLOT = (size_t)ROWS * (D + 2);
-  const int n = hd.more + 1;
+  const int n = hd.more + 1, row = hd.rt * ROWS + r;
   auto slot = [&](int k) { return a.slots + (size_t)(2 * (hd.v + k) + (k == 0)) * SLOT; };
   const Work<ROWS> w(a);
   int len, m;
   w.lens(hd.pair, len, m);
-  float top = -INFINITY;
-  for (int k = tid; k < n; k += MERGE_NT) top = fmaxf(top, slot(k)[ROWS * D + r]);
-#pragma unroll
-  for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-  if (lane == 0) tops[warp] = top;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < MERGE_WARPS; i++) top = fmaxf(top, tops[i]);
-  if (top == -INFINITY) top = 0.f;
+  const bool there = row < m * w.group;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  float l = 0.f;
-#pragma unroll 7
-  for (int k = warp; k < n; k += MERGE_WARPS) {
-    const float* s = slot(k);
-    const float4 x = __ldcg(reinterpret_cast<const float4*>(s + r * D) + lane);
-    const float f = ex2(__ldcg(s + ROWS * D + r) - top);
-    l = fmaf(__ldcg(s + ROWS * D + ROWS + r), f, l);
-    acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y); acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);
-  }
-  sums[warp][lane] = acc;
-  if (lane == 0) norms[warp] = l;
-  __syncthreads();
-  const int row = hd.rt * ROWS + r;
-  if (warp != 0 || row >= m * w.group) return;
+  float top = -INFINITY, l = 0.f;
+  if (there) {
+    for (int k0 = first; k0 < n; k0 += 7 * WPR) {
+      float4 x[7];
+      float tk[7], lk[7];
 #pragma unroll
-  for (int i = 1; i < MERGE_WARPS; i++) {
-    const float4 x = sums[i][lane];
-    acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
-    l += norms[i];
+      for (int e = 0; e < 7; e++) {
+        const int k = k0 + e * WPR;
+        tk[e] = -INFINITY;
+        if (k >= n) continue;
+        const float* s = slot(k);
+        x[e] = __ldcg(reinterpret_cast<const float4*>(s + (size_t)r * D) + lane);
+        tk[e] = __ldcg(s + ROWS * D + r);
+        lk[e] = __ldcg(s + ROWS * D + ROWS + r);
+      }
+      float mn = top;
+#pragma unroll
+      for (int e = 0; e < 7; e++) mn = fmaxf(mn, tk[e]);
+      const float ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(top - ref);
+      l *= f0;
+      acc.x *= f0; acc.y *= f0; acc.z *= f0; acc.w *= f0;
+      top = mn;
+#pragma unroll
+      for (int e = 0; e < 7; e++) {
+        if (k0 + e * WPR >= n) continue;
+        const float f = ex2(tk[e] - ref);
+        l = fmaf(lk[e], f, l);
+        acc.x = fmaf(x[e].x, f, acc.x); acc.y = fmaf(x[e].y, f, acc.y); acc.z = fmaf(x[e].z, f, acc.z); acc.w = fmaf(x[e].w, f, acc.w);
+      }
+    }
   }
+  if (WPR > 1) {
+    sums[warp][lane] = acc;
+    if (lane == 0) stat[warp] = make_float2(top, l);
+    __syncthreads();
+    if (first != 0) return;
+    float mn = top;
+#pragma unroll
+    for (int i = 1; i < WPR; i++) mn = fmaxf(mn, stat[warp + i].x);
+    const float ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(top - ref);
+    l *= f0;
+    acc.x *= f0; acc.y *= f0; acc.z *= f0; acc.w *= f0;
+#pragma unroll
+    for (int i = 1; i < WPR; i++) {
+      const float f = ex2(stat[warp + i].x - ref);
+      const float4 x = sums[warp + i][lane];
+      l = fmaf(stat[warp + i].y, f, l);
+      acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y); acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);
+    }
+  }
+  if (!there) return;
   T o[4] = {from_f<T>(l == 0.f ? 0.f : acc.x / l), from_f<T>(l == 0.f ? 0.f : acc.y / l), from_f<T>(l == 0.f ? 0.f : acc.z / l),
             from_f<T>(l == 0.f ? 0.f : acc.w / l)};
   *reinterpret_cast<uint2*>(out_row<T>(a, hd.pair, hd.h, row) + 4 * lane) = *reinterpret_cast<const uint2*>(o);
+}
+template <class T, int ROWS> inline cudaError_t launch_merge(const AttnArgs& a, int ranges, cudaStream_t s) {
+  constexpr int WPR = ROWS <= 8 ? 8 : 1;
+  const Heads<ROWS> heads(a.layer_count * a.c.batch, a.c.n_kv, a.c.group, a.n_new, ranges);
+  const long long rows = (long long)a.n_new * a.c.group;
+  const int most = (int)(rows < ROWS ? rows : ROWS), per = MERGE_NT / 32 / WPR;
+  return launch_dependent(k_paged_merge<T, ROWS, WPR>, dim3(heads.count(ranges), (most + per - 1) / per), MERGE_NT, 0, s, 1, a);
 }
 
 // okq_paged_decode.cu: up to DECODE_ROWS rows, DECODE_PIPES pipelines per block
 constexpr int DECODE_ROWS = 8, DECODE_PIPES = 3;
 cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int grid, cudaStream_t s);
-inline size_t attn_workspace(int ranges, int rows) { return (size_t)ranges * (32 + 2 * (size_t)rows * (D + 2) * sizeof(float)); }
+// okq_paged_prompt.cu: any number of rows, one pipeline per block
+constexpr int PROMPT_ROWS = 256;
+cudaError_t launch_paged_prompt(const AttnArgs& a, int dtype, int grid, cudaStream_t s);
+
+// the pool's codes as rows of 128 bytes, copied 32 at a time
+inline bool codes_map(CUtensorMap& map, const PagedView& c, bool swizzled) {
+  EncodeTiledFn enc = encode_tiled();
+  if (!enc) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)c.n_layers * c.n_pages * c.n_kv * 2 * c.page}, str[1] = {(cuuint64_t)D};
+  const cuuint32_t box[2] = {(cuuint32_t)D, (cuuint32_t)PB}, estr[2] = {1, 1};
+  return enc(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, c.codes, dims, str, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 }  // namespace okq

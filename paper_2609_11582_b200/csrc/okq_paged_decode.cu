@@ -17,7 +17,6 @@
 //
 // Bound by memory: 256 bytes per token and head; an SM's share of the copy rate is a tile in about 1400 cycles.
 #include "okq_paged_attn.cuh"
-#include "okq_tc.cuh"
 
 namespace okq {
 
@@ -454,23 +453,14 @@ template <class T> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map,
     attr_done(attr_mask, dev);
   }
   cudaError_t e = launch_dependent(k_paged_decode<T>, dim3(grid), NT, SMEM, s, 1, map, a, WAIT_LIMIT_CLOCKS);
-  const Heads<R> heads(a.layer_count * a.c.batch, a.c.n_kv, a.c.group, a.n_new, G * grid);
-  if (e == cudaSuccess) e = launch_dependent(k_paged_merge<T, R>, dim3(heads.count(G * grid), R), MERGE_NT, 0, s, 1, a);
-  return e;
+  return e == cudaSuccess ? launch_merge<T, R>(a, G * grid, s) : e;
 }
 
 }  // namespace
 
 cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int grid, cudaStream_t s) {
-  EncodeTiledFn enc = encode_tiled();
-  if (!enc) return cudaErrorInvalidValue;
   CUtensorMap map;
-  const PagedView& c = a.c;
-  const cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)c.n_layers * c.n_pages * c.n_kv * 2 * c.page}, str[1] = {(cuuint64_t)D};
-  const cuuint32_t box[2] = {(cuuint32_t)D, (cuuint32_t)PB}, estr[2] = {1, 1};
-  if (enc(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, c.codes, dims, str, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-    return cudaErrorInvalidValue;
+  if (!codes_map(map, a.c, true)) return cudaErrorInvalidValue;
   return dtype == OKQ_FP16 ? launch<__half>(a, map, grid, s) : launch<__nv_bfloat16>(a, map, grid, s);
 }
 

@@ -1,0 +1,564 @@
+// Attention over the 8-bit paged cache for more than eight query rows per (layer, sequence, KV head): prompts, pieces of prompts,
+// drafted tokens.  Causal against the end of the sequence.
+//
+// Both products are fp16 on tcgen05 (kind::f16, fp32 accumulation in tensor memory):
+//   S[row][token] = Q[row][channel] K[token][channel]   the cache's codes are fp16 numbers as they are (|code| <= 127); queries are scaled
+//                                                       to a power of two per row, so that bf16 ones are fp16 numbers too
+//   O[row][channel] += P[row][token] V[token][channel]  P = 2^14 p w in fp16, in place of the scores in tensor memory, with
+//                                                       w = scale_v / (the largest one so far) of the token's block
+// and the scales of the blocks enter where they cost nothing: those of the keys in the factor of the exponent, those of the values as
+// log2(w) in its offset; the normaliser takes a block's sum divided by w.
+// The softmax' reference m is set 3 above a row's maximum and moves when the maximum passes it (log2 units): O is multiplied then,
+// by the row's own threads.  So a numerator keeps fp16's 11 bits down to 2^-25 of the largest.
+//
+// A block of threads has 256 rows (two tiles A and B of 128) and walks the tokens, 128 at a time: a loader warp (32-token blocks by
+// page), four warps that turn codes into fp16 (0x6400 | (code + 128) is 1024 + 128 + code; the rest is one subtraction per two) in the
+// layout of the products, an MMA warp, four softmax warps to each tile of rows (lane = row).  While one tile's softmax runs the
+// tensor cores have the other's products.
+//
+// Bound by the exponentials (16 per cycle and SM: 2048 cycles for 256 x 128 scores) and the products (2048 cycles at fp16's rate).
+#include "okq_paged_attn.cuh"
+
+namespace okq {
+
+namespace {
+
+constexpr int R = PROMPT_ROWS, M = 128;         // rows of a block, of a tile
+constexpr int SIDE = PT * D;                    // bytes of a tile's keys or values as codes
+constexpr int HALF = PT * 64 * 2;               // 64 channels of 128 rows in fp16
+constexpr int W_CONV = 8, W_MMA = 12, W_LOAD = 13;
+constexpr int NT = 14 * 32;
+constexpr uint32_t S_COL = 0, O_COL = 256;      // + 128 per tile; P lies on the first half of S
+constexpr size_t SLOT = (size_t)R * (D + 2);
+constexpr float P_SHIFT = 14.f, LEAD = 3.f, LEAST_W = 5.9604645e-8f;   // 2^-24
+
+struct Info {            // of a tile, by block
+  float ks[4];           // key scales
+  float lw[4];           // log2 of w, and the shift
+  float iw[4];           // 2^-14 / w
+  float mul[4];          // what codes are multiplied by: 1, less where w is below 2^-24, 0 for scales of 0 and NaN
+  float vref;            // the largest value scale so far, up to a factor of 2
+  float fv;              // what the sums are multiplied by where it has changed, 1 otherwise
+  int lost;              // blocks whose value scale is NaN, a bit for each
+  int pad;
+};
+
+struct PromptSmem {
+  __align__(1024) unsigned char q[2][2][HALF];   // [tile][channels / 64]
+  __align__(1024) unsigned char k[2][2][HALF];   // two tiles of tokens
+  __align__(1024) unsigned char v[2][2][HALF];
+  __align__(1024) int8_t code[2][SIDE];          // keys, values of the coming tile
+  __align__(16) Info info[4];
+  __align__(8) unsigned long long code_full[2], code_free[2], info_full[4], k_full[2], k_free[2], v_full[2], v_free[2], s_full[2], p_full[2], o_full[2], q_full[2];
+  FindSmem<1> find;
+  uint32_t tmem_slot;
+  long long limit;
+  volatile int abort;
+  volatile int tmem_busy;
+};
+
+// MN-major operand, 128-byte swizzle: 64 channels by 8 tokens are 1024 bytes, the other 64 channels lie HALF further
+__device__ __forceinline__ uint64_t make_desc_mn(uint32_t saddr) {
+  return (uint64_t)((saddr >> 4) & 0x3fff) | ((uint64_t)(HALF >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t ad, uint64_t bd, uint32_t idesc, bool acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
+               ::"r"(d), "l"(ad), "l"(bd), "r"(idesc), "r"(acc ? 1u : 0u) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t at, uint64_t bd, uint32_t idesc, bool acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n"
+               ::"r"(d), "r"(at), "l"(bd), "r"(idesc), "r"(acc ? 1u : 0u) : "memory");
+}
+__device__ __forceinline__ void commit(unsigned long long* b) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&r)[32]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+               : "=f"(r[0]),"=f"(r[1]),"=f"(r[2]),"=f"(r[3]),"=f"(r[4]),"=f"(r[5]),"=f"(r[6]),"=f"(r[7]),"=f"(r[8]),"=f"(r[9]),"=f"(r[10]),"=f"(r[11]),"=f"(r[12]),"=f"(r[13]),"=f"(r[14]),"=f"(r[15]),
+                 "=f"(r[16]),"=f"(r[17]),"=f"(r[18]),"=f"(r[19]),"=f"(r[20]),"=f"(r[21]),"=f"(r[22]),"=f"(r[23]),"=f"(r[24]),"=f"(r[25]),"=f"(r[26]),"=f"(r[27]),"=f"(r[28]),"=f"(r[29]),"=f"(r[30]),"=f"(r[31])
+               : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&r)[32]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};\n"
+               ::"r"(taddr), "f"(r[0]),"f"(r[1]),"f"(r[2]),"f"(r[3]),"f"(r[4]),"f"(r[5]),"f"(r[6]),"f"(r[7]),"f"(r[8]),"f"(r[9]),"f"(r[10]),"f"(r[11]),"f"(r[12]),"f"(r[13]),"f"(r[14]),"f"(r[15]),
+                 "f"(r[16]),"f"(r[17]),"f"(r[18]),"f"(r[19]),"f"(r[20]),"f"(r[21]),"f"(r[22]),"f"(r[23]),"f"(r[24]),"f"(r[25]),"f"(r[26]),"f"(r[27]),"f"(r[28]),"f"(r[29]),"f"(r[30]),"f"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};\n"
+               ::"r"(taddr), "r"(r[0]),"r"(r[1]),"r"(r[2]),"r"(r[3]),"r"(r[4]),"r"(r[5]),"r"(r[6]),"r"(r[7]),"r"(r[8]),"r"(r[9]),"r"(r[10]),"r"(r[11]),"r"(r[12]),"r"(r[13]),"r"(r[14]),"r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory"); }
+__device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory"); }
+__device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory"); }
+
+// four codes as two pairs of fp16 numbers
+__device__ __forceinline__ uint2 codes_to_half(uint32_t w) {
+  w ^= 0x80808080u;
+  const __half2 bias = __floats2half2_rn(1152.f, 1152.f);
+  uint32_t lo = __byte_perm(w, 0x64646464u, 0x4140), hi = __byte_perm(w, 0x64646464u, 0x4342);
+  const __half2 a = __hsub2(*reinterpret_cast<__half2*>(&lo), bias), b = __hsub2(*reinterpret_cast<__half2*>(&hi), bias);
+  return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+
+// The 32 rows of a warp in a row tile: rotated, scaled by a power of two, swizzled; returns the factor of the exponent that undoes the
+// scaling for the lane's own row (times the softmax scale, whose sign goes to the queries).  Eight lanes to a row, sixteen channels each.
+template <class T>
+__device__ __forceinline__ float prepare_queries(const AttnArgs& a, const Cursor<R>& cur, int row0, unsigned char* q, int lane) {
+  const PagedView& c = a.c;
+  const int li = cur.pair / c.batch, b = cur.pair % c.batch, rows = cur.m * c.group;
+  const int j = lane & 7, nc = a.rope.half >> 3;
+  const bool turns = a.rope.freq && j < nc;
+  const int c0 = !a.rope.freq || j < nc ? 8 * j : 2 * a.rope.half + 16 * (j - nc);
+  const int c1 = !a.rope.freq ? c0 + 64 : j < nc ? c0 + a.rope.half : c0 + 8;
+  float mine = 0.f;
+#pragma unroll 2
+  for (int it = 0; it < 8; it++) {
+    const int rl = 4 * it + (lane >> 3), row = cur.rt * R + row0 + rl;    // row inside the warp, of the item's queries
+    Vec8<T> x[2] = {};
+    if (row < rows) {
+      const T* src = static_cast<const T*>(a.q.p) + li * a.q.s[0] + b * a.q.s[1] + (cur.h * c.group + row % c.group) * a.q.s[2] + (row / c.group) * a.q.s[3];
+      x[0] = *reinterpret_cast<const Vec8<T>*>(src + c0);
+      x[1] = *reinterpret_cast<const Vec8<T>*>(src + c1);
+      if (turns) {
+        float cs[8], sn[8];
+        turns8(a.rope, a.rope.positions + (size_t)b * a.n_new + row / c.group, (size_t)c.batch * a.n_new, c0, cs, sn);
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          float u = to_f(x[0].v[e]), w = to_f(x[1].v[e]);
+          rotate_pair(u, w, cs[e], sn[e]);
+          x[0].v[e] = from_f<T>(u);
+          x[1].v[e] = from_f<T>(w);
+        }
+      }
+    }
+    unsigned mx = 0;
+#pragma unroll
+    for (int e = 0; e < 16; e++) mx = max(mx, __float_as_uint(to_f(x[e >> 3].v[e & 7])) & 0x7fffffffu);
+#pragma unroll
+    for (int d = 4; d >= 1; d >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+    // 2^-e brings the largest magnitude to [1, 2) (4 at the end of the range); rows too small for that, and those with an infinity or NaN, are zeros here
+    const int e2 = min((int)(mx >> 23) - 127, 126);
+    const bool fine = mx < 0x7f800000u && e2 > -100;
+    const float up = fine ? __uint_as_float((uint32_t)(127 - e2) << 23) * (a.scale2 < 0.f ? -1.f : 1.f) : 0.f;
+    const float back = mx >= 0x7f800000u ? NAN : fine ? __uint_as_float((uint32_t)(127 + e2) << 23) * fabsf(a.scale2) : 0.f;
+#pragma unroll
+    for (int z = 0; z < 2; z++) {
+      const int ch = z ? c1 : c0;
+      __half2 y[4];
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const float u = to_f(x[z].v[2 * e]), w = to_f(x[z].v[2 * e + 1]);
+        y[e] = __floats2half2_rn(fine ? u * up : 0.f, fine ? w * up : 0.f);
+      }
+      const int r = (row0 & (M - 1)) + rl;
+      *reinterpret_cast<uint4*>(q + (ch >> 6) * HALF + r * 128 + ((((ch & 63) >> 3) ^ (r & 7)) << 4)) = *reinterpret_cast<const uint4*>(y);
+    }
+    const float got = __shfl_sync(0xffffffffu, back, 8 * (lane & 3));    // rows 4 it .. 4 it + 3 are in lanes 0, 8, 16, 24
+    if (lane >> 2 == it) mine = got;
+  }
+  return mine;
+}
+
+template <class T>
+__global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ CUtensorMap map, const AttnArgs a, long long wait_limit) {
+  extern __shared__ unsigned char raw_smem[];
+  PromptSmem& sm = *reinterpret_cast<PromptSmem*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~(uintptr_t)1023);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    auto init = [](unsigned long long* b, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(smem_u32(b)), "r"(count)); };
+    for (int i = 0; i < 2; i++) {
+      init(&sm.code_full[i], 1); init(&sm.code_free[i], 4);
+      init(&sm.k_full[i], 4); init(&sm.k_free[i], 1);
+      init(&sm.v_full[i], 4); init(&sm.v_free[i], 1);
+      init(&sm.s_full[i], 1); init(&sm.p_full[i], 4); init(&sm.o_full[i], 1); init(&sm.q_full[i], 4);
+    }
+    for (int i = 0; i < 4; i++) init(&sm.info_full[i], 1);
+    sm.abort = 0;
+    sm.tmem_busy = 0;
+    sm.limit = wait_limit;
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(&sm.tmem_slot)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+  }
+  before_sync();
+  __syncthreads();
+  after_sync();
+  const uint32_t tmem = sm.tmem_slot;
+  depend_wait();
+
+  const PagedView& c = a.c;
+  const Work<R> work(a);
+  const int v = blockIdx.x;                     // this block's range
+  const Cuts cuts = find_places<R, NT, 1>(sm.find, work, gridDim.x, v, 0);
+  const Heads<R> heads(work.pairs, c.n_kv, c.group, a.n_new, gridDim.x);
+  const int g0 = cuts.start(v), n_my = cuts.size(v);
+  Cursor<R> cur{};
+  if (n_my > 0) cur = place<R, 1>(sm.find, work, 0);
+
+  if (warp == W_LOAD) {
+    // ------------------------------------------------------------------ loader: blocks of the tiles to come, as in the decode kernel
+    Cursor<R> ahead = cur;
+    int t_nx = 0, l_nx = 0, h_nx = 0, page_nx = -1;
+    bool in_nx = false, fresh_nx = false;
+    int row_now = -1, row_nx = -1;               // -1: nothing to copy
+    float ks_now = 0.f, vs_now = 0.f, ks_nx = 0.f, vs_nx = 0.f;
+    bool fresh_now = false;
+    auto entries = [&](int n) {
+      int pair = 0, len = 0;
+      for (int i = 0; i < n; i++) {
+        if (lane >> 2 == i) { t_nx = ahead.tile * PT + PB * (lane & 3); len = ahead.len; pair = ahead.pair; h_nx = ahead.h; fresh_nx = ahead.tile == 0; }
+        ahead.next(work);
+      }
+      in_nx = lane >> 2 < n && t_nx < len;
+      l_nx = a.layer + pair / c.batch;
+      if (in_nx) page_nx = __ldg(&c.table[(size_t)(pair % c.batch) * c.max_pages + (t_nx >> c.page_shift)]);
+    };
+    auto scales = [&] {
+      row_nx = -1;
+      ks_nx = vs_nx = 0.f;
+      if (!in_nx) return;
+      if ((unsigned)page_nx >= (unsigned)c.n_pages) {
+        ks_nx = vs_nx = NAN;
+        set_status(c.status, OKQ_ERR_INVALID_ARG);
+      } else {
+        const size_t row = c.code_row(l_nx, page_nx, h_nx, 0) + (t_nx & (c.page - 1));
+        row_nx = (int)row;
+        ks_nx = __ldg(&c.scales[row / PB]);
+        vs_nx = __ldg(&c.scales[(row + c.page) / PB]);
+      }
+    };
+    int armed[2] = {0, 0};
+    float vref = 0.f;
+    if (n_my > 0) { entries(min(8, n_my)); scales(); }
+    for (int i = 0; i < n_my; i++) {
+      const int k = i & 7;
+      if (k == 0) {
+        row_now = row_nx; ks_now = ks_nx; vs_now = vs_nx; fresh_now = fresh_nx;
+        if (i + 8 < n_my) entries(min(8, n_my - i - 8));
+        else in_nx = false;
+      }
+      const bool mine = lane >> 2 == k, there = mine && row_now >= 0;
+      const int blocks = __popc(__ballot_sync(0xffffffffu, there)), j = lane & 3;
+      bool out = false;
+#pragma unroll
+      for (int side = 0; side < 2; side++) {
+        if (i >= 1 && !mbar_wait(sm, &sm.code_free[side], (uint32_t)(i - 1) & 1u)) { out = true; break; }
+        const uint32_t bar = smem_u32(&sm.code_full[side]);
+        if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(bar), "r"(blocks * PB * D) : "memory");
+        __syncwarp();
+        if (there)
+          asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n"
+                       ::"r"(smem_u32(sm.code[side]) + j * PB * D), "l"(reinterpret_cast<uint64_t>(&map)), "r"(0), "r"(row_now + side * c.page), "r"(bar) : "memory");
+        armed[side] = i + 1;
+      }
+      if (out) break;
+      // what the other roles need to know of the tile (its entry was read before the keys of tile i - 1 could be turned into fp16)
+      const float vs = __shfl_sync(0xffffffffu, vs_now, 4 * k + j), ks = __shfl_sync(0xffffffffu, ks_now, 4 * k + j);
+      const bool first = i == 0 || __shfl_sync(0xffffffffu, (int)fresh_now, 4 * k) != 0;
+      float big = vs != vs ? 0.f : vs;
+      big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+      big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+      float fv = 1.f;
+      if (first) vref = big > 0.f ? big : 1.f;
+      else if (big >= 2.f * vref) { fv = vref / big; vref = big; }
+      const float w = vs / vref, wu = fmaxf(w, LEAST_W);      // (fmaxf: NaN gives the least)
+      Info& info = sm.info[i & 3];
+      if (lane < 4) {
+        info.ks[lane] = ks;
+        info.lw[lane] = log2f(wu) + P_SHIFT;
+        info.iw[lane] = 1.f / (wu * 16384.f);
+        info.mul[lane] = vs != vs ? 0.f : w < LEAST_W ? w / LEAST_W : 1.f;
+      }
+      const unsigned lost = __ballot_sync(0xffffffffu, lane < 4 && vs != vs);
+      if (lane == 0) { info.vref = vref; info.fv = fv; info.lost = (int)lost; }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.info_full[i & 3]);
+      if (k == 4) scales();
+    }
+    if (sm.abort || armed[1] < n_my)   // no copy may still be landing when the block ends
+      for (int side = 0; side < 2; side++)
+        if (armed[side] > 0) mbar_drain(&sm.code_full[side], (uint32_t)(armed[side] - 1) & 1u);
+    write_empty<T>(a, work, heads, v, gridDim.x, lane);
+  } else if (warp == W_MMA) {
+    // ------------------------------------------------------------------ products
+    constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(PT >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+    constexpr uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(M >> 4) << 24);   // B MN-major
+    int n_q[2] = {0, 0}, n_s[2] = {0, 0}, n_p[2] = {0, 0}, n_o[2] = {0, 0};
+    auto score = [&](int i, int t) {      // rows of tile t against the keys of token tile i
+      if (elect_one()) {
+        after_sync();
+        const uint64_t ad = make_desc_sw128(smem_u32(sm.q[t][0])), bd = make_desc_sw128(smem_u32(sm.k[i & 1][0]));
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+          const uint64_t off = (uint64_t)(((k & 3) * 32 + (k >> 2) * HALF) >> 4);
+          mma_ss(tmem + S_COL + M * t, ad + off, bd + off, id_s, k != 0);
+        }
+        commit(&sm.s_full[t]);
+      }
+      __syncwarp();
+      n_s[t]++;
+    };
+    auto values = [&](int i, int t, bool acc) {
+      if (elect_one()) {
+        after_sync();
+        const uint64_t bd = make_desc_mn(smem_u32(sm.v[i & 1][0]));
+#pragma unroll
+        for (int k = 0; k < 8; k++)
+          mma_ts(tmem + O_COL + D * t, tmem + S_COL + M * t + 8u * k, bd + (uint64_t)(k * 2048 >> 4), id_o, acc || k != 0);   // 16 tokens further
+        commit(&sm.o_full[t]);
+      }
+      __syncwarp();
+      n_o[t]++;
+    };
+    auto give = [&](unsigned long long* b) {   // a buffer, once the products issued so far are through
+      if (elect_one()) commit(b);
+      __syncwarp();
+    };
+    bool go = true;
+    for (int i = 0; i < n_my && go;) {
+      const bool two = cur.m * c.group - cur.rt * R > M;
+      const int n = min(cur.nt - cur.tile, n_my - i);
+      go = mbar_wait(sm, &sm.q_full[0], (uint32_t)(n_q[0]++) & 1u) && (!two || mbar_wait(sm, &sm.q_full[1], (uint32_t)(n_q[1]++) & 1u)) &&
+           mbar_wait(sm, &sm.k_full[i & 1], (uint32_t)(i >> 1) & 1u);
+      if (!go) break;
+      score(i, 0);
+      if (two) score(i, 1);
+      give(&sm.k_free[i & 1]);
+      for (int k = 0; k < n && go; k++, i++) {
+        if (!(go = mbar_wait(sm, &sm.p_full[0], (uint32_t)(n_p[0]++) & 1u) && mbar_wait(sm, &sm.v_full[i & 1], (uint32_t)(i >> 1) & 1u))) break;
+        values(i, 0, k > 0);
+        if (k + 1 < n) {
+          if (!(go = mbar_wait(sm, &sm.k_full[(i + 1) & 1], (uint32_t)((i + 1) >> 1) & 1u))) break;
+          score(i + 1, 0);
+        }
+        if (two) {
+          if (!(go = mbar_wait(sm, &sm.p_full[1], (uint32_t)(n_p[1]++) & 1u))) break;
+          values(i, 1, k > 0);
+          if (k + 1 < n) score(i + 1, 1);
+        }
+        give(&sm.v_free[i & 1]);
+        if (k + 1 < n) give(&sm.k_free[(i + 1) & 1]);
+      }
+      cur.next_item(work);
+    }
+    for (int t = 0; t < 2; t++) {
+      if (n_s[t] > 0 && !mbar_drain(&sm.s_full[t], (uint32_t)(n_s[t] - 1) & 1u)) sm.tmem_busy = 1;
+      if (n_o[t] > 0 && !mbar_drain(&sm.o_full[t], (uint32_t)(n_o[t] - 1) & 1u)) sm.tmem_busy = 1;
+    }
+  } else if (warp >= W_CONV) {
+    // ------------------------------------------------------------------ codes to fp16: eight lanes to a token, sixteen channels each
+    const int ct = tid - 32 * W_CONV, j = ct & 7;
+    for (int i = 0; i < n_my; i++) {
+      const int buf = i & 1;
+#pragma unroll
+      for (int side = 0; side < 2; side++) {
+        if (side) mbar_wait(sm, &sm.info_full[i & 3], (uint32_t)(i >> 2) & 1u);
+        mbar_wait(sm, &sm.code_full[side], (uint32_t)i & 1u);
+        if (i >= 2) mbar_wait(sm, side ? &sm.v_free[buf] : &sm.k_free[buf], (uint32_t)((i >> 1) - 1) & 1u);
+        unsigned char* to = side ? sm.v[buf][0] : sm.k[buf][0];
+#pragma unroll
+        for (int z = 0; z < 8; z++) {
+          const int t = 16 * z + (ct >> 3);
+          const uint4 w = *reinterpret_cast<const uint4*>(sm.code[side] + t * D + 16 * j);
+          uint2 h[4] = {codes_to_half(w.x), codes_to_half(w.y), codes_to_half(w.z), codes_to_half(w.w)};
+          if (side) {
+            const float mul = sm.info[i & 3].mul[t >> 5];
+            if (mul != 1.f) {
+              const __half2 m2 = __floats2half2_rn(mul, mul);
+#pragma unroll
+              for (int e = 0; e < 4; e++) {
+                __half2* y = reinterpret_cast<__half2*>(&h[e]);
+                y[0] = __hmul2(y[0], m2);
+                y[1] = __hmul2(y[1], m2);
+              }
+            }
+          }
+          // chunks 2 (j & 3) and the next of the row's 64 channels; the two halves' lanes in opposite order, for the banks' sake
+          unsigned char* row = to + (j >> 2) * HALF + t * 128;
+          const int a0 = (2 * (j & 3)) ^ (t & 7), a1 = (2 * (j & 3) + 1) ^ (t & 7);
+          const uint4 y0 = make_uint4(h[0].x, h[0].y, h[1].x, h[1].y), y1 = make_uint4(h[2].x, h[2].y, h[3].x, h[3].y);
+          *reinterpret_cast<uint4*>(row + (j < 4 ? a0 : a1) * 16) = j < 4 ? y0 : y1;
+          *reinterpret_cast<uint4*>(row + (j < 4 ? a1 : a0) * 16) = j < 4 ? y1 : y0;
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(side ? &sm.v_full[buf] : &sm.k_full[buf]);
+          mbar_arrive(&sm.code_free[side]);
+        }
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ softmax: lane = row (after a timeout they run on, waits failing at once)
+    const int t = warp >> 2, quarter = warp & 3, row0 = M * t + 32 * quarter;
+    const uint32_t lanes = (uint32_t)(32 * quarter) << 16, s_at = tmem + S_COL + M * t + lanes, o_at = tmem + O_COL + D * t + lanes;
+    int n_s = 0, n_o = 0;
+    bool whole = cur.tile == 0, began = cur.tile != 0;
+    if (!heads.by_item && tid == 0) a.heads[v].more = 0;
+    for (int i = 0; i < n_my;) {
+      const int n = min(cur.nt - cur.tile, n_my - i), rows = cur.m * c.group - cur.rt * R;
+      const bool ends = cur.tile + n == cur.nt, active = rows > M * t;
+      const int row = row0 + lane, last_seen = cur.len - cur.m + (cur.rt * R + row) / c.group;   // last token that the row sees
+      const int least = cur.len - cur.m + (cur.rt * R + row0) / c.group;                         // .. that the warp's first row sees
+      float m = -INFINITY, l = 0.f, vref = 1.f;
+      if (active) {
+        // (the tile's own products of the item before are through)
+        const float back = prepare_queries<T>(a, cur, row0, sm.q[t][0], lane);
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.q_full[t]);
+        for (int k = 0; k < n; k++) {
+          const int tile = cur.tile + k, at = tile * PT;
+          mbar_wait(sm, &sm.info_full[(i + k) & 3], (uint32_t)((i + k) >> 2) & 1u);
+          const Info& info = sm.info[(i + k) & 3];
+          mbar_wait(sm, &sm.s_full[t], (uint32_t)(n_s++) & 1u);
+          after_sync();
+          const bool edge = at + PT - 1 > least || info.lost;
+          float cb[4], mx = -INFINITY;
+#pragma unroll
+          for (int b = 0; b < 4; b++) {
+            cb[b] = back * info.ks[b];
+            float x[32];
+            tmem_ld32(s_at + 32u * b, x);
+            tmem_wait_ld();
+            if (edge) {
+#pragma unroll
+              for (int e = 0; e < 32; e++)
+                if (at + 32 * b + e > last_seen) x[e] = -INFINITY;
+            }
+            float y[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+            for (int e = 4; e < 32; e++) y[e & 3] = fmaxf(y[e & 3], x[e]);
+            const float top = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+            mx = fmaxf(mx, top == -INFINITY ? top : top * cb[b]);
+          }
+          // a new reference: the row's sums so far are multiplied
+          const float fv = info.fv;
+          vref = info.vref;
+          const bool passed = mx > m;
+          if (__any_sync(0xffffffffu, passed) || (fv != 1.f && k > 0)) {
+            const float mn = passed ? mx + LEAD : m, f = passed ? ex2(m - mn) : 1.f;   // (0 for the first)
+            m = mn;
+            l *= f;
+            if (k > 0) {
+#pragma unroll
+              for (int b = 0; b < 4; b++) {
+                float x[32];
+                tmem_ld32(o_at + 32u * b, x);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; e++) x[e] *= f * fv;
+                tmem_st32(o_at + 32u * b, x);
+              }
+              tmem_wait_st();
+            }
+          }
+          const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+          for (int b = 0; b < 4; b++) {
+            float x[32];
+            tmem_ld32(s_at + 32u * b, x);
+            const float off = info.lw[b] - ref;
+            tmem_wait_ld();
+            if (edge) {
+#pragma unroll
+              for (int e = 0; e < 32; e++)
+                if (at + 32 * b + e > last_seen) x[e] = -INFINITY;
+            }
+            float sum[2] = {0.f, 0.f};
+            uint32_t u[16];
+#pragma unroll
+            for (int e = 0; e < 16; e++) {
+              const float x0 = x[2 * e], x1 = x[2 * e + 1];
+              float p0 = ex2(fmaf(x0, cb[b], off)), p1 = ex2(fmaf(x1, cb[b], off));
+              if (edge) {   // (a factor of zero or NaN makes NaN of -inf)
+                if (x0 == -INFINITY) p0 = 0.f;
+                if (x1 == -INFINITY) p1 = 0.f;
+              }
+              sum[0] += p0;
+              sum[1] += p1;
+              const __half2 h = __floats2half2_rn(p0, p1);
+              u[e] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            l = fmaf(sum[0] + sum[1], info.iw[b], l);
+            if ((info.lost >> b & 1) && at + 32 * b <= last_seen) l = NAN;
+            tmem_st16(s_at + 16u * b, u);
+          }
+          tmem_wait_st();
+          before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.p_full[t]);
+        }
+        n_o += n;
+        mbar_wait(sm, &sm.o_full[t], (uint32_t)(n_o - 1) & 1u);
+        after_sync();
+        if (sm.abort) l = NAN;
+        const bool direct = whole && ends;
+        float* slot = a.slots + (size_t)(2 * v + (began ? 0 : 1)) * SLOT;
+        const float unit = vref * (1.f / 16384.f), f = direct ? (l == 0.f ? 0.f : unit / l) : unit;
+        const bool there = row < rows;
+        T* dst = there && direct ? out_row<T>(a, cur.pair, cur.h, cur.rt * R + row) : nullptr;
+#pragma unroll
+        for (int b = 0; b < 4; b++) {
+          float x[32];
+          tmem_ld32(o_at + 32u * b, x);
+          tmem_wait_ld();
+          if (!there) continue;
+          if (direct) {
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+              Vec8<T> y;
+#pragma unroll
+              for (int z = 0; z < 8; z++) y.v[z] = from_f<T>(x[8 * e + z] * f);
+              *reinterpret_cast<Vec8<T>*>(dst + 32 * b + 8 * e) = y;
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+              *reinterpret_cast<float4*>(slot + (size_t)row * D + 32 * b + 4 * e) = make_float4(x[4 * e] * f, x[4 * e + 1] * f, x[4 * e + 2] * f, x[4 * e + 3] * f);
+          }
+        }
+        before_sync();
+        if (there && !direct) { slot[(size_t)R * D + row] = m; slot[(size_t)R * D + R + row] = l; }
+      }
+      if (!began && (heads.by_item || !ends) && tid == 0)
+        a.heads[heads.at(v, c.n_kv, cur.pair, cur.h, cur.rt)] = Head{ends ? 0 : cuts.range_of(g0 + i - cur.tile + cur.nt - 1) - v, v, cur.pair, cur.h, cur.rt, {}};
+      whole = true;
+      began = false;
+      i += n;
+      cur.next_item(work);
+    }
+  }
+  before_sync();
+  __syncthreads();
+  if (tid == 0 && sm.abort) set_status(c.status, OKQ_ERR_TIMEOUT);
+  if (warp == 0 && !sm.tmem_busy) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
+}
+
+template <class T> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map, int grid, cudaStream_t s) {
+  static thread_local unsigned long long attr_mask = 0;
+  int dev = 0;
+  constexpr int SMEM = (int)sizeof(PromptSmem) + 1024;
+  static_assert(SMEM <= 227 * 1024, "shared memory of one block");
+  if (attr_needed(attr_mask, dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(k_paged_prompt<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    if (e != cudaSuccess) return e;
+    attr_done(attr_mask, dev);
+  }
+  cudaError_t e = launch_dependent(k_paged_prompt<T>, dim3(grid), NT, SMEM, s, 1, map, a, WAIT_LIMIT_CLOCKS);
+  return e == cudaSuccess ? launch_merge<T, R>(a, grid, s) : e;
+}
+
+}  // namespace
+
+cudaError_t launch_paged_prompt(const AttnArgs& a, int dtype, int grid, cudaStream_t s) {
+  CUtensorMap map;
+  if (!codes_map(map, a.c, false)) return cudaErrorInvalidValue;
+  return dtype == OKQ_FP16 ? launch<__half>(a, map, grid, s) : launch<__nv_bfloat16>(a, map, grid, s);
+}
+
+}  // namespace okq
