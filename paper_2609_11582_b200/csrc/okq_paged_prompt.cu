@@ -161,6 +161,59 @@ __device__ __forceinline__ float prepare_queries(const AttnArgs& a, const Cursor
   return mine;
 }
 
+// The lane's row of a score tile, 32 columns (a block of tokens) at a time; `seen`: last column that the row sees.  The loops are not
+// unrolled: the code of one block stays in the instruction caches, which the eight warps share with five other roles.
+template <bool EDGE>
+__device__ __forceinline__ float row_max(uint32_t s_at, const Info& info, float back, int seen) {
+  float mx = -INFINITY;
+#pragma unroll 1
+  for (int b = 0; b < 4; b++) {
+    const float cb = back * info.ks[b];
+    float x[32];
+    tmem_ld32(s_at + 32u * b, x);
+    tmem_wait_ld();
+    if (EDGE) {
+#pragma unroll
+      for (int e = 0; e < 32; e++)
+        if (32 * b + e > seen) x[e] = -INFINITY;
+    }
+    float y[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+    for (int e = 4; e < 32; e++) y[e & 3] = fmaxf(y[e & 3], x[e]);
+    const float top = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+    mx = fmaxf(mx, EDGE && top == -INFINITY ? top : top * cb);
+  }
+  return mx;
+}
+template <bool EDGE>
+__device__ __forceinline__ float numerators(uint32_t s_at, const Info& info, float back, float ref, int seen, float l) {
+#pragma unroll 1
+  for (int b = 0; b < 4; b++) {
+    const float cb = back * info.ks[b], off = info.lw[b] - ref;
+    float x[32];
+    tmem_ld32(s_at + 32u * b, x);
+    tmem_wait_ld();
+    float sum[2] = {0.f, 0.f};
+    uint32_t u[16];
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+      float p0 = ex2(fmaf(x[2 * e], cb, off)), p1 = ex2(fmaf(x[2 * e + 1], cb, off));
+      if (EDGE) {
+        if (32 * b + 2 * e > seen) p0 = 0.f;
+        if (32 * b + 2 * e + 1 > seen) p1 = 0.f;
+      }
+      sum[0] += p0;
+      sum[1] += p1;
+      const __half2 h = __floats2half2_rn(p0, p1);
+      u[e] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    l = fmaf(sum[0] + sum[1], info.iw[b], l);
+    if (EDGE && (info.lost >> b & 1) && 32 * b <= seen) l = NAN;
+    tmem_st16(s_at + 16u * b, u);
+  }
+  return l;
+}
+
 template <class T>
 __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ CUtensorMap map, const AttnArgs a, long long wait_limit) {
   extern __shared__ unsigned char raw_smem[];
@@ -418,24 +471,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
           mbar_wait(sm, &sm.s_full[t], (uint32_t)(n_s++) & 1u);
           after_sync();
           const bool edge = at + PT - 1 > least || info.lost;
-          float cb[4], mx = -INFINITY;
-#pragma unroll
-          for (int b = 0; b < 4; b++) {
-            cb[b] = back * info.ks[b];
-            float x[32];
-            tmem_ld32(s_at + 32u * b, x);
-            tmem_wait_ld();
-            if (edge) {
-#pragma unroll
-              for (int e = 0; e < 32; e++)
-                if (at + 32 * b + e > last_seen) x[e] = -INFINITY;
-            }
-            float y[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-            for (int e = 4; e < 32; e++) y[e & 3] = fmaxf(y[e & 3], x[e]);
-            const float top = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
-            mx = fmaxf(mx, top == -INFINITY ? top : top * cb[b]);
-          }
+          const float mx = edge ? row_max<true>(s_at, info, back, last_seen - at) : row_max<false>(s_at, info, back, last_seen - at);
           // a new reference: the row's sums so far are multiplied
           const float fv = info.fv;
           vref = info.vref;
@@ -445,7 +481,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
             m = mn;
             l *= f;
             if (k > 0) {
-#pragma unroll
+#pragma unroll 1
               for (int b = 0; b < 4; b++) {
                 float x[32];
                 tmem_ld32(o_at + 32u * b, x);
@@ -458,36 +494,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
             }
           }
           const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-          for (int b = 0; b < 4; b++) {
-            float x[32];
-            tmem_ld32(s_at + 32u * b, x);
-            const float off = info.lw[b] - ref;
-            tmem_wait_ld();
-            if (edge) {
-#pragma unroll
-              for (int e = 0; e < 32; e++)
-                if (at + 32 * b + e > last_seen) x[e] = -INFINITY;
-            }
-            float sum[2] = {0.f, 0.f};
-            uint32_t u[16];
-#pragma unroll
-            for (int e = 0; e < 16; e++) {
-              const float x0 = x[2 * e], x1 = x[2 * e + 1];
-              float p0 = ex2(fmaf(x0, cb[b], off)), p1 = ex2(fmaf(x1, cb[b], off));
-              if (edge) {   // (a factor of zero or NaN makes NaN of -inf)
-                if (x0 == -INFINITY) p0 = 0.f;
-                if (x1 == -INFINITY) p1 = 0.f;
-              }
-              sum[0] += p0;
-              sum[1] += p1;
-              const __half2 h = __floats2half2_rn(p0, p1);
-              u[e] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            l = fmaf(sum[0] + sum[1], info.iw[b], l);
-            if ((info.lost >> b & 1) && at + 32 * b <= last_seen) l = NAN;
-            tmem_st16(s_at + 16u * b, u);
-          }
+          l = edge ? numerators<true>(s_at, info, back, ref, last_seen - at, l) : numerators<false>(s_at, info, back, ref, last_seen - at, l);
           tmem_wait_st();
           before_sync();
           __syncwarp();
