@@ -15,6 +15,16 @@ namespace okq {
 
 constexpr int PT = 128;   // tokens of a tile
 
+// Wait of a whole warp for one phase of an mbarrier: one look first, since most phases are complete when they are asked for and the
+// bounded wait's clock and abort flag cost a hundred cycles.
+template <class SM> __device__ __forceinline__ bool bar_wait(SM& sm, unsigned long long* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}\n"
+               : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+  if (__all_sync(0xffffffffu, ok != 0)) return true;
+  return mbar_wait(sm, bar, parity);
+}
+
 struct QRows {
   const void* p;
   int64_t s[4];

@@ -259,8 +259,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     int items = 0, armed = 0, scored = 0, done = 0;
     auto score = [&](int i, bool fresh) {
       const int s = i % NS;
-      if (fresh && !mbar_wait(sm, &sy.q_full, (uint32_t)(items++) & 1u)) return false;
-      if (!mbar_wait(sm, &sy.full[s], (uint32_t)(i / NS) & 1u)) return false;
+      if (fresh && !bar_wait(sm, &sy.q_full, (uint32_t)(items++) & 1u)) return false;
+      if (!bar_wait(sm, &sy.full[s], (uint32_t)(i / NS) & 1u)) return false;
       if (elect_one()) {
         asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
         const uint64_t ad = make_desc_sw128(smem_u32(pipe.k[s])), bd = make_desc_sw128(smem_u32(pipe.q));
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       bool go = score(0, true);
       for (int i = 0; i < n_my && go; i++) {
         cur.next(work);
-        if (!mbar_wait(sm, &sy.p_full, (uint32_t)i & 1u)) break;
+        if (!bar_wait(sm, &sy.p_full, (uint32_t)i & 1u)) break;
         const int s = i % NS;
         if (elect_one()) {
           asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         // (the workers have read the scores of tile i; the next item's queries are not ready before they have its sums too)
         const bool fresh = cur.tile == 0;
         if (i + 1 < n_my && !fresh) go = score(i + 1, false);
-        if (go && armed < n_my && (go = mbar_wait(sm, &sy.o_full, (uint32_t)i & 1u))) load(armed++);
+        if (go && armed < n_my && (go = bar_wait(sm, &sy.o_full, (uint32_t)i & 1u))) load(armed++);
         if (go && i + 1 < n_my && fresh) go = score(i + 1, true);
       }
     }
@@ -323,11 +323,11 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       }
       cur.next(work);
       const bool last = i + 1 == n_my || cur.tile == 0;
-      mbar_wait(sm, &sy.full[s], (uint32_t)(i / NS) & 1u);   // (long complete: for the loader's scales)
+      bar_wait(sm, &sy.full[s], (uint32_t)(i / NS) & 1u);   // (long complete: for the loader's scales)
       // scales of this warp's block of 32 tokens; the largest value scale of the tile
       const float ks = sy.scale[s][role], vs = sy.scale[s][4 + role];
       const float vref = fmaxf(fmaxf(sy.scale[s][4], sy.scale[s][5]), fmaxf(sy.scale[s][6], sy.scale[s][7]));
-      mbar_wait(sm, &sy.s_full, (uint32_t)i & 1u);
+      bar_wait(sm, &sy.s_full, (uint32_t)i & 1u);
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
       float x[R];
       {
@@ -393,7 +393,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
 
       // the tile's sums: lane = channel
       const float unit = vref > 0.f ? vref * (1.f / 4294967040.f) : 0.f;
-      mbar_wait(sm, &sy.o_full, (uint32_t)i & 1u);
+      bar_wait(sm, &sy.o_full, (uint32_t)i & 1u);
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
       {
         int y[4][8];

@@ -8,13 +8,16 @@
 //                                                       w = scale_v / (the largest one so far) of the token's block
 // and the scales of the blocks enter where they cost nothing: those of the keys in the factor of the exponent, those of the values as
 // log2(w) in its offset; the normaliser takes a block's sum divided by w.
-// The softmax' reference m is set 3 above a row's maximum and moves when the maximum passes it (log2 units): O is multiplied then,
-// by the row's own threads.  So a numerator keeps fp16's 11 bits down to 2^-25 of the largest.
+// The softmax' reference m is set 6 above a row's maximum and moves when the maximum passes it (log2 units): O is multiplied then,
+// by the row's own threads (3 above: every other step of a drifting sequence).  A numerator keeps fp16's 11 bits down to 2^-22 of the
+// largest.
 //
-// A block of threads has 256 rows (two tiles A and B of 128) and walks the tokens, 128 at a time: a loader warp (32-token blocks by
-// page), four warps that turn codes into fp16 (0x6400 | (code + 128) is 1024 + 128 + code; the rest is one subtraction per two) in the
-// layout of the products, an MMA warp, four softmax warps to each tile of rows (lane = row).  While one tile's softmax runs the
-// tensor cores have the other's products.
+// A block of threads has 256 rows, in two streams A and B of 128, and walks the tokens in steps of 64: a loader warp (32-token blocks
+// by page, two tiles of 128 tokens ahead), four warps that turn codes into fp16 (0x6400 | (code + 128) is 1024 + 128 + code; the rest is
+// one subtraction per two) in the layout of the products, to each stream an MMA warp (one for both is busy with waits and issue: 3.9
+// us a tile) and four softmax warps (lane = row).  A stream has
+// two places for scores, so that the next step's are there when a softmax ends.  Where an item has no more than 128 rows, both streams
+// have the same ones: A takes the first 64 tokens of every tile, B the others, and their sums are put together at the end.
 //
 // Bound by the exponentials (16 per cycle and SM: 2048 cycles for 256 x 128 scores) and the products (2048 cycles at fp16's rate).
 #include "okq_paged_attn.cuh"
@@ -23,14 +26,16 @@ namespace okq {
 
 namespace {
 
-constexpr int R = PROMPT_ROWS, M = 128;         // rows of a block, of a tile
+constexpr int R = PROMPT_ROWS, M = 128;         // rows of a block, of a stream
+constexpr int PH = PT / 2;                      // tokens of a step
 constexpr int SIDE = PT * D;                    // bytes of a tile's keys or values as codes
-constexpr int HALF = PT * 64 * 2;               // 64 channels of 128 rows in fp16
-constexpr int W_CONV = 8, W_MMA = 12, W_LOAD = 13;
-constexpr int NT = 14 * 32;
-constexpr uint32_t S_COL = 0, O_COL = 256;      // + 128 per tile; P lies on the first half of S
+constexpr int Q_HALF = M * 128, KV_HALF = PH * 128;   // 64 channels in fp16, of a stream's queries and of a step's keys or values
+constexpr int NR = 3;                           // ring of steps' keys, and values, in fp16
+constexpr int W_CONV = 8, W_MMA = 12, W_LOAD = 14;   // (an MMA warp to each stream)
+constexpr int NT = 15 * 32;
+constexpr uint32_t S_COL = 0, O_COL = 256;      // + 128 per stream, + 64 per place for scores; numerators lie on its first half
 constexpr size_t SLOT = (size_t)R * (D + 2);
-constexpr float P_SHIFT = 14.f, LEAD = 3.f, LEAST_W = 5.9604645e-8f;   // 2^-24
+constexpr float P_SHIFT = 14.f, LEAD = 6.f, LEAST_W = 5.9604645e-8f;   // 2^-24
 
 struct Info {            // of a tile, by block
   float ks[4];           // key scales
@@ -40,16 +45,17 @@ struct Info {            // of a tile, by block
   float vref;            // the largest value scale so far, up to a factor of 2
   float fv;              // what the sums are multiplied by where it has changed, 1 otherwise
   int lost;              // blocks whose value scale is NaN, a bit for each
-  int pad;
+  int plain;             // all of mul are 1
 };
 
 struct PromptSmem {
-  __align__(1024) unsigned char q[2][2][HALF];   // [tile][channels / 64]
-  __align__(1024) unsigned char k[2][2][HALF];   // two tiles of tokens
-  __align__(1024) unsigned char v[2][2][HALF];
-  __align__(1024) int8_t code[2][SIDE];          // keys, values of the coming tile
+  __align__(1024) unsigned char q[2][2][Q_HALF];   // [stream][channels / 64]
+  __align__(1024) unsigned char k[NR][2][KV_HALF];
+  __align__(1024) unsigned char v[NR][2][KV_HALF];
+  __align__(1024) int8_t code[2][2][SIDE];         // [keys, values][tile mod 2]
   __align__(16) Info info[4];
-  __align__(8) unsigned long long code_full[2], code_free[2], info_full[4], k_full[2], k_free[2], v_full[2], v_free[2], s_full[2], p_full[2], o_full[2], q_full[2];
+  __align__(8) unsigned long long code_full[2][2], code_free[2][2], info_full[4], k_full[NR], k_free[NR], v_full[NR], v_free[NR];
+  __align__(8) unsigned long long s_full[2][2], p_full[2][2], o_full[2], q_full[2];   // [stream][place]
   FindSmem<1> find;
   uint32_t tmem_slot;
   long long limit;
@@ -57,9 +63,9 @@ struct PromptSmem {
   volatile int tmem_busy;
 };
 
-// MN-major operand, 128-byte swizzle: 64 channels by 8 tokens are 1024 bytes, the other 64 channels lie HALF further
+// MN-major operand, 128-byte swizzle: 64 channels by 8 tokens are 1024 bytes, the other 64 channels lie KV_HALF further
 __device__ __forceinline__ uint64_t make_desc_mn(uint32_t saddr) {
-  return (uint64_t)((saddr >> 4) & 0x3fff) | ((uint64_t)(HALF >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+  return (uint64_t)((saddr >> 4) & 0x3fff) | ((uint64_t)(KV_HALF >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t ad, uint64_t bd, uint32_t idesc, bool acc) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
@@ -78,14 +84,14 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&r)[32]) {
                  "=f"(r[16]),"=f"(r[17]),"=f"(r[18]),"=f"(r[19]),"=f"(r[20]),"=f"(r[21]),"=f"(r[22]),"=f"(r[23]),"=f"(r[24]),"=f"(r[25]),"=f"(r[26]),"=f"(r[27]),"=f"(r[28]),"=f"(r[29]),"=f"(r[30]),"=f"(r[31])
                : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&r)[32]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};\n"
-               ::"r"(taddr), "f"(r[0]),"f"(r[1]),"f"(r[2]),"f"(r[3]),"f"(r[4]),"f"(r[5]),"f"(r[6]),"f"(r[7]),"f"(r[8]),"f"(r[9]),"f"(r[10]),"f"(r[11]),"f"(r[12]),"f"(r[13]),"f"(r[14]),"f"(r[15]),
-                 "f"(r[16]),"f"(r[17]),"f"(r[18]),"f"(r[19]),"f"(r[20]),"f"(r[21]),"f"(r[22]),"f"(r[23]),"f"(r[24]),"f"(r[25]),"f"(r[26]),"f"(r[27]),"f"(r[28]),"f"(r[29]),"f"(r[30]),"f"(r[31]) : "memory");
-}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};\n"
                ::"r"(taddr), "r"(r[0]),"r"(r[1]),"r"(r[2]),"r"(r[3]),"r"(r[4]),"r"(r[5]),"r"(r[6]),"r"(r[7]),"r"(r[8]),"r"(r[9]),"r"(r[10]),"r"(r[11]),"r"(r[12]),"r"(r[13]),"r"(r[14]),"r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+               : "=f"(r[0]),"=f"(r[1]),"=f"(r[2]),"=f"(r[3]),"=f"(r[4]),"=f"(r[5]),"=f"(r[6]),"=f"(r[7]),"=f"(r[8]),"=f"(r[9]),"=f"(r[10]),"=f"(r[11]),"=f"(r[12]),"=f"(r[13]),"=f"(r[14]),"=f"(r[15])
+               : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
@@ -105,7 +111,7 @@ __device__ __forceinline__ uint2 codes_to_half(uint32_t w) {
 // The 32 rows of a warp in a row tile: rotated, scaled by a power of two, swizzled; returns the factor of the exponent that undoes the
 // scaling for the lane's own row (times the softmax scale, whose sign goes to the queries).  Eight lanes to a row, sixteen channels each.
 template <class T>
-__device__ __forceinline__ float prepare_queries(const AttnArgs& a, const Cursor<R>& cur, int row0, unsigned char* q, int lane) {
+__device__ __forceinline__ float prepare_queries(const AttnArgs& a, const Cursor<R>& cur, int row0, unsigned char* q, bool store, int lane) {
   const PagedView& c = a.c;
   const int li = cur.pair / c.batch, b = cur.pair % c.batch, rows = cur.m * c.group;
   const int j = lane & 7, nc = a.rope.half >> 3;
@@ -153,7 +159,7 @@ __device__ __forceinline__ float prepare_queries(const AttnArgs& a, const Cursor
         y[e] = __floats2half2_rn(fine ? u * up : 0.f, fine ? w * up : 0.f);
       }
       const int r = (row0 & (M - 1)) + rl;
-      *reinterpret_cast<uint4*>(q + (ch >> 6) * HALF + r * 128 + ((((ch & 63) >> 3) ^ (r & 7)) << 4)) = *reinterpret_cast<const uint4*>(y);
+      if (store) *reinterpret_cast<uint4*>(q + (ch >> 6) * Q_HALF + r * 128 + ((((ch & 63) >> 3) ^ (r & 7)) << 4)) = *reinterpret_cast<const uint4*>(y);
     }
     const float got = __shfl_sync(0xffffffffu, back, 8 * (lane & 3));    // rows 4 it .. 4 it + 3 are in lanes 0, 8, 16, 24
     if (lane >> 2 == it) mine = got;
@@ -161,54 +167,48 @@ __device__ __forceinline__ float prepare_queries(const AttnArgs& a, const Cursor
   return mine;
 }
 
-// The lane's row of a score tile, 32 columns (a block of tokens) at a time; `seen`: last column that the row sees.  The loops are not
-// unrolled: the code of one block stays in the instruction caches, which the eight warps share with five other roles.
+// The lane's row of a step's scores, two blocks of 32 tokens, b0 the tile's number of the first; `seen`: last column that the row sees.
 template <bool EDGE>
-__device__ __forceinline__ float row_max(uint32_t s_at, const Info& info, float back, int seen) {
+__device__ __forceinline__ float row_max(float (&x)[2][32], const Info& info, int b0, float back, int seen) {
   float mx = -INFINITY;
-#pragma unroll 1
-  for (int b = 0; b < 4; b++) {
-    const float cb = back * info.ks[b];
-    float x[32];
-    tmem_ld32(s_at + 32u * b, x);
-    tmem_wait_ld();
+#pragma unroll
+  for (int b = 0; b < 2; b++) {
     if (EDGE) {
 #pragma unroll
       for (int e = 0; e < 32; e++)
-        if (32 * b + e > seen) x[e] = -INFINITY;
+        if (32 * b + e > seen) x[b][e] = -INFINITY;
     }
-    float y[4] = {x[0], x[1], x[2], x[3]};
+    float y[4] = {x[b][0], x[b][1], x[b][2], x[b][3]};
 #pragma unroll
-    for (int e = 4; e < 32; e++) y[e & 3] = fmaxf(y[e & 3], x[e]);
+    for (int e = 4; e < 32; e++) y[e & 3] = fmaxf(y[e & 3], x[b][e]);
     const float top = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
-    mx = fmaxf(mx, EDGE && top == -INFINITY ? top : top * cb);
+    mx = fmaxf(mx, EDGE && top == -INFINITY ? top : top * (back * info.ks[b0 + b]));
   }
   return mx;
 }
 template <bool EDGE>
-__device__ __forceinline__ float numerators(uint32_t s_at, const Info& info, float back, float ref, int seen, float l) {
-#pragma unroll 1
-  for (int b = 0; b < 4; b++) {
-    const float cb = back * info.ks[b], off = info.lw[b] - ref;
-    float x[32];
-    tmem_ld32(s_at + 32u * b, x);
-    tmem_wait_ld();
-    float sum[2] = {0.f, 0.f};
+__device__ __forceinline__ float numerators(const float (&x)[2][32], uint32_t s_at, const Info& info, int b0, float back, float ref, int seen, float l) {
+#pragma unroll
+  for (int b = 0; b < 2; b++) {
+    const float cb = back * info.ks[b0 + b], off = info.lw[b0 + b] - ref;
+    const F2 cb2 = f2(cb, cb), off2 = f2(off, off);
+    F2 sum[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
     uint32_t u[16];
 #pragma unroll
     for (int e = 0; e < 16; e++) {
-      float p0 = ex2(fmaf(x[2 * e], cb, off)), p1 = ex2(fmaf(x[2 * e + 1], cb, off));
-      if (EDGE) {
+      const float2 z = un2(fma2(f2(x[b][2 * e], x[b][2 * e + 1]), cb2, off2));
+      float p0 = ex2(z.x), p1 = ex2(z.y);
+      if (EDGE) {   // (-inf times a scale of zero is NaN)
         if (32 * b + 2 * e > seen) p0 = 0.f;
         if (32 * b + 2 * e + 1 > seen) p1 = 0.f;
       }
-      sum[0] += p0;
-      sum[1] += p1;
+      sum[e & 1] = add2(sum[e & 1], f2(p0, p1));
       const __half2 h = __floats2half2_rn(p0, p1);
       u[e] = *reinterpret_cast<const uint32_t*>(&h);
     }
-    l = fmaf(sum[0] + sum[1], info.iw[b], l);
-    if (EDGE && (info.lost >> b & 1) && 32 * b <= seen) l = NAN;
+    const float2 total = un2(add2(sum[0], sum[1]));
+    l = fmaf(total.x + total.y, info.iw[b0 + b], l);
+    if (EDGE && (info.lost >> (b0 + b) & 1) && 32 * b <= seen) l = NAN;
     tmem_st16(s_at + 16u * b, u);
   }
   return l;
@@ -221,13 +221,12 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     auto init = [](unsigned long long* b, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(smem_u32(b)), "r"(count)); };
-    for (int i = 0; i < 2; i++) {
-      init(&sm.code_full[i], 1); init(&sm.code_free[i], 4);
-      init(&sm.k_full[i], 4); init(&sm.k_free[i], 1);
-      init(&sm.v_full[i], 4); init(&sm.v_free[i], 1);
-      init(&sm.s_full[i], 1); init(&sm.p_full[i], 4); init(&sm.o_full[i], 1); init(&sm.q_full[i], 4);
+    for (int i = 0; i < 4; i++) {
+      init(&sm.code_full[0][0] + i, 1); init(&sm.code_free[0][0] + i, 4); init(&sm.info_full[i], 1);
+      init(&sm.s_full[0][0] + i, 1); init(&sm.p_full[0][0] + i, 4);
     }
-    for (int i = 0; i < 4; i++) init(&sm.info_full[i], 1);
+    for (int i = 0; i < NR; i++) { init(&sm.k_full[i], 4); init(&sm.k_free[i], 2); init(&sm.v_full[i], 4); init(&sm.v_free[i], 2); }
+    for (int i = 0; i < 2; i++) { init(&sm.o_full[i], 1); init(&sm.q_full[i], 4); }
     sm.abort = 0;
     sm.tmem_busy = 0;
     sm.limit = wait_limit;
@@ -299,17 +298,18 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       bool out = false;
 #pragma unroll
       for (int side = 0; side < 2; side++) {
-        if (i >= 1 && !mbar_wait(sm, &sm.code_free[side], (uint32_t)(i - 1) & 1u)) { out = true; break; }
-        const uint32_t bar = smem_u32(&sm.code_full[side]);
+        if (i >= 2 && !bar_wait(sm, &sm.code_free[side][i & 1], (uint32_t)((i >> 1) - 1) & 1u)) { out = true; break; }
+        const uint32_t bar = smem_u32(&sm.code_full[side][i & 1]);
         if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(bar), "r"(blocks * PB * D) : "memory");
         __syncwarp();
         if (there)
           asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n"
-                       ::"r"(smem_u32(sm.code[side]) + j * PB * D), "l"(reinterpret_cast<uint64_t>(&map)), "r"(0), "r"(row_now + side * c.page), "r"(bar) : "memory");
+                       ::"r"(smem_u32(sm.code[side][i & 1]) + j * PB * D), "l"(reinterpret_cast<uint64_t>(&map)), "r"(0), "r"(row_now + side * c.page), "r"(bar) : "memory");
         armed[side] = i + 1;
       }
       if (out) break;
-      // what the other roles need to know of the tile (its entry was read before the keys of tile i - 1 could be turned into fp16)
+      // what the other roles need to know of the tile (tile i - 4, whose place it takes, is through: the values of tile i - 2 are in fp16,
+      // so those of tile i - 4 have been used)
       const float vs = __shfl_sync(0xffffffffu, vs_now, 4 * k + j), ks = __shfl_sync(0xffffffffu, ks_now, 4 * k + j);
       const bool first = i == 0 || __shfl_sync(0xffffffffu, (int)fresh_now, 4 * k) != 0;
       float big = vs != vs ? 0.f : vs;
@@ -326,112 +326,127 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
         info.iw[lane] = 1.f / (wu * 16384.f);
         info.mul[lane] = vs != vs ? 0.f : w < LEAST_W ? w / LEAST_W : 1.f;
       }
-      const unsigned lost = __ballot_sync(0xffffffffu, lane < 4 && vs != vs);
-      if (lane == 0) { info.vref = vref; info.fv = fv; info.lost = (int)lost; }
+      const unsigned lost = __ballot_sync(0xffffffffu, lane < 4 && vs != vs), small = __ballot_sync(0xffffffffu, lane < 4 && !(w >= LEAST_W));
+      if (lane == 0) { info.vref = vref; info.fv = fv; info.lost = (int)lost; info.plain = small == 0; }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.info_full[i & 3]);
       if (k == 4) scales();
     }
     if (sm.abort || armed[1] < n_my)   // no copy may still be landing when the block ends
       for (int side = 0; side < 2; side++)
-        if (armed[side] > 0) mbar_drain(&sm.code_full[side], (uint32_t)(armed[side] - 1) & 1u);
+        for (int i = max(0, armed[side] - 2); i < armed[side]; i++) mbar_drain(&sm.code_full[side][i & 1], (uint32_t)(i >> 1) & 1u);
     write_empty<T>(a, work, heads, v, gridDim.x, lane);
-  } else if (warp == W_MMA) {
-    // ------------------------------------------------------------------ products
-    constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(PT >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+  } else if (warp >= W_MMA) {
+    // ------------------------------------------------------------------ products of stream t
+    const int t = warp - W_MMA;
+    constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(PH >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
     constexpr uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(M >> 4) << 24);   // B MN-major
-    int n_q[2] = {0, 0}, n_s[2] = {0, 0}, n_p[2] = {0, 0}, n_o[2] = {0, 0};
-    auto score = [&](int i, int t) {      // rows of tile t against the keys of token tile i
+    const uint32_t s_at = tmem + S_COL + 128u * t, o_at = tmem + O_COL + 128u * t;
+    int items = 0, n_o = 0;                       // items so far, steps through
+    uint32_t scored = 0, ph_s = 0, ph_p = 0;      // by place for scores, a bit each: whether any were issued; phases to come
+    bool go = true;
+    // A step's buffers are free when both streams are through with them: its products, or, in a dual item, a look at the steps that are
+    // the other stream's (a stream that did not look at every phase of a barrier could take one for the one after the next).
+    auto score = [&](int x, int place, uint64_t ad) {
+      const int s = x % NR;
+      if (!(go = go && bar_wait(sm, &sm.k_full[s], (uint32_t)(x / NR) & 1u))) return;
       if (elect_one()) {
         after_sync();
-        const uint64_t ad = make_desc_sw128(smem_u32(sm.q[t][0])), bd = make_desc_sw128(smem_u32(sm.k[i & 1][0]));
-#pragma unroll
-        for (int k = 0; k < 8; k++) {
-          const uint64_t off = (uint64_t)(((k & 3) * 32 + (k >> 2) * HALF) >> 4);
-          mma_ss(tmem + S_COL + M * t, ad + off, bd + off, id_s, k != 0);
-        }
-        commit(&sm.s_full[t]);
-      }
-      __syncwarp();
-      n_s[t]++;
-    };
-    auto values = [&](int i, int t, bool acc) {
-      if (elect_one()) {
-        after_sync();
-        const uint64_t bd = make_desc_mn(smem_u32(sm.v[i & 1][0]));
+        const uint64_t bd = make_desc_sw128(smem_u32(sm.k[s][0]));
 #pragma unroll
         for (int k = 0; k < 8; k++)
-          mma_ts(tmem + O_COL + D * t, tmem + S_COL + M * t + 8u * k, bd + (uint64_t)(k * 2048 >> 4), id_o, acc || k != 0);   // 16 tokens further
-        commit(&sm.o_full[t]);
+          mma_ss(s_at + 64u * place, ad + (uint64_t)(((k & 3) * 32 + (k >> 2) * Q_HALF) >> 4), bd + (uint64_t)(((k & 3) * 32 + (k >> 2) * KV_HALF) >> 4), id_s, k != 0);
+        commit(&sm.s_full[t][place]);
+        commit(&sm.k_free[s]);
       }
       __syncwarp();
-      n_o[t]++;
+      scored |= 1u << place;
+      ph_s ^= 1u << place;
     };
-    auto give = [&](unsigned long long* b) {   // a buffer, once the products issued so far are through
-      if (elect_one()) commit(b);
-      __syncwarp();
+    auto pass = [&](int x, bool values) {   // step x is the other stream's
+      const int s = x % NR;
+      if (!(go = go && bar_wait(sm, values ? &sm.v_full[s] : &sm.k_full[s], (uint32_t)(x / NR) & 1u))) return;
+      if (lane == 0) mbar_arrive(values ? &sm.v_free[s] : &sm.k_free[s]);
     };
-    bool go = true;
     for (int i = 0; i < n_my && go;) {
-      const bool two = cur.m * c.group - cur.rt * R > M;
-      const int n = min(cur.nt - cur.tile, n_my - i);
-      go = mbar_wait(sm, &sm.q_full[0], (uint32_t)(n_q[0]++) & 1u) && (!two || mbar_wait(sm, &sm.q_full[1], (uint32_t)(n_q[1]++) & 1u)) &&
-           mbar_wait(sm, &sm.k_full[i & 1], (uint32_t)(i >> 1) & 1u);
-      if (!go) break;
-      score(i, 0);
-      if (two) score(i, 1);
-      give(&sm.k_free[i & 1]);
-      for (int k = 0; k < n && go; k++, i++) {
-        if (!(go = mbar_wait(sm, &sm.p_full[0], (uint32_t)(n_p[0]++) & 1u) && mbar_wait(sm, &sm.v_full[i & 1], (uint32_t)(i >> 1) & 1u))) break;
-        values(i, 0, k > 0);
-        if (k + 1 < n) {
-          if (!(go = mbar_wait(sm, &sm.k_full[(i + 1) & 1], (uint32_t)((i + 1) >> 1) & 1u))) break;
-          score(i + 1, 0);
-        }
-        if (two) {
-          if (!(go = mbar_wait(sm, &sm.p_full[1], (uint32_t)(n_p[1]++) & 1u))) break;
-          values(i, 1, k > 0);
-          if (k + 1 < n) score(i + 1, 1);
-        }
-        give(&sm.v_free[i & 1]);
-        if (k + 1 < n) give(&sm.k_free[(i + 1) & 1]);
+      const bool dual = cur.m * c.group - cur.rt * R <= M;        // both streams have the same rows
+      const int n = min(cur.nt - cur.tile, n_my - i), steps = dual ? n : 2 * n;
+      const int x0 = 2 * i + (dual ? t : 0), dx = dual ? 2 : 1;   // step y is step x0 + dx y of the range
+      const uint64_t ad = make_desc_sw128(smem_u32(sm.q[dual ? 0 : t][0]));
+      go = bar_wait(sm, &sm.q_full[t], (uint32_t)(items++) & 1u);
+      // (in a dual item stream A passes the step before each but the first of its own, and in the end the last one; B the step before each)
+      for (int y = 0; y < min(2, steps); y++) {
+        if (dual && (t || y)) pass(x0 + dx * y - 1, false);
+        score(x0 + dx * y, y, ad);
       }
+      for (int y = 0; y < steps && go; y++) {
+        const int x = x0 + dx * y, s = x % NR, place = y & 1;
+        if (dual && (t || y)) pass(x - 1, true);
+        if (!(go = go && bar_wait(sm, &sm.p_full[t][place], ph_p >> place & 1u) && bar_wait(sm, &sm.v_full[s], (uint32_t)(x / NR) & 1u))) break;
+        ph_p ^= 1u << place;
+        if (elect_one()) {
+          after_sync();
+          const uint64_t bd = make_desc_mn(smem_u32(sm.v[s][0]));
+#pragma unroll
+          for (int k = 0; k < 4; k++)   // 16 tokens further
+            mma_ts(o_at, s_at + 64u * place + 8u * k, bd + (uint64_t)(k * 2048 >> 4), id_o, y > 0 || k != 0);
+          commit(&sm.o_full[t]);
+          commit(&sm.v_free[s]);
+        }
+        __syncwarp();
+        n_o++;
+        if (y + 2 < steps) {
+          if (dual) pass(x + 2 * dx - 1, false);
+          score(x + 2 * dx, place, ad);
+        }
+      }
+      if (dual && t == 0) {
+        pass(x0 + 2 * steps - 1, false);
+        pass(x0 + 2 * steps - 1, true);
+      }
+      i += n;
       cur.next_item(work);
     }
-    for (int t = 0; t < 2; t++) {
-      if (n_s[t] > 0 && !mbar_drain(&sm.s_full[t], (uint32_t)(n_s[t] - 1) & 1u)) sm.tmem_busy = 1;
-      if (n_o[t] > 0 && !mbar_drain(&sm.o_full[t], (uint32_t)(n_o[t] - 1) & 1u)) sm.tmem_busy = 1;
-    }
+#pragma unroll
+    for (int p = 0; p < 2; p++)
+      if ((scored >> p & 1u) && !mbar_drain(&sm.s_full[t][p], (ph_s >> p & 1u) ^ 1u)) sm.tmem_busy = 1;
+    if (n_o > 0 && !mbar_drain(&sm.o_full[t], (uint32_t)(n_o - 1) & 1u)) sm.tmem_busy = 1;
   } else if (warp >= W_CONV) {
     // ------------------------------------------------------------------ codes to fp16: eight lanes to a token, sixteen channels each
     const int ct = tid - 32 * W_CONV, j = ct & 7;
-    for (int i = 0; i < n_my; i++) {
-      const int buf = i & 1;
+    for (int x = 0; x < 2 * n_my; x++) {
+      const int i = x >> 1, half = x & 1, s = x % NR;
+      if (!half) {
+        bar_wait(sm, &sm.info_full[i & 3], (uint32_t)(i >> 2) & 1u);
+        bar_wait(sm, &sm.code_full[0][i & 1], (uint32_t)(i >> 1) & 1u);
+        bar_wait(sm, &sm.code_full[1][i & 1], (uint32_t)(i >> 1) & 1u);
+      }
+      const bool plain = sm.info[i & 3].plain;
+      uint4 w[2][4];
+#pragma unroll
+      for (int side = 0; side < 2; side++)
+#pragma unroll
+        for (int z = 0; z < 4; z++) w[side][z] = *reinterpret_cast<const uint4*>(sm.code[side][i & 1] + (half * PH + 16 * z + (ct >> 3)) * D + 16 * j);
+      // (keys do not wait for the values' place: the scores of a step are wanted two steps before its values)
 #pragma unroll
       for (int side = 0; side < 2; side++) {
-        if (side) mbar_wait(sm, &sm.info_full[i & 3], (uint32_t)(i >> 2) & 1u);
-        mbar_wait(sm, &sm.code_full[side], (uint32_t)i & 1u);
-        if (i >= 2) mbar_wait(sm, side ? &sm.v_free[buf] : &sm.k_free[buf], (uint32_t)((i >> 1) - 1) & 1u);
-        unsigned char* to = side ? sm.v[buf][0] : sm.k[buf][0];
+        if (x >= NR) bar_wait(sm, side ? &sm.v_free[s] : &sm.k_free[s], (uint32_t)(x / NR - 1) & 1u);
 #pragma unroll
-        for (int z = 0; z < 8; z++) {
+        for (int z = 0; z < 4; z++) {
           const int t = 16 * z + (ct >> 3);
-          const uint4 w = *reinterpret_cast<const uint4*>(sm.code[side] + t * D + 16 * j);
-          uint2 h[4] = {codes_to_half(w.x), codes_to_half(w.y), codes_to_half(w.z), codes_to_half(w.w)};
-          if (side) {
-            const float mul = sm.info[i & 3].mul[t >> 5];
-            if (mul != 1.f) {
-              const __half2 m2 = __floats2half2_rn(mul, mul);
+          uint2 h[4] = {codes_to_half(w[side][z].x), codes_to_half(w[side][z].y), codes_to_half(w[side][z].z), codes_to_half(w[side][z].w)};
+          if (side && !plain) {
+            const float mul = sm.info[i & 3].mul[2 * half + (t >> 5)];
+            const __half2 m2 = __floats2half2_rn(mul, mul);
 #pragma unroll
-              for (int e = 0; e < 4; e++) {
-                __half2* y = reinterpret_cast<__half2*>(&h[e]);
-                y[0] = __hmul2(y[0], m2);
-                y[1] = __hmul2(y[1], m2);
-              }
+            for (int e = 0; e < 4; e++) {
+              __half2* y = reinterpret_cast<__half2*>(&h[e]);
+              y[0] = __hmul2(y[0], m2);
+              y[1] = __hmul2(y[1], m2);
             }
           }
           // chunks 2 (j & 3) and the next of the row's 64 channels; the two halves' lanes in opposite order, for the banks' sake
-          unsigned char* row = to + (j >> 2) * HALF + t * 128;
+          unsigned char* row = (side ? sm.v[s][0] : sm.k[s][0]) + (j >> 2) * KV_HALF + t * 128;
           const int a0 = (2 * (j & 3)) ^ (t & 7), a1 = (2 * (j & 3) + 1) ^ (t & 7);
           const uint4 y0 = make_uint4(h[0].x, h[0].y, h[1].x, h[1].y), y1 = make_uint4(h[2].x, h[2].y, h[3].x, h[3].y);
           *reinterpret_cast<uint4*>(row + (j < 4 ? a0 : a1) * 16) = j < 4 ? y0 : y1;
@@ -440,100 +455,141 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
         fence_async_smem();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(side ? &sm.v_full[buf] : &sm.k_full[buf]);
-          mbar_arrive(&sm.code_free[side]);
+          mbar_arrive(side ? &sm.v_full[s] : &sm.k_full[s]);
+          if (half) mbar_arrive(&sm.code_free[side][i & 1]);
         }
       }
     }
   } else {
     // ------------------------------------------------------------------ softmax: lane = row (after a timeout they run on, waits failing at once)
-    const int t = warp >> 2, quarter = warp & 3, row0 = M * t + 32 * quarter;
-    const uint32_t lanes = (uint32_t)(32 * quarter) << 16, s_at = tmem + S_COL + M * t + lanes, o_at = tmem + O_COL + D * t + lanes;
-    int n_s = 0, n_o = 0;
+    const int t = warp >> 2, quarter = warp & 3;
+    const uint32_t lanes = (uint32_t)(32 * quarter) << 16, s_at = tmem + S_COL + 128u * t + lanes, o_at = tmem + O_COL + 128u * t + lanes;
+    int n_s[2] = {0, 0}, n_o = 0;
     bool whole = cur.tile == 0, began = cur.tile != 0;
     if (!heads.by_item && tid == 0) a.heads[v].more = 0;
     for (int i = 0; i < n_my;) {
       const int n = min(cur.nt - cur.tile, n_my - i), rows = cur.m * c.group - cur.rt * R;
-      const bool ends = cur.tile + n == cur.nt, active = rows > M * t;
-      const int row = row0 + lane, last_seen = cur.len - cur.m + (cur.rt * R + row) / c.group;   // last token that the row sees
-      const int least = cur.len - cur.m + (cur.rt * R + row0) / c.group;                         // .. that the warp's first row sees
+      const bool ends = cur.tile + n == cur.nt, dual = rows <= M;
+      const int row0 = (dual ? 0 : M * t) + 32 * quarter, row = row0 + lane, steps = dual ? n : 2 * n;
+      // (the stream's own products of the item before are through)
+      // (stream B of a dual item takes its rows' factors only: its place holds the item's statistics in the end)
+      const float back = prepare_queries<T>(a, cur, row0, sm.q[t][0], !dual || t == 0, lane);
+      fence_async_smem();
+      if (dual) asm volatile("bar.sync 1, 256;\n" ::: "memory");   // stream A's queries are B's too
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.q_full[t]);
+      const int last_seen = cur.len - cur.m + (cur.rt * R + row) / c.group;   // last token that the row sees
+      const int least = cur.len - cur.m + (cur.rt * R + row0) / c.group;      // .. that the warp's first row sees
       float m = -INFINITY, l = 0.f, vref = 1.f;
-      if (active) {
-        // (the tile's own products of the item before are through)
-        const float back = prepare_queries<T>(a, cur, row0, sm.q[t][0], lane);
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.q_full[t]);
-        for (int k = 0; k < n; k++) {
-          const int tile = cur.tile + k, at = tile * PT;
-          mbar_wait(sm, &sm.info_full[(i + k) & 3], (uint32_t)((i + k) >> 2) & 1u);
-          const Info& info = sm.info[(i + k) & 3];
-          mbar_wait(sm, &sm.s_full[t], (uint32_t)(n_s++) & 1u);
-          after_sync();
-          const bool edge = at + PT - 1 > least || info.lost;
-          const float mx = edge ? row_max<true>(s_at, info, back, last_seen - at) : row_max<false>(s_at, info, back, last_seen - at);
-          // a new reference: the row's sums so far are multiplied
-          const float fv = info.fv;
-          vref = info.vref;
-          const bool passed = mx > m;
-          if (__any_sync(0xffffffffu, passed) || (fv != 1.f && k > 0)) {
-            const float mn = passed ? mx + LEAD : m, f = passed ? ex2(m - mn) : 1.f;   // (0 for the first)
-            m = mn;
-            l *= f;
-            if (k > 0) {
-#pragma unroll 1
-              for (int b = 0; b < 4; b++) {
-                float x[32];
-                tmem_ld32(o_at + 32u * b, x);
-                tmem_wait_ld();
-#pragma unroll
-                for (int e = 0; e < 32; e++) x[e] *= f * fv;
-                tmem_st32(o_at + 32u * b, x);
-              }
-              tmem_wait_st();
-            }
-          }
-          const float ref = m == -INFINITY ? 0.f : m;
-          l = edge ? numerators<true>(s_at, info, back, ref, last_seen - at, l) : numerators<false>(s_at, info, back, ref, last_seen - at, l);
-          tmem_wait_st();
-          before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sm.p_full[t]);
-        }
-        n_o += n;
-        mbar_wait(sm, &sm.o_full[t], (uint32_t)(n_o - 1) & 1u);
+      for (int y = 0; y < steps; y++) {
+        const int k = dual ? y : y >> 1, half = dual ? t : y & 1, place = y & 1, at = (cur.tile + k) * PT + PH * half;
+        const uint32_t p_at = s_at + 64u * place;
+        bar_wait(sm, &sm.info_full[(i + k) & 3], (uint32_t)((i + k) >> 2) & 1u);
+        const Info& info = sm.info[(i + k) & 3];
+        bar_wait(sm, &sm.s_full[t][place], (uint32_t)(place ? n_s[1]++ : n_s[0]++) & 1u);
         after_sync();
-        if (sm.abort) l = NAN;
-        const bool direct = whole && ends;
-        float* slot = a.slots + (size_t)(2 * v + (began ? 0 : 1)) * SLOT;
-        const float unit = vref * (1.f / 16384.f), f = direct ? (l == 0.f ? 0.f : unit / l) : unit;
-        const bool there = row < rows;
-        T* dst = there && direct ? out_row<T>(a, cur.pair, cur.h, cur.rt * R + row) : nullptr;
+        float x[2][32];
+        tmem_ld32(p_at, x[0]);
+        tmem_ld32(p_at + 32u, x[1]);
+        const bool edge = at + PH - 1 > least || info.lost;
+        tmem_wait_ld();
+        const float mx = edge ? row_max<true>(x, info, 2 * half, back, last_seen - at) : row_max<false>(x, info, 2 * half, back, last_seen - at);
+        // a new reference: the row's sums so far are multiplied, once their last product is through
+        const float fv = dual || !half ? info.fv : 1.f;
+        vref = info.vref;
+        const bool passed = mx > m;
+        if (__any_sync(0xffffffffu, passed) || (fv != 1.f && y > 0)) {
+          const float mn = passed ? mx + LEAD : m, f = passed ? ex2(m - mn) : 1.f;   // (0 for the first)
+          m = mn;
+          l *= f;
+          if (y > 0) {
+            bar_wait(sm, &sm.o_full[t], (uint32_t)(n_o + y - 1) & 1u);
+            after_sync();
+#pragma unroll 1
+            for (int b = 0; b < 8; b++) {
+              float o[16];
+              tmem_ld16(o_at + 16u * b, o);
+              tmem_wait_ld();
 #pragma unroll
-        for (int b = 0; b < 4; b++) {
-          float x[32];
-          tmem_ld32(o_at + 32u * b, x);
-          tmem_wait_ld();
-          if (!there) continue;
-          if (direct) {
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-              Vec8<T> y;
-#pragma unroll
-              for (int z = 0; z < 8; z++) y.v[z] = from_f<T>(x[8 * e + z] * f);
-              *reinterpret_cast<Vec8<T>*>(dst + 32 * b + 8 * e) = y;
+              for (int e = 0; e < 16; e++) o[e] *= f * fv;
+              tmem_st16(o_at + 16u * b, reinterpret_cast<const uint32_t(&)[16]>(o));
             }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; e++)
-              *reinterpret_cast<float4*>(slot + (size_t)row * D + 32 * b + 4 * e) = make_float4(x[4 * e] * f, x[4 * e + 1] * f, x[4 * e + 2] * f, x[4 * e + 3] * f);
           }
         }
+        const float ref = m == -INFINITY ? 0.f : m;
+        l = edge ? numerators<true>(x, p_at, info, 2 * half, back, ref, last_seen - at, l)
+                 : numerators<false>(x, p_at, info, 2 * half, back, ref, last_seen - at, l);
+        tmem_wait_st();
         before_sync();
-        if (there && !direct) { slot[(size_t)R * D + row] = m; slot[(size_t)R * D + R + row] = l; }
+        __syncwarp();
+        // Phases of o_full are told apart by one bit: the last but one is waited for while the last cannot be complete, since all that is
+        // known without a wait is that the third last is.
+        if (y > 0 && y + 1 == steps) bar_wait(sm, &sm.o_full[t], (uint32_t)(n_o + y - 1) & 1u);
+        if (lane == 0) mbar_arrive(&sm.p_full[t][place]);
       }
+      n_o += steps;
+      bar_wait(sm, &sm.o_full[t], (uint32_t)(n_o - 1) & 1u);
+      if (sm.abort) l = NAN;
+      float f = 1.f, f_other = 0.f;
+      if (dual) {
+        const int r = 32 * quarter + lane;
+        float2* stat = reinterpret_cast<float2*>(sm.q[1][0]);
+        stat[M * t + r] = make_float2(m, l);
+        before_sync();
+        asm volatile("bar.sync 1, 256;\n" ::: "memory");   // both streams' sums are complete
+        const float2 y = stat[M * (t ^ 1) + r];
+        const float mn = fmaxf(m, y.x), at = mn == -INFINITY ? 0.f : mn;
+        f = ex2(m - at);
+        f_other = ex2(y.x - at);
+        l = l * f + y.y * f_other;
+        m = mn;
+      }
+      after_sync();
+      const bool direct = whole && ends;
+      float* slot = a.slots + (size_t)(2 * v + (began ? 0 : 1)) * SLOT;
+      float unit = vref * (1.f / 16384.f);
+      if (direct) unit = l == 0.f ? 0.f : unit / l;
+      f *= unit;
+      f_other *= unit;
+      const bool there = row < rows;
+      T* dst = there && direct ? out_row<T>(a, cur.pair, cur.h, cur.rt * R + row) : nullptr;
+      // (a dual item's streams have 64 channels each)
+      const uint32_t o_own = tmem + O_COL + lanes;
+#pragma unroll 1
+      for (int b = dual ? 4 * t : 0; b < (dual ? 4 * t + 4 : 8); b++) {
+        float x[16];
+        tmem_ld16(o_at + 16u * b, x);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 16; e++) x[e] *= f;
+        if (dual) {
+          float y[16];
+          tmem_ld16(o_own + 128u * (t ^ 1) + 16u * b, y);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; e++) x[e] = fmaf(y[e], f_other, x[e]);
+        }
+        if (!there) continue;
+        if (direct) {
+#pragma unroll
+          for (int e = 0; e < 2; e++) {
+            Vec8<T> y;
+#pragma unroll
+            for (int z = 0; z < 8; z++) y.v[z] = from_f<T>(x[8 * e + z]);
+            *reinterpret_cast<Vec8<T>*>(dst + 16 * b + 8 * e) = y;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; e++)
+            *reinterpret_cast<float4*>(slot + (size_t)row * D + 16 * b + 4 * e) = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+        }
+      }
+      before_sync();
+      if (there && !direct && (!dual || t == 0)) { slot[(size_t)R * D + row] = m; slot[(size_t)R * D + R + row] = l; }
+      if (dual) asm volatile("bar.sync 1, 256;\n" ::: "memory");   // the next item's products may replace the sums
       if (!began && (heads.by_item || !ends) && tid == 0)
-        a.heads[heads.at(v, c.n_kv, cur.pair, cur.h, cur.rt)] = Head{ends ? 0 : cuts.range_of(g0 + i - cur.tile + cur.nt - 1) - v, v, cur.pair, cur.h, cur.rt, {}};
+        a.heads[heads.at(v, c.n_kv, cur.pair, cur.h, cur.rt)] =
+            Head{ends ? 0 : cuts.range_of(g0 + i - cur.tile + cur.nt - 1) - v, v, cur.pair, cur.h, cur.rt, {}};
       whole = true;
       began = false;
       i += n;
