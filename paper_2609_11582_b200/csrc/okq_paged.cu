@@ -55,11 +55,103 @@ __device__ __forceinline__ Quotient quotient_by(float scale) {
   return Quotient{scale, __fdiv_rn(1.f, scale), !(scale > 0.f) ? 0 : scale >= 7.9e-31f ? 1 : 2};
 }
 
+// One block's keys and values by NT threads: thread tid has row tid / 8, two chunks of eight channels of either side.
+struct Chunks {
+  int t, j, c0, c1;
+  bool turns;
+  // (the chunks that a rotated pair of channels lies in, as okq_rope_apply deals them)
+  __device__ __forceinline__ Chunks(int tid, const RopeView& rope) : t(tid >> 3), j(tid & 7) {
+    const int nc = rope.half >> 3;
+    turns = rope.freq && j < nc;
+    c0 = !rope.freq || j < nc ? 8 * j : 2 * rope.half + 16 * (j - nc);
+    c1 = !rope.freq ? c0 + 64 : j < nc ? c0 + rope.half : c0 + 8;
+  }
+};
+template <class T> struct BlockRows { Vec8<T> x[2][2]; };
+// block blk of the `m` new tokens behind `len`
+template <class T>
+__device__ __forceinline__ void load_block(const PagedView& c, int l, int li, int b, int h, int len, int m, int blk, const Rows& k, const Rows& v,
+                                           const Chunks& at, BlockRows<T>& y) {
+  const int first = len - len % PB + blk * PB, rows = min(PB, len + m - first), i = first + at.t - len;   // i: among the new tokens, negative for raw ones
+#pragma unroll
+  for (int side = 0; side < 2; side++) {
+    if (at.t < rows) {
+      const T* src = i < 0 ? c.raw_of<T>(l, b, h, side) + (size_t)at.t * D : (side ? v : k).at<T>(li, b, h, i);
+      y.x[side][0] = *reinterpret_cast<const Vec8<T>*>(src + at.c0);
+      y.x[side][1] = *reinterpret_cast<const Vec8<T>*>(src + at.c1);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; e++) y.x[side][0].v[e] = y.x[side][1].v[e] = from_f<T>(0.f);
+    }
+  }
+}
+template <class T>
+__device__ __forceinline__ void store_block(const PagedView& c, int l, int b, int h, int len, int m, int blk, int n_new, const RopeView& rope,
+                                            const Chunks& at, BlockRows<T>& y, unsigned (*top)[NT / 32]) {
+  const int first = len - len % PB + blk * PB, rows = min(PB, len + m - first), i = first + at.t - len;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const bool there = at.t < rows;
+  auto& x = y.x;
+  if (at.turns && there && i >= 0) {
+    float cs[8], sn[8];
+    turns8(rope, rope.positions + (size_t)b * n_new + i, (size_t)c.batch * n_new, at.c0, cs, sn);
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      float u = to_f(x[0][0].v[e]), w = to_f(x[0][1].v[e]);
+      rotate_pair(u, w, cs[e], sn[e]);
+      x[0][0].v[e] = from_f<T>(u);
+      x[0][1].v[e] = from_f<T>(w);
+    }
+  }
+  // magnitudes as integers: their order is the numbers' own, with infinities and NaN at the top
+#pragma unroll
+  for (int side = 0; side < 2; side++) {
+    unsigned mx = 0;
+#pragma unroll
+    for (int e = 0; e < 16; e++) mx = max(mx, __float_as_uint(to_f(x[side][e >> 3].v[e & 7])) & 0x7fffffffu);
+    mx = __reduce_max_sync(0xffffffffu, mx);
+    if (lane == 0) top[side][warp] = mx;
+  }
+  __syncthreads();
+  const int page = c.page_of(b, first);
+#pragma unroll
+  for (int side = 0; side < 2; side++) {
+    unsigned mx = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 32; w++) mx = max(mx, top[side][w]);
+    const float amax = __uint_as_float(mx);
+    float scale = __fdiv_rn(amax, 127.f);
+    if (mx >= 0x7f800000u) scale = __uint_as_float(0x7fc00000u);   // infinities, NaN
+    const Quotient by = quotient_by(scale);
+    const size_t row = c.code_row(l, page, h, side) + (first & (c.page - 1));
+    if (there) {
+      int8_t* dst = c.codes + (row + at.t) * D;
+#pragma unroll
+      for (int half = 0; half < 2; half++) {
+        uint32_t q[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) q[e] = by.code(to_f(x[side][half].v[e]));
+        uint2 w;
+        w.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+        w.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+        *reinterpret_cast<uint2*>(dst + (half ? at.c1 : at.c0)) = w;
+      }
+      if (rows < PB && i >= 0) {   // a block that stays unfinished
+        T* keep = c.raw_of<T>(l, b, h, side) + (size_t)at.t * D;
+        *reinterpret_cast<Vec8<T>*>(keep + at.c0) = x[side][0];
+        *reinterpret_cast<Vec8<T>*>(keep + at.c1) = x[side][1];
+      }
+    }
+    if (tid == side) c.scales[row / PB] = scale;
+  }
+}
+
 template <class T>
 __global__ void __launch_bounds__(NT) k_paged_append(const PagedView c, int layer, const Rows k, const Rows v, int n_new, const int32_t* new_len,
                                                      const RopeView rope, int n_blocks) {
+  __shared__ unsigned top[2][NT / 32];
   depend_wait();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x;
   long long u = blockIdx.x;
   int blk = (int)(u % n_blocks);
   u /= n_blocks;
@@ -73,85 +165,48 @@ __global__ void __launch_bounds__(NT) k_paged_append(const PagedView c, int laye
   const int last = (r + m - 1) / PB;
   const bool follows = r > 0 && last > 0 && (r + m) % PB != 0;
   if (follows && blk == last) return;
-
-  // thread: row t = tid / 8, two chunks of eight channels, keys and values (the chunks that a rotated pair of channels lies in, as
-  // okq_rope_apply deals them)
-  const int t = tid >> 3, j = tid & 7, nc = rope.half >> 3;
-  const bool turns = rope.freq && j < nc;
-  const int c0 = !rope.freq || j < nc ? 8 * j : 2 * rope.half + 16 * (j - nc);
-  const int c1 = !rope.freq ? c0 + 64 : j < nc ? c0 + rope.half : c0 + 8;
-  __shared__ unsigned top[2][NT / 32];
+  const Chunks at(tid, rope);
+  BlockRows<T> y;
   for (;; blk = last) {
-    const int first = len - r + blk * PB, rows = min(PB, end - first);
-    const int i = first + t - len;    // number among the new tokens, negative for raw ones
-    const bool there = t < rows;
-    Vec8<T> x[2][2];
-#pragma unroll
-    for (int side = 0; side < 2; side++) {
-      if (there) {
-        const T* src = i < 0 ? c.raw_of<T>(l, b, h, side) + (size_t)t * D : (side ? v : k).at<T>(li, b, h, i);
-        x[side][0] = *reinterpret_cast<const Vec8<T>*>(src + c0);
-        x[side][1] = *reinterpret_cast<const Vec8<T>*>(src + c1);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; e++) x[side][0].v[e] = x[side][1].v[e] = from_f<T>(0.f);
-      }
-    }
-    if (turns && there && i >= 0) {
-      float cs[8], sn[8];
-      turns8(rope, rope.positions + (size_t)b * n_new + i, (size_t)c.batch * n_new, c0, cs, sn);
-#pragma unroll
-      for (int e = 0; e < 8; e++) {
-        float a = to_f(x[0][0].v[e]), d = to_f(x[0][1].v[e]);
-        rotate_pair(a, d, cs[e], sn[e]);
-        x[0][0].v[e] = from_f<T>(a);
-        x[0][1].v[e] = from_f<T>(d);
-      }
-    }
-    // magnitudes as integers: their order is the numbers' own, with infinities and NaN at the top
-#pragma unroll
-    for (int side = 0; side < 2; side++) {
-      unsigned mx = 0;
-#pragma unroll
-      for (int e = 0; e < 16; e++) mx = max(mx, __float_as_uint(to_f(x[side][e >> 3].v[e & 7])) & 0x7fffffffu);
-      mx = __reduce_max_sync(0xffffffffu, mx);
-      if (lane == 0) top[side][warp] = mx;
-    }
-    __syncthreads();
-    const int page = c.page_of(b, first);
-#pragma unroll
-    for (int side = 0; side < 2; side++) {
-      unsigned mx = 0;
-#pragma unroll
-      for (int w = 0; w < NT / 32; w++) mx = max(mx, top[side][w]);
-      const float amax = __uint_as_float(mx);
-      float scale = __fdiv_rn(amax, 127.f);
-      if (mx >= 0x7f800000u) scale = __uint_as_float(0x7fc00000u);   // infinities, NaN
-      const Quotient by = quotient_by(scale);
-      const size_t row = c.code_row(l, page, h, side) + (first & (c.page - 1));
-      if (there) {
-        int8_t* dst = c.codes + (row + t) * D;
-#pragma unroll
-        for (int half = 0; half < 2; half++) {
-          uint32_t q[8];
-#pragma unroll
-          for (int e = 0; e < 8; e++) q[e] = by.code(to_f(x[side][half].v[e]));
-          uint2 w;
-          w.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
-          w.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
-          *reinterpret_cast<uint2*>(dst + (half ? c1 : c0)) = w;
-        }
-        if (rows < PB && i >= 0) {   // a block that stays unfinished
-          T* keep = c.raw_of<T>(l, b, h, side) + (size_t)t * D;
-          *reinterpret_cast<Vec8<T>*>(keep + c0) = x[side][0];
-          *reinterpret_cast<Vec8<T>*>(keep + c1) = x[side][1];
-        }
-      }
-      if (tid == side) c.scales[row / PB] = scale;
-    }
+    load_block<T>(c, l, li, b, h, len, m, blk, k, v, at, y);
+    store_block<T>(c, l, b, h, len, m, blk, n_new, rope, at, y, top);
     if (!follows || blk != 0) return;
     __syncthreads();
   }
+}
+
+// The same for up to FEW new tokens (two blocks of a sequence at most) in one launch: a cluster has a (layer, sequence), each of its
+// blocks every MOST-th head, and the length is advanced when all of them have read it.
+constexpr int FEW = PB, MOST = 8;
+template <class T>
+__global__ void __launch_bounds__(NT) k_paged_append_few(const PagedView c, int layer, const Rows k, const Rows v, int n_new, const int32_t* new_len,
+                                                         const RopeView rope, int size) {
+  __shared__ unsigned top[2][2][NT / 32];
+  depend_wait();
+  const int tid = threadIdx.x, rank = blockIdx.x % size, u = blockIdx.x / size, b = u % c.batch, li = u / c.batch, l = layer + li;
+  const int m = count_of(new_len, b, n_new), len = c.held(l, b), r = len % PB;
+  if (m == 0) return;                       // (the whole cluster)
+  const int bad = __syncthreads_or(pages_missing(c, b, len, m, tid, NT));
+  if (!bad) {
+    const Chunks at(tid, rope);
+    const int last = (r + m - 1) / PB;      // 0 or 1
+    int turn = 0;
+    for (int h = rank; h < c.n_kv; h += size)
+      for (int blk = 0; blk <= last; blk++, turn ^= 1) {
+        BlockRows<T> y;
+        load_block<T>(c, l, li, b, h, len, m, blk, k, v, at, y);
+        store_block<T>(c, l, b, h, len, m, blk, n_new, rope, at, y, top[turn]);   // (its barrier is behind the loads: raw tokens are read before they are replaced)
+      }
+  }
+  if (size > 1) {
+    asm volatile("barrier.cluster.arrive.aligned;\n" ::: "memory");
+    asm volatile("barrier.cluster.wait.aligned;\n" ::: "memory");
+  } else {
+    __syncthreads();
+  }
+  if (tid != 0 || rank != 0) return;
+  if (bad) set_status(c.status, OKQ_ERR_CAPACITY);
+  else c.seq_len[(size_t)l * c.batch + b] = len + m;
 }
 
 // lengths after an append, and the status of sequences that could not take theirs; one warp per (layer, sequence)
@@ -209,6 +264,11 @@ okq_status failed(cudaError_t e) {
 template <class T>
 okq_status launch_append(const PagedView& c, int layer, int layer_count, const Rows& k, const Rows& v, int n_new, const int32_t* new_len,
                          const RopeView& rope, cudaStream_t s) {
+  if (n_new <= FEW) {
+    const int size = c.n_kv < MOST ? c.n_kv : MOST;
+    const cudaError_t e = launch_dependent(k_paged_append_few<T>, dim3((unsigned)(layer_count * c.batch * size)), NT, 0, s, size, c, layer, k, v, n_new, new_len, rope, size);
+    return e != cudaSuccess ? failed(e) : launch_status();
+  }
   const int n_blocks = (PB - 1 + n_new + PB - 1) / PB;
   const long long grid = (long long)layer_count * c.batch * c.n_kv * n_blocks;
   if (grid > 0x7fffffffll) return OKQ_ERR_UNSUPPORTED;
