@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -148,20 +149,19 @@ def lib():
         L.okq_turboquant_encode.argtypes = [C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         L.okq_turboquant_decode.restype = C.c_int
         L.okq_turboquant_decode.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
-        paged, i32, ptr, rope = C.POINTER(okq_paged), C.c_int32, C.c_void_p, C.POINTER(okq_rope)
+        paged, i32, ptr = C.POINTER(okq_paged), C.c_int32, C.c_void_p   # (ptr: also strides and small structs, as packed bytes)
         L.okq_paged_sizes.restype = C.c_int
         L.okq_paged_sizes.argtypes = [paged, C.POINTER(C.c_size_t)]
         L.okq_paged_workspace_bytes.restype = C.c_size_t
         L.okq_paged_workspace_bytes.argtypes = [paged, i32, i32]
         L.okq_rope_apply.restype = C.c_int
-        L.okq_rope_apply.argtypes = [rope, i32, i32, i32, C.POINTER(okq_rope_tensor), C.POINTER(okq_rope_tensor), i32, ptr]
+        L.okq_rope_apply.argtypes = [ptr, i32, i32, i32, ptr, ptr, i32, ptr]
         L.okq_paged_append.restype = C.c_int
-        L.okq_paged_append.argtypes = [paged, i32, i32, ptr, C.POINTER(C.c_int64), ptr, C.POINTER(C.c_int64), i32, ptr, rope, ptr]
+        L.okq_paged_append.argtypes = [paged, i32, i32, ptr, ptr, ptr, ptr, i32, ptr, ptr, ptr]
         L.okq_paged_read.restype = C.c_int
         L.okq_paged_read.argtypes = [paged, i32, i32, i32, i32, ptr, ptr, ptr]
         L.okq_paged_attention.restype = C.c_int
-        L.okq_paged_attention.argtypes = [paged, i32, i32, ptr, C.POINTER(C.c_int64), i32, ptr, rope, C.c_float, ptr, C.c_size_t, ptr,
-                                          C.POINTER(C.c_int64), ptr]
+        L.okq_paged_attention.argtypes = [paged, i32, i32, ptr, ptr, i32, ptr, ptr, C.c_float, ptr, C.c_size_t, ptr, ptr, ptr]
         L.okq_pages_reserve.restype = C.c_int
         L.okq_pages_reserve.argtypes = [paged, ptr, ptr]
         L.okq_pages_fork.restype = C.c_int
@@ -497,7 +497,9 @@ def turboquant_decode(codes: torch.Tensor, norms: torch.Tensor, signs: torch.Ten
 
 # ---------------------------------------------------------------- 8-bit paged cache and rotary positions (okq_paged.h)
 DTYPE_CODES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
-_I64x3, _I64x4 = C.c_int64 * 3, C.c_int64 * 4
+_strides4 = struct.Struct("4q").pack                 # int64_t[4]
+_rope_struct = struct.Struct("4i2Q").pack            # okq_rope
+_rope_tensor_struct = struct.Struct("2Q6qi4x").pack  # okq_rope_tensor
 
 
 def _here(*tensors):
@@ -565,8 +567,7 @@ class Rope:
         assert freq.dtype == torch.float64 and freq.numel() == sum(sections) and freq.is_contiguous()
         self.positions, self.freq = positions, freq
         self.batch, self.n = positions.shape[1], positions.shape[2]
-        self.c = okq_rope((C.c_int32 * 3)(*sections), 1 if interleaved else 0, freq.data_ptr(), positions.data_ptr())
-        self.ref = C.byref(self.c)
+        self.ref = _rope_struct(*sections, 1 if interleaved else 0, freq.data_ptr(), positions.data_ptr())
 
 
 def _rope_ref(rope, batch, n):
@@ -576,41 +577,42 @@ def _rope_ref(rope, batch, n):
     return rope.ref
 
 
-def _rope_tensor(x, out):
-    assert x.dim() == 4 and x.shape == out.shape and x.dtype == out.dtype and x.shape[3] == HEAD_DIM
+def _rope_tensor(x, out, dtype, shape):
     xs, os = x.stride(), out.stride()
-    assert xs[3] == 1 and os[3] == 1
-    return C.byref(okq_rope_tensor(x.data_ptr(), out.data_ptr(), xs[:3], os[:3], x.shape[1]))
+    assert x.shape == out.shape == shape and x.dtype == out.dtype == dtype and xs[3] == os[3] == 1
+    return _rope_tensor_struct(x.data_ptr(), out.data_ptr(), xs[0], xs[1], xs[2], os[0], os[1], os[2], shape[1])
 
 
 def rope_apply(rope: Rope, q, q_out, k=None, k_out=None, inverse=False, stream=None):
     """Rotates q and k, [batch, heads, n, 128] of fp16, bf16 or fp32 (last dim contiguous, any other strides), into q_out and k_out
     (which may be the inputs).  inverse=True is the transpose: gradients of the outputs in, gradients of the inputs out."""
     _here(q, q_out, k, k_out, rope.positions, rope.freq)
-    batch, _, n, _ = q.shape
-    assert (rope.batch, rope.n) == (batch, n) and (k is None or (k.dtype == q.dtype and k.shape[0] == batch and k.shape[2] == n))
-    st = (_lib or lib()).okq_rope_apply(rope.ref, DTYPE_CODES[q.dtype], batch, n, _rope_tensor(q, q_out),
-                                        None if k is None else _rope_tensor(k, k_out), 1 if inverse else 0, _stream(stream))
+    batch, heads, n, _ = q.shape
+    dtype = q.dtype
+    assert (rope.batch, rope.n) == (batch, n), "positions are [3, batch, n] of the call's own tokens"
+    q_ref = _rope_tensor(q, q_out, dtype, (batch, heads, n, HEAD_DIM))
+    k_ref = None if k is None else _rope_tensor(k, k_out, dtype, (batch, k.shape[1], n, HEAD_DIM))
+    st = (_lib or lib()).okq_rope_apply(rope.ref, DTYPE_CODES[dtype], batch, n, q_ref, k_ref, 1 if inverse else 0, _stream(stream))
     if st != OK:
         raise OkqError(st, "okq_rope_apply")
 
 
-def _rows(cache, x, layer_count, heads):
+def _rows(cache, x, layer_count, heads, n):
     """Strides of a [layer_count, batch, heads, n, 128] tensor of the cache's dtype."""
     s = x.stride()
-    assert x.dtype == cache.dtype and x.dim() == 5 and s[4] == 1
-    assert x.shape[0] == layer_count and x.shape[1] == cache.batch and x.shape[2] == heads and x.shape[4] == HEAD_DIM
-    return _I64x4(*s[:4])
+    assert x.dtype == cache.dtype and x.shape == (layer_count, cache.batch, heads, n, HEAD_DIM) and s[4] == 1
+    return _strides4(s[0], s[1], s[2], s[3])
 
 
 def paged_append(cache: PagedCache, layer: int, layer_count: int, k, v, new_len=None, rope=None, stream=None):
     """k, v: [layer_count, batch, n_kv_heads, n_new, 128]; new_len: int32 [batch], new tokens of each sequence (all n_new without it);
     rope: a Rope of [3, batch, n_new] positions that the keys are given first."""
     _here(cache.codes, k, v, new_len, None if rope is None else rope.positions)
-    assert k.shape == v.shape and (new_len is None or (new_len.dtype == torch.int32 and new_len.is_contiguous()))
-    st = (_lib or lib()).okq_paged_append(cache.ref, layer, layer_count, k.data_ptr(), _rows(cache, k, layer_count, cache.n_kv_heads), v.data_ptr(),
-                                          _rows(cache, v, layer_count, cache.n_kv_heads), k.shape[3], _ptr(new_len),
-                                          _rope_ref(rope, cache.batch, k.shape[3]), _stream(stream))
+    n = k.shape[3]
+    assert new_len is None or (new_len.dtype == torch.int32 and new_len.is_contiguous() and new_len.numel() == cache.batch)
+    st = (_lib or lib()).okq_paged_append(cache.ref, layer, layer_count, k.data_ptr(), _rows(cache, k, layer_count, cache.n_kv_heads, n),
+                                          v.data_ptr(), _rows(cache, v, layer_count, cache.n_kv_heads, n), n, _ptr(new_len),
+                                          _rope_ref(rope, cache.batch, n), _stream(stream))
     if st != OK:
         raise OkqError(st, "okq_paged_append")
 
@@ -632,12 +634,12 @@ def paged_attention(cache: PagedCache, layer: int, layer_count: int, q, workspac
     """q, out: [layer_count, batch, n_q_heads, n_new, 128] of the cache's dtype (last dim contiguous); the queries are those of each
     sequence's newest n_new (q_len[b] with q_len, int32 [batch]) tokens; rope: a Rope that the queries are given first."""
     _here(cache.codes, q, workspace, out, q_len, None if rope is None else rope.positions)
-    assert q.shape == out.shape and (q_len is None or (q_len.dtype == torch.int32 and q_len.is_contiguous()))
-    st = (_lib or lib()).okq_paged_attention(cache.ref, layer, layer_count, q.data_ptr(), _rows(cache, q, layer_count, cache.n_q_heads), q.shape[3],
-                                             _ptr(q_len), _rope_ref(rope, cache.batch, q.shape[3]),
-                                             HEAD_DIM ** -0.5 if sm_scale is None else sm_scale, _ptr(workspace),
-                                             0 if workspace is None else workspace.nbytes, out.data_ptr(),
-                                             _rows(cache, out, layer_count, cache.n_q_heads), _stream(stream))
+    n = q.shape[3]
+    assert q_len is None or (q_len.dtype == torch.int32 and q_len.is_contiguous() and q_len.numel() == cache.batch)
+    st = (_lib or lib()).okq_paged_attention(cache.ref, layer, layer_count, q.data_ptr(), _rows(cache, q, layer_count, cache.n_q_heads, n), n,
+                                             _ptr(q_len), _rope_ref(rope, cache.batch, n), HEAD_DIM ** -0.5 if sm_scale is None else sm_scale,
+                                             _ptr(workspace), 0 if workspace is None else workspace.nbytes, out.data_ptr(),
+                                             _rows(cache, out, layer_count, cache.n_q_heads, n), _stream(stream))
     if st != OK:
         raise OkqError(st, "okq_paged_attention")
 
