@@ -52,7 +52,7 @@ template <int ROWS> struct Work {
   const AttnArgs& a;
   __device__ __forceinline__ explicit Work(const AttnArgs& args) : pairs(args.layer_count * args.c.batch), n_kv(args.c.n_kv), group(args.c.group), a(args) {}
   __device__ __forceinline__ void lens(int pair, int& len, int& m) const {   // tokens held, queries
-    const int li = pair / a.c.batch, b = pair - li * a.c.batch;
+    const int li = a.layer_count == 1 ? 0 : pair / a.c.batch, b = pair - li * a.c.batch;
     const int n = a.c.seq_len[(size_t)(a.layer + li) * a.c.batch + b], q = a.q_len ? a.q_len[b] : a.n_new;   // (both loads before either is used)
     len = max(0, min(n, a.c.room()));
     m = max(0, min(q, a.n_new));
@@ -110,17 +110,17 @@ struct Cuts {
 // consecutive pairs.
 template <int G> struct FindSmem {
   int warp[32];
-  int place[G][4];
+  int place[G][6];
 };
 template <int ROWS, int NT, int G>
 __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS>& w, int ranges, int v0, int step) {
   const int tid = threadIdx.x, lane = tid & 31, wp = tid >> 5;
   const int chunk = (w.pairs + NT - 1) / NT, p0 = min(w.pairs, tid * chunk), p1 = min(w.pairs, p0 + chunk);
-  int mine = 0;
+  int len = 0, m = 0, per_head = 0, mine = 0;    // (of the last pair looked at: with no more pairs than threads, the only one)
   for (int p = p0; p < p1; p++) {
-    int len, m;
     w.lens(p, len, m);
-    mine += w.head_tiles(len, m) * w.n_kv;
+    per_head = w.head_tiles(len, m);
+    mine += per_head * w.n_kv;
   }
   int v = mine;
 #pragma unroll
@@ -138,22 +138,24 @@ __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS>& w
     total += x;
   }
   const Cuts cuts(total, ranges);
+  if (mine > 0) {
 #pragma unroll
-  for (int g = 0; g < G; g++) {
-    const int target = cuts.start(v0 + g * step);
-    if (target < before || target >= before + mine) continue;
-    int at = before;
-    for (int p = p0; p < p1; p++) {
-      int len, m;
-      w.lens(p, len, m);
-      const int per_head = w.head_tiles(len, m);
-      if (target >= at + per_head * w.n_kv) { at += per_head * w.n_kv; continue; }
+    for (int g = 0; g < G; g++) {
+      const int target = cuts.start(v0 + g * step);
+      if (target < before || target >= before + mine) continue;
+      int at = before, p = p0;
+      if (chunk > 1)
+        for (;; p++) {
+          w.lens(p, len, m);
+          per_head = w.head_tiles(len, m);
+          if (target < at + per_head * w.n_kv) break;
+          at += per_head * w.n_kv;
+        }
       const int h = (target - at) / per_head;
       at += h * per_head;
       int rt = 0;
       while (target >= at + w.tiles(len, m, rt)) at += w.tiles(len, m, rt++);
-      sm.place[g][0] = p; sm.place[g][1] = h; sm.place[g][2] = rt; sm.place[g][3] = target - at;
-      break;
+      sm.place[g][0] = p; sm.place[g][1] = h; sm.place[g][2] = rt; sm.place[g][3] = target - at; sm.place[g][4] = len; sm.place[g][5] = m;
     }
   }
   __syncthreads();
@@ -162,8 +164,8 @@ __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS>& w
 // the place found for range v0 + g * step; not to be called for a range without tiles
 template <int ROWS, int G> __device__ __forceinline__ Cursor<ROWS> place(const FindSmem<G>& sm, const Work<ROWS>& w, int g) {
   Cursor<ROWS> c;
-  c.pair = sm.place[g][0]; c.h = sm.place[g][1]; c.rt = sm.place[g][2]; c.tile = sm.place[g][3];
-  c.load(w);
+  c.pair = sm.place[g][0]; c.h = sm.place[g][1]; c.rt = sm.place[g][2]; c.tile = sm.place[g][3]; c.len = sm.place[g][4]; c.m = sm.place[g][5];
+  c.nt = w.tiles(c.len, c.m, c.rt);
   return c;
 }
 

@@ -180,6 +180,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&sm.tmem_slot)), "n"(COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
   }
+  if (warp == 4 * G && lane == 0) asm volatile("prefetch.tensormap [%0];\n" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
@@ -408,13 +409,23 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       }
       fresh = last;
       if (last) {
+        // over the lanes, eight rows at once: bits 4 .. 2 of a lane choose its row, then the four lanes of a row
+        float w[R];
 #pragma unroll
-        for (int r = 0; r < R; r++) {
-          float w = sum[r];
+        for (int r = 0; r < R; r++) w[r] = sum[r];
 #pragma unroll
-          for (int d = 16; d >= 1; d >>= 1) w += __shfl_xor_sync(0xffffffffu, w, d);
-          if (lane == 0) sy.sum[role][r] = w;
+        for (int d = 16, n = 4; d >= 4; d >>= 1, n >>= 1) {
+          const bool upper = (lane & d) != 0;
+#pragma unroll
+          for (int r = 0; r < 4; r++)
+            if (r < n) {
+              const float give = upper ? w[r] : w[r + n], keep = upper ? w[r + n] : w[r];
+              w[r] = keep + __shfl_xor_sync(0xffffffffu, give, d);
+            }
         }
+        w[0] += __shfl_xor_sync(0xffffffffu, w[0], 2);
+        w[0] += __shfl_xor_sync(0xffffffffu, w[0], 1);
+        if ((lane & 3) == 0) sy.sum[role][lane >> 2] = w[0];
         asm volatile("bar.sync %0, 128;\n" ::"r"(1 + g) : "memory");
         const bool ends = cur.tile == 0, direct = whole && ends;
         float* slot = a.slots + (size_t)(2 * v + (began ? 0 : 1)) * SLOT;
