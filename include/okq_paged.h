@@ -63,8 +63,8 @@ size_t okq_paged_workspace_bytes(const okq_paged* cache, int32_t layer_count, in
  *                  (OKQ_ERR_INVALID_ARG where 3 sections[1] - 2 or 3 sections[2] - 1 is not a pair)
  *   freq       device double [pairs], radians per position
  *   positions  device int32 [3][batch][n]
- * Text alone: three equal positions.  The angle is taken in 64 bits, sine and cosine are rounded to fp32, so that far positions are as
- * exact as near ones.
+ * Text alone: three equal positions.  The angle is taken and reduced in 64 bits, so that far positions are as
+ * exact as near ones (sine and cosine to two units in their last place).
  */
 typedef struct okq_rope {
   int32_t sections[3];

@@ -72,29 +72,16 @@ struct RopeView {
   }
 };
 
-// cos and sin of pos * freq, correct to fp32's last place: the angle is brought to [-pi/4, pi/4] in 64 bits (fp32 would lose the
-// fraction of a turn from a few thousand positions on) and the two Taylor series, to x^12 / 12! and x^13 / 13!, leave 4e-13 and 5e-14.
-// About 20 operations of the fp64 pipe, which runs at half the fp32 rate here: a tenth of what a token's 32 rows cost.
+// cos and sin of an angle given in 64 bits: it is brought to a quarter of a turn around 0 there (fp32 would lose the fraction of a turn
+// from a few thousand positions on) and rounded to fp32 once, an error of 2^-25 of a quarter; sincospif adds its two units in the last
+// place.  Six operations of the fp64 pipe; with the series in 64 bits too a query's rotation took 5 us of an attention call.
 __device__ __forceinline__ void turn(double angle, float& c, float& s) {
   const double quarter = angle * 0.63661977236758134308;    // 2 / pi
-  const double k = rint(quarter);
-  const double x = (quarter - k) * 1.57079632679489661923, z = x * x;
-  double sn = 1.0 / 6227020800.0;
-  sn = fma(sn, z, -1.0 / 39916800.0);
-  sn = fma(sn, z, 1.0 / 362880.0);
-  sn = fma(sn, z, -1.0 / 5040.0);
-  sn = fma(sn, z, 1.0 / 120.0);
-  sn = fma(sn, z, -1.0 / 6.0);
-  sn = fma(sn * z, x, x);
-  double cs = 1.0 / 479001600.0;
-  cs = fma(cs, z, -1.0 / 3628800.0);
-  cs = fma(cs, z, 1.0 / 40320.0);
-  cs = fma(cs, z, -1.0 / 720.0);
-  cs = fma(cs, z, 1.0 / 24.0);
-  cs = fma(cs, z, -0.5);
-  cs = fma(cs, z, 1.0);
-  const int q = (int)((long long)k & 3);
-  const float a = (float)((q & 1) ? sn : cs), b = (float)((q & 1) ? cs : sn);
+  const double t = quarter + 6755399441055744.0;            // 1.5 * 2^52: rounds to an integer, whose low bits are t's
+  const int q = __double2loint(t) & 3;
+  float sn, cs;
+  sincospif(0.5f * (float)(quarter - (t - 6755399441055744.0)), &sn, &cs);
+  const float a = (q & 1) ? sn : cs, b = (q & 1) ? cs : sn;
   c = (q == 1 || q == 2) ? -a : a;
   s = (q & 2) ? -b : b;
 }

@@ -42,14 +42,15 @@ def positions(g, batch, n, kind):
 
 
 def rope_bound(x, ref, half, dtype):
-    """Rounding of cos and sin (half a step of fp32 each), of one product and of the sum: 3 * 2^-24 (|a| + |b|); the angle itself,
-    1e-6 for positions near 2^31 (2^-53 relative of up to 2e9 radians is 2e-7, twice); the result's own rounding."""
+    """Cos and sin to two units of fp32 (2^-22) and half a unit of their angle (2^-24), rounding of one product and of the sum (2^-24
+    each): 6 * 2^-24 (|a| + |b|); the angle itself, 1e-6 for positions near 2^31 (2^-53 relative of up to 2e9 radians is 2e-7,
+    twice); the result's own rounding."""
     mag = np.abs(x)
     pair = np.zeros_like(mag)
     pair[..., :half] = pair[..., half:2 * half] = mag[..., :half] + mag[..., half:2 * half]
     eps = torch.finfo(dtype).eps / 2
     tiny = {F16: 2.0 ** -25, BF16: 0.0, F32: 0.0}[dtype]
-    inner = (3 * 2.0 ** -24 + 1e-6) * pair
+    inner = (6 * 2.0 ** -24 + 1e-6) * pair
     return inner + (0 if dtype == F32 else eps * (np.abs(ref) + inner)) + tiny
 
 
