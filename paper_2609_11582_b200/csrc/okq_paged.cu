@@ -68,10 +68,11 @@ struct Chunks {
   }
 };
 template <class T> struct BlockRows { Vec8<T> x[2][2]; };
+using Turns = float2[PB][72];   // cosines and sines of a block's new rows: pair 8 j + e in place 8 e + j, rows apart in the banks
 // block blk of the `m` new tokens behind `len`
 template <class T>
 __device__ __forceinline__ void load_block(const PagedView& c, int l, int li, int b, int h, int len, int m, int blk, const Rows& k, const Rows& v,
-                                           const Chunks& at, BlockRows<T>& y) {
+                                           int n_new, const RopeView& rope, const Chunks& at, BlockRows<T>& y, Turns& turns) {
   const int first = len - len % PB + blk * PB, rows = min(PB, len + m - first), i = first + at.t - len;   // i: among the new tokens, negative for raw ones
 #pragma unroll
   for (int side = 0; side < 2; side++) {
@@ -84,21 +85,30 @@ __device__ __forceinline__ void load_block(const PagedView& c, int l, int li, in
       for (int e = 0; e < 8; e++) y.x[side][0].v[e] = y.x[side][1].v[e] = from_f<T>(0.f);
     }
   }
+  if (rope.freq) {   // (one turn at a time, a pair to a thread: code that runs once is paid for by its length)
+    const int first_new = max(0, len - first), n = rows - first_new, pair = threadIdx.x & 63;
+    const double f = pair < rope.half ? rope.freq[pair] : 0.0;
+    const int32_t* pos = rope.positions + rope.axis(pair) * ((size_t)c.batch * n_new) + (size_t)b * n_new + (first + first_new - len);
+#pragma unroll 1
+    for (int e = threadIdx.x >> 6; e < n; e += NT / 64) {
+      float2& y = turns[first_new + e][8 * (pair & 7) + (pair >> 3)];
+      turn((double)pos[e] * f, y.x, y.y);
+    }
+    __syncthreads();
+  }
 }
 template <class T>
-__device__ __forceinline__ void store_block(const PagedView& c, int l, int b, int h, int len, int m, int blk, int n_new, const RopeView& rope,
-                                            const Chunks& at, BlockRows<T>& y, unsigned (*top)[NT / 32]) {
+__device__ __forceinline__ void store_block(const PagedView& c, int l, int b, int h, int len, int m, int blk, const Chunks& at,
+                                            BlockRows<T>& y, const Turns& turns, unsigned (*top)[NT / 32]) {
   const int first = len - len % PB + blk * PB, rows = min(PB, len + m - first), i = first + at.t - len;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const bool there = at.t < rows;
   auto& x = y.x;
   if (at.turns && there && i >= 0) {
-    float cs[8], sn[8];
-    turns8(rope, rope.positions + (size_t)b * n_new + i, (size_t)c.batch * n_new, at.c0, cs, sn);
 #pragma unroll
     for (int e = 0; e < 8; e++) {
       float u = to_f(x[0][0].v[e]), w = to_f(x[0][1].v[e]);
-      rotate_pair(u, w, cs[e], sn[e]);
+      rotate_pair(u, w, turns[at.t][8 * e + at.j].x, turns[at.t][8 * e + at.j].y);
       x[0][0].v[e] = from_f<T>(u);
       x[0][1].v[e] = from_f<T>(w);
     }
@@ -150,6 +160,7 @@ template <class T>
 __global__ void __launch_bounds__(NT) k_paged_append(const PagedView c, int layer, const Rows k, const Rows v, int n_new, const int32_t* new_len,
                                                      const RopeView rope, int n_blocks) {
   __shared__ unsigned top[2][NT / 32];
+  __shared__ Turns turns;
   depend_wait();
   const int tid = threadIdx.x;
   long long u = blockIdx.x;
@@ -168,8 +179,8 @@ __global__ void __launch_bounds__(NT) k_paged_append(const PagedView c, int laye
   const Chunks at(tid, rope);
   BlockRows<T> y;
   for (;; blk = last) {
-    load_block<T>(c, l, li, b, h, len, m, blk, k, v, at, y);
-    store_block<T>(c, l, b, h, len, m, blk, n_new, rope, at, y, top);
+    load_block<T>(c, l, li, b, h, len, m, blk, k, v, n_new, rope, at, y, turns);
+    store_block<T>(c, l, b, h, len, m, blk, at, y, turns, top);
     if (!follows || blk != 0) return;
     __syncthreads();
   }
@@ -182,22 +193,22 @@ template <class T>
 __global__ void __launch_bounds__(NT) k_paged_append_few(const PagedView c, int layer, const Rows k, const Rows v, int n_new, const int32_t* new_len,
                                                          const RopeView rope, int size) {
   __shared__ unsigned top[2][2][NT / 32];
+  __shared__ Turns turns;
   depend_wait();
   const int tid = threadIdx.x, rank = blockIdx.x % size, u = blockIdx.x / size, b = u % c.batch, li = u / c.batch, l = layer + li;
   const int m = count_of(new_len, b, n_new), len = c.held(l, b), r = len % PB;
   if (m == 0) return;                       // (the whole cluster)
-  const int bad = __syncthreads_or(pages_missing(c, b, len, m, tid, NT));
-  if (!bad) {
-    const Chunks at(tid, rope);
-    const int last = (r + m - 1) / PB;      // 0 or 1
-    int turn = 0;
-    for (int h = rank; h < c.n_kv; h += size)
-      for (int blk = 0; blk <= last; blk++, turn ^= 1) {
-        BlockRows<T> y;
-        load_block<T>(c, l, li, b, h, len, m, blk, k, v, at, y);
-        store_block<T>(c, l, b, h, len, m, blk, n_new, rope, at, y, top[turn]);   // (its barrier is behind the loads: raw tokens are read before they are replaced)
-      }
-  }
+  const Chunks at(tid, rope);
+  const int last = (r + m - 1) / PB;        // 0 or 1
+  int turn = 0, bad = 0;
+  for (int h = rank; h < c.n_kv && !bad; h += size)
+    for (int blk = 0; blk <= last; blk++, turn ^= 1) {
+      BlockRows<T> y;
+      load_block<T>(c, l, li, b, h, len, m, blk, k, v, n_new, rope, at, y, turns);
+      // (the first rows are on their way while the table is looked at)
+      if (h == rank && blk == 0 && (bad = __syncthreads_or(pages_missing(c, b, len, m, tid, NT)))) break;
+      store_block<T>(c, l, b, h, len, m, blk, at, y, turns, top[turn]);   // (its barrier is behind the loads: raw tokens are read before they are replaced)
+    }
   if (size > 1) {
     asm volatile("barrier.cluster.arrive.aligned;\n" ::: "memory");
     asm volatile("barrier.cluster.wait.aligned;\n" ::: "memory");
@@ -316,6 +327,7 @@ PagedView paged_view(const okq_paged* c) {
   while ((1 << v.page_shift) < v.page) v.page_shift++;
   v.n_pages = c->n_pages; v.max_pages = c->max_pages;
   v.codes = c->codes; v.scales = c->scales; v.raw = c->raw;
+  v.inv_group = (unsigned)(((1ull << 32) + v.group - 1) / v.group);
   v.table = c->table; v.refs = c->refs; v.seq_len = c->seq_len; v.status = c->status;
   return v;
 }

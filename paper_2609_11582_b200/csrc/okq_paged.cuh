@@ -16,7 +16,9 @@ struct PagedView {
   float* scales;
   void* raw;
   int32_t *table, *refs, *seq_len, *status;
+  unsigned inv_group;   // ceil(2^32 / group): row / group without a division, exact for rows below 2^29
 
+  __device__ __forceinline__ int query_of(int row) const { return group == 1 ? row : (int)__umulhi((unsigned)row, inv_group); }
   // first code of a page's head, keys (side 0) or values (side 1)
   __host__ __device__ size_t code_row(int l, int p, int h, int side) const {
     return ((((size_t)l * n_pages + p) * n_kv + h) * 2 + side) * page;   // in rows of 128

@@ -17,6 +17,7 @@ struct Plan {
 // false: more tiles than their numbers hold, were all sequences as long as their rows of the table
 bool make_plan(const okq_paged* c, int layer_count, int n_new, Plan& p) {
   const long long group = c->n_q_heads / c->n_kv_heads, rows = n_new * group;
+  if (rows > 1 << 29) return false;
   p.decode = rows <= DECODE_ROWS;
   const int per = p.decode ? DECODE_ROWS : PROMPT_ROWS;
   const double items = (double)layer_count * c->batch * c->n_kv_heads * (double)((rows + per - 1) / per);

@@ -51,15 +51,19 @@ template <int ROWS> struct Work {
   int pairs, n_kv, group;
   const AttnArgs& a;
   __device__ __forceinline__ explicit Work(const AttnArgs& args) : pairs(args.layer_count * args.c.batch), n_kv(args.c.n_kv), group(args.c.group), a(args) {}
-  __device__ __forceinline__ void lens(int pair, int& len, int& m) const {   // tokens held, queries
-    const int li = a.layer_count == 1 ? 0 : pair / a.c.batch, b = pair - li * a.c.batch;
+  __device__ __forceinline__ void lens(int li, int b, int& len, int& m) const {   // tokens held, queries
     const int n = a.c.seq_len[(size_t)(a.layer + li) * a.c.batch + b], q = a.q_len ? a.q_len[b] : a.n_new;   // (both loads before either is used)
     len = max(0, min(n, a.c.room()));
     m = max(0, min(q, a.n_new));
   }
+  __device__ __forceinline__ int layer_of(int pair) const { return a.layer_count == 1 ? 0 : pair / a.c.batch; }
+  __device__ __forceinline__ void lens(int pair, int& len, int& m) const {
+    const int li = layer_of(pair);
+    lens(li, pair - li * a.c.batch, len, m);
+  }
   __device__ __forceinline__ int row_tiles(int m) const { return (m * group + ROWS - 1) / ROWS; }
   __device__ __forceinline__ int tiles(int len, int m, int rt) const {
-    const int last = (min(m * group, (rt + 1) * ROWS) - 1) / group;   // query of the last row
+    const int last = a.c.query_of(min(m * group, (rt + 1) * ROWS) - 1);   // query of the last row
     const int seen = len - m + last + 1;
     return seen <= 0 ? 0 : (seen + PT - 1) / PT;
   }
@@ -73,8 +77,8 @@ template <int ROWS> struct Work {
 // A place in the line of tiles.
 template <int ROWS> struct Cursor {
   int pair, h, rt, tile;     // item and tile inside it
+  int li, b;                 // layer (of the call's) and sequence of the pair
   int len, m, nt;            // of the item: tokens, queries, tiles
-  __device__ __forceinline__ void load(const Work<ROWS>& w) { w.lens(pair, len, m); nt = m ? w.tiles(len, m, rt) : 0; }
   __device__ __forceinline__ void next_item(const Work<ROWS>& w) {
     tile = 0;
     for (;;) {
@@ -83,7 +87,9 @@ template <int ROWS> struct Cursor {
       else {
         h = 0;
         if (++pair >= w.pairs) return;
-        load(w);
+        if (++b == w.a.c.batch) { b = 0; li++; }
+        w.lens(li, b, len, m);
+        nt = m ? w.tiles(len, m, 0) : 0;
       }
       if (nt > 0) return;
     }
@@ -165,13 +171,19 @@ __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS>& w
 template <int ROWS, int G> __device__ __forceinline__ Cursor<ROWS> place(const FindSmem<G>& sm, const Work<ROWS>& w, int g) {
   Cursor<ROWS> c;
   c.pair = sm.place[g][0]; c.h = sm.place[g][1]; c.rt = sm.place[g][2]; c.tile = sm.place[g][3]; c.len = sm.place[g][4]; c.m = sm.place[g][5];
+  c.li = w.layer_of(c.pair);
+  c.b = c.pair - c.li * w.a.c.batch;
   c.nt = w.tiles(c.len, c.m, c.rt);
   return c;
 }
 
-template <class T> __device__ __forceinline__ T* out_row(const AttnArgs& a, int pair, int h, int row) {
-  const int li = pair / a.c.batch, b = pair % a.c.batch, g = a.c.group;
-  return static_cast<T*>(a.o.p) + li * a.o.s[0] + b * a.o.s[1] + (h * g + row % g) * a.o.s[2] + (row / g) * a.o.s[3];
+template <class T> __device__ __forceinline__ T* out_row(const AttnArgs& a, int li, int b, int h, int row) {
+  const int qi = a.c.query_of(row);
+  return static_cast<T*>(a.o.p) + li * a.o.s[0] + b * a.o.s[1] + (h * a.c.group + row - qi * a.c.group) * a.o.s[2] + qi * a.o.s[3];
+}
+template <class T> __device__ __forceinline__ const T* query_row(const AttnArgs& a, int li, int b, int h, int row) {
+  const int qi = a.c.query_of(row);
+  return static_cast<const T*>(a.q.p) + li * a.q.s[0] + b * a.q.s[1] + (h * a.c.group + row - qi * a.c.group) * a.q.s[2] + qi * a.q.s[3];
 }
 
 // What is left for the merge: the item goes on in the `more` ranges behind range v (0: its output is written).  Heads are numbered by
@@ -193,7 +205,8 @@ template <int ROWS> struct Heads {
 template <class T, int ROWS> __device__ __forceinline__ void write_empty(const AttnArgs& a, const Work<ROWS>& w, const Heads<ROWS>& heads, int who, int n_who, int lane) {
   for (int pair = who; pair < w.pairs; pair += n_who) {
     int len, m;
-    w.lens(pair, len, m);
+    const int li = w.layer_of(pair), b = pair - li * a.c.batch;
+    w.lens(li, b, len, m);
     for (int rt = 0; rt < heads.row_tiles; rt++) {
       const bool rows = rt < w.row_tiles(m);
       if (rows && w.tiles(len, m, rt) > 0) continue;
@@ -201,7 +214,7 @@ template <class T, int ROWS> __device__ __forceinline__ void write_empty(const A
         for (int h = lane; h < w.n_kv; h += 32) a.heads[heads.at(0, w.n_kv, pair, h, rt)].more = 0;
       if (!rows) continue;
       for (int row = rt * ROWS; row < min(m * w.group, (rt + 1) * ROWS); row++)
-        for (int h = 0; h < w.n_kv; h++) *reinterpret_cast<uint2*>(out_row<T>(a, pair, h, row) + 4 * lane) = make_uint2(0u, 0u);
+        for (int h = 0; h < w.n_kv; h++) *reinterpret_cast<uint2*>(out_row<T>(a, li, b, h, row) + 4 * lane) = make_uint2(0u, 0u);
     }
   }
 }
@@ -225,7 +238,8 @@ __global__ void __launch_bounds__(MERGE_NT) k_paged_merge(const AttnArgs a) {
   auto slot = [&](int k) { return a.slots + (size_t)(2 * (hd.v + k) + (k == 0)) * SLOT; };
   const Work<ROWS> w(a);
   int len, m;
-  w.lens(hd.pair, len, m);
+  const int li = w.layer_of(hd.pair), b = hd.pair - li * a.c.batch;
+  w.lens(li, b, len, m);
   const bool there = row < m * w.group;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float top = -INFINITY, l = 0.f;
@@ -281,7 +295,7 @@ __global__ void __launch_bounds__(MERGE_NT) k_paged_merge(const AttnArgs a) {
   if (!there) return;
   T o[4] = {from_f<T>(l == 0.f ? 0.f : acc.x / l), from_f<T>(l == 0.f ? 0.f : acc.y / l), from_f<T>(l == 0.f ? 0.f : acc.z / l),
             from_f<T>(l == 0.f ? 0.f : acc.w / l)};
-  *reinterpret_cast<uint2*>(out_row<T>(a, hd.pair, hd.h, row) + 4 * lane) = *reinterpret_cast<const uint2*>(o);
+  *reinterpret_cast<uint2*>(out_row<T>(a, li, b, hd.h, row) + 4 * lane) = *reinterpret_cast<const uint2*>(o);
 }
 template <class T, int ROWS> inline cudaError_t launch_merge(const AttnArgs& a, int ranges, cudaStream_t s) {
   constexpr int WPR = ROWS <= 8 ? 8 : 1;

@@ -82,46 +82,27 @@ struct Block {
   float ks, vs;
 };
 
-// Two of an item's rows, row and row + 1: limbs (swizzled) and scales.  One warp, four channels per lane.
+// Two of an item's rows, r0 and r0 + 1: limbs (swizzled) and scales.  One warp, four channels per lane.  `turns`: cosines and sines of
+// the item's queries, [query][64 pairs].
 template <class T>
-__device__ __forceinline__ void prepare_queries(const AttnArgs& a, const Cursor<R>& cur, int r0, int8_t* qbuf, float* qscale, int lane) {
-  const PagedView& c = a.c;
-  const int li = cur.pair / c.batch, b = cur.pair % c.batch, rows = cur.m * c.group;
-  uint2 raw[2];
-#pragma unroll
-  for (int e = 0; e < 2; e++) {
-    const int row = cur.rt * R + r0 + e;
-    raw[e] = make_uint2(0u, 0u);
-    if (row < rows)
-      raw[e] = *reinterpret_cast<const uint2*>(static_cast<const T*>(a.q.p) + li * a.q.s[0] + b * a.q.s[1] +
-                                               (cur.h * c.group + row % c.group) * a.q.s[2] + (row / c.group) * a.q.s[3] + 4 * lane);
-  }
+__device__ __forceinline__ void prepare_queries(const AttnArgs& a, const Cursor<R>& cur, int r0, const uint2 (&raw)[2], const float2* turns, int8_t* qbuf,
+                                                float* qscale, int lane) {
   const int step = a.rope.half >> 2;   // lanes from a channel to its partner
-  const bool turns = a.rope.freq && lane < 2 * step, low = lane < step;
-  const int other = !turns ? lane : low ? lane + step : lane - step, pair0 = 4 * (low ? lane : lane - step);
-  float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
-  int at = -1;                         // query that they belong to
+  const bool turned = a.rope.freq && lane < 2 * step, low = lane < step;
+  const int other = !turned ? lane : low ? lane + step : lane - step, pair0 = 4 * (low ? lane : lane - step);
 #pragma unroll
   for (int e = 0; e < 2; e++) {
-    const int r = r0 + e, row = cur.rt * R + r;
+    const int r = r0 + e;
     const T* y = reinterpret_cast<const T*>(&raw[e]);
     float x[4] = {to_f(y[0]), to_f(y[1]), to_f(y[2]), to_f(y[3])};
-    if (a.rope.freq && row < rows) {
-      if (row / c.group != at) {
-        at = row / c.group;
-        if (turns) {
-          const size_t st = (size_t)c.batch * a.n_new;
-#pragma unroll
-          for (int z = 0; z < 4; z++)
-            turn((double)a.rope.positions[a.rope.axis(pair0 + z) * st + (size_t)b * a.n_new + at] * a.rope.freq[pair0 + z], cs[z], sn[z]);
-        }
-      }
+    if (a.rope.freq) {
+      const float2* cs = turns + 64 * a.c.query_of(r) + pair0;
 #pragma unroll
       for (int z = 0; z < 4; z++) {
         const float o = __shfl_sync(0xffffffffu, x[z], other);
-        if (turns) {
+        if (turned) {
           float u = low ? x[z] : o, w = low ? o : x[z];
-          rotate_pair(u, w, cs[z], sn[z]);
+          rotate_pair(u, w, cs[z].x, cs[z].y);
           x[z] = to_f(from_f<T>(low ? u : w));
         }
       }
@@ -208,16 +189,15 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     bool in_nx = false;
     Block now{-1, 0.f, 0.f}, nxt{-1, 0.f, 0.f};
     auto entries = [&](int n) {
-      int pair = 0, len = 0;
+      int b = 0, len = 0;
       for (int i = 0; i < n; i++) {
-        if (lane >> 2 == i) { t_nx = ahead.tile * PT + PB * (lane & 3); len = ahead.len; pair = ahead.pair; h_nx = ahead.h; }
+        if (lane >> 2 == i) { t_nx = ahead.tile * PT + PB * (lane & 3); len = ahead.len; l_nx = a.layer + ahead.li; b = ahead.b; h_nx = ahead.h; }
         ahead.next(work);
       }
       in_nx = lane >> 2 < n && t_nx < len;
-      l_nx = a.layer + pair / c.batch;
       if (in_nx) {
         const int j = t_nx >> c.page_shift;
-        page_nx = __ldg(&c.table[(size_t)(pair % c.batch) * c.max_pages + j]);   // (held() keeps j inside the row)
+        page_nx = __ldg(&c.table[(size_t)b * c.max_pages + j]);   // (held() keeps j inside the row)
       }
     };
     auto scales = [&] {
@@ -313,9 +293,31 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     if (!heads.by_item && tid == g * 128) a.heads[v].more = 0;
     for (int i = 0; i < n_my; i++) {
       const int s = i % NS, b = i & 1;
-      const int pair = cur.pair, h = cur.h, rt = cur.rt, tile = cur.tile, len = cur.len, m = cur.m, nt = cur.nt;
+      const int pair = cur.pair, li = cur.li, bq = cur.b, h = cur.h, tile = cur.tile, len = cur.len, m = cur.m, nt = cur.nt;
       if (fresh) {   // (the products of the item before are through: their sums have been read)
-        prepare_queries<T>(a, cur, 2 * role, pipe.q, sy.qscale, lane);
+        // rows, and the turns of the item's queries (at most eight) in the place of the numerators
+        const int rows = cur.m * c.group;
+        uint2 raw[2];
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          raw[e] = make_uint2(0u, 0u);
+          if (2 * role + e < rows) raw[e] = *reinterpret_cast<const uint2*>(query_row<T>(a, cur.li, cur.b, cur.h, 2 * role + e) + 4 * lane);
+        }
+        float2* turns = reinterpret_cast<float2*>(pipe.p);
+        if (a.rope.freq) {
+          const size_t st = (size_t)c.batch * a.n_new;
+          const int pair = ch & 63;
+          const double f = pair < a.rope.half ? a.rope.freq[pair] : 0.0;
+          const int32_t* pos = a.rope.positions + a.rope.axis(pair) * st + (size_t)cur.b * a.n_new;
+#pragma unroll 1
+          for (int qi = ch >> 6; qi < cur.m; qi += 2) {
+            float2 y;
+            turn((double)pos[qi] * f, y.x, y.y);
+            turns[64 * qi + pair] = y;
+          }
+          asm volatile("bar.sync %0, 128;\n" ::"r"(1 + g) : "memory");
+        }
+        prepare_queries<T>(a, cur, 2 * role, raw, turns, pipe.q, sy.qscale, lane);
         fence_async_smem();
         asm volatile("bar.sync %0, 128;\n" ::"r"(1 + g) : "memory");
         if (lane == 0) mbar_arrive(&sy.q_full);
@@ -344,7 +346,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       if (tile * PT + PT > len - m + 1) {   // some row does not see all of the tile
 #pragma unroll
         for (int r = 0; r < R; r++)
-          if (t >= len - m + 1 + (rt * R + r) / c.group) x[r] = -INFINITY;
+          if (t >= len - m + 1 + c.query_of(r)) x[r] = -INFINITY;
       }
       {
         float w[R];
@@ -430,13 +432,13 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         const bool ends = cur.tile == 0, direct = whole && ends;
         float* slot = a.slots + (size_t)(2 * v + (began ? 0 : 1)) * SLOT;
         if (!began && (heads.by_item || !ends) && tid == g * 128)   // (the same thread as above)
-          a.heads[heads.at(v, c.n_kv, pair, h, rt)] = Head{ends ? 0 : cuts.range_of(g0 + i - tile + nt - 1) - v, v, pair, h, rt, {}};
+          a.heads[heads.at(v, c.n_kv, pair, h, 0)] = Head{ends ? 0 : cuts.range_of(g0 + i - tile + nt - 1) - v, v, pair, h, 0, {}};
 #pragma unroll
         for (int r = 0; r < R; r++) {
           float l = (sy.sum[0][r] + sy.sum[1][r]) + (sy.sum[2][r] + sy.sum[3][r]);
           if (sm.abort) l = NAN;
           if (direct) {
-            if (rt * R + r < m * c.group) out_row<T>(a, pair, h, rt * R + r)[ch] = from_f<T>(l == 0.f ? 0.f : o[r] / l);
+            if (r < m * c.group) out_row<T>(a, li, bq, h, r)[ch] = from_f<T>(l == 0.f ? 0.f : o[r] / l);
           } else {
             slot[r * D + ch] = o[r];
             if (ch == r) { slot[R * D + r] = top[r]; slot[R * D + R + r] = l; }

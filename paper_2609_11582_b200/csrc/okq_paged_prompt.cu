@@ -113,7 +113,7 @@ __device__ __forceinline__ uint2 codes_to_half(uint32_t w) {
 template <class T>
 __device__ __forceinline__ float prepare_queries(const AttnArgs& a, const Cursor<R>& cur, int row0, unsigned char* q, bool store, int lane) {
   const PagedView& c = a.c;
-  const int li = cur.pair / c.batch, b = cur.pair % c.batch, rows = cur.m * c.group;
+  const int rows = cur.m * c.group;
   const int j = lane & 7, nc = a.rope.half >> 3;
   const bool turns = a.rope.freq && j < nc;
   const int c0 = !a.rope.freq || j < nc ? 8 * j : 2 * a.rope.half + 16 * (j - nc);
@@ -124,12 +124,12 @@ __device__ __forceinline__ float prepare_queries(const AttnArgs& a, const Cursor
     const int rl = 4 * it + (lane >> 3), row = cur.rt * R + row0 + rl;    // row inside the warp, of the item's queries
     Vec8<T> x[2] = {};
     if (row < rows) {
-      const T* src = static_cast<const T*>(a.q.p) + li * a.q.s[0] + b * a.q.s[1] + (cur.h * c.group + row % c.group) * a.q.s[2] + (row / c.group) * a.q.s[3];
+      const T* src = query_row<T>(a, cur.li, cur.b, cur.h, row);
       x[0] = *reinterpret_cast<const Vec8<T>*>(src + c0);
       x[1] = *reinterpret_cast<const Vec8<T>*>(src + c1);
       if (turns) {
         float cs[8], sn[8];
-        turns8(a.rope, a.rope.positions + (size_t)b * a.n_new + row / c.group, (size_t)c.batch * a.n_new, c0, cs, sn);
+        turns8(a.rope, a.rope.positions + (size_t)cur.b * a.n_new + c.query_of(row), (size_t)c.batch * a.n_new, c0, cs, sn);
 #pragma unroll
         for (int e = 0; e < 8; e++) {
           float u = to_f(x[0].v[e]), w = to_f(x[1].v[e]);
@@ -260,14 +260,13 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     float ks_now = 0.f, vs_now = 0.f, ks_nx = 0.f, vs_nx = 0.f;
     bool fresh_now = false;
     auto entries = [&](int n) {
-      int pair = 0, len = 0;
+      int b = 0, len = 0;
       for (int i = 0; i < n; i++) {
-        if (lane >> 2 == i) { t_nx = ahead.tile * PT + PB * (lane & 3); len = ahead.len; pair = ahead.pair; h_nx = ahead.h; fresh_nx = ahead.tile == 0; }
+        if (lane >> 2 == i) { t_nx = ahead.tile * PT + PB * (lane & 3); len = ahead.len; l_nx = a.layer + ahead.li; b = ahead.b; h_nx = ahead.h; fresh_nx = ahead.tile == 0; }
         ahead.next(work);
       }
       in_nx = lane >> 2 < n && t_nx < len;
-      l_nx = a.layer + pair / c.batch;
-      if (in_nx) page_nx = __ldg(&c.table[(size_t)(pair % c.batch) * c.max_pages + (t_nx >> c.page_shift)]);
+      if (in_nx) page_nx = __ldg(&c.table[(size_t)b * c.max_pages + (t_nx >> c.page_shift)]);
     };
     auto scales = [&] {
       row_nx = -1;
@@ -478,8 +477,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       if (dual) asm volatile("bar.sync 1, 256;\n" ::: "memory");   // stream A's queries are B's too
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.q_full[t]);
-      const int last_seen = cur.len - cur.m + (cur.rt * R + row) / c.group;   // last token that the row sees
-      const int least = cur.len - cur.m + (cur.rt * R + row0) / c.group;      // .. that the warp's first row sees
+      const int last_seen = cur.len - cur.m + c.query_of(cur.rt * R + row);   // last token that the row sees
+      const int least = cur.len - cur.m + c.query_of(cur.rt * R + row0);      // .. that the warp's first row sees
       float m = -INFINITY, l = 0.f, vref = 1.f;
       for (int y = 0; y < steps; y++) {
         const int k = dual ? y : y >> 1, half = dual ? t : y & 1, place = y & 1, at = (cur.tile + k) * PT + PH * half;
@@ -552,7 +551,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       f *= unit;
       f_other *= unit;
       const bool there = row < rows;
-      T* dst = there && direct ? out_row<T>(a, cur.pair, cur.h, cur.rt * R + row) : nullptr;
+      T* dst = there && direct ? out_row<T>(a, cur.li, cur.b, cur.h, cur.rt * R + row) : nullptr;
       // (a dual item's streams have 64 channels each)
       const uint32_t o_own = tmem + O_COL + lanes;
 #pragma unroll 1
