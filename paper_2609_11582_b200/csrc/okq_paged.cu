@@ -5,6 +5,7 @@
 // new ones from the caller's tensor), takes the maximum and writes codes, scale and, for the block that stays unfinished, the raw
 // copies.  Requantising the unfinished block with every append costs at most 16 KB of reads per head and makes the cache
 // independent of how its tokens were dealt over calls; keeping the codes and only lowering their scale would round twice.
+#include "okq_device.cuh"
 #include "okq_paged.cuh"
 
 namespace okq {
@@ -39,15 +40,21 @@ __device__ __forceinline__ int pages_missing(const PagedView& c, int b, int len,
 struct Quotient {
   float scale, r;
   int how;   // 0: codes 0 (a scale of zero or NaN), 1: residual step, 2: division
-  __device__ __forceinline__ uint32_t code(float x) const {
-    float q = 0.f;
+  template <class T> __device__ __forceinline__ void codes(const Vec8<T>& x, uint32_t (&q)[8]) const {
     if (how == 1) {
-      q = __fmul_rn(x, r);
-      q = __fmaf_rn(__fmaf_rn(-q, scale, x), r, q);
-    } else if (how == 2) {
-      q = fminf(fmaxf(__fdiv_rn(x, scale), -127.f), 127.f);   // (a subnormal scale may be too small by half of itself)
+      const F2 r2 = f2(r, r), s2 = f2(-scale, -scale), one = f2(12582912.f, 12582912.f);
+#pragma unroll
+      for (int e = 0; e < 4; e++) {   // (packed pairs round like single operations)
+        const F2 v = f2(to_f(x.v[2 * e]), to_f(x.v[2 * e + 1])), a = mul2(v, r2);
+        const float2 y = un2(add2(fma2(fma2(a, s2, v), r2, a), one));
+        q[2 * e] = __float_as_uint(y.x);
+        q[2 * e + 1] = __float_as_uint(y.y);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; e++)   // (a subnormal scale may be too small by half of itself)
+        q[e] = how == 0 ? 0u : __float_as_uint(__fadd_rn(fminf(fmaxf(__fdiv_rn(to_f(x.v[e]), scale), -127.f), 127.f), 12582912.f));
     }
-    return __float_as_uint(__fadd_rn(q, 12582912.f));
   }
 };
 
@@ -55,160 +62,156 @@ __device__ __forceinline__ Quotient quotient_by(float scale) {
   return Quotient{scale, __fdiv_rn(1.f, scale), !(scale > 0.f) ? 0 : scale >= 7.9e-31f ? 1 : 2};
 }
 
-// One block's keys and values by NT threads: thread tid has row tid / 8, two chunks of eight channels of either side.
+// One block's keys, or values, by NT threads: thread tid has row tid / 8 and two chunks of eight channels.
 struct Chunks {
   int t, j, c0, c1;
   bool turns;
   // (the chunks that a rotated pair of channels lies in, as okq_rope_apply deals them)
-  __device__ __forceinline__ Chunks(int tid, const RopeView& rope) : t(tid >> 3), j(tid & 7) {
+  __device__ __forceinline__ Chunks(int tid, const RopeView& rope, bool keys) : t(tid >> 3), j(tid & 7) {
     const int nc = rope.half >> 3;
-    turns = rope.freq && j < nc;
-    c0 = !rope.freq || j < nc ? 8 * j : 2 * rope.half + 16 * (j - nc);
-    c1 = !rope.freq ? c0 + 64 : j < nc ? c0 + rope.half : c0 + 8;
+    const bool deal = rope.freq && keys;
+    turns = deal && j < nc;
+    c0 = !deal || j < nc ? 8 * j : 2 * rope.half + 16 * (j - nc);
+    c1 = !deal ? c0 + 64 : j < nc ? c0 + rope.half : c0 + 8;
   }
 };
-template <class T> struct BlockRows { Vec8<T> x[2][2]; };
+template <class T> struct BlockRows { Vec8<T> x[2]; };
 using Turns = float2[PB][72];   // cosines and sines of a block's new rows: pair 8 j + e in place 8 e + j, rows apart in the banks
+struct BlockSmem {
+  unsigned top[2][NT / 32];     // (two blocks in turn)
+  Turns turns;
+};
 // block blk of the `m` new tokens behind `len`
 template <class T>
-__device__ __forceinline__ void load_block(const PagedView& c, int l, int li, int b, int h, int len, int m, int blk, const Rows& k, const Rows& v,
-                                           int n_new, const RopeView& rope, const Chunks& at, BlockRows<T>& y, Turns& turns) {
+__device__ __forceinline__ void load_block(const PagedView& c, int l, int li, int b, int h, int side, int len, int m, int blk, const Rows& src, int n_new,
+                                           const RopeView& rope, const Chunks& at, BlockRows<T>& y, BlockSmem& sm) {
   const int first = len - len % PB + blk * PB, rows = min(PB, len + m - first), i = first + at.t - len;   // i: among the new tokens, negative for raw ones
+  if (at.t < rows) {
+    const T* p = i < 0 ? c.raw_of<T>(l, b, h, side) + (size_t)at.t * D : src.at<T>(li, b, h, i);
+    y.x[0] = *reinterpret_cast<const Vec8<T>*>(p + at.c0);
+    y.x[1] = *reinterpret_cast<const Vec8<T>*>(p + at.c1);
+  } else {
 #pragma unroll
-  for (int side = 0; side < 2; side++) {
-    if (at.t < rows) {
-      const T* src = i < 0 ? c.raw_of<T>(l, b, h, side) + (size_t)at.t * D : (side ? v : k).at<T>(li, b, h, i);
-      y.x[side][0] = *reinterpret_cast<const Vec8<T>*>(src + at.c0);
-      y.x[side][1] = *reinterpret_cast<const Vec8<T>*>(src + at.c1);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; e++) y.x[side][0].v[e] = y.x[side][1].v[e] = from_f<T>(0.f);
-    }
+    for (int e = 0; e < 8; e++) y.x[0].v[e] = y.x[1].v[e] = from_f<T>(0.f);
   }
-  if (rope.freq) {   // (one turn at a time, a pair to a thread: code that runs once is paid for by its length)
+  if (rope.freq && side == 0) {   // (one turn at a time, a pair to a thread: code that runs once is paid for by its length)
     const int first_new = max(0, len - first), n = rows - first_new, pair = threadIdx.x & 63;
     const double f = pair < rope.half ? rope.freq[pair] : 0.0;
     const int32_t* pos = rope.positions + rope.axis(pair) * ((size_t)c.batch * n_new) + (size_t)b * n_new + (first + first_new - len);
 #pragma unroll 1
     for (int e = threadIdx.x >> 6; e < n; e += NT / 64) {
-      float2& y = turns[first_new + e][8 * (pair & 7) + (pair >> 3)];
-      turn((double)pos[e] * f, y.x, y.y);
+      float2& w = sm.turns[first_new + e][8 * (pair & 7) + (pair >> 3)];
+      turn((double)pos[e] * f, w.x, w.y);
     }
     __syncthreads();
   }
 }
 template <class T>
-__device__ __forceinline__ void store_block(const PagedView& c, int l, int b, int h, int len, int m, int blk, const Chunks& at,
-                                            BlockRows<T>& y, const Turns& turns, unsigned (*top)[NT / 32]) {
+__device__ __forceinline__ void store_block(const PagedView& c, int l, int b, int h, int side, int len, int m, int blk, const Chunks& at,
+                                            BlockRows<T>& y, BlockSmem& sm, int which) {
   const int first = len - len % PB + blk * PB, rows = min(PB, len + m - first), i = first + at.t - len;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const bool there = at.t < rows;
-  auto& x = y.x;
   if (at.turns && there && i >= 0) {
 #pragma unroll
     for (int e = 0; e < 8; e++) {
-      float u = to_f(x[0][0].v[e]), w = to_f(x[0][1].v[e]);
-      rotate_pair(u, w, turns[at.t][8 * e + at.j].x, turns[at.t][8 * e + at.j].y);
-      x[0][0].v[e] = from_f<T>(u);
-      x[0][1].v[e] = from_f<T>(w);
+      const float2 cs = sm.turns[at.t][8 * e + at.j];
+      float u = to_f(y.x[0].v[e]), w = to_f(y.x[1].v[e]);
+      rotate_pair(u, w, cs.x, cs.y);
+      y.x[0].v[e] = from_f<T>(u);
+      y.x[1].v[e] = from_f<T>(w);
     }
   }
   // magnitudes as integers: their order is the numbers' own, with infinities and NaN at the top
+  unsigned mx = 0;
 #pragma unroll
-  for (int side = 0; side < 2; side++) {
-    unsigned mx = 0;
-#pragma unroll
-    for (int e = 0; e < 16; e++) mx = max(mx, __float_as_uint(to_f(x[side][e >> 3].v[e & 7])) & 0x7fffffffu);
-    mx = __reduce_max_sync(0xffffffffu, mx);
-    if (lane == 0) top[side][warp] = mx;
-  }
-  __syncthreads();
+  for (int e = 0; e < 16; e++) mx = max(mx, __float_as_uint(to_f(y.x[e >> 3].v[e & 7])) & 0x7fffffffu);
+  mx = __reduce_max_sync(0xffffffffu, mx);
+  if (lane == 0) sm.top[which][warp] = mx;
   const int page = c.page_of(b, first);
+  __syncthreads();
 #pragma unroll
-  for (int side = 0; side < 2; side++) {
-    unsigned mx = 0;
+  for (int w = 0; w < NT / 32; w++) mx = max(mx, sm.top[which][w]);
+  float scale = __fdiv_rn(__uint_as_float(mx), 127.f);
+  if (mx >= 0x7f800000u) scale = __uint_as_float(0x7fc00000u);   // infinities, NaN
+  const Quotient by = quotient_by(scale);
+  const size_t row = c.code_row(l, page, h, side) + (first & (c.page - 1));
+  if (there) {
+    int8_t* dst = c.codes + (row + at.t) * D;
 #pragma unroll
-    for (int w = 0; w < NT / 32; w++) mx = max(mx, top[side][w]);
-    const float amax = __uint_as_float(mx);
-    float scale = __fdiv_rn(amax, 127.f);
-    if (mx >= 0x7f800000u) scale = __uint_as_float(0x7fc00000u);   // infinities, NaN
-    const Quotient by = quotient_by(scale);
-    const size_t row = c.code_row(l, page, h, side) + (first & (c.page - 1));
-    if (there) {
-      int8_t* dst = c.codes + (row + at.t) * D;
-#pragma unroll
-      for (int half = 0; half < 2; half++) {
-        uint32_t q[8];
-#pragma unroll
-        for (int e = 0; e < 8; e++) q[e] = by.code(to_f(x[side][half].v[e]));
-        uint2 w;
-        w.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
-        w.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
-        *reinterpret_cast<uint2*>(dst + (half ? at.c1 : at.c0)) = w;
-      }
-      if (rows < PB && i >= 0) {   // a block that stays unfinished
-        T* keep = c.raw_of<T>(l, b, h, side) + (size_t)at.t * D;
-        *reinterpret_cast<Vec8<T>*>(keep + at.c0) = x[side][0];
-        *reinterpret_cast<Vec8<T>*>(keep + at.c1) = x[side][1];
-      }
+    for (int half = 0; half < 2; half++) {
+      uint32_t q[8];
+      by.codes(y.x[half], q);
+      uint2 w;
+      w.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+      w.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+      *reinterpret_cast<uint2*>(dst + (half ? at.c1 : at.c0)) = w;
     }
-    if (tid == side) c.scales[row / PB] = scale;
+    if (rows < PB && i >= 0) {   // a block that stays unfinished
+      T* keep = c.raw_of<T>(l, b, h, side) + (size_t)at.t * D;
+      *reinterpret_cast<Vec8<T>*>(keep + at.c0) = y.x[0];
+      *reinterpret_cast<Vec8<T>*>(keep + at.c1) = y.x[1];
+    }
   }
+  if (tid == 0) c.scales[row / PB] = scale;
 }
 
+// A thread block has one side of a 32-token block: keys and values apart keep a thread to 16 numbers and five blocks on an SM (both in
+// one took 124 registers: two blocks, 199 us for 28 layers x 4097 tokens x 4 heads).
 template <class T>
 __global__ void __launch_bounds__(NT) k_paged_append(const PagedView c, int layer, const Rows k, const Rows v, int n_new, const int32_t* new_len,
                                                      const RopeView rope, int n_blocks) {
-  __shared__ unsigned top[2][NT / 32];
-  __shared__ Turns turns;
+  __shared__ BlockSmem sm;
   depend_wait();
   const int tid = threadIdx.x;
-  long long u = blockIdx.x;
-  int blk = (int)(u % n_blocks);
-  u /= n_blocks;
-  const int h = (int)(u % c.n_kv);
-  u /= c.n_kv;
-  const int b = (int)(u % c.batch), li = (int)(u / c.batch), l = layer + li;
+  unsigned u = blockIdx.x;
+  int blk = (int)(u % (unsigned)n_blocks);
+  u /= (unsigned)n_blocks;
+  const int side = (int)(u & 1);
+  u >>= 1;
+  const int h = (int)(u % (unsigned)c.n_kv);
+  u /= (unsigned)c.n_kv;
+  const int li = (int)(u / (unsigned)c.batch), b = (int)(u - (unsigned)li * c.batch), l = layer + li;
   const int m = count_of(new_len, b, n_new), len = c.held(l, b), r = len % PB, end = len + m;
   if (m == 0 || len - r + blk * PB >= end) return;
-  if (__syncthreads_or(pages_missing(c, b, len, m, tid, NT))) return;
   // The raw tokens are read by the first block and replaced by the last, so one thread block does both, in that order.
   const int last = (r + m - 1) / PB;
   const bool follows = r > 0 && last > 0 && (r + m) % PB != 0;
   if (follows && blk == last) return;
-  const Chunks at(tid, rope);
+  const Chunks at(tid, rope, side == 0);
   BlockRows<T> y;
-  for (;; blk = last) {
-    load_block<T>(c, l, li, b, h, len, m, blk, k, v, n_new, rope, at, y, turns);
-    store_block<T>(c, l, b, h, len, m, blk, at, y, turns, top);
-    if (!follows || blk != 0) return;
-    __syncthreads();
-  }
+  load_block<T>(c, l, li, b, h, side, len, m, blk, side ? v : k, n_new, rope, at, y, sm);
+  if (__syncthreads_or(pages_missing(c, b, len, m, tid, NT))) return;   // (while the rows are on their way)
+  store_block<T>(c, l, b, h, side, len, m, blk, at, y, sm, 0);
+  if (!follows || blk != 0) return;
+  load_block<T>(c, l, li, b, h, side, len, m, last, side ? v : k, n_new, rope, at, y, sm);
+  store_block<T>(c, l, b, h, side, len, m, last, at, y, sm, 1);
 }
 
 // The same for up to FEW new tokens (two blocks of a sequence at most) in one launch: a cluster has a (layer, sequence), each of its
-// blocks every MOST-th head, and the length is advanced when all of them have read it.
+// blocks every size-th side of a head, and the length is advanced when all of them have read it.
 constexpr int FEW = PB, MOST = 8;
 template <class T>
 __global__ void __launch_bounds__(NT) k_paged_append_few(const PagedView c, int layer, const Rows k, const Rows v, int n_new, const int32_t* new_len,
                                                          const RopeView rope, int size) {
-  __shared__ unsigned top[2][2][NT / 32];
-  __shared__ Turns turns;
+  __shared__ BlockSmem sm;
   depend_wait();
-  const int tid = threadIdx.x, rank = blockIdx.x % size, u = blockIdx.x / size, b = u % c.batch, li = u / c.batch, l = layer + li;
+  const int tid = threadIdx.x, rank = blockIdx.x % size, u = blockIdx.x / size, li = u / c.batch, b = u - li * c.batch, l = layer + li;
   const int m = count_of(new_len, b, n_new), len = c.held(l, b), r = len % PB;
   if (m == 0) return;                       // (the whole cluster)
-  const Chunks at(tid, rope);
   const int last = (r + m - 1) / PB;        // 0 or 1
-  int turn = 0, bad = 0;
-  for (int h = rank; h < c.n_kv && !bad; h += size)
-    for (int blk = 0; blk <= last; blk++, turn ^= 1) {
+  int which = 0, bad = 0;
+  for (int e = rank; e < 2 * c.n_kv && !bad; e += size) {
+    const int h = e >> 1, side = e & 1;
+    const Chunks at(tid, rope, side == 0);
+    for (int blk = 0; blk <= last; blk++, which ^= 1) {
       BlockRows<T> y;
-      load_block<T>(c, l, li, b, h, len, m, blk, k, v, n_new, rope, at, y, turns);
+      load_block<T>(c, l, li, b, h, side, len, m, blk, side ? v : k, n_new, rope, at, y, sm);
       // (the first rows are on their way while the table is looked at)
-      if (h == rank && blk == 0 && (bad = __syncthreads_or(pages_missing(c, b, len, m, tid, NT)))) break;
-      store_block<T>(c, l, b, h, len, m, blk, at, y, turns, top[turn]);   // (its barrier is behind the loads: raw tokens are read before they are replaced)
+      if (e == rank && blk == 0 && (bad = __syncthreads_or(pages_missing(c, b, len, m, tid, NT)))) break;
+      store_block<T>(c, l, b, h, side, len, m, blk, at, y, sm, which);   // (its barrier is behind the loads: raw tokens are read before they are replaced)
     }
+  }
   if (size > 1) {
     asm volatile("barrier.cluster.arrive.aligned;\n" ::: "memory");
     asm volatile("barrier.cluster.wait.aligned;\n" ::: "memory");
@@ -276,12 +279,12 @@ template <class T>
 okq_status launch_append(const PagedView& c, int layer, int layer_count, const Rows& k, const Rows& v, int n_new, const int32_t* new_len,
                          const RopeView& rope, cudaStream_t s) {
   if (n_new <= FEW) {
-    const int size = c.n_kv < MOST ? c.n_kv : MOST;
+    const int size = 2 * c.n_kv < MOST ? 2 * c.n_kv : MOST;
     const cudaError_t e = launch_dependent(k_paged_append_few<T>, dim3((unsigned)(layer_count * c.batch * size)), NT, 0, s, size, c, layer, k, v, n_new, new_len, rope, size);
     return e != cudaSuccess ? failed(e) : launch_status();
   }
   const int n_blocks = (PB - 1 + n_new + PB - 1) / PB;
-  const long long grid = (long long)layer_count * c.batch * c.n_kv * n_blocks;
+  const long long grid = 2ll * layer_count * c.batch * c.n_kv * n_blocks;
   if (grid > 0x7fffffffll) return OKQ_ERR_UNSUPPORTED;
   cudaError_t e = launch_dependent(k_paged_append<T>, dim3((unsigned)grid), NT, 0, s, 1, c, layer, k, v, n_new, new_len, rope, n_blocks);
   if (e != cudaSuccess) return failed(e);
