@@ -12,7 +12,8 @@ namespace okq {
 
 namespace {
 
-constexpr int NT = 256;
+constexpr int NT = 256;    // threads of a block, but for the append kernels
+constexpr int AT = 128;
 
 // rows of one call's keys or values
 struct Rows {
@@ -62,154 +63,211 @@ __device__ __forceinline__ Quotient quotient_by(float scale) {
   return Quotient{scale, __fdiv_rn(1.f, scale), !(scale > 0.f) ? 0 : scale >= 7.9e-31f ? 1 : 2};
 }
 
-// One block's keys, or values, by NT threads: thread tid has row tid / 8 and two chunks of eight channels.
+// One block's keys, or values, by AT threads: thread tid has row tid / 4 and four chunks of eight channels, two of them apart by the
+// pairs of a rotation, as okq_rope_apply deals them.
 struct Chunks {
-  int t, j, c0, c1;
-  bool turns;
-  // (the chunks that a rotated pair of channels lies in, as okq_rope_apply deals them)
-  __device__ __forceinline__ Chunks(int tid, const RopeView& rope, bool keys) : t(tid >> 3), j(tid & 7) {
+  int t, j, c[4];
+  bool turns[2];
+  __device__ __forceinline__ Chunks(int tid, const RopeView& rope, bool keys) : t(tid >> 2), j(tid & 3) {
     const int nc = rope.half >> 3;
     const bool deal = rope.freq && keys;
-    turns = deal && j < nc;
-    c0 = !deal || j < nc ? 8 * j : 2 * rope.half + 16 * (j - nc);
-    c1 = !deal ? c0 + 64 : j < nc ? c0 + rope.half : c0 + 8;
+#pragma unroll
+    for (int z = 0; z < 2; z++) {
+      const int k = j + 4 * z;
+      turns[z] = deal && k < nc;
+      c[2 * z] = !deal || k < nc ? 8 * k : 2 * rope.half + 16 * (k - nc);
+      c[2 * z + 1] = !deal ? 8 * k + 64 : k < nc ? 8 * k + rope.half : c[2 * z] + 8;
+    }
   }
 };
-template <class T> struct BlockRows { Vec8<T> x[2]; };
+template <class T> struct BlockRows { Vec8<T> x[4]; };
+// largest magnitude of two numbers each, NaN where there is one
+__device__ __forceinline__ __half2 top2(__half2 a, __half2 b) { return __hmax2_nan(a, __habs2(b)); }
+__device__ __forceinline__ __nv_bfloat162 top2(__nv_bfloat162 a, __nv_bfloat162 b) { return __hmax2_nan(a, __habs2(b)); }
+template <class T> struct Pair;
+template <> struct Pair<__half> { using type = __half2; };
+template <> struct Pair<__nv_bfloat16> { using type = __nv_bfloat162; };
 using Turns = float2[PB][72];   // cosines and sines of a block's new rows: pair 8 j + e in place 8 e + j, rows apart in the banks
 struct BlockSmem {
-  unsigned top[2][NT / 32];     // (two blocks in turn)
+  unsigned top[2][AT / 32];     // (two blocks in turn)
   Turns turns;
 };
-// block blk of the `m` new tokens behind `len`
+// What a thread block knows of the sequence that it appends `m` tokens to, and its side of the head.
+struct Append {
+  int l, li, b, h, side, len, m, n_new;
+  __device__ __forceinline__ int first(int blk) const { return len - len % PB + blk * PB; }
+  __device__ __forceinline__ int rows(int blk) const { return min(PB, len + m - first(blk)); }
+};
+// block blk of the new tokens: rows, raw ones first
 template <class T>
-__device__ __forceinline__ void load_block(const PagedView& c, int l, int li, int b, int h, int side, int len, int m, int blk, const Rows& src, int n_new,
-                                           const RopeView& rope, const Chunks& at, BlockRows<T>& y, BlockSmem& sm) {
-  const int first = len - len % PB + blk * PB, rows = min(PB, len + m - first), i = first + at.t - len;   // i: among the new tokens, negative for raw ones
-  if (at.t < rows) {
-    const T* p = i < 0 ? c.raw_of<T>(l, b, h, side) + (size_t)at.t * D : src.at<T>(li, b, h, i);
-    y.x[0] = *reinterpret_cast<const Vec8<T>*>(p + at.c0);
-    y.x[1] = *reinterpret_cast<const Vec8<T>*>(p + at.c1);
+__device__ __forceinline__ void load_rows(const PagedView& c, const Append& w, int blk, const Rows& src, const Chunks& at, BlockRows<T>& y) {
+  const int i = w.first(blk) + at.t - w.len;   // among the new tokens, negative for raw ones
+  if (at.t < w.rows(blk)) {
+    const T* p = i < 0 ? c.raw_of<T>(w.l, w.b, w.h, w.side) + (size_t)at.t * D : src.at<T>(w.li, w.b, w.h, i);
+#pragma unroll
+    for (int z = 0; z < 4; z++) y.x[z] = *reinterpret_cast<const Vec8<T>*>(p + at.c[z]);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; e++) y.x[0].v[e] = y.x[1].v[e] = from_f<T>(0.f);
-  }
-  if (rope.freq && side == 0) {   // (one turn at a time, a pair to a thread: code that runs once is paid for by its length)
-    const int first_new = max(0, len - first), n = rows - first_new, pair = threadIdx.x & 63;
-    const double f = pair < rope.half ? rope.freq[pair] : 0.0;
-    const int32_t* pos = rope.positions + rope.axis(pair) * ((size_t)c.batch * n_new) + (size_t)b * n_new + (first + first_new - len);
-#pragma unroll 1
-    for (int e = threadIdx.x >> 6; e < n; e += NT / 64) {
-      float2& w = sm.turns[first_new + e][8 * (pair & 7) + (pair >> 3)];
-      turn((double)pos[e] * f, w.x, w.y);
-    }
-    __syncthreads();
+    for (int e = 0; e < 32; e++) y.x[e >> 3].v[e & 7] = from_f<T>(0.f);
   }
 }
+// the turns of its new rows (one at a time, a pair to a thread: code that runs once is paid for by its length)
+__device__ __forceinline__ void make_turns(const PagedView& c, const Append& w, int blk, const RopeView& rope, BlockSmem& sm) {
+  const int first = w.first(blk), first_new = max(0, w.len - first), n = w.rows(blk) - first_new, pair = threadIdx.x & 63;
+  const double f = pair < rope.half ? rope.freq[pair] : 0.0;
+  const int32_t* pos = rope.positions + rope.axis(pair) * ((size_t)c.batch * w.n_new) + (size_t)w.b * w.n_new + (first + first_new - w.len);
+#pragma unroll 1
+  for (int e = threadIdx.x >> 6; e < n; e += AT / 64) {
+    float2& z = sm.turns[first_new + e][8 * (pair & 7) + (pair >> 3)];
+    turn((double)pos[e] * f, z.x, z.y);
+  }
+}
+// rotates them; the warp's largest magnitude goes to top[which] (as an integer: the order is the numbers' own, infinities and NaN at the top)
 template <class T>
-__device__ __forceinline__ void store_block(const PagedView& c, int l, int b, int h, int side, int len, int m, int blk, const Chunks& at,
-                                            BlockRows<T>& y, BlockSmem& sm, int which) {
-  const int first = len - len % PB + blk * PB, rows = min(PB, len + m - first), i = first + at.t - len;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const bool there = at.t < rows;
-  if (at.turns && there && i >= 0) {
+__device__ __forceinline__ void turn_rows(const Append& w, int blk, const Chunks& at, BlockRows<T>& y, BlockSmem& sm, int which) {
+  if (at.t < w.rows(blk) && w.first(blk) + at.t >= w.len) {
 #pragma unroll
-    for (int e = 0; e < 8; e++) {
-      const float2 cs = sm.turns[at.t][8 * e + at.j];
-      float u = to_f(y.x[0].v[e]), w = to_f(y.x[1].v[e]);
-      rotate_pair(u, w, cs.x, cs.y);
-      y.x[0].v[e] = from_f<T>(u);
-      y.x[1].v[e] = from_f<T>(w);
+    for (int z = 0; z < 2; z++) {
+      if (!at.turns[z]) continue;
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const float2 cs = sm.turns[at.t][8 * e + at.j + 4 * z];
+        float u = to_f(y.x[2 * z].v[e]), v = to_f(y.x[2 * z + 1].v[e]);
+        rotate_pair(u, v, cs.x, cs.y);
+        y.x[2 * z].v[e] = from_f<T>(u);
+        y.x[2 * z + 1].v[e] = from_f<T>(v);
+      }
     }
   }
-  // magnitudes as integers: their order is the numbers' own, with infinities and NaN at the top
+  using P = typename Pair<T>::type;
+  const P* v = reinterpret_cast<const P*>(&y);
+  P mx = __habs2(v[0]);
+#pragma unroll
+  for (int e = 1; e < 16; e++) mx = top2(mx, v[e]);
+  const unsigned both = max(__float_as_uint(to_f(mx.x)) & 0x7fffffffu, __float_as_uint(to_f(mx.y)) & 0x7fffffffu);
+  const unsigned all = __reduce_max_sync(0xffffffffu, both);
+  if ((threadIdx.x & 31) == 0) sm.top[which][threadIdx.x >> 5] = all;
+}
+template <class T>
+__device__ __forceinline__ void store_codes(const PagedView& c, const Append& w, int blk, int page, const Chunks& at, const BlockRows<T>& y, const BlockSmem& sm, int which) {
+  const int first = w.first(blk), rows = w.rows(blk);
   unsigned mx = 0;
 #pragma unroll
-  for (int e = 0; e < 16; e++) mx = max(mx, __float_as_uint(to_f(y.x[e >> 3].v[e & 7])) & 0x7fffffffu);
-  mx = __reduce_max_sync(0xffffffffu, mx);
-  if (lane == 0) sm.top[which][warp] = mx;
-  const int page = c.page_of(b, first);
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < NT / 32; w++) mx = max(mx, sm.top[which][w]);
+  for (int e = 0; e < AT / 32; e++) mx = max(mx, sm.top[which][e]);
   float scale = __fdiv_rn(__uint_as_float(mx), 127.f);
   if (mx >= 0x7f800000u) scale = __uint_as_float(0x7fc00000u);   // infinities, NaN
   const Quotient by = quotient_by(scale);
-  const size_t row = c.code_row(l, page, h, side) + (first & (c.page - 1));
-  if (there) {
+  const size_t row = c.code_row(w.l, page, w.h, w.side) + (first & (c.page - 1));
+  if (at.t < rows) {
     int8_t* dst = c.codes + (row + at.t) * D;
 #pragma unroll
-    for (int half = 0; half < 2; half++) {
+    for (int z = 0; z < 4; z++) {
       uint32_t q[8];
-      by.codes(y.x[half], q);
-      uint2 w;
-      w.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
-      w.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
-      *reinterpret_cast<uint2*>(dst + (half ? at.c1 : at.c0)) = w;
+      by.codes(y.x[z], q);
+      uint2 u;
+      u.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+      u.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+      *reinterpret_cast<uint2*>(dst + at.c[z]) = u;
     }
-    if (rows < PB && i >= 0) {   // a block that stays unfinished
-      T* keep = c.raw_of<T>(l, b, h, side) + (size_t)at.t * D;
-      *reinterpret_cast<Vec8<T>*>(keep + at.c0) = y.x[0];
-      *reinterpret_cast<Vec8<T>*>(keep + at.c1) = y.x[1];
+    if (rows < PB && first + at.t >= w.len) {   // a block that stays unfinished
+      T* keep = c.raw_of<T>(w.l, w.b, w.h, w.side) + (size_t)at.t * D;
+#pragma unroll
+      for (int z = 0; z < 4; z++) *reinterpret_cast<Vec8<T>*>(keep + at.c[z]) = y.x[z];
     }
   }
-  if (tid == 0) c.scales[row / PB] = scale;
+  if (threadIdx.x == 0) c.scales[row / PB] = scale;
 }
 
-// A thread block has one side of a 32-token block: keys and values apart keep a thread to 16 numbers and five blocks on an SM (both in
-// one took 124 registers: two blocks, 199 us for 28 layers x 4097 tokens x 4 heads).
+// A thread block has one side of `per` consecutive 32-token blocks and loads each while it quantises the one before: keys and values
+// apart keep a thread to 16 numbers (both in one took 124 registers, two blocks on an SM: 199 us for 28 layers x 4097 tokens x 4
+// heads, against 121 apart and one by one).
 template <class T>
-__global__ void __launch_bounds__(NT) k_paged_append(const PagedView c, int layer, const Rows k, const Rows v, int n_new, const int32_t* new_len,
-                                                     const RopeView rope, int n_blocks) {
+__global__ void __launch_bounds__(AT, 8) k_paged_append(const PagedView c, int layer, const Rows k, const Rows v, int n_new, const int32_t* new_len,
+                                                     const RopeView rope, int n_ranges, int per) {
   __shared__ BlockSmem sm;
   depend_wait();
   const int tid = threadIdx.x;
   unsigned u = blockIdx.x;
-  int blk = (int)(u % (unsigned)n_blocks);
-  u /= (unsigned)n_blocks;
-  const int side = (int)(u & 1);
+  Append w;
+  const int blk0 = (int)(u % (unsigned)n_ranges) * per;
+  u /= (unsigned)n_ranges;
+  w.side = (int)(u & 1);
   u >>= 1;
-  const int h = (int)(u % (unsigned)c.n_kv);
+  w.h = (int)(u % (unsigned)c.n_kv);
   u /= (unsigned)c.n_kv;
-  const int li = (int)(u / (unsigned)c.batch), b = (int)(u - (unsigned)li * c.batch), l = layer + li;
-  const int m = count_of(new_len, b, n_new), len = c.held(l, b), r = len % PB, end = len + m;
-  if (m == 0 || len - r + blk * PB >= end) return;
+  w.li = (int)(u / (unsigned)c.batch);
+  w.b = (int)(u - (unsigned)w.li * c.batch);
+  w.l = layer + w.li;
+  w.n_new = n_new;
+  w.m = count_of(new_len, w.b, n_new);
+  w.len = c.held(w.l, w.b);
+  const int r = w.len % PB, blocks = (r + w.m + PB - 1) / PB;
+  if (w.m == 0 || blk0 >= blocks) return;
   // The raw tokens are read by the first block and replaced by the last, so one thread block does both, in that order.
-  const int last = (r + m - 1) / PB;
-  const bool follows = r > 0 && last > 0 && (r + m) % PB != 0;
-  if (follows && blk == last) return;
-  const Chunks at(tid, rope, side == 0);
-  BlockRows<T> y;
-  load_block<T>(c, l, li, b, h, side, len, m, blk, side ? v : k, n_new, rope, at, y, sm);
-  if (__syncthreads_or(pages_missing(c, b, len, m, tid, NT))) return;   // (while the rows are on their way)
-  store_block<T>(c, l, b, h, side, len, m, blk, at, y, sm, 0);
-  if (!follows || blk != 0) return;
-  load_block<T>(c, l, li, b, h, side, len, m, last, side ? v : k, n_new, rope, at, y, sm);
-  store_block<T>(c, l, b, h, side, len, m, last, at, y, sm, 1);
+  const int last = blocks - 1;
+  const bool follows = r > 0 && last >= per && (r + w.m) % PB != 0;
+  int n = min(per, blocks - blk0);
+  if (follows && blk0 == 0) n = per + 1;
+  if (follows && blk0 > 0 && blk0 + n > last && --n == 0) return;
+  auto block = [&](int e) { return follows && blk0 == 0 && e == per ? last : blk0 + e; };
+  const Rows& src = w.side ? v : k;
+  const Chunks at(tid, rope, w.side == 0);
+  const bool turns = rope.freq && w.side == 0;
+  BlockRows<T> y, z;
+  load_rows<T>(c, w, blk0, src, at, y);
+  if (turns) make_turns(c, w, blk0, rope, sm);
+  if (__syncthreads_or(pages_missing(c, w.b, w.len, w.m, tid, AT))) return;   // (while the rows are on their way)
+  for (int e = 0; e < n; e++) {
+    const int blk = block(e), page = c.page_of(w.b, w.first(blk));
+    turn_rows<T>(w, blk, at, y, sm, e & 1);
+    __syncthreads();
+    if (e + 1 < n) {
+      load_rows<T>(c, w, block(e + 1), src, at, z);
+      if (turns) make_turns(c, w, block(e + 1), rope, sm);
+    }
+    store_codes<T>(c, w, blk, page, at, y, sm, e & 1);
+    if (turns) __syncthreads();
+    y = z;
+  }
 }
 
 // The same for up to FEW new tokens (two blocks of a sequence at most) in one launch: a cluster has a (layer, sequence), each of its
 // blocks every size-th side of a head, and the length is advanced when all of them have read it.
 constexpr int FEW = PB, MOST = 8;
 template <class T>
-__global__ void __launch_bounds__(NT) k_paged_append_few(const PagedView c, int layer, const Rows k, const Rows v, int n_new, const int32_t* new_len,
+__global__ void __launch_bounds__(AT) k_paged_append_few(const PagedView c, int layer, const Rows k, const Rows v, int n_new, const int32_t* new_len,
                                                          const RopeView rope, int size) {
   __shared__ BlockSmem sm;
   depend_wait();
-  const int tid = threadIdx.x, rank = blockIdx.x % size, u = blockIdx.x / size, li = u / c.batch, b = u - li * c.batch, l = layer + li;
-  const int m = count_of(new_len, b, n_new), len = c.held(l, b), r = len % PB;
-  if (m == 0) return;                       // (the whole cluster)
-  const int last = (r + m - 1) / PB;        // 0 or 1
+  const int tid = threadIdx.x, rank = blockIdx.x % size, u = blockIdx.x / size;
+  Append w;
+  w.li = u / c.batch;
+  w.b = u - w.li * c.batch;
+  w.l = layer + w.li;
+  w.n_new = n_new;
+  w.m = count_of(new_len, w.b, n_new);
+  w.len = c.held(w.l, w.b);
+  const int r = w.len % PB;
+  if (w.m == 0) return;                       // (the whole cluster)
+  const int last = (r + w.m - 1) / PB;        // 0 or 1
   int which = 0, bad = 0;
   for (int e = rank; e < 2 * c.n_kv && !bad; e += size) {
-    const int h = e >> 1, side = e & 1;
-    const Chunks at(tid, rope, side == 0);
+    w.h = e >> 1;
+    w.side = e & 1;
+    const Chunks at(tid, rope, w.side == 0);
     for (int blk = 0; blk <= last; blk++, which ^= 1) {
       BlockRows<T> y;
-      load_block<T>(c, l, li, b, h, side, len, m, blk, side ? v : k, n_new, rope, at, y, sm);
+      load_rows<T>(c, w, blk, w.side ? v : k, at, y);
+      if (rope.freq && w.side == 0) {
+        make_turns(c, w, blk, rope, sm);
+        __syncthreads();
+      }
       // (the first rows are on their way while the table is looked at)
-      if (e == rank && blk == 0 && (bad = __syncthreads_or(pages_missing(c, b, len, m, tid, NT)))) break;
-      store_block<T>(c, l, b, h, side, len, m, blk, at, y, sm, which);   // (its barrier is behind the loads: raw tokens are read before they are replaced)
+      if (e == rank && blk == 0 && (bad = __syncthreads_or(pages_missing(c, w.b, w.len, w.m, tid, AT)))) break;
+      const int page = c.page_of(w.b, w.first(blk));
+      turn_rows<T>(w, blk, at, y, sm, which);
+      __syncthreads();                        // (behind the loads: raw tokens are read before they are replaced)
+      store_codes<T>(c, w, blk, page, at, y, sm, which);
     }
   }
   if (size > 1) {
@@ -220,7 +278,7 @@ __global__ void __launch_bounds__(NT) k_paged_append_few(const PagedView c, int 
   }
   if (tid != 0 || rank != 0) return;
   if (bad) set_status(c.status, OKQ_ERR_CAPACITY);
-  else c.seq_len[(size_t)l * c.batch + b] = len + m;
+  else c.seq_len[(size_t)w.l * c.batch + w.b] = w.len + w.m;
 }
 
 // lengths after an append, and the status of sequences that could not take theirs; one warp per (layer, sequence)
@@ -280,13 +338,15 @@ okq_status launch_append(const PagedView& c, int layer, int layer_count, const R
                          const RopeView& rope, cudaStream_t s) {
   if (n_new <= FEW) {
     const int size = 2 * c.n_kv < MOST ? 2 * c.n_kv : MOST;
-    const cudaError_t e = launch_dependent(k_paged_append_few<T>, dim3((unsigned)(layer_count * c.batch * size)), NT, 0, s, size, c, layer, k, v, n_new, new_len, rope, size);
+    const cudaError_t e = launch_dependent(k_paged_append_few<T>, dim3((unsigned)(layer_count * c.batch * size)), AT, 0, s, size, c, layer, k, v, n_new, new_len, rope, size);
     return e != cudaSuccess ? failed(e) : launch_status();
   }
+  // blocks in a row: as many as leave each SM sixteen thread blocks or more, four at most
   const int n_blocks = (PB - 1 + n_new + PB - 1) / PB;
-  const long long grid = 2ll * layer_count * c.batch * c.n_kv * n_blocks;
-  if (grid > 0x7fffffffll) return OKQ_ERR_UNSUPPORTED;
-  cudaError_t e = launch_dependent(k_paged_append<T>, dim3((unsigned)grid), NT, 0, s, 1, c, layer, k, v, n_new, new_len, rope, n_blocks);
+  const long long units = 2ll * layer_count * c.batch * c.n_kv, want = units * n_blocks / (16ll * sm_count());
+  const int per = want < 1 ? 1 : want > 4 ? 4 : (int)want, n_ranges = (n_blocks + per - 1) / per;
+  if (units * n_ranges > 0x7fffffffll) return OKQ_ERR_UNSUPPORTED;
+  cudaError_t e = launch_dependent(k_paged_append<T>, dim3((unsigned)(units * n_ranges)), AT, 0, s, 1, c, layer, k, v, n_new, new_len, rope, n_ranges, per);
   if (e != cudaSuccess) return failed(e);
   const int warps = NT / 32;
   e = launch_dependent(k_paged_advance, dim3((layer_count * c.batch + warps - 1) / warps), NT, 0, s, 1, c, layer, layer_count, n_new, new_len);
