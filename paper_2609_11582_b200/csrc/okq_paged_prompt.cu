@@ -54,8 +54,11 @@ struct PromptSmem {
   __align__(1024) unsigned char v[NR][2][KV_HALF];
   __align__(1024) int8_t code[2][2][SIDE];         // [keys, values][tile mod 2]
   __align__(16) Info info[4];
-  __align__(8) unsigned long long code_full[2][2], code_free[2][2], info_full[4], k_full[NR], k_free[NR], v_full[NR], v_free[NR];
+  __align__(8) unsigned long long code_full[2][2], code_free[2][2], info_full[4], k_free[NR], v_free[NR];
   __align__(8) unsigned long long s_full[2][2], p_full[2][2], o_full[2], q_full[2];   // [stream][place]
+  // steps of keys, and values, that are in fp16, by converting warp: numbers and not phases, since a stream of a dual item looks at every
+  // other step only and could take a phase for the one after the next
+  __align__(8) volatile int done[2][2];
   FindSmem<1> find;
   uint32_t tmem_slot;
   long long limit;
@@ -106,6 +109,25 @@ __device__ __forceinline__ uint2 codes_to_half(uint32_t w) {
   uint32_t lo = __byte_perm(w, 0x64646464u, 0x4140), hi = __byte_perm(w, 0x64646464u, 0x4342);
   const __half2 a = __hsub2(*reinterpret_cast<__half2*>(&lo), bias), b = __hsub2(*reinterpret_cast<__half2*>(&hi), bias);
   return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+
+// Wait of a warp until both converting warps have done step x, with the limit of every wait.
+__device__ __forceinline__ bool step_ready(PromptSmem& sm, const volatile int* done, int x) {
+  const uint32_t at = smem_u32(const_cast<const int*>(done));
+  const long long t0 = clock64();
+  bool ok = true;
+  for (;;) {
+    int a, b;
+    asm volatile("ld.volatile.shared.v2.s32 {%0, %1}, [%2];\n" : "=r"(a), "=r"(b) : "r"(at) : "memory");
+    if (a > x && b > x) break;
+    if (sm.abort || clock64() - t0 > sm.limit) {
+      ok = false;
+      break;
+    }
+  }
+  if (!ok) sm.abort = 1;
+  __threadfence_block();
+  return __all_sync(0xffffffffu, ok);
 }
 
 // The 32 rows of a warp in a row tile: rotated, scaled by a power of two, swizzled; returns the factor of the exponent that undoes the
@@ -222,10 +244,11 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
   if (tid == 0) {
     auto init = [](unsigned long long* b, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(smem_u32(b)), "r"(count)); };
     for (int i = 0; i < 4; i++) {
-      init(&sm.code_full[0][0] + i, 1); init(&sm.code_free[0][0] + i, 4); init(&sm.info_full[i], 1);
+      init(&sm.code_full[0][0] + i, 1); init(&sm.code_free[0][0] + i, 2); init(&sm.info_full[i], 1);
       init(&sm.s_full[0][0] + i, 1); init(&sm.p_full[0][0] + i, 4);
     }
-    for (int i = 0; i < NR; i++) { init(&sm.k_full[i], 4); init(&sm.k_free[i], 2); init(&sm.v_full[i], 4); init(&sm.v_free[i], 2); }
+    for (int i = 0; i < NR; i++) { init(&sm.k_free[i], 2); init(&sm.v_free[i], 2); }
+    for (int i = 0; i < 4; i++) sm.done[i >> 1][i & 1] = 0;
     for (int i = 0; i < 2; i++) { init(&sm.o_full[i], 1); init(&sm.q_full[i], 4); }
     sm.abort = 0;
     sm.tmem_busy = 0;
@@ -344,11 +367,10 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     int items = 0, n_o = 0;                       // items so far, steps through
     uint32_t scored = 0, ph_s = 0, ph_p = 0;      // by place for scores, a bit each: whether any were issued; phases to come
     bool go = true;
-    // A step's buffers are free when both streams are through with them: its products, or, in a dual item, a look at the steps that are
-    // the other stream's (a stream that did not look at every phase of a barrier could take one for the one after the next).
-    auto score = [&](int x, int place, uint64_t ad) {
+    // A step's buffers are free when both streams are through with them; the one stream that uses a step of a dual item says so twice.
+    auto score = [&](int x, int place, uint64_t ad, bool dual) {
       const int s = x % NR;
-      if (!(go = go && bar_wait(sm, &sm.k_full[s], (uint32_t)(x / NR) & 1u))) return;
+      if (!(go = go && step_ready(sm, sm.done[0], x))) return;
       if (elect_one()) {
         after_sync();
         const uint64_t bd = make_desc_sw128(smem_u32(sm.k[s][0]));
@@ -357,15 +379,11 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
           mma_ss(s_at + 64u * place, ad + (uint64_t)(((k & 3) * 32 + (k >> 2) * Q_HALF) >> 4), bd + (uint64_t)(((k & 3) * 32 + (k >> 2) * KV_HALF) >> 4), id_s, k != 0);
         commit(&sm.s_full[t][place]);
         commit(&sm.k_free[s]);
+        if (dual) commit(&sm.k_free[s]);
       }
       __syncwarp();
       scored |= 1u << place;
       ph_s ^= 1u << place;
-    };
-    auto pass = [&](int x, bool values) {   // step x is the other stream's
-      const int s = x % NR;
-      if (!(go = go && bar_wait(sm, values ? &sm.v_full[s] : &sm.k_full[s], (uint32_t)(x / NR) & 1u))) return;
-      if (lane == 0) mbar_arrive(values ? &sm.v_free[s] : &sm.k_free[s]);
     };
     for (int i = 0; i < n_my && go;) {
       const bool dual = cur.m * c.group - cur.rt * R <= M;        // both streams have the same rows
@@ -373,15 +391,10 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       const int x0 = 2 * i + (dual ? t : 0), dx = dual ? 2 : 1;   // step y is step x0 + dx y of the range
       const uint64_t ad = make_desc_sw128(smem_u32(sm.q[dual ? 0 : t][0]));
       go = bar_wait(sm, &sm.q_full[t], (uint32_t)(items++) & 1u);
-      // (in a dual item stream A passes the step before each but the first of its own, and in the end the last one; B the step before each)
-      for (int y = 0; y < min(2, steps); y++) {
-        if (dual && (t || y)) pass(x0 + dx * y - 1, false);
-        score(x0 + dx * y, y, ad);
-      }
+      for (int y = 0; y < min(2, steps); y++) score(x0 + dx * y, y, ad, dual);
       for (int y = 0; y < steps && go; y++) {
         const int x = x0 + dx * y, s = x % NR, place = y & 1;
-        if (dual && (t || y)) pass(x - 1, true);
-        if (!(go = go && bar_wait(sm, &sm.p_full[t][place], ph_p >> place & 1u) && bar_wait(sm, &sm.v_full[s], (uint32_t)(x / NR) & 1u))) break;
+        if (!(go = go && bar_wait(sm, &sm.p_full[t][place], ph_p >> place & 1u) && step_ready(sm, sm.done[1], x))) break;
         ph_p ^= 1u << place;
         if (elect_one()) {
           after_sync();
@@ -391,17 +404,11 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
             mma_ts(o_at, s_at + 64u * place + 8u * k, bd + (uint64_t)(k * 2048 >> 4), id_o, y > 0 || k != 0);
           commit(&sm.o_full[t]);
           commit(&sm.v_free[s]);
+          if (dual) commit(&sm.v_free[s]);
         }
         __syncwarp();
         n_o++;
-        if (y + 2 < steps) {
-          if (dual) pass(x + 2 * dx - 1, false);
-          score(x + 2 * dx, place, ad);
-        }
-      }
-      if (dual && t == 0) {
-        pass(x0 + 2 * steps - 1, false);
-        pass(x0 + 2 * steps - 1, true);
+        if (y + 2 < steps) score(x + 2 * dx, place, ad, dual);
       }
       i += n;
       cur.next_item(work);
@@ -412,51 +419,48 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     if (n_o > 0 && !mbar_drain(&sm.o_full[t], (uint32_t)(n_o - 1) & 1u)) sm.tmem_busy = 1;
   } else if (warp >= W_CONV) {
     // ------------------------------------------------------------------ codes to fp16: eight lanes to a token, sixteen channels each
-    const int ct = tid - 32 * W_CONV, j = ct & 7;
+    // Two warps have the keys, two the values.
+    const int side = (warp - W_CONV) >> 1, who = (warp - W_CONV) & 1, ct = 32 * who + lane, j = ct & 7;
     for (int x = 0; x < 2 * n_my; x++) {
       const int i = x >> 1, half = x & 1, s = x % NR;
       if (!half) {
-        bar_wait(sm, &sm.info_full[i & 3], (uint32_t)(i >> 2) & 1u);
-        bar_wait(sm, &sm.code_full[0][i & 1], (uint32_t)(i >> 1) & 1u);
-        bar_wait(sm, &sm.code_full[1][i & 1], (uint32_t)(i >> 1) & 1u);
+        if (side) bar_wait(sm, &sm.info_full[i & 3], (uint32_t)(i >> 2) & 1u);
+        bar_wait(sm, &sm.code_full[side][i & 1], (uint32_t)(i >> 1) & 1u);
       }
-      const bool plain = sm.info[i & 3].plain;
-      uint4 w[2][4];
+      const bool plain = !side || sm.info[i & 3].plain;
+      const int8_t* from = sm.code[side][i & 1] + (half * PH + (ct >> 3)) * D + 16 * j;
+      uint4 w[8];
 #pragma unroll
-      for (int side = 0; side < 2; side++)
+      for (int z = 0; z < 8; z++) w[z] = *reinterpret_cast<const uint4*>(from + 8 * z * D);
+      if (x >= NR) bar_wait(sm, side ? &sm.v_free[s] : &sm.k_free[s], (uint32_t)(x / NR - 1) & 1u);
+      unsigned char* to = (side ? sm.v[s][0] : sm.k[s][0]) + (j >> 2) * KV_HALF + (ct >> 3) * 128;
 #pragma unroll
-        for (int z = 0; z < 4; z++) w[side][z] = *reinterpret_cast<const uint4*>(sm.code[side][i & 1] + (half * PH + 16 * z + (ct >> 3)) * D + 16 * j);
-      // (keys do not wait for the values' place: the scores of a step are wanted two steps before its values)
+      for (int z = 0; z < 8; z++) {
+        const int t = 8 * z + (ct >> 3);
+        uint2 h[4] = {codes_to_half(w[z].x), codes_to_half(w[z].y), codes_to_half(w[z].z), codes_to_half(w[z].w)};
+        if (!plain) {
+          const float mul = sm.info[i & 3].mul[2 * half + (t >> 5)];
+          const __half2 m2 = __floats2half2_rn(mul, mul);
 #pragma unroll
-      for (int side = 0; side < 2; side++) {
-        if (x >= NR) bar_wait(sm, side ? &sm.v_free[s] : &sm.k_free[s], (uint32_t)(x / NR - 1) & 1u);
-#pragma unroll
-        for (int z = 0; z < 4; z++) {
-          const int t = 16 * z + (ct >> 3);
-          uint2 h[4] = {codes_to_half(w[side][z].x), codes_to_half(w[side][z].y), codes_to_half(w[side][z].z), codes_to_half(w[side][z].w)};
-          if (side && !plain) {
-            const float mul = sm.info[i & 3].mul[2 * half + (t >> 5)];
-            const __half2 m2 = __floats2half2_rn(mul, mul);
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-              __half2* y = reinterpret_cast<__half2*>(&h[e]);
-              y[0] = __hmul2(y[0], m2);
-              y[1] = __hmul2(y[1], m2);
-            }
+          for (int e = 0; e < 4; e++) {
+            __half2* y = reinterpret_cast<__half2*>(&h[e]);
+            y[0] = __hmul2(y[0], m2);
+            y[1] = __hmul2(y[1], m2);
           }
-          // chunks 2 (j & 3) and the next of the row's 64 channels; the two halves' lanes in opposite order, for the banks' sake
-          unsigned char* row = (side ? sm.v[s][0] : sm.k[s][0]) + (j >> 2) * KV_HALF + t * 128;
-          const int a0 = (2 * (j & 3)) ^ (t & 7), a1 = (2 * (j & 3) + 1) ^ (t & 7);
-          const uint4 y0 = make_uint4(h[0].x, h[0].y, h[1].x, h[1].y), y1 = make_uint4(h[2].x, h[2].y, h[3].x, h[3].y);
-          *reinterpret_cast<uint4*>(row + (j < 4 ? a0 : a1) * 16) = j < 4 ? y0 : y1;
-          *reinterpret_cast<uint4*>(row + (j < 4 ? a1 : a0) * 16) = j < 4 ? y1 : y0;
         }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(side ? &sm.v_full[s] : &sm.k_full[s]);
-          if (half) mbar_arrive(&sm.code_free[side][i & 1]);
-        }
+        // chunks 2 (j & 3) and the next of the row's 64 channels; the two halves' lanes in opposite order, for the banks' sake
+        unsigned char* row = to + 8 * z * 128;
+        const int a0 = (2 * (j & 3)) ^ (t & 7), a1 = (2 * (j & 3) + 1) ^ (t & 7);
+        const uint4 y0 = make_uint4(h[0].x, h[0].y, h[1].x, h[1].y), y1 = make_uint4(h[2].x, h[2].y, h[3].x, h[3].y);
+        *reinterpret_cast<uint4*>(row + (j < 4 ? a0 : a1) * 16) = j < 4 ? y0 : y1;
+        *reinterpret_cast<uint4*>(row + (j < 4 ? a1 : a0) * 16) = j < 4 ? y1 : y0;
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        __threadfence_block();
+        sm.done[side][who] = x + 1;
+        if (half) mbar_arrive(&sm.code_free[side][i & 1]);
       }
     }
   } else {
