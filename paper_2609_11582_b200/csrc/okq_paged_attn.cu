@@ -22,7 +22,7 @@ bool make_plan(const okq_paged* c, int layer_count, int n_new, Plan& p) {
   const int per = p.decode ? DECODE_ROWS : PROMPT_ROWS;
   const double items = (double)layer_count * c->batch * c->n_kv_heads * (double)((rows + per - 1) / per);
   const long long per_item = ((long long)c->max_pages * c->page_tokens + PT - 1) / PT;
-  if (items * (double)per_item > 2147483647.0) return false;
+  if (items * (double)(per_item + (p.decode ? DECODE_EXTRA : PROMPT_EXTRA)) > 2147483647.0) return false;
   const long long tiles = (long long)items * per_item, n = sm_count();
   p.grid = (int)(tiles < n ? tiles : n);
   p.ranges = p.grid * (p.decode ? DECODE_PIPES : 1);

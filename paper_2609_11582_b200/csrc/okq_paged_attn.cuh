@@ -1,8 +1,9 @@
 // What the two attention kernels over the 8-bit paged cache share: how the work is cut and numbered, partial results, the merge.
 //
 // An item is a (layer, sequence, KV head) with up to ROWS of its query rows (row = query * group + head of the group), a tile 128 of its
-// tokens.  Items follow one another in one long line of tiles, which is cut into as many even ranges as there are pipelines on the GPU
-// (fewer where there are fewer tiles), whatever the lengths are, which only the device knows.  A piece is what a range holds of an
+// tokens.  Items follow one another in one long line of units, a unit for each tile and EXTRA behind an item's last for what an item
+// costs besides (its queries, its output), and the line is cut into as many even ranges as there are pipelines on the GPU (fewer where
+// there are fewer units), whatever the lengths are, which only the device knows.  A piece is what a range holds of an
 // item: all of it (its pipeline writes the output), or a part, whose unnormalised sums, maximum and normaliser go to one of the
 // range's two slots (2 v for an item that began in an earlier range, 2 v + 1 for one that goes on in a later one).  k_paged_merge
 // puts parts together, in order.
@@ -47,7 +48,7 @@ struct AttnArgs {
 };
 
 // tiles that an item reads: those up to the last token that its last row sees
-template <int ROWS> struct Work {
+template <int ROWS, int EXTRA> struct Work {
   int pairs, n_kv, group;
   const AttnArgs& a;
   __device__ __forceinline__ explicit Work(const AttnArgs& args) : pairs(args.layer_count * args.c.batch), n_kv(args.c.n_kv), group(args.c.group), a(args) {}
@@ -67,26 +68,29 @@ template <int ROWS> struct Work {
     const int seen = len - m + last + 1;
     return seen <= 0 ? 0 : (seen + PT - 1) / PT;
   }
-  __device__ __forceinline__ int head_tiles(int len, int m) const {   // of all row tiles of one head
+  __device__ __forceinline__ int units(int nt) const { return nt > 0 ? nt + EXTRA : 0; }
+  __device__ __forceinline__ int head_units(int len, int m) const {   // of all row tiles of one head
     int s = 0;
-    for (int rt = 0; rt < row_tiles(m); rt++) s += tiles(len, m, rt);
+    for (int rt = 0; rt < row_tiles(m); rt++) s += units(tiles(len, m, rt));
     return s;
   }
 };
 
-// A place in the line of tiles.
-template <int ROWS> struct Cursor {
+// A walk over the tiles of a range.
+template <int ROWS, int EXTRA> struct Cursor {
   int pair, h, rt, tile;     // item and tile inside it
   int li, b;                 // layer (of the call's) and sequence of the pair
   int len, m, nt;            // of the item: tokens, queries, tiles
-  __device__ __forceinline__ void next_item(const Work<ROWS>& w) {
+  int left;                  // units of the range from this tile on
+  bool ok, ended;            // there is a tile here; the tile before was its item's last
+  __device__ __forceinline__ void next_item(const Work<ROWS, EXTRA>& w) {
     tile = 0;
     for (;;) {
       if (++rt < w.row_tiles(m)) nt = w.tiles(len, m, rt);
       else if (rt = 0, ++h < w.n_kv) nt = m ? w.tiles(len, m, 0) : 0;
       else {
         h = 0;
-        if (++pair >= w.pairs) return;
+        if (++pair >= w.pairs) { ok = false; return; }
         if (++b == w.a.c.batch) { b = 0; li++; }
         w.lens(li, b, len, m);
         nt = m ? w.tiles(len, m, 0) : 0;
@@ -94,38 +98,45 @@ template <int ROWS> struct Cursor {
       if (nt > 0) return;
     }
   }
-  __device__ __forceinline__ void next(const Work<ROWS>& w) {
-    if (++tile == nt) next_item(w);
+  __device__ __forceinline__ int piece() const { return min(nt - tile, left); }   // tiles of the item in the range, from this one on
+  __device__ __forceinline__ void skip(const Work<ROWS, EXTRA>& w, int n) {       // no more than piece()
+    tile += n;
+    left -= n;
+    ended = tile == nt;
+    if (ended) left -= EXTRA;
+    ok = left > 0;
+    if (ended && ok) next_item(w);
   }
+  __device__ __forceinline__ void next(const Work<ROWS, EXTRA>& w) { skip(w, 1); }
 };
 
-// The line of `total` tiles in `ranges` parts, as even as they go: the first `extra` of them have one tile more.  With fewer tiles than
-// ranges the last ranges have none.  (Numbers of tiles have 32 bits: the caller sees to it.)
+// The line of `total` units in `ranges` parts, as even as they go: the first `extra` of them have one unit more.  With fewer units than
+// ranges the last ranges have none.  (Numbers of units have 32 bits: the caller sees to it.)
 struct Cuts {
   int total, each, extra;
   __device__ __forceinline__ Cuts(int t, int ranges) : total(t), each(t / ranges), extra(t - each * ranges) {}
   __device__ __forceinline__ int start(int v) const { return v * each + min(v, extra); }
   __device__ __forceinline__ int size(int v) const { return each + (v < extra); }
-  __device__ __forceinline__ int range_of(int tile) const {
+  __device__ __forceinline__ int range_of(int unit) const {
     const int wide = extra * (each + 1);
-    return tile < wide ? tile / (each + 1) : extra + (tile - wide) / each;
+    return unit < wide ? unit / (each + 1) : extra + (unit - wide) / each;
   }
 };
 
-// All threads of a block find the line's length and where the first tiles of the block's ranges v0, v0 + step, .. lie.  Threads hold
+// All threads of a block find the line's length and where the first units of the block's ranges v0, v0 + step, .. lie.  Threads hold
 // consecutive pairs.
 template <int G> struct FindSmem {
   int warp[32];
   int place[G][6];
 };
-template <int ROWS, int NT, int G>
-__device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS>& w, int ranges, int v0, int step) {
+template <int ROWS, int EXTRA, int NT, int G>
+__device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS, EXTRA>& w, int ranges, int v0, int step) {
   const int tid = threadIdx.x, lane = tid & 31, wp = tid >> 5;
   const int chunk = (w.pairs + NT - 1) / NT, p0 = min(w.pairs, tid * chunk), p1 = min(w.pairs, p0 + chunk);
   int len = 0, m = 0, per_head = 0, mine = 0;    // (of the last pair looked at: with no more pairs than threads, the only one)
   for (int p = p0; p < p1; p++) {
     w.lens(p, len, m);
-    per_head = w.head_tiles(len, m);
+    per_head = w.head_units(len, m);
     mine += per_head * w.n_kv;
   }
   int v = mine;
@@ -153,27 +164,36 @@ __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS>& w
       if (chunk > 1)
         for (;; p++) {
           w.lens(p, len, m);
-          per_head = w.head_tiles(len, m);
+          per_head = w.head_units(len, m);
           if (target < at + per_head * w.n_kv) break;
           at += per_head * w.n_kv;
         }
       const int h = (target - at) / per_head;
       at += h * per_head;
       int rt = 0;
-      while (target >= at + w.tiles(len, m, rt)) at += w.tiles(len, m, rt++);
+      while (target >= at + w.units(w.tiles(len, m, rt))) at += w.units(w.tiles(len, m, rt++));
       sm.place[g][0] = p; sm.place[g][1] = h; sm.place[g][2] = rt; sm.place[g][3] = target - at; sm.place[g][4] = len; sm.place[g][5] = m;
     }
   }
   __syncthreads();
   return cuts;
 }
-// the place found for range v0 + g * step; not to be called for a range without tiles
-template <int ROWS, int G> __device__ __forceinline__ Cursor<ROWS> place(const FindSmem<G>& sm, const Work<ROWS>& w, int g) {
-  Cursor<ROWS> c;
+// the first tile of range v = v0 + g * step
+template <int ROWS, int EXTRA, int G>
+__device__ __forceinline__ Cursor<ROWS, EXTRA> place(const FindSmem<G>& sm, const Work<ROWS, EXTRA>& w, const Cuts& cuts, int v, int g) {
+  Cursor<ROWS, EXTRA> c{};
+  c.left = cuts.size(v);
+  c.ok = c.left > 0;
+  if (!c.ok) return c;
   c.pair = sm.place[g][0]; c.h = sm.place[g][1]; c.rt = sm.place[g][2]; c.tile = sm.place[g][3]; c.len = sm.place[g][4]; c.m = sm.place[g][5];
   c.li = w.layer_of(c.pair);
   c.b = c.pair - c.li * w.a.c.batch;
   c.nt = w.tiles(c.len, c.m, c.rt);
+  if (c.tile >= c.nt) {   // behind an item's last tile
+    c.left -= c.nt + EXTRA - c.tile;
+    c.ok = c.left > 0;
+    if (c.ok) c.next_item(w);
+  }
   return c;
 }
 
@@ -202,7 +222,8 @@ template <int ROWS> struct Heads {
 };
 
 // Zeros for the rows of items without tiles (queries that see nothing), and the heads of these items.  `who` of `n_who` warps.
-template <class T, int ROWS> __device__ __forceinline__ void write_empty(const AttnArgs& a, const Work<ROWS>& w, const Heads<ROWS>& heads, int who, int n_who, int lane) {
+template <class T, int ROWS, int EXTRA>
+__device__ __forceinline__ void write_empty(const AttnArgs& a, const Work<ROWS, EXTRA>& w, const Heads<ROWS>& heads, int who, int n_who, int lane) {
   for (int pair = who; pair < w.pairs; pair += n_who) {
     int len, m;
     const int li = w.layer_of(pair), b = pair - li * a.c.batch;
@@ -236,7 +257,7 @@ __global__ void __launch_bounds__(MERGE_NT) k_paged_merge(const AttnArgs a) {
   constexpr size_t SLOT = (size_t)ROWS * (D + 2);
   const int n = hd.more + 1, row = hd.rt * ROWS + r;
   auto slot = [&](int k) { return a.slots + (size_t)(2 * (hd.v + k) + (k == 0)) * SLOT; };
-  const Work<ROWS> w(a);
+  const Work<ROWS, 0> w(a);
   int len, m;
   const int li = w.layer_of(hd.pair), b = hd.pair - li * a.c.batch;
   w.lens(li, b, len, m);
@@ -305,11 +326,12 @@ template <class T, int ROWS> inline cudaError_t launch_merge(const AttnArgs& a, 
   return launch_dependent(k_paged_merge<T, ROWS, WPR>, dim3(heads.count(ranges), (most + per - 1) / per), MERGE_NT, 0, s, 1, a);
 }
 
-// okq_paged_decode.cu: up to DECODE_ROWS rows, DECODE_PIPES pipelines per block
-constexpr int DECODE_ROWS = 8, DECODE_PIPES = 3;
+// okq_paged_decode.cu: up to DECODE_ROWS rows, DECODE_PIPES pipelines per block.  An item's own costs in tiles: queries, the first tile's
+// latency and the output take about as long as one and a half.
+constexpr int DECODE_ROWS = 8, DECODE_PIPES = 3, DECODE_EXTRA = 1;
 cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int grid, cudaStream_t s);
-// okq_paged_prompt.cu: any number of rows, one pipeline per block
-constexpr int PROMPT_ROWS = 256;
+// okq_paged_prompt.cu: any number of rows, one pipeline per block.  An item of a single tile takes 8 to 10 us, a further tile 2 to 3.
+constexpr int PROMPT_ROWS = 256, PROMPT_EXTRA = 3;
 cudaError_t launch_paged_prompt(const AttnArgs& a, int dtype, int grid, cudaStream_t s);
 
 // the pool's codes as rows of 128 bytes, copied 32 at a time

@@ -22,7 +22,7 @@ namespace okq {
 
 namespace {
 
-constexpr int R = DECODE_ROWS, G = DECODE_PIPES;
+constexpr int R = DECODE_ROWS, G = DECODE_PIPES, EXTRA = DECODE_EXTRA;
 constexpr int NS = 2;                     // ring of a pipeline
 constexpr int SIDE = PT * D;              // bytes of a tile's keys or values
 constexpr int WARPS = 5, SERVICE = 4;     // of a pipeline; the service warp's number in it
@@ -85,7 +85,7 @@ struct Block {
 // Two of an item's rows, r0 and r0 + 1: limbs (swizzled) and scales.  One warp, four channels per lane.  `turns`: cosines and sines of
 // the item's queries, [query][64 pairs].
 template <class T>
-__device__ __forceinline__ void prepare_queries(const AttnArgs& a, const Cursor<R>& cur, int r0, const uint2 (&raw)[2], const float2* turns, int8_t* qbuf,
+__device__ __forceinline__ void prepare_queries(const AttnArgs& a, const Cursor<R, EXTRA>& cur, int r0, const uint2 (&raw)[2], const float2* turns, int8_t* qbuf,
                                                 float* qscale, int lane) {
   const int step = a.rope.half >> 2;   // lanes from a channel to its partner
   const bool turned = a.rope.freq && lane < 2 * step, low = lane < step;
@@ -169,13 +169,11 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
   depend_wait();
 
   const PagedView& c = a.c;
-  const Work<R> work(a);
-  const Cuts cuts = find_places<R, NT, G>(sm.find, work, G * gridDim.x, blockIdx.x, gridDim.x);
-  const int v = blockIdx.x + g * gridDim.x;     // this pipeline's range
-  const int g0 = cuts.start(v), n_my = cuts.size(v);
+  const Work<R, EXTRA> work(a);
+  const Cuts cuts = find_places<R, EXTRA, NT, G>(sm.find, work, G * gridDim.x, blockIdx.x, gridDim.x);
+  const int v = blockIdx.x + g * gridDim.x, end = cuts.start(v) + cuts.size(v);     // this pipeline's range, and the unit behind it
   const Heads<R> heads(work.pairs, c.n_kv, c.group, a.n_new, G * gridDim.x);
-  Cursor<R> cur{};
-  if (n_my > 0) cur = place<R, G>(sm.find, work, g);
+  Cursor<R, EXTRA> cur = place<R, EXTRA, G>(sm.find, work, cuts, v, g);
 
   if (role == SERVICE) {
     // ------------------------------------------------------------------ copies and products
@@ -184,17 +182,18 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     constexpr uint32_t id_o = shape | (1u << 7) | (1u << 15) | (1u << 16);                     // A signed, B unsigned, both MN-major
     // Blocks of the tiles to come, eight tiles at a time, a lane for each block: entries of the page table when the batch before
     // begins, their scales halfway through it, so that neither load is waited for.
-    Cursor<R> ahead = cur;      // first tile that has not been looked up
+    Cursor<R, EXTRA> ahead = cur;      // first tile that has not been looked up
+    int n_now = 0, n_nx = 0;           // tiles of a batch
     int t_nx = 0, l_nx = 0, h_nx = 0, page_nx = -1;
     bool in_nx = false;
     Block now{-1, 0.f, 0.f}, nxt{-1, 0.f, 0.f};
-    auto entries = [&](int n) {
+    auto entries = [&] {
       int b = 0, len = 0;
-      for (int i = 0; i < n; i++) {
-        if (lane >> 2 == i) { t_nx = ahead.tile * PT + PB * (lane & 3); len = ahead.len; l_nx = a.layer + ahead.li; b = ahead.b; h_nx = ahead.h; }
+      for (n_nx = 0; n_nx < 8 && ahead.ok; n_nx++) {
+        if (lane >> 2 == n_nx) { t_nx = ahead.tile * PT + PB * (lane & 3); len = ahead.len; l_nx = a.layer + ahead.li; b = ahead.b; h_nx = ahead.h; }
         ahead.next(work);
       }
-      in_nx = lane >> 2 < n && t_nx < len;
+      in_nx = lane >> 2 < n_nx && t_nx < len;
       if (in_nx) {
         const int j = t_nx >> c.page_shift;
         page_nx = __ldg(&c.table[(size_t)b * c.max_pages + j]);   // (held() keeps j inside the row)
@@ -215,8 +214,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       const int k = i & 7, s = i % NS;
       if (k == 0) {
         now = nxt;
-        if (i + 8 < n_my) entries(min(8, n_my - i - 8));
-        else in_nx = false;
+        n_now = n_nx;
+        entries();
       }
       const bool mine = lane >> 2 == k, there = mine && now.row >= 0;
       const int blocks = __popc(__ballot_sync(0xffffffffu, there));
@@ -253,14 +252,16 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       scored = i + 1;
       return true;
     };
-    if (n_my > 0) {
-      entries(min(8, n_my));
+    auto more = [&] { return (armed & 7) == 0 ? n_nx > 0 : (armed & 7) < n_now; };   // there is a tile `armed`
+    bool go = cur.ok;
+    if (go) {
+      entries();
       scales();
-      for (; armed < min(NS, n_my); armed++) load(armed);
-      bool go = score(0, true);
-      for (int i = 0; i < n_my && go; i++) {
+      while (armed < NS && more()) load(armed++);
+      go = score(0, true);
+      for (int i = 0; go; i++) {
         cur.next(work);
-        if (!bar_wait(sm, &sy.p_full, (uint32_t)i & 1u)) break;
+        if (!bar_wait(sm, &sy.p_full, (uint32_t)i & 1u)) { go = false; break; }
         const int s = i % NS;
         if (elect_one()) {
           asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
@@ -272,14 +273,14 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         __syncwarp();
         done = i + 1;
         // (the workers have read the scores of tile i; the next item's queries are not ready before they have its sums too)
-        const bool fresh = cur.tile == 0;
-        if (i + 1 < n_my && !fresh) go = score(i + 1, false);
-        if (go && armed < n_my && (go = bar_wait(sm, &sy.o_full, (uint32_t)i & 1u))) load(armed++);
-        if (go && i + 1 < n_my && fresh) go = score(i + 1, true);
+        if (cur.ok && !cur.ended) go = score(i + 1, false);
+        if (go && more() && (go = bar_wait(sm, &sy.o_full, (uint32_t)i & 1u))) load(armed++);
+        if (go && cur.ok && cur.ended) go = score(i + 1, true);
+        if (!cur.ok) break;
       }
     }
     // Nothing may be in flight when the block ends or tensor memory is released; if the last products do not answer, it stays allocated.
-    if (sm.abort || done < n_my)
+    if (!go)
       for (int i = max(0, armed - NS); i < armed; i++) mbar_drain(&sy.full[i % NS], (uint32_t)(i / NS) & 1u);
     if (scored >= 1 && !mbar_drain(&sy.s_full, (uint32_t)(scored - 1) & 1u)) sm.tmem_busy = 1;
     if (done >= 1 && !mbar_drain(&sy.o_full, (uint32_t)(done - 1) & 1u)) sm.tmem_busy = 1;
@@ -291,8 +292,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     float top[R], sum[R], qs[R], o[R];
     bool fresh = true, whole = cur.tile == 0, began = cur.tile != 0;   // the piece has its item's first tile; the item began in an earlier range
     if (!heads.by_item && tid == g * 128) a.heads[v].more = 0;
-    for (int i = 0; i < n_my; i++) {
-      const int s = i % NS, b = i & 1;
+    for (int i = 0; cur.ok; i++) {
+      const int s = i % NS, b = i & 1, item0 = end - cur.left - cur.tile;   // (the item's first unit)
       const int pair = cur.pair, li = cur.li, bq = cur.b, h = cur.h, tile = cur.tile, len = cur.len, m = cur.m, nt = cur.nt;
       if (fresh) {   // (the products of the item before are through: their sums have been read)
         // rows, and the turns of the item's queries (at most eight) in the place of the numerators
@@ -325,7 +326,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         for (int r = 0; r < R; r++) { qs[r] = sy.qscale[r]; top[r] = -INFINITY; sum[r] = o[r] = 0.f; }
       }
       cur.next(work);
-      const bool last = i + 1 == n_my || cur.tile == 0;
+      const bool last = cur.ended || !cur.ok;
       bar_wait(sm, &sy.full[s], (uint32_t)(i / NS) & 1u);   // (long complete: for the loader's scales)
       // scales of this warp's block of 32 tokens; the largest value scale of the tile
       const float ks = sy.scale[s][role], vs = sy.scale[s][4 + role];
@@ -429,10 +430,10 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         w[0] += __shfl_xor_sync(0xffffffffu, w[0], 1);
         if ((lane & 3) == 0) sy.sum[role][lane >> 2] = w[0];
         asm volatile("bar.sync %0, 128;\n" ::"r"(1 + g) : "memory");
-        const bool ends = cur.tile == 0, direct = whole && ends;
+        const bool ends = cur.ended, direct = whole && ends;
         float* slot = a.slots + (size_t)(2 * v + (began ? 0 : 1)) * SLOT;
         if (!began && (heads.by_item || !ends) && tid == g * 128)   // (the same thread as above)
-          a.heads[heads.at(v, c.n_kv, pair, h, 0)] = Head{ends ? 0 : cuts.range_of(g0 + i - tile + nt - 1) - v, v, pair, h, 0, {}};
+          a.heads[heads.at(v, c.n_kv, pair, h, 0)] = Head{ends ? 0 : cuts.range_of(item0 + nt - 1) - v, v, pair, h, 0, {}};
 #pragma unroll
         for (int r = 0; r < R; r++) {
           float l = (sy.sum[0][r] + sy.sum[1][r]) + (sy.sum[2][r] + sy.sum[3][r]);

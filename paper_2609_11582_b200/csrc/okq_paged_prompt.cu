@@ -26,7 +26,7 @@ namespace okq {
 
 namespace {
 
-constexpr int R = PROMPT_ROWS, M = 128;         // rows of a block, of a stream
+constexpr int R = PROMPT_ROWS, EXTRA = PROMPT_EXTRA, M = 128;         // rows of a block, of a stream
 constexpr int PH = PT / 2;                      // tokens of a step
 constexpr int SIDE = PT * D;                    // bytes of a tile's keys or values as codes
 constexpr int Q_HALF = M * 128, KV_HALF = PH * 128;   // 64 channels in fp16, of a stream's queries and of a step's keys or values
@@ -133,7 +133,7 @@ __device__ __forceinline__ bool step_ready(PromptSmem& sm, const volatile int* d
 // The 32 rows of a warp in a row tile: rotated, scaled by a power of two, swizzled; returns the factor of the exponent that undoes the
 // scaling for the lane's own row (times the softmax scale, whose sign goes to the queries).  Eight lanes to a row, sixteen channels each.
 template <class T>
-__device__ __forceinline__ float prepare_queries(const AttnArgs& a, const Cursor<R>& cur, int row0, unsigned char* q, bool store, int lane) {
+__device__ __forceinline__ float prepare_queries(const AttnArgs& a, const Cursor<R, EXTRA>& cur, int row0, unsigned char* q, bool store, int lane) {
   const PagedView& c = a.c;
   const int rows = cur.m * c.group;
   const int j = lane & 7, nc = a.rope.half >> 3;
@@ -266,29 +266,29 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
   depend_wait();
 
   const PagedView& c = a.c;
-  const Work<R> work(a);
+  const Work<R, EXTRA> work(a);
   const int v = blockIdx.x;                     // this block's range
-  const Cuts cuts = find_places<R, NT, 1>(sm.find, work, gridDim.x, v, 0);
+  const Cuts cuts = find_places<R, EXTRA, NT, 1>(sm.find, work, gridDim.x, v, 0);
+  const int end = cuts.start(v) + cuts.size(v); // the unit behind it
   const Heads<R> heads(work.pairs, c.n_kv, c.group, a.n_new, gridDim.x);
-  const int g0 = cuts.start(v), n_my = cuts.size(v);
-  Cursor<R> cur{};
-  if (n_my > 0) cur = place<R, 1>(sm.find, work, 0);
+  Cursor<R, EXTRA> cur = place<R, EXTRA, 1>(sm.find, work, cuts, v, 0);
 
   if (warp == W_LOAD) {
     // ------------------------------------------------------------------ loader: blocks of the tiles to come, as in the decode kernel
-    Cursor<R> ahead = cur;
+    Cursor<R, EXTRA> ahead = cur;
+    int n_now = 0, n_nx = 0;
     int t_nx = 0, l_nx = 0, h_nx = 0, page_nx = -1;
     bool in_nx = false, fresh_nx = false;
     int row_now = -1, row_nx = -1;               // -1: nothing to copy
     float ks_now = 0.f, vs_now = 0.f, ks_nx = 0.f, vs_nx = 0.f;
     bool fresh_now = false;
-    auto entries = [&](int n) {
+    auto entries = [&] {
       int b = 0, len = 0;
-      for (int i = 0; i < n; i++) {
-        if (lane >> 2 == i) { t_nx = ahead.tile * PT + PB * (lane & 3); len = ahead.len; l_nx = a.layer + ahead.li; b = ahead.b; h_nx = ahead.h; fresh_nx = ahead.tile == 0; }
+      for (n_nx = 0; n_nx < 8 && ahead.ok; n_nx++) {
+        if (lane >> 2 == n_nx) { t_nx = ahead.tile * PT + PB * (lane & 3); len = ahead.len; l_nx = a.layer + ahead.li; b = ahead.b; h_nx = ahead.h; fresh_nx = ahead.tile == 0; }
         ahead.next(work);
       }
-      in_nx = lane >> 2 < n && t_nx < len;
+      in_nx = lane >> 2 < n_nx && t_nx < len;
       if (in_nx) page_nx = __ldg(&c.table[(size_t)b * c.max_pages + (t_nx >> c.page_shift)]);
     };
     auto scales = [&] {
@@ -307,17 +307,19 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     };
     int armed[2] = {0, 0};
     float vref = 0.f;
-    if (n_my > 0) { entries(min(8, n_my)); scales(); }
-    for (int i = 0; i < n_my; i++) {
+    bool out = false;
+    entries();
+    scales();
+    for (int i = 0; !out; i++) {
       const int k = i & 7;
       if (k == 0) {
+        n_now = n_nx;
         row_now = row_nx; ks_now = ks_nx; vs_now = vs_nx; fresh_now = fresh_nx;
-        if (i + 8 < n_my) entries(min(8, n_my - i - 8));
-        else in_nx = false;
+        entries();
       }
+      if (k >= n_now) break;
       const bool mine = lane >> 2 == k, there = mine && row_now >= 0;
       const int blocks = __popc(__ballot_sync(0xffffffffu, there)), j = lane & 3;
-      bool out = false;
 #pragma unroll
       for (int side = 0; side < 2; side++) {
         if (i >= 2 && !bar_wait(sm, &sm.code_free[side][i & 1], (uint32_t)((i >> 1) - 1) & 1u)) { out = true; break; }
@@ -354,7 +356,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       if (lane == 0) mbar_arrive(&sm.info_full[i & 3]);
       if (k == 4) scales();
     }
-    if (sm.abort || armed[1] < n_my)   // no copy may still be landing when the block ends
+    if (sm.abort || out)   // no copy may still be landing when the block ends
       for (int side = 0; side < 2; side++)
         for (int i = max(0, armed[side] - 2); i < armed[side]; i++) mbar_drain(&sm.code_full[side][i & 1], (uint32_t)(i >> 1) & 1u);
     write_empty<T>(a, work, heads, v, gridDim.x, lane);
@@ -385,9 +387,9 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       scored |= 1u << place;
       ph_s ^= 1u << place;
     };
-    for (int i = 0; i < n_my && go;) {
+    for (int i = 0; cur.ok && go;) {
       const bool dual = cur.m * c.group - cur.rt * R <= M;        // both streams have the same rows
-      const int n = min(cur.nt - cur.tile, n_my - i), steps = dual ? n : 2 * n;
+      const int n = cur.piece(), steps = dual ? n : 2 * n;
       const int x0 = 2 * i + (dual ? t : 0), dx = dual ? 2 : 1;   // step y is step x0 + dx y of the range
       const uint64_t ad = make_desc_sw128(smem_u32(sm.q[dual ? 0 : t][0]));
       go = bar_wait(sm, &sm.q_full[t], (uint32_t)(items++) & 1u);
@@ -411,7 +413,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
         if (y + 2 < steps) score(x + 2 * dx, place, ad, dual);
       }
       i += n;
-      cur.next_item(work);
+      cur.skip(work, n);
     }
 #pragma unroll
     for (int p = 0; p < 2; p++)
@@ -421,7 +423,13 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     // ------------------------------------------------------------------ codes to fp16: eight lanes to a token, sixteen channels each
     // Two warps have the keys, two the values.
     const int side = (warp - W_CONV) >> 1, who = (warp - W_CONV) & 1, ct = 32 * who + lane, j = ct & 7;
-    for (int x = 0; x < 2 * n_my; x++) {
+    for (int x = 0, end_x = 0;; x++) {
+      if (x == end_x) {   // the next item's steps
+        if (!cur.ok) break;
+        const int n = cur.piece();
+        end_x += 2 * n;
+        cur.skip(work, n);
+      }
       const int i = x >> 1, half = x & 1, s = x % NR;
       if (!half) {
         if (side) bar_wait(sm, &sm.info_full[i & 3], (uint32_t)(i >> 2) & 1u);
@@ -470,8 +478,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     int n_s[2] = {0, 0}, n_o = 0;
     bool whole = cur.tile == 0, began = cur.tile != 0;
     if (!heads.by_item && tid == 0) a.heads[v].more = 0;
-    for (int i = 0; i < n_my;) {
-      const int n = min(cur.nt - cur.tile, n_my - i), rows = cur.m * c.group - cur.rt * R;
+    for (int i = 0; cur.ok;) {
+      const int n = cur.piece(), rows = cur.m * c.group - cur.rt * R, item0 = end - cur.left - cur.tile;   // (the item's first unit)
       const bool ends = cur.tile + n == cur.nt, dual = rows <= M;
       const int row0 = (dual ? 0 : M * t) + 32 * quarter, row = row0 + lane, steps = dual ? n : 2 * n;
       // (the stream's own products of the item before are through)
@@ -592,11 +600,11 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       if (dual) asm volatile("bar.sync 1, 256;\n" ::: "memory");   // the next item's products may replace the sums
       if (!began && (heads.by_item || !ends) && tid == 0)
         a.heads[heads.at(v, c.n_kv, cur.pair, cur.h, cur.rt)] =
-            Head{ends ? 0 : cuts.range_of(g0 + i - cur.tile + cur.nt - 1) - v, v, cur.pair, cur.h, cur.rt, {}};
+            Head{ends ? 0 : cuts.range_of(item0 + cur.nt - 1) - v, v, cur.pair, cur.h, cur.rt, {}};
       whole = true;
       began = false;
       i += n;
-      cur.next_item(work);
+      cur.skip(work, n);
     }
   }
   before_sync();
