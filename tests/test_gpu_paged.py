@@ -467,6 +467,81 @@ def test_attention_graphs_share_a_workspace(n):
         assert torch.equal(outs[i], got[i])
 
 
+def random_cache(g, L, batch, H, Hq, page, dtype, lens):
+    """A cache filled with numbers rather than through appends: lens[b] tokens, pages in an order of their own."""
+    width = max(1, max((n + page - 1) // page for n in lens))
+    n_pages = sum((n + page - 1) // page for n in lens) + 2
+    c = B.PagedCache(L, batch, H, Hq, n_pages, width, page, dtype)
+    c.codes.copy_(torch.randint(-127, 128, c.codes.shape, generator=g, dtype=torch.int8))
+    c.scales.copy_(torch.rand(c.scales.shape, generator=g) * 0.02 + 0.002)
+    order, k = torch.randperm(n_pages, generator=g).tolist(), 0
+    table = torch.full((batch, width), -1, dtype=torch.int32)
+    for b, n in enumerate(lens):
+        for j in range((n + page - 1) // page):
+            table[b, j] = order[k]
+            k += 1
+    c.table.copy_(table)
+    c.seq_len.copy_(torch.tensor(lens, dtype=torch.int32).expand(L, batch))
+    return c
+
+
+def check_random(c, q, out, q_len, poison):
+    """Against softmax attention in 64 bits (torch, on the GPU), sequence by sequence."""
+    G, n, P = c.n_q_heads // c.n_kv_heads, q.shape[3], c.page_tokens
+    lens = c.seq_len[0].tolist()
+    for b, T in enumerate(lens):
+        m = n if q_len is None else max(0, min(n, q_len[b]))
+        assert (out[:, b, :, m:] == poison).all()
+        if m == 0:
+            continue
+        pages = c.table[b, :(T + P - 1) // P].long()
+        x = (c.codes[:, pages].double().unflatten(5 - 1, (-1, BLOCK)) * c.scales[:, pages].double()[..., None, None]).flatten(4, 5)   # [L, w, H, 2, P, 128]
+        x = x.permute(0, 2, 3, 1, 4, 5).flatten(3, 4)[:, :, :, :T]
+        k, v = x[:, :, 0], x[:, :, 1]
+        s = torch.einsum("lhgnd,lhtd->lhgnt", q[:, b, :, :m].double().unflatten(1, (-1, G)), k) * D ** -0.5
+        seen = T - m + 1 + torch.arange(m, device="cuda")
+        late = torch.arange(T, device="cuda")[None] >= seen[:, None]
+        top = s.masked_fill(late, 0).abs().amax(-1) if T else torch.zeros(s.shape[:-1], device="cuda", dtype=torch.float64)
+        w = torch.softmax(s.masked_fill(late, -float("inf")), -1).nan_to_num(0.0)
+        ref, mag = w @ v[:, :, None], w @ v[:, :, None].abs()
+        got = out[:, b, :, :m].double().unflatten(1, (-1, G))
+        # attention_bound, here as tensors
+        inner = 2.0 ** -24 * (8 * top[..., None] + 32) + (2.0 ** -11 if n * G > 8 else 0)
+        err = inner * mag
+        bound = err + torch.finfo(q.dtype).eps / 2 * (ref.abs() + err) + (2.0 ** -25 if q.dtype == F16 else 1e-38)
+        assert ((got - ref).abs() <= bound).all(), (b, T, m, ((got - ref).abs() / bound).max().item())
+
+
+# (layers, batch, KV heads, group, page, queries, longest): more items than ranges, items of one tile, row tiles of every kind (256 rows,
+# up to 128 and between) behind one another in a range, ranges that end inside items, sequences that are empty
+SCHEDULES = [(3, 64, 8, 4, 32, 1, 300), (1, 300, 4, 2, 64, 1, 130), (2, 1, 1, 8, 32, 1, 9000), (28, 9, 4, 7, 64, 1, 700), (1, 2, 8, 1, 256, 8, 40000),
+             (1, 40, 4, 7, 32, 5, 400), (2, 33, 8, 4, 64, 40, 300), (1, 5, 2, 7, 128, 700, 1500), (1, 1, 1, 8, 64, 1000, 1000), (3, 17, 3, 5, 32, 130, 140),
+             (1, 200, 2, 8, 32, 20, 90), (1, 2, 1, 1, 64, 3000, 3500), (1, 3, 4, 8, 256, 33, 30000), (4, 50, 4, 1, 64, 300, 310)]
+
+
+@pytest.mark.parametrize("shape", SCHEDULES, ids=str)
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_attention_schedules(shape, dtype):
+    L, batch, H, G, page, n, longest = shape
+    g = gen(sum(shape))
+    for ragged in (False, True):
+        lens = [longest] * batch if not ragged else [int(longest * x ** 2) for x in torch.rand(batch, generator=g).tolist()]
+        if ragged:
+            lens[-1] = 0
+        q_len = None if not ragged else torch.randint(-1, n + 2, (batch,), generator=g).tolist()
+        c = random_cache(g, L, batch, H, H * G, page, dtype, lens)
+        q = randn(g, L, batch, H * G, n, D, dtype=dtype).cuda()
+        out = torch.full_like(q, 5.0)
+        ws = torch.full((B.paged_workspace_bytes(c, L, n),), 0xff, dtype=torch.uint8, device="cuda")
+        ql = None if q_len is None else torch.tensor(q_len, dtype=torch.int32).cuda()
+        B.paged_attention(c, 0, L, q, ws, out, ql)
+        assert c.device_status() == 0
+        check_random(c, q, out, q_len, 5.0)
+        again = torch.full_like(q, 5.0)
+        B.paged_attention(c, 0, L, q, ws, again, ql)
+        assert torch.equal(out, again)
+
+
 def test_offsets_beyond_32_bits():
     """A pool of 5 GB whose last pages are the ones in use."""
     m = Model(1, 2, 4, 8, max_pages=2, page=256, dtype=F16, n_pages=20000)
