@@ -240,9 +240,9 @@ __device__ __forceinline__ void write_empty(const AttnArgs& a, const Work<ROWS, 
   }
 }
 
-constexpr int MERGE_NT = 256;
+constexpr int MERGE_NT = 512;
 
-// Block (x, y): rows of the item of head x, if it is in parts.  WPR warps to a row (all eight where a handful of rows can be in hundreds
+// Block (x, y): rows of the item of head x, if it is in parts.  WPR warps to a row (all sixteen where a handful of rows can be in hundreds
 // of parts, one where hundreds of rows are in a few), of which each has every WPR-th part, a lane four channels.  Bound by latency: a
 // few megabytes of parts at most; all of a part is loaded at once, seven parts in flight.
 template <class T, int ROWS, int WPR>
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(MERGE_NT) k_paged_merge(const AttnArgs a) {
   *reinterpret_cast<uint2*>(out_row<T>(a, li, b, hd.h, row) + 4 * lane) = *reinterpret_cast<const uint2*>(o);
 }
 template <class T, int ROWS> inline cudaError_t launch_merge(const AttnArgs& a, int ranges, cudaStream_t s) {
-  constexpr int WPR = ROWS <= 8 ? 8 : 1;
+  constexpr int WPR = ROWS <= 8 ? MERGE_NT / 32 : 1;
   const Heads<ROWS> heads(a.layer_count * a.c.batch, a.c.n_kv, a.c.group, a.n_new, ranges);
   const long long rows = (long long)a.n_new * a.c.group;
   const int most = (int)(rows < ROWS ? rows : ROWS), per = MERGE_NT / 32 / WPR;
