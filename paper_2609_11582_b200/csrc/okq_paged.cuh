@@ -24,15 +24,16 @@ struct PagedView {
     return ((((size_t)l * n_pages + p) * n_kv + h) * 2 + side) * page;   // in rows of 128
   }
   __device__ float* scale_of(int l, int p, int h, int side) const { return scales + code_row(l, p, h, side) / PB; }
+  // (tables and lengths are read past the first cache: a kernel placed early may find what stood there before its predecessor's end)
   // page with token t of sequence b, -1 where there is none or the entry names none of the pool
   __device__ int page_of(int b, int t) const {
     const int j = t >> page_shift;
-    const int p = j < max_pages ? table[(size_t)b * max_pages + j] : -1;
+    const int p = j < max_pages ? __ldcg(&table[(size_t)b * max_pages + j]) : -1;
     return (unsigned)p < (unsigned)n_pages ? p : -1;
   }
   __device__ int room() const { return max_pages << page_shift; }   // tokens that a row has entries for
   __device__ int held(int l, int b) const {                         // tokens of a sequence
-    const int n = seq_len[(size_t)l * batch + b];
+    const int n = __ldcg(&seq_len[(size_t)l * batch + b]);
     return n < 0 ? 0 : n > room() ? room() : n;
   }
   template <class T> __device__ T* raw_of(int l, int b, int h, int side) const {
@@ -45,7 +46,7 @@ __device__ __forceinline__ void set_status(int32_t* status, int code) { atomicCA
 // what a call asks for of n: all of it, or the sequence's own number
 __device__ __forceinline__ int count_of(const int32_t* lens, int b, int n) {
   if (!lens) return n;
-  const int m = lens[b];
+  const int m = __ldcg(&lens[b]);
   return m < 0 ? 0 : m > n ? n : m;
 }
 

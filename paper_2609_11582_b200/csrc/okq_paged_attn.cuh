@@ -53,7 +53,7 @@ template <int ROWS, int EXTRA> struct Work {
   const AttnArgs& a;
   __device__ __forceinline__ explicit Work(const AttnArgs& args) : pairs(args.layer_count * args.c.batch), n_kv(args.c.n_kv), group(args.c.group), a(args) {}
   __device__ __forceinline__ void lens(int li, int b, int& len, int& m) const {   // tokens held, queries
-    const int n = a.c.seq_len[(size_t)(a.layer + li) * a.c.batch + b], q = a.q_len ? a.q_len[b] : a.n_new;   // (both loads before either is used)
+    const int n = __ldcg(&a.c.seq_len[(size_t)(a.layer + li) * a.c.batch + b]), q = a.q_len ? __ldcg(&a.q_len[b]) : a.n_new;   // (both loads before either is used)
     len = max(0, min(n, a.c.room()));
     m = max(0, min(q, a.n_new));
   }
@@ -329,7 +329,8 @@ template <class T, int ROWS> inline cudaError_t launch_merge(const AttnArgs& a, 
 // okq_paged_decode.cu: up to DECODE_ROWS rows, DECODE_PIPES pipelines per block.  An item's own costs in tiles: queries, the first tile's
 // latency and the output take about as long as one and a half.
 constexpr int DECODE_ROWS = 8, DECODE_PIPES = 3, DECODE_EXTRA = 1;
-cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int grid, cudaStream_t s);
+cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int grid, int cluster, cudaStream_t s);   // cluster 0: ranges of the line, merge
+int decode_clusters(int size);   // clusters of so many blocks (at most eight) that run at once
 // okq_paged_prompt.cu: any number of rows, one pipeline per block.  An item of a single tile takes 8 to 10 us, a further tile 2 to 3.
 constexpr int PROMPT_ROWS = 256, PROMPT_EXTRA = 3;
 cudaError_t launch_paged_prompt(const AttnArgs& a, int dtype, int grid, cudaStream_t s);

@@ -29,6 +29,7 @@ constexpr int WARPS = 5, SERVICE = 4;     // of a pipeline; the service warp's n
 constexpr int NT = G * WARPS * 32;
 constexpr uint32_t S_COL = 0, O_COL = 32, PIPE_COLS = 64, COLS = 256;
 constexpr size_t SLOT = (size_t)R * (D + 2);
+constexpr int MOST_CLUSTER = 8;
 
 struct Pipe {
   __align__(1024) int8_t k[NS][SIDE];
@@ -81,6 +82,26 @@ struct Block {
   int row;        // row of its keys in the pool; -1: behind the sequence's end, -2: its page is missing
   float ks, vs;
 };
+
+// Sums over the lanes of eight rows at once, to `to` by row: bits 4 .. 2 of a lane choose its row, then the four lanes of a row.
+__device__ __forceinline__ void lane_sums(const float (&x)[R], float* to, int lane) {
+  float w[R];
+#pragma unroll
+  for (int r = 0; r < R; r++) w[r] = x[r];
+#pragma unroll
+  for (int d = 16, n = 4; d >= 4; d >>= 1, n >>= 1) {
+    const bool upper = (lane & d) != 0;
+#pragma unroll
+    for (int r = 0; r < 4; r++)
+      if (r < n) {
+        const float give = upper ? w[r] : w[r + n], keep = upper ? w[r + n] : w[r];
+        w[r] = keep + __shfl_xor_sync(0xffffffffu, give, d);
+      }
+  }
+  w[0] += __shfl_xor_sync(0xffffffffu, w[0], 2);
+  w[0] += __shfl_xor_sync(0xffffffffu, w[0], 1);
+  if ((lane & 3) == 0) to[lane >> 2] = w[0];
+}
 
 // Two of an item's rows, r0 and r0 + 1: limbs (swizzled) and scales.  One warp, four channels per lane.  `turns`: cosines and sines of
 // the item's queries, [query][64 pairs].
@@ -135,8 +156,10 @@ __device__ __forceinline__ void prepare_queries(const AttnArgs& a, const Cursor<
   }
 }
 
-template <class T>
-__global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ CUtensorMap map, const AttnArgs a, long long wait_limit) {
+// CLUSTER: every (layer, sequence, KV head) has a cluster of `size` blocks, whose pipelines share its tiles evenly, and its parts are put
+// together in the cluster's shared memory: one launch.  Otherwise pipelines have even ranges of the whole line and k_paged_merge follows.
+template <class T, bool CLUSTER>
+__global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ CUtensorMap map, const AttnArgs a, int size, long long wait_limit) {
   extern __shared__ unsigned char raw_smem[];
   DecodeSmem& sm = *reinterpret_cast<DecodeSmem*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~(uintptr_t)1023);
   const int tid = threadIdx.x, lane = tid & 31;
@@ -170,10 +193,29 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
 
   const PagedView& c = a.c;
   const Work<R, EXTRA> work(a);
-  const Cuts cuts = find_places<R, EXTRA, NT, G>(sm.find, work, G * gridDim.x, blockIdx.x, gridDim.x);
-  const int v = blockIdx.x + g * gridDim.x, end = cuts.start(v) + cuts.size(v);     // this pipeline's range, and the unit behind it
   const Heads<R> heads(work.pairs, c.n_kv, c.group, a.n_new, G * gridDim.x);
-  Cursor<R, EXTRA> cur = place<R, EXTRA, G>(sm.find, work, cuts, v, g);
+  Cuts cuts(0, 1);
+  int v = 0, end = 0;            // this pipeline's range of the line, and the unit behind it
+  Cursor<R, EXTRA> cur{};
+  const int unit = CLUSTER ? blockIdx.x / size : 0, rank = CLUSTER ? blockIdx.x - unit * size : 0;
+  if (CLUSTER) {
+    cur.pair = unit / c.n_kv;
+    cur.h = unit - cur.pair * c.n_kv;
+    cur.li = work.layer_of(cur.pair);
+    cur.b = cur.pair - cur.li * c.batch;
+    work.lens(cur.li, cur.b, cur.len, cur.m);
+    cur.nt = cur.m ? work.tiles(cur.len, cur.m, 0) : 0;
+    const Cuts share(cur.nt, G * size);
+    cur.tile = share.start(g * size + rank);
+    cur.left = share.size(g * size + rank);
+    cur.ok = cur.left > 0;
+  } else {
+    cuts = find_places<R, EXTRA, NT, G>(sm.find, work, G * gridDim.x, blockIdx.x, gridDim.x);
+    v = blockIdx.x + g * gridDim.x;
+    end = cuts.start(v) + cuts.size(v);
+    cur = place<R, EXTRA, G>(sm.find, work, cuts, v, g);
+  }
+  const int rows = cur.m * c.group;   // (CLUSTER: of the item)
 
   if (role == SERVICE) {
     // ------------------------------------------------------------------ copies and products
@@ -196,7 +238,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       in_nx = lane >> 2 < n_nx && t_nx < len;
       if (in_nx) {
         const int j = t_nx >> c.page_shift;
-        page_nx = __ldg(&c.table[(size_t)b * c.max_pages + j]);   // (held() keeps j inside the row)
+        page_nx = __ldcg(&c.table[(size_t)b * c.max_pages + j]);   // (held() keeps j inside the row)
       }
     };
     auto scales = [&] {
@@ -207,7 +249,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         set_status(c.status, OKQ_ERR_INVALID_ARG);
       } else {
         const size_t row = c.code_row(l_nx, page_nx, h_nx, 0) + (t_nx & (c.page - 1));
-        nxt = Block{(int)row, __ldg(&c.scales[row / PB]), __ldg(&c.scales[(row + c.page) / PB])};
+        nxt = Block{(int)row, __ldcg(&c.scales[row / PB]), __ldcg(&c.scales[(row + c.page) / PB])};
       }
     };
     auto load = [&](int i) {   // tile i into the ring, whose place is free
@@ -284,14 +326,18 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       for (int i = max(0, armed - NS); i < armed; i++) mbar_drain(&sy.full[i % NS], (uint32_t)(i / NS) & 1u);
     if (scored >= 1 && !mbar_drain(&sy.s_full, (uint32_t)(scored - 1) & 1u)) sm.tmem_busy = 1;
     if (done >= 1 && !mbar_drain(&sy.o_full, (uint32_t)(done - 1) & 1u)) sm.tmem_busy = 1;
-    write_empty<T>(a, work, heads, v, G * gridDim.x, lane);
+    if (!CLUSTER) write_empty<T>(a, work, heads, v, G * gridDim.x, lane);
   } else {
     // ------------------------------------------------------------------ workers (after a timeout they run on, waits failing at once)
     const uint32_t lanes = (uint32_t)(32 * role) << 16;
     const int ch = 32 * role + lane;
     float top[R], sum[R], qs[R], o[R];
     bool fresh = true, whole = cur.tile == 0, began = cur.tile != 0;   // the piece has its item's first tile; the item began in an earlier range
-    if (!heads.by_item && tid == g * 128) a.heads[v].more = 0;
+    if (CLUSTER) {
+#pragma unroll
+      for (int r = 0; r < R; r++) { top[r] = -INFINITY; sum[r] = o[r] = 0.f; }
+    }
+    if (!CLUSTER && !heads.by_item && tid == g * 128) a.heads[v].more = 0;
     for (int i = 0; cur.ok; i++) {
       const int s = i % NS, b = i & 1, item0 = end - cur.left - cur.tile;   // (the item's first unit)
       const int pair = cur.pair, li = cur.li, bq = cur.b, h = cur.h, tile = cur.tile, len = cur.len, m = cur.m, nt = cur.nt;
@@ -411,24 +457,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         }
       }
       fresh = last;
-      if (last) {
-        // over the lanes, eight rows at once: bits 4 .. 2 of a lane choose its row, then the four lanes of a row
-        float w[R];
-#pragma unroll
-        for (int r = 0; r < R; r++) w[r] = sum[r];
-#pragma unroll
-        for (int d = 16, n = 4; d >= 4; d >>= 1, n >>= 1) {
-          const bool upper = (lane & d) != 0;
-#pragma unroll
-          for (int r = 0; r < 4; r++)
-            if (r < n) {
-              const float give = upper ? w[r] : w[r + n], keep = upper ? w[r + n] : w[r];
-              w[r] = keep + __shfl_xor_sync(0xffffffffu, give, d);
-            }
-        }
-        w[0] += __shfl_xor_sync(0xffffffffu, w[0], 2);
-        w[0] += __shfl_xor_sync(0xffffffffu, w[0], 1);
-        if ((lane & 3) == 0) sy.sum[role][lane >> 2] = w[0];
+      if (last && !CLUSTER) {
+        lane_sums(sum, sy.sum[role], lane);
         asm volatile("bar.sync %0, 128;\n" ::"r"(1 + g) : "memory");
         const bool ends = cur.ended, direct = whole && ends;
         float* slot = a.slots + (size_t)(2 * v + (began ? 0 : 1)) * SLOT;
@@ -449,33 +479,127 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         began = false;
       }
     }
+    if (CLUSTER) {   // this pipeline's part, in the place of its first tile: all of its copies and products are through
+      lane_sums(sum, sy.sum[role], lane);
+      asm volatile("bar.sync %0, 128;\n" ::"r"(1 + g) : "memory");
+      float* part = reinterpret_cast<float*>(pipe.k[0]);
+#pragma unroll
+      for (int r = 0; r < R; r++) {
+        part[r * D + ch] = o[r];
+        if (ch == r) {
+          const float l = (sy.sum[0][r] + sy.sum[1][r]) + (sy.sum[2][r] + sy.sum[3][r]);
+          part[R * D + r] = top[r];
+          part[R * D + R + r] = sm.abort ? NAN : l;
+        }
+      }
+    }
   }
   asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory");
   __syncthreads();
   if (tid == 0 && sm.abort) set_status(c.status, OKQ_ERR_TIMEOUT);
   if (warp == 0 && !sm.tmem_busy) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(sm.tmem_slot), "n"(COLS) : "memory");
+  if (!CLUSTER) return;
+  // the item's rows dealt over the cluster's blocks, 128 threads (channels) to a row
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+  // (pipeline i of every block by threads 128 i .. 128 i + 127: all loads of a row in flight at once)
+  const int ch = tid & 127, pi = tid >> 7;
+  float* mine = reinterpret_cast<float*>(sm.pipe[pi < G ? pi : 0].p);
+  for (int r = rank; r < rows; r += size) {
+    if (pi < G) {
+      float t[MOST_CLUSTER], l[MOST_CLUSTER], o[MOST_CLUSTER];
+      const uint32_t here = smem_u32(sm.pipe[pi].k[0]);
+#pragma unroll
+      for (int k = 0; k < MOST_CLUSTER; k++) {
+        t[k] = -INFINITY;
+        l[k] = o[k] = 0.f;
+        if (k < size) {
+          uint32_t there;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(there) : "r"(here), "r"(k));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(t[k]) : "r"(there + 4 * (R * D + r)));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(l[k]) : "r"(there + 4 * (R * D + R + r)));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(o[k]) : "r"(there + 4 * (r * D + ch)));
+        }
+      }
+      float top = t[0], ls = 0.f, os = 0.f;
+#pragma unroll
+      for (int k = 1; k < MOST_CLUSTER; k++) top = fmaxf(top, t[k]);
+      const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int k = 0; k < MOST_CLUSTER; k++) {
+        const float f = ex2(t[k] - ref);
+        ls = fmaf(l[k], f, ls);
+        os = fmaf(o[k], f, os);
+      }
+      mine[ch] = os;
+      if (ch == 0) { mine[D] = top; mine[D + 1] = ls; }
+    }
+    __syncthreads();
+    if (pi == 0) {
+      float top = -INFINITY, l = 0.f, o = 0.f;
+#pragma unroll
+      for (int g2 = 0; g2 < G; g2++) top = fmaxf(top, reinterpret_cast<const float*>(sm.pipe[g2].p)[D]);
+      if (top == -INFINITY) top = 0.f;
+#pragma unroll
+      for (int g2 = 0; g2 < G; g2++) {
+        const float* y = reinterpret_cast<const float*>(sm.pipe[g2].p);
+        const float f = ex2(y[D] - top);
+        l = fmaf(y[D + 1], f, l);
+        o = fmaf(y[ch], f, o);
+      }
+      out_row<T>(a, cur.li, cur.b, cur.h, r)[ch] = from_f<T>(l == 0.f ? 0.f : o / l);
+    }
+    __syncthreads();
+  }
+  asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;\n" ::: "memory");   // no block ends while its parts are read
 }
 
-template <class T> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map, int grid, cudaStream_t s) {
+template <class T, bool CLUSTER> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map, int grid, int size, cudaStream_t s) {
   static thread_local unsigned long long attr_mask = 0;
   int dev = 0;
   constexpr int SMEM = (int)sizeof(DecodeSmem) + 1024;
   static_assert(SMEM <= 227 * 1024, "shared memory of one block");
   if (attr_needed(attr_mask, dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(k_paged_decode<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(k_paged_decode<T, CLUSTER>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
     if (e != cudaSuccess) return e;
     attr_done(attr_mask, dev);
   }
-  cudaError_t e = launch_dependent(k_paged_decode<T>, dim3(grid), NT, SMEM, s, 1, map, a, WAIT_LIMIT_CLOCKS);
-  return e == cudaSuccess ? launch_merge<T, R>(a, G * grid, s) : e;
+  cudaError_t e = launch_dependent(k_paged_decode<T, CLUSTER>, dim3(grid), NT, SMEM, s, CLUSTER ? size : 1, map, a, size, WAIT_LIMIT_CLOCKS);
+  return e == cudaSuccess && !CLUSTER ? launch_merge<T, R>(a, G * grid, s) : e;
 }
 
 }  // namespace
 
-cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int grid, cudaStream_t s) {
+// clusters of `size` blocks that the current device holds at once
+int decode_clusters(int size) {
+  static thread_local int known_dev = -1, known[MOST_CLUSTER + 1];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return 0; }
+  if (dev != known_dev) {
+    for (int k = 1; k <= MOST_CLUSTER; k++) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(k);
+      cfg.blockDim = dim3(NT);
+      cfg.dynamicSmemBytes = sizeof(DecodeSmem) + 1024;
+      cudaLaunchAttribute at[1];
+      at[0].id = cudaLaunchAttributeClusterDimension;
+      at[0].val.clusterDim.x = k; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+      cfg.attrs = at;
+      cfg.numAttrs = 1;
+      known[k] = 0;
+      if (cudaFuncSetAttribute(k_paged_decode<__half, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes) != cudaSuccess ||
+          cudaOccupancyMaxActiveClusters(&known[k], k_paged_decode<__half, true>, &cfg) != cudaSuccess)
+        (void)cudaGetLastError();
+    }
+    known_dev = dev;
+  }
+  return known[size];
+}
+
+cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int grid, int cluster, cudaStream_t s) {
   CUtensorMap map;
   if (!codes_map(map, a.c, true)) return cudaErrorInvalidValue;
-  return dtype == OKQ_FP16 ? launch<__half>(a, map, grid, s) : launch<__nv_bfloat16>(a, map, grid, s);
+  if (cluster > 0) return dtype == OKQ_FP16 ? launch<__half, true>(a, map, grid, cluster, s) : launch<__nv_bfloat16, true>(a, map, grid, cluster, s);
+  return dtype == OKQ_FP16 ? launch<__half, false>(a, map, grid, 1, s) : launch<__nv_bfloat16, false>(a, map, grid, 1, s);
 }
 
 }  // namespace okq

@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
         ahead.next(work);
       }
       in_nx = lane >> 2 < n_nx && t_nx < len;
-      if (in_nx) page_nx = __ldg(&c.table[(size_t)b * c.max_pages + (t_nx >> c.page_shift)]);
+      if (in_nx) page_nx = __ldcg(&c.table[(size_t)b * c.max_pages + (t_nx >> c.page_shift)]);
     };
     auto scales = [&] {
       row_nx = -1;
@@ -301,8 +301,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       } else {
         const size_t row = c.code_row(l_nx, page_nx, h_nx, 0) + (t_nx & (c.page - 1));
         row_nx = (int)row;
-        ks_nx = __ldg(&c.scales[row / PB]);
-        vs_nx = __ldg(&c.scales[(row + c.page) / PB]);
+        ks_nx = __ldcg(&c.scales[row / PB]);
+        vs_nx = __ldcg(&c.scales[(row + c.page) / PB]);
       }
     };
     int armed[2] = {0, 0};
