@@ -135,18 +135,14 @@ __device__ __forceinline__ void prepare_queries(const AttnArgs& a, const Cursor<
     // fixed point: 127 * 2^16 for the largest; numbers too small for a quotient (and infinities, NaN) have limbs of 0
     const float big = __uint_as_float(mx);
     const bool fine = mx < 0x7f800000u && big > 1e-30f;
-    const float f = fine ? 8323072.f / big : 0.f;
-    uint32_t limb[3] = {0u, 0u, 0u};
+    const float f = fine ? __fdividef(8323072.f, big) : 0.f;   // (two units off at most, the same for all of the row's numbers)
+    // signed digits to the base 256: with 128 added to each, the bytes of one sum
+    uint32_t u[4];
 #pragma unroll
-    for (int z = 0; z < 4; z++) {
-      int v = fine ? __float2int_rn(x[z] * f) : 0;
-#pragma unroll
-      for (int n = 0; n < 3; n++) {
-        const int d = (int)(signed char)(v & 0xff);
-        limb[n] |= (uint32_t)(d & 0xff) << (8 * z);
-        v = (v - d) >> 8;
-      }
-    }
+    for (int z = 0; z < 4; z++) u[z] = (uint32_t)((fine ? __float2int_rn(x[z] * f) : 0) + 0x808080) ^ 0x808080u;
+    const uint32_t lo = __byte_perm(u[0], u[1], 0x5140), hi = __byte_perm(u[2], u[3], 0x5140);   // bytes 0, 0, 1, 1
+    const uint32_t limb[3] = {__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632),
+                              __byte_perm(__byte_perm(u[0], u[1], 0x0062), __byte_perm(u[2], u[3], 0x0062), 0x5410)};
 #pragma unroll
     for (int n = 0; n < 3; n++) {
       const int line = 8 * n + r;
@@ -504,6 +500,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
   // (pipeline i of every block by threads 128 i .. 128 i + 127: all loads of a row in flight at once)
   const int ch = tid & 127, pi = tid >> 7;
   float* mine = reinterpret_cast<float*>(sm.pipe[pi < G ? pi : 0].p);
+  bool arrived = false;
   for (int r = rank; r < rows; r += size) {
     if (pi < G) {
       float t[MOST_CLUSTER], l[MOST_CLUSTER], o[MOST_CLUSTER];
@@ -534,6 +531,10 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       if (ch == 0) { mine[D] = top; mine[D + 1] = ls; }
     }
     __syncthreads();
+    if (r + size >= rows) {   // this block has read all that it needs of the others
+      asm volatile("barrier.cluster.arrive.aligned;\n" ::: "memory");
+      arrived = true;
+    }
     if (pi == 0) {
       float top = -INFINITY, l = 0.f, o = 0.f;
 #pragma unroll
@@ -550,7 +551,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     }
     __syncthreads();
   }
-  asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;\n" ::: "memory");   // no block ends while its parts are read
+  if (!arrived) asm volatile("barrier.cluster.arrive.aligned;\n" ::: "memory");
+  asm volatile("barrier.cluster.wait.aligned;\n" ::: "memory");   // no block ends while its parts are read
 }
 
 template <class T, bool CLUSTER> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map, int grid, int size, cudaStream_t s) {
