@@ -124,6 +124,19 @@ okq_status okq_paged_attention(const okq_paged* cache, int32_t layer, int32_t la
                                int32_t n_new, const int32_t* q_len, const okq_rope* rope, float sm_scale, void* workspace,
                                size_t workspace_bytes, void* out, const int64_t out_strides[4], void* stream);
 
+/* Testing aid for the bounded waits of okq_paged_attention, as okq_debug_bulk_timeout is for the 2-bit path's quantiser: nothing of a
+ * sequence's codes is delivered and every wait is limited to `limit_clocks` SM clocks.  The kernel returns by itself, outputs of
+ * sequences that hold tokens are NaN, the status word becomes OKQ_ERR_TIMEOUT. */
+okq_status okq_debug_paged_timeout(const okq_paged* cache, int32_t layer, int32_t layer_count, const void* q, const int64_t q_strides[4],
+                                   int32_t n_new, void* workspace, size_t workspace_bytes, void* out, const int64_t out_strides[4],
+                                   int64_t limit_clocks, void* stream);
+
+/* How okq_paged_attention would take a call; for tests of the rules.  Positive: the decode kernel with a cluster of so many blocks per
+ * (layer, sequence, KV head); OKQ_PLAN_LINE: the decode kernel over even ranges, and the merge; OKQ_PLAN_PROMPT: the prompt kernel; 0:
+ * refused.  Only sizes are looked at. */
+enum { OKQ_PLAN_LINE = -1, OKQ_PLAN_PROMPT = -2 };
+int32_t okq_debug_paged_plan(const okq_paged* cache, int32_t layer_count, int32_t n_new);
+
 /*
  * The pages.  All of it happens on the device, in stream order, without the host; free pages are handed out lowest index first, to
  * sequences and entries in ascending order, so that results do not depend on timing.  Indices out of range are skipped and set the

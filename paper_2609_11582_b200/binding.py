@@ -162,6 +162,10 @@ def lib():
         L.okq_paged_read.argtypes = [paged, i32, i32, i32, i32, ptr, ptr, ptr]
         L.okq_paged_attention.restype = C.c_int
         L.okq_paged_attention.argtypes = [paged, i32, i32, ptr, ptr, i32, ptr, ptr, C.c_float, ptr, C.c_size_t, ptr, ptr, ptr]
+        L.okq_debug_paged_timeout.restype = C.c_int
+        L.okq_debug_paged_timeout.argtypes = [paged, i32, i32, ptr, ptr, i32, ptr, C.c_size_t, ptr, ptr, C.c_int64, ptr]
+        L.okq_debug_paged_plan.restype = i32
+        L.okq_debug_paged_plan.argtypes = [paged, i32, i32]
         L.okq_pages_reserve.restype = C.c_int
         L.okq_pages_reserve.argtypes = [paged, ptr, ptr]
         L.okq_pages_fork.restype = C.c_int
@@ -186,7 +190,7 @@ def exported_symbols():
             "okq_ladder_codebook", "okq_ladder_quantize_keys", "okq_ladder_quantize_values",
             "okq_debug_ladder_timeout", "okq_ladder_decode_attention", "okq_turboquant_encode", "okq_turboquant_decode",
             "okq_paged_sizes", "okq_paged_workspace_bytes", "okq_rope_apply", "okq_paged_append", "okq_paged_read",
-            "okq_paged_attention", "okq_pages_reserve", "okq_pages_fork", "okq_pages_release", "okq_pages_copy",
+            "okq_paged_attention", "okq_debug_paged_timeout", "okq_debug_paged_plan", "okq_pages_reserve", "okq_pages_fork", "okq_pages_release", "okq_pages_copy",
             "okq_pages_compact"]
 
 
@@ -642,6 +646,23 @@ def paged_attention(cache: PagedCache, layer: int, layer_count: int, q, workspac
                                              _rows(cache, out, layer_count, cache.n_q_heads, n), _stream(stream))
     if st != OK:
         raise OkqError(st, "okq_paged_attention")
+
+
+def debug_paged_timeout(cache: PagedCache, layer: int, layer_count: int, q, workspace, out, limit_clocks: int = 20_000_000, stream=None):
+    """okq_debug_paged_timeout: paged_attention with nothing delivered and waits limited to `limit_clocks` SM clocks (testing aid)."""
+    _here(cache.codes, q, workspace, out)
+    n = q.shape[3]
+    _check(lib().okq_debug_paged_timeout(cache.ref, layer, layer_count, q.data_ptr(), _rows(cache, q, layer_count, cache.n_q_heads, n), n,
+                                         _ptr(workspace), workspace.nbytes, out.data_ptr(), _rows(cache, out, layer_count, cache.n_q_heads, n),
+                                         limit_clocks, _stream(stream)), "okq_debug_paged_timeout")
+
+
+PLAN_LINE, PLAN_PROMPT = -1, -2
+
+
+def paged_plan(cache: PagedCache, layer_count: int, n_new: int = 1) -> int:
+    """okq_debug_paged_plan: which kernel a paged_attention call would take."""
+    return lib().okq_debug_paged_plan(cache.ref, layer_count, n_new)
 
 
 def _indices(x, n=None):

@@ -57,9 +57,9 @@ size_t okq_paged_workspace_bytes(const okq_paged* cache, int32_t layer_count, in
   return ((p.bytes > pages ? p.bytes : pages) + 255) & ~(size_t)255;
 }
 
-okq_status okq_paged_attention(const okq_paged* cache, int32_t layer, int32_t layer_count, const void* q, const int64_t qs[4], int32_t n_new,
-                               const int32_t* q_len, const okq_rope* rope, float sm_scale, void* workspace, size_t workspace_bytes, void* out,
-                               const int64_t os[4], void* stream) {
+static okq_status attention(const okq_paged* cache, int32_t layer, int32_t layer_count, const void* q, const int64_t qs[4], int32_t n_new,
+                            const int32_t* q_len, const okq_rope* rope, float sm_scale, void* workspace, size_t workspace_bytes, void* out,
+                            const int64_t os[4], long long limit, int withhold, void* stream) {
   using namespace okq;
   okq_status st = check_paged_layers(cache, layer, layer_count);
   if (st != OKQ_OK) return st;
@@ -74,7 +74,7 @@ okq_status okq_paged_attention(const okq_paged* cache, int32_t layer, int32_t la
   if (!make_plan(cache, layer_count, n_new, p)) return OKQ_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < okq_paged_workspace_bytes(cache, layer_count, n_new)) return OKQ_ERR_WORKSPACE;
   AttnArgs a{paged_view(cache), {q, {qs[0], qs[1], qs[2], qs[3]}}, {out, {os[0], os[1], os[2], os[3]}}, q_len, r, layer, layer_count, n_new,
-             sm_scale * 1.44269504088896340736f, static_cast<Head*>(workspace),
+             sm_scale * 1.44269504088896340736f, limit, withhold, static_cast<Head*>(workspace),
              reinterpret_cast<float*>(static_cast<char*>(workspace) + p.heads)};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = p.decode ? launch_paged_decode(a, cache->dtype, p.grid, p.cluster, s) : launch_paged_prompt(a, cache->dtype, p.grid, s);
@@ -84,6 +84,25 @@ okq_status okq_paged_attention(const okq_paged* cache, int32_t layer, int32_t la
     return OKQ_ERR_CUDA;
   }
   return launch_status();
+}
+
+okq_status okq_paged_attention(const okq_paged* cache, int32_t layer, int32_t layer_count, const void* q, const int64_t qs[4], int32_t n_new,
+                               const int32_t* q_len, const okq_rope* rope, float sm_scale, void* workspace, size_t workspace_bytes, void* out,
+                               const int64_t os[4], void* stream) {
+  return attention(cache, layer, layer_count, q, qs, n_new, q_len, rope, sm_scale, workspace, workspace_bytes, out, os, okq::WAIT_LIMIT_CLOCKS, 0, stream);
+}
+
+okq_status okq_debug_paged_timeout(const okq_paged* cache, int32_t layer, int32_t layer_count, const void* q, const int64_t qs[4], int32_t n_new,
+                                   void* workspace, size_t workspace_bytes, void* out, const int64_t os[4], int64_t limit_clocks, void* stream) {
+  if (limit_clocks <= 0) return OKQ_ERR_INVALID_ARG;
+  return attention(cache, layer, layer_count, q, qs, n_new, nullptr, nullptr, 0.08838834764831845f, workspace, workspace_bytes, out, os, limit_clocks, 1, stream);
+}
+
+int32_t okq_debug_paged_plan(const okq_paged* cache, int32_t layer_count, int32_t n_new) {
+  using namespace okq;
+  Plan p;
+  if (check_paged(cache, false) != OKQ_OK || layer_count <= 0 || layer_count > cache->n_layers || n_new <= 0 || !make_plan(cache, layer_count, n_new, p)) return 0;
+  return p.decode ? (p.cluster ? p.cluster : OKQ_PLAN_LINE) : OKQ_PLAN_PROMPT;
 }
 
 }  // extern "C"

@@ -43,6 +43,8 @@ struct AttnArgs {
   RopeView rope;
   int layer, layer_count, n_new;
   float scale2;     // softmax scale times log2(e)
+  long long limit;  // SM clocks that a wait may take
+  int withhold;     // testing aid: the first tile of every range is never delivered, so that the waits for it run out
   struct Head* heads;   // [Heads::count]
   float* slots;         // [2 * ranges][ROWS * (128 + 2)]: sums, maxima, normalisers
 };

@@ -155,7 +155,7 @@ __device__ __forceinline__ void prepare_queries(const AttnArgs& a, const Cursor<
 // CLUSTER: every (layer, sequence, KV head) has a cluster of `size` blocks, whose pipelines share its tiles evenly, and its parts are put
 // together in the cluster's shared memory: one launch.  Otherwise pipelines have even ranges of the whole line and k_paged_merge follows.
 template <class T, bool CLUSTER>
-__global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ CUtensorMap map, const AttnArgs a, int size, long long wait_limit) {
+__global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ CUtensorMap map, const AttnArgs a, int size) {
   extern __shared__ unsigned char raw_smem[];
   DecodeSmem& sm = *reinterpret_cast<DecodeSmem*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~(uintptr_t)1023);
   const int tid = threadIdx.x, lane = tid & 31;
@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     init(&mine.q_full, 4);
     sm.abort = 0;
     sm.tmem_busy = 0;
-    sm.limit = wait_limit;
+    sm.limit = a.limit;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
   if (warp == 0) {
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     if (go) {
       entries();
       scales();
-      while (armed < NS && more()) load(armed++);
+      while (armed < NS && more() && !a.withhold) load(armed++);
       go = score(0, true);
       for (int i = 0; go; i++) {
         cur.next(work);
@@ -565,7 +565,7 @@ template <class T, bool CLUSTER> cudaError_t launch(const AttnArgs& a, const CUt
     if (e != cudaSuccess) return e;
     attr_done(attr_mask, dev);
   }
-  cudaError_t e = launch_dependent(k_paged_decode<T, CLUSTER>, dim3(grid), NT, SMEM, s, CLUSTER ? size : 1, map, a, size, WAIT_LIMIT_CLOCKS);
+  cudaError_t e = launch_dependent(k_paged_decode<T, CLUSTER>, dim3(grid), NT, SMEM, s, CLUSTER ? size : 1, map, a, size);
   return e == cudaSuccess && !CLUSTER ? launch_merge<T, R>(a, G * grid, s) : e;
 }
 

@@ -237,7 +237,7 @@ __device__ __forceinline__ float numerators(const float (&x)[2][32], uint32_t s_
 }
 
 template <class T>
-__global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ CUtensorMap map, const AttnArgs a, long long wait_limit) {
+__global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ CUtensorMap map, const AttnArgs a) {
   extern __shared__ unsigned char raw_smem[];
   PromptSmem& sm = *reinterpret_cast<PromptSmem*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~(uintptr_t)1023);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     for (int i = 0; i < 2; i++) { init(&sm.o_full[i], 1); init(&sm.q_full[i], 4); }
     sm.abort = 0;
     sm.tmem_busy = 0;
-    sm.limit = wait_limit;
+    sm.limit = a.limit;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
   }
   if (warp == 0) {
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     };
     int armed[2] = {0, 0};
     float vref = 0.f;
-    bool out = false;
+    bool out = a.withhold != 0;
     entries();
     scales();
     for (int i = 0; !out; i++) {
@@ -623,7 +623,7 @@ template <class T> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map,
     if (e != cudaSuccess) return e;
     attr_done(attr_mask, dev);
   }
-  cudaError_t e = launch_dependent(k_paged_prompt<T>, dim3(grid), NT, SMEM, s, 1, map, a, WAIT_LIMIT_CLOCKS);
+  cudaError_t e = launch_dependent(k_paged_prompt<T>, dim3(grid), NT, SMEM, s, 1, map, a);
   return e == cudaSuccess ? launch_merge<T, R>(a, grid, s) : e;
 }
 

@@ -542,6 +542,33 @@ def test_attention_schedules(shape, dtype):
         assert torch.equal(out, again)
 
 
+def test_attention_plans():
+    """The rule of sizes: a cluster for few short items, even ranges for many or long ones, the prompt kernel from nine rows on."""
+    def plan(L, batch, H, Hq, tokens, n):
+        c = B.PagedCache(L, batch, H, Hq, 4, (tokens + 63) // 64, 64)
+        return B.paged_plan(c, L, n)
+    assert plan(1, 1, 1, 7, 2048, 1) == 8 and plan(1, 4, 4, 28, 4096, 1) in (4, 5, 6) and plan(1, 30, 4, 4, 130, 1) in (1, 2)
+    assert plan(1, 1, 4, 28, 131072, 1) == plan(1, 16, 4, 32, 32768, 1) == plan(28, 8, 4, 28, 512, 1) == B.PLAN_LINE
+    assert plan(1, 1, 1, 7, 2048, 2) == plan(1, 1, 1, 8, 64, 2) == B.PLAN_PROMPT and plan(1, 1, 1, 1, 2048, 8) == 8
+
+
+@pytest.mark.parametrize("batch,H,n,tokens", [(1, 1, 1, 2000), (30, 8, 1, 1500), (1, 2, 40, 2000), (2, 2, 300, 700)])
+def test_attention_waits_are_bounded(batch, H, n, tokens):
+    """With nothing delivered every role's wait runs out: NaN, the status word, and a device that goes on."""
+    g = gen(11)
+    c = random_cache(g, 1, batch, H, 7 * H, 64, F16, [tokens] * batch)
+    q = randn(g, 1, batch, 7 * H, n, D).cuda()
+    out, ws = torch.zeros_like(q), torch.empty(B.paged_workspace_bytes(c, 1, n), dtype=torch.uint8, device="cuda")
+    B.debug_paged_timeout(c, 0, 1, q, ws, out, limit_clocks=2_000_000)
+    torch.cuda.synchronize()
+    assert c.device_status() == B.ERR_TIMEOUT and torch.isnan(out).all()
+    c.status.zero_()
+    out.fill_(5.0)
+    B.paged_attention(c, 0, 1, q, ws, out)
+    check_random(c, q, out, None, 5.0)
+    assert c.device_status() == 0
+
+
 def test_offsets_beyond_32_bits():
     """A pool of 5 GB whose last pages are the ones in use."""
     m = Model(1, 2, 4, 8, max_pages=2, page=256, dtype=F16, n_pages=20000)

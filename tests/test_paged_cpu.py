@@ -110,6 +110,13 @@ def test_other_refusals(L):
     assert L.okq_pages_compact(c, P16 + 2, P16, 1 << 20, None) == B.ERR_ALIGNMENT
 
 
+def test_plan_and_debug_refusals(L):
+    assert L.okq_debug_paged_plan(cache(), 1, 100) == B.PLAN_PROMPT and L.okq_debug_paged_plan(cache(), 1, 1) != 0
+    for c, layers, n in ((cache(dtype=2), 1, 1), (cache(), 0, 1), (cache(), 3, 1), (cache(), 1, 0), (cache(), 1, 1 << 27)):
+        assert L.okq_debug_paged_plan(c, layers, n) == 0
+    assert L.okq_debug_paged_timeout(cache(), 0, 1, P16, S4, 1, P16, 1 << 30, P16, S4, 0, None) == B.ERR_INVALID_ARG
+
+
 def test_rope_refusals(L):
     def t(**kw):
         d = dict(in_=P16, out=P16, in_strides=(8, 8, 8), out_strides=(8, 8, 8), heads=2)
