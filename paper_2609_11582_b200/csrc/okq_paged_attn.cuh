@@ -254,7 +254,8 @@ __global__ void __launch_bounds__(MERGE_NT) k_paged_merge(const AttnArgs a) {
   __shared__ float2 stat[WARPS];
   depend_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = blockIdx.y * (WARPS / WPR) + warp / WPR, first = warp % WPR;
-  const Head hd = a.heads[blockIdx.x];
+  const int4 h0 = __ldcg(reinterpret_cast<const int4*>(&a.heads[blockIdx.x]));
+  const Head hd{h0.x, h0.y, h0.z, h0.w, __ldcg(&a.heads[blockIdx.x].rt), {}};
   if (hd.more == 0) return;
   constexpr size_t SLOT = (size_t)ROWS * (D + 2);
   const int n = hd.more + 1, row = hd.rt * ROWS + r;

@@ -2,7 +2,8 @@
 //
 // The tables and counts are a few hundred kilobytes at most and every decision depends on the ones before it (which page is free next),
 // so one thread block of 1024 takes them, 4096 entries at a time; what moves (codes, scales, raw tokens) is left in a list and
-// copied by a second kernel on the whole GPU, bound by memory: bytes read and written once.
+// copied by a second kernel on the whole GPU, bound by memory: bytes read and written once.  Tables and counts are read past the first
+// cache: a kernel placed before its predecessor's end may find there what its predecessor read.
 #include "okq_paged.cuh"
 
 namespace okq {
@@ -59,7 +60,7 @@ __device__ __forceinline__ void free_refill(FreePages& f, const PagedView& c) {
     int is[PER], n = 0;
 #pragma unroll
     for (int e = 0; e < PER; e++) {
-      is[e] = p0 + e < c.n_pages && c.refs[p0 + e] == 0;
+      is[e] = p0 + e < c.n_pages && __ldcg(&c.refs[p0 + e]) == 0;
       n += is[e];
     }
     __syncthreads();
@@ -81,12 +82,12 @@ __global__ void __launch_bounds__(NT) k_pages_reserve(const PagedView c, const i
   auto wanted = [&](long long e) -> bool {   // entry e = (sequence, place) lacks a page that the call asks for
     if (e >= entries) return false;
     const int b = (int)(e / c.max_pages), j = (int)(e - (long long)b * c.max_pages);
-    return (long long)j << c.page_shift < tokens[b] && c.table[e] < 0;
+    return (long long)j << c.page_shift < __ldcg(&tokens[b]) && __ldcg(&c.table[e]) < 0;
   };
   // all or nothing: what is asked for, then what is free
   long long need = 0, have = 0;
   int over = 0;
-  for (int b = tid; b < c.batch; b += NT) over |= tokens[b] > c.room();
+  for (int b = tid; b < c.batch; b += NT) over |= __ldcg(&tokens[b]) > c.room();
   if (__syncthreads_or(over)) {
     if (tid == 0) set_status(c.status, OKQ_ERR_CAPACITY);
     return;
@@ -100,7 +101,7 @@ __global__ void __launch_bounds__(NT) k_pages_reserve(const PagedView c, const i
   for (int p0 = 0; p0 < c.n_pages; p0 += CHUNK) {
     int n = 0;
 #pragma unroll
-    for (int e = 0; e < PER; e++) n += p0 + e * NT + tid < c.n_pages && c.refs[p0 + e * NT + tid] == 0;
+    for (int e = 0; e < PER; e++) n += p0 + e * NT + tid < c.n_pages && __ldcg(&c.refs[p0 + e * NT + tid]) == 0;
     have += n;
   }
   block_scan(f.sc, (int)need);   // (both fit 32 bits: entries and pages do)
@@ -150,7 +151,7 @@ __device__ __forceinline__ int fork_wrong(const PagedView& c, int a, int d, int 
   int wrong = 0;
   for (int l = t; l < c.n_layers; l += n) wrong |= c.held(l, a) != len;
   for (int j = t; j < c.max_pages; j += n) {
-    wrong |= c.table[(size_t)d * c.max_pages + j] >= 0;                                   // the destination has pages
+    wrong |= __ldcg(&c.table[(size_t)d * c.max_pages + j]) >= 0;                                   // the destination has pages
     wrong |= (long long)j << c.page_shift < len && c.page_of(a, j << c.page_shift) < 0;   // the source lacks one
   }
   return wrong;
@@ -158,7 +159,7 @@ __device__ __forceinline__ int fork_wrong(const PagedView& c, int a, int d, int 
 // full pages and lengths of a pair
 __device__ __forceinline__ void fork_share(const PagedView& c, int a, int d, int len, int t, int n) {
   for (int j = t; j < len >> c.page_shift; j += n) {
-    const int p = c.table[(size_t)a * c.max_pages + j];
+    const int p = __ldcg(&c.table[(size_t)a * c.max_pages + j]);
     c.table[(size_t)d * c.max_pages + j] = p;
     atomicAdd(&c.refs[p], 1);
   }
@@ -180,9 +181,9 @@ __global__ void __launch_bounds__(NT) k_pages_fork(const PagedView c, const int3
   if (apart) {
     int meet = 0;
     for (int i = warp; i < count; i += NT / 32) {
-      const int a = src[i], d = dst[i];
+      const int a = __ldcg(&src[i]), d = __ldcg(&dst[i]);
       int bad = (unsigned)a >= (unsigned)c.batch || (unsigned)d >= (unsigned)c.batch || a == d ? OKQ_ERR_INVALID_ARG : 0;
-      for (int k = lane; k < count; k += 32) meet |= k != i && (dst[k] == d || dst[k] == a);
+      for (int k = lane; k < count; k += 32) meet |= k != i && (__ldcg(&dst[k]) == d || __ldcg(&dst[k]) == a);
       const int len = bad ? 0 : c.held(0, a);
       if (!bad && __any_sync(0xffffffffu, fork_wrong(c, a, d, len, lane, 32))) bad = OKQ_ERR_INVALID_ARG;
       if (lane == 0) { bad_of[i] = bad; len_of[i] = len; }
@@ -210,10 +211,10 @@ __global__ void __launch_bounds__(NT) k_pages_fork(const PagedView c, const int3
     if (part && fresh < 0) bad = OKQ_ERR_CAPACITY;
     if (mine) {
       int4 todo = make_int4(-1, -1, -1, -1);
-      const int a = src[tid], d = dst[tid], full = len >> c.page_shift;
+      const int a = __ldcg(&src[tid]), d = __ldcg(&dst[tid]), full = len >> c.page_shift;
       if (!bad && len > 0) { todo.z = a; todo.w = d; }
       if (!bad && part) {
-        todo.x = c.table[(size_t)a * c.max_pages + full];
+        todo.x = __ldcg(&c.table[(size_t)a * c.max_pages + full]);
         todo.y = fresh;
         c.table[(size_t)d * c.max_pages + full] = fresh;
         c.refs[fresh] = 1;
@@ -224,11 +225,11 @@ __global__ void __launch_bounds__(NT) k_pages_fork(const PagedView c, const int3
     }
     __syncthreads();
     for (int i = warp; i < count; i += NT / 32)
-      if (!bad_of[i]) fork_share(c, src[i], dst[i], len_of[i], lane, 32);
+      if (!bad_of[i]) fork_share(c, __ldcg(&src[i]), __ldcg(&dst[i]), len_of[i], lane, 32);
     return;
   }
   for (int i = 0; i < count; i++) {
-    const int a = src[i], d = dst[i];
+    const int a = __ldcg(&src[i]), d = __ldcg(&dst[i]);
     int bad = (unsigned)a >= (unsigned)c.batch || (unsigned)d >= (unsigned)c.batch || a == d ? OKQ_ERR_INVALID_ARG : 0;
     int len = 0;
     if (tid == 0) root = make_int2(-1, a);
@@ -253,7 +254,7 @@ __global__ void __launch_bounds__(NT) k_pages_fork(const PagedView c, const int3
       if (!bad && len > 0) { todo.z = root.y; todo.w = d; }
       if (!bad && part) {
         const int fresh = f.queue[f.head++];
-        todo.x = root.x >= 0 ? root.x : c.table[(size_t)a * c.max_pages + full];
+        todo.x = root.x >= 0 ? root.x : __ldcg(&c.table[(size_t)a * c.max_pages + full]);
         todo.y = fresh;
         c.table[(size_t)d * c.max_pages + full] = fresh;
         c.refs[fresh] = 1;
@@ -303,7 +304,7 @@ __global__ void __launch_bounds__(CT) k_fork_copy(const PagedView c, const int4*
 // one block per named sequence
 __global__ void __launch_bounds__(CT) k_pages_release(const PagedView c, const int32_t* seqs) {
   depend_wait();
-  const int b = seqs[blockIdx.x];
+  const int b = __ldcg(&seqs[blockIdx.x]);
   if ((unsigned)b >= (unsigned)c.batch) {
     if (threadIdx.x == 0) set_status(c.status, OKQ_ERR_INVALID_ARG);
     return;
@@ -324,9 +325,9 @@ __global__ void __launch_bounds__(CT) k_pages_release(const PagedView c, const i
 __global__ void __launch_bounds__(CT) k_pages_copy(const PagedView c, const int32_t* src, const int32_t* dst, int count) {
   depend_wait();
   const int i = blockIdx.x, tid = threadIdx.x;
-  const int a = src[i], d = dst[i];
+  const int a = __ldcg(&src[i]), d = __ldcg(&dst[i]);
   int bad = (unsigned)a >= (unsigned)c.n_pages || (unsigned)d >= (unsigned)c.n_pages;
-  for (int k = tid; k < count; k += CT) bad |= k != i && (dst[k] == d || src[k] == d);
+  for (int k = tid; k < count; k += CT) bad |= k != i && (__ldcg(&dst[k]) == d || __ldcg(&src[k]) == d);
   if (__syncthreads_or(bad)) {
     if (tid == 0) set_status(c.status, OKQ_ERR_INVALID_ARG);
     return;
@@ -340,7 +341,7 @@ __global__ void __launch_bounds__(NT) k_compact_plan(const PagedView c, int32_t*
   depend_wait();
   const int tid = threadIdx.x;
   int live = 0;
-  for (int p = tid; p < c.n_pages; p += NT) live += c.refs[p] > 0;
+  for (int p = tid; p < c.n_pages; p += NT) live += __ldcg(&c.refs[p]) > 0;
   block_scan(sc, live);
   const int n = sc.total;
   __syncthreads();
@@ -352,7 +353,7 @@ __global__ void __launch_bounds__(NT) k_compact_plan(const PagedView c, int32_t*
 #pragma unroll
     for (int e = 0; e < PER; e++) {
       const int p = q0 + PER * tid + e;
-      const bool in = p < c.n_pages, used = in && c.refs[p] > 0;
+      const bool in = p < c.n_pages, used = in && __ldcg(&c.refs[p]) > 0;
       hole[e] = in && !used && p < n;
       mover[e] = used && p >= n;
       nh += hole[e];
@@ -375,7 +376,7 @@ __global__ void __launch_bounds__(NT) k_compact_plan(const PagedView c, int32_t*
   for (int k = tid; k < movers; k += NT) {   // (written by this block: visible behind the barrier)
     const int2 m = pairs[k];
     to[m.x] = m.y;
-    c.refs[m.y] = c.refs[m.x];
+    c.refs[m.y] = __ldcg(&c.refs[m.x]);
     c.refs[m.x] = 0;
   }
   if (tid == 0) {
@@ -395,7 +396,7 @@ __global__ void __launch_bounds__(CT) k_compact_move(const PagedView c, const in
   }
   const long long entries = (long long)c.batch * c.max_pages;
   for (long long e = (long long)blockIdx.x * CT + tid; e < entries; e += (long long)gridDim.x * CT) {
-    const int p = c.table[e];
+    const int p = __ldcg(&c.table[e]);
     if ((unsigned)p < (unsigned)c.n_pages) c.table[e] = to[p];
   }
 }
