@@ -475,7 +475,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     // ------------------------------------------------------------------ softmax: lane = row (after a timeout they run on, waits failing at once)
     const int t = warp >> 2, quarter = warp & 3;
     const uint32_t lanes = (uint32_t)(32 * quarter) << 16, s_at = tmem + S_COL + 128u * t + lanes, o_at = tmem + O_COL + 128u * t + lanes;
-    int n_s[2] = {0, 0}, n_o = 0;
+    uint32_t ph_s = 0;   // phases of s_full to come, by place
+    int n_o = 0;
     bool whole = cur.tile == 0, began = cur.tile != 0;
     if (!heads.by_item && tid == 0) a.heads[v].more = 0;
     for (int i = 0; cur.ok;) {
@@ -489,55 +490,65 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       if (dual) asm volatile("bar.sync 1, 256;\n" ::: "memory");   // stream A's queries are B's too
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.q_full[t]);
-      const int last_seen = cur.len - cur.m + c.query_of(cur.rt * R + row);   // last token that the row sees
-      const int least = cur.len - cur.m + c.query_of(cur.rt * R + row0);      // .. that the warp's first row sees
-      float m = -INFINITY, l = 0.f, vref = 1.f;
-      for (int y = 0; y < steps; y++) {
-        const int k = dual ? y : y >> 1, half = dual ? t : y & 1, place = y & 1, at = (cur.tile + k) * PT + PH * half;
-        const uint32_t p_at = s_at + 64u * place;
-        bar_wait(sm, &sm.info_full[(i + k) & 3], (uint32_t)((i + k) >> 2) & 1u);
-        const Info& info = sm.info[(i + k) & 3];
-        bar_wait(sm, &sm.s_full[t][place], (uint32_t)(place ? n_s[1]++ : n_s[0]++) & 1u);
-        after_sync();
-        float x[2][32];
-        tmem_ld32(p_at, x[0]);
-        tmem_ld32(p_at + 32u, x[1]);
-        const bool edge = at + PH - 1 > least || info.lost;
-        tmem_wait_ld();
-        const float mx = edge ? row_max<true>(x, info, 2 * half, back, last_seen - at) : row_max<false>(x, info, 2 * half, back, last_seen - at);
-        // a new reference: the row's sums so far are multiplied, once their last product is through
-        const float fv = dual || !half ? info.fv : 1.f;
-        vref = info.vref;
-        const bool passed = mx > m;
-        if (__any_sync(0xffffffffu, passed) || (fv != 1.f && y > 0)) {
-          const float mn = passed ? mx + LEAD : m, f = passed ? ex2(m - mn) : 1.f;   // (0 for the first)
-          m = mn;
-          l *= f;
-          if (y > 0) {
-            bar_wait(sm, &sm.o_full[t], (uint32_t)(n_o + y - 1) & 1u);
-            after_sync();
+      float m = -INFINITY, l = 0.f;
+      {
+        // (what the loop keeps in registers besides 64 scores: as little as can be)
+        int seen = cur.len - cur.m + c.query_of(cur.rt * R + row) - cur.tile * PT - (dual ? PH * t : 0);   // last column of the step that the row sees
+        int half = dual ? t : 0, tile = i;
+        for (int y = 0; y < steps; y++) {
+          const uint32_t p_at = s_at + 64u * (y & 1);
+          bar_wait(sm, &sm.info_full[tile & 3], (uint32_t)(tile >> 2) & 1u);
+          const Info& info = sm.info[tile & 3];
+          bar_wait(sm, &sm.s_full[t][y & 1], ph_s >> (y & 1) & 1u);
+          ph_s ^= 1u << (y & 1);
+          after_sync();
+          float x[2][32];
+          tmem_ld32(p_at, x[0]);
+          tmem_ld32(p_at + 32u, x[1]);
+          const bool edge = __any_sync(0xffffffffu, seen < PH - 1) || info.lost;
+          tmem_wait_ld();
+          const float mx = edge ? row_max<true>(x, info, 2 * half, back, seen) : row_max<false>(x, info, 2 * half, back, seen);
+          // a new reference: the row's sums so far are multiplied, once their last product is through
+          const float fv = dual || !half ? info.fv : 1.f;
+          const bool passed = mx > m;
+          if (__any_sync(0xffffffffu, passed) || (fv != 1.f && y > 0)) {
+            const float mn = passed ? mx + LEAD : m, f = passed ? ex2(m - mn) : 1.f;   // (0 for the first)
+            m = mn;
+            l *= f;
+            if (y > 0) {
+              bar_wait(sm, &sm.o_full[t], (uint32_t)(n_o + y - 1) & 1u);
+              after_sync();
 #pragma unroll 1
-            for (int b = 0; b < 8; b++) {
-              float o[16];
-              tmem_ld16(o_at + 16u * b, o);
-              tmem_wait_ld();
+              for (int b = 0; b < 8; b++) {
+                float o[16];
+                tmem_ld16(o_at + 16u * b, o);
+                tmem_wait_ld();
 #pragma unroll
-              for (int e = 0; e < 16; e++) o[e] *= f * fv;
-              tmem_st16(o_at + 16u * b, reinterpret_cast<const uint32_t(&)[16]>(o));
+                for (int e = 0; e < 16; e++) o[e] *= f * fv;
+                tmem_st16(o_at + 16u * b, reinterpret_cast<const uint32_t(&)[16]>(o));
+              }
             }
           }
+          const float ref = m == -INFINITY ? 0.f : m;
+          l = edge ? numerators<true>(x, p_at, info, 2 * half, back, ref, seen, l) : numerators<false>(x, p_at, info, 2 * half, back, ref, seen, l);
+          tmem_wait_st();
+          before_sync();
+          __syncwarp();
+          // Phases of o_full are told apart by one bit: the last but one is waited for while the last cannot be complete, since all that is
+          // known without a wait is that the third last is.
+          if (y > 0 && y + 1 == steps) bar_wait(sm, &sm.o_full[t], (uint32_t)(n_o + y - 1) & 1u);
+          if (lane == 0) mbar_arrive(&sm.p_full[t][y & 1]);
+          if (dual) {
+            tile++;
+            seen -= PT;
+          } else {
+            tile += half;
+            half ^= 1;
+            seen -= PH;
+          }
         }
-        const float ref = m == -INFINITY ? 0.f : m;
-        l = edge ? numerators<true>(x, p_at, info, 2 * half, back, ref, last_seen - at, l)
-                 : numerators<false>(x, p_at, info, 2 * half, back, ref, last_seen - at, l);
-        tmem_wait_st();
-        before_sync();
-        __syncwarp();
-        // Phases of o_full are told apart by one bit: the last but one is waited for while the last cannot be complete, since all that is
-        // known without a wait is that the third last is.
-        if (y > 0 && y + 1 == steps) bar_wait(sm, &sm.o_full[t], (uint32_t)(n_o + y - 1) & 1u);
-        if (lane == 0) mbar_arrive(&sm.p_full[t][place]);
       }
+      const float vref = sm.info[(i + n - 1) & 3].vref;   // (its place is not taken before this warp is at the next item)
       n_o += steps;
       bar_wait(sm, &sm.o_full[t], (uint32_t)(n_o - 1) & 1u);
       if (sm.abort) l = NAN;
