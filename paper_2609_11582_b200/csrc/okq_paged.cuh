@@ -60,7 +60,7 @@ template <> __device__ __forceinline__ __half from_f(float x) { return __float2h
 template <> __device__ __forceinline__ __nv_bfloat16 from_f(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ float from_f(float x) { return x; }
 
-template <class T> struct alignas(sizeof(T) * 8) Vec8 { T v[8]; };   // eight channels
+template <class T> struct alignas(16) Vec8 { T v[8]; };   // eight channels (tensors and strides are multiples of 16 bytes, of fp32 too)
 
 // ---- rotary positions
 struct RopeView {

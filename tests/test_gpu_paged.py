@@ -95,6 +95,18 @@ def test_rope_in_place_and_strided():
     assert torch.equal(q, want_q) and torch.equal(k, want_k) and torch.equal(qkv[:, :, 7:], v)
 
 
+def test_rope_rows_at_odd_multiples_of_16_bytes():
+    g = gen(4)
+    pos = positions(g, 2, 19, "near").cuda()
+    rope = B.Rope(pos, B.rope_frequencies(1e4, 64), (16, 24, 24))
+    for dtype, off in ((F32, 4), (BF16, 8), (F16, 8)):
+        q, out = (randn(g, 2, 3, 19, D + off, dtype=dtype).cuda()[..., off:] for _ in range(2))
+        want, behind = torch.empty_like(q.contiguous()), out._base[..., :off].clone()
+        B.rope_apply(rope, q.contiguous(), want)
+        B.rope_apply(rope, q, out)
+        assert torch.equal(out, want) and torch.equal(out._base[..., :off], behind)
+
+
 @pytest.mark.parametrize("sections,interleaved", SECTIONS[:2])
 def test_rope_gradient(sections, interleaved):
     """The inverse is the gradient of the formula's 64-bit form, and agrees with differences of the call itself."""
