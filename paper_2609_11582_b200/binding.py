@@ -545,6 +545,8 @@ class PagedCache:
                 "refs": ((n_pages,), torch.int32), "seq_len": ((n_layers, batch), torch.int32)}
         for name, (shape, dt) in want.items():
             assert tuple(b[name].shape) == shape and b[name].dtype == dt and b[name].is_contiguous(), name
+            if b[name].device != b["codes"].device:
+                raise ValueError(f"codes on {b['codes'].device}, {name} on {b[name].device}")
         self.codes, self.scales, self.raw, self.table, self.refs, self.seq_len = (b[n] for n in want)
         self.n_layers, self.batch, self.n_kv_heads, self.n_q_heads = n_layers, batch, n_kv_heads, n_q_heads
         self.n_pages, self.max_pages, self.page_tokens, self.dtype, self.device = n_pages, max_pages, page_tokens, dtype, self.codes.device
@@ -569,6 +571,8 @@ class Rope:
     def __init__(self, positions, freq, sections, interleaved=False):
         assert positions.dtype == torch.int32 and positions.dim() == 3 and positions.shape[0] == 3 and positions.is_contiguous()
         assert freq.dtype == torch.float64 and freq.numel() == sum(sections) and freq.is_contiguous()
+        if freq.device != positions.device:
+            raise ValueError(f"positions on {positions.device}, freq on {freq.device}")
         self.positions, self.freq = positions, freq
         self.batch, self.n = positions.shape[1], positions.shape[2]
         self.ref = _rope_struct(*sections, 1 if interleaved else 0, freq.data_ptr(), positions.data_ptr())

@@ -138,6 +138,17 @@ def test_tensors_of_the_host_are_refused():
         B.rope_apply(B.Rope(torch.zeros(3, 1, 1, dtype=torch.int32), torch.zeros(64, dtype=torch.float64), (16, 24, 24)), x, x)
 
 
+def test_tensors_on_two_devices_are_refused():
+    with pytest.raises(ValueError):
+        B.Rope(torch.zeros(3, 1, 1, dtype=torch.int32, device="meta"), torch.zeros(64, dtype=torch.float64), (16, 24, 24))
+    cache = B.PagedCache(1, 1, 1, 1, 2, 2, device="cpu")
+    buffers = {n: getattr(cache, n) for n in ("codes", "scales", "raw", "table", "refs", "seq_len")}
+    B.PagedCache(1, 1, 1, 1, buffers=buffers)
+    for n in buffers:
+        with pytest.raises(ValueError):
+            B.PagedCache(1, 1, 1, 1, buffers={**buffers, n: buffers[n].to("meta")})
+
+
 # ------------------------------------------------------------------------------------------------ the oracle
 def test_oracle_axes():
     assert O.rope_axes((2, 3, 3), False) == [0, 0, 1, 1, 1, 2, 2, 2]
