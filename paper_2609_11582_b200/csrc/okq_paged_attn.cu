@@ -1,7 +1,8 @@
 // Attention over the 8-bit paged cache (okq_paged_attention): checks, workspace, and which of the two kernels takes a call.
 //
-// Up to eight query rows per KV head (row = query x head of the GQA group) go to the decode kernel, whose products have eight columns
-// for them; more to the prompt kernel, with 256 rows per block.
+// Rows (query x head of the GQA group) of a KV head are cut into row tiles: eight rows in the decode kernel, whose products have eight
+// columns for them and read the codes as they are, 256 in the prompt kernel, which turns codes into fp16.  Both read a head's tokens once
+// per row tile.
 #include "okq_paged_attn.cuh"
 
 namespace okq {
@@ -10,33 +11,42 @@ namespace {
 
 struct Plan {
   bool decode;
-  int grid, ranges;         // blocks, parts of the line of tiles
+  int grid, ranges;         // blocks of the line of tiles, its parts
   int cluster;              // decode: blocks to a (layer, sequence, KV head), 0 where the line is cut evenly
   size_t heads, bytes;      // of the workspace: heads, all
 };
 
-// false: more tiles than their numbers hold, were all sequences as long as their rows of the table
+// Which kernel, for sequences as long as their rows of the table (lengths are the device's).  Measured in turn, us:
+//   rows up to 16: the decode kernel (12 rows, 16 sequences x 4 heads of up to 12345 tokens 43 against 62; 32768 each 174 against 228)
+//   up to 24 where two thirds of the three readings come from the second-level cache (1 sequence x 4 heads of 131072 tokens 58 against
+//   75; 16 x 4 of 32768 253 against 232; 32 rows: 76 against 76 and 333 against 234)
+//   any number of rows with items so few that each can have a cluster of blocks: one launch, no search for the first tile, no merge
+//   kernel, parts put together in shared memory.  An item has no more than its cluster's pipelines then, so both sides are reckoned in
+//   tiles (2 us), fixed costs included (64 rows of 1 head of 2048 tokens 8.0 against 17.2, 192 rows of 4 heads of 1000 tokens 14.1 against
+//   22.8; 8 rows, 4 heads of 131072 tokens: 34 in the line, 90 as clusters; 96 rows of 8 heads of 4000 tokens 22 by the prompt kernel).
+// False: more units than their numbers hold.
 bool make_plan(const okq_paged* c, int layer_count, int n_new, Plan& p) {
-  const long long group = c->n_q_heads / c->n_kv_heads, rows = n_new * group;
+  const long long rows = (long long)n_new * (c->n_q_heads / c->n_kv_heads);
   if (rows > 1 << 29) return false;
-  p.decode = rows <= DECODE_ROWS;
+  const long long per_item = ((long long)c->max_pages * c->page_tokens + PT - 1) / PT, n = sm_count();
+  const double heads = (double)layer_count * c->batch * c->n_kv_heads;
+  auto items_of = [&](int per) { return heads * (double)((rows + per - 1) / per); };
+  const double few = items_of(DECODE_ROWS), many = items_of(PROMPT_ROWS);
+  auto in_line = [&](double items, int extra, int pipes) { return (long long)(items * (double)(per_item + extra) / (double)(pipes * n)) + 1; };
+  p.decode = rows <= 2 * DECODE_ROWS || (rows <= 3 * DECODE_ROWS && heads * (double)per_item <= 8192.0);   // (tiles of 32 KB)
+  p.cluster = 0;
+  if (few <= n) {
+    const long long other = p.decode ? in_line(few, DECODE_EXTRA, DECODE_PIPES) + 2 : in_line(many, PROMPT_EXTRA, 1) + 4;
+    for (int size = 8; size >= 1 && p.cluster == 0; size--)   // (the largest that all run at once: 15 of eight blocks, 22 of six, 33 of four, 74 of two)
+      if (few <= decode_clusters(size) && (per_item + DECODE_PIPES * size - 1) / (DECODE_PIPES * size) <= other) p.cluster = size;
+    if (p.cluster) p.decode = true;
+  }
   const int per = p.decode ? DECODE_ROWS : PROMPT_ROWS;
-  const double items = (double)layer_count * c->batch * c->n_kv_heads * (double)((rows + per - 1) / per);
-  const long long per_item = ((long long)c->max_pages * c->page_tokens + PT - 1) / PT;
+  const double items = p.decode ? few : many;
   if (items * (double)(per_item + (p.decode ? DECODE_EXTRA : PROMPT_EXTRA)) > 2147483647.0) return false;
-  const long long tiles = (long long)items * per_item, n = sm_count();
+  const long long tiles = (long long)items * per_item;
   p.grid = (int)(tiles < n ? tiles : n);
   p.ranges = p.grid * (p.decode ? DECODE_PIPES : 1);
-  // A cluster to each item where there are few of them: one launch, no search for the first tile, about two tiles' time less; but an item has
-  // no more than its cluster's pipelines.  Both sides in tiles of a pipeline, for sequences as long as their rows of the table (2 us a tile;
-  // 1 item of 2048 tokens 10.4 us as the line, 7.3 as a cluster; 4 items of 131072 the line's 34 us against 90).
-  p.cluster = 0;
-  if (p.decode && items <= n) {
-    const long long in_line = (long long)(items * (double)(per_item + DECODE_EXTRA) / (DECODE_PIPES * n)) + 1 + 2;
-    for (int size = 8; size >= 1 && p.cluster == 0; size--)   // (the largest that all run at once: 15 of eight blocks, 22 of six, 33 of four, 74 of two)
-      if (items <= decode_clusters(size) && (per_item + DECODE_PIPES * size - 1) / (DECODE_PIPES * size) <= in_line) p.cluster = size;
-    if (p.cluster) p.grid = (int)items * p.cluster;
-  }
   p.heads = (size_t)p.ranges * sizeof(Head);   // (the workspace is the line's, whichever it is)
   p.bytes = p.heads + (size_t)2 * p.ranges * per * (D + 2) * sizeof(float);
   return true;

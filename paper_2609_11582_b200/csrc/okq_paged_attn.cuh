@@ -244,9 +244,8 @@ __device__ __forceinline__ void write_empty(const AttnArgs& a, const Work<ROWS, 
 
 constexpr int MERGE_NT = 512;
 
-// Block (x, y): rows of the item of head x, if it is in parts.  WPR warps to a row (all sixteen where a handful of rows can be in hundreds
-// of parts, one where hundreds of rows are in a few), of which each has every WPR-th part, a lane four channels.  Bound by latency: a
-// few megabytes of parts at most; all of a part is loaded at once, seven parts in flight.
+// Block (x, y): rows of the item of head x, if it is in parts.  WPR warps to a row, of which each has every WPR-th part, a lane four
+// channels.  Bound by latency: a few megabytes of parts at most; all of a part is loaded at once, seven parts in flight.
 template <class T, int ROWS, int WPR>
 __global__ void __launch_bounds__(MERGE_NT) k_paged_merge(const AttnArgs a) {
   constexpr int WARPS = MERGE_NT / 32;
@@ -321,20 +320,28 @@ __global__ void __launch_bounds__(MERGE_NT) k_paged_merge(const AttnArgs a) {
             from_f<T>(l == 0.f ? 0.f : acc.w / l)};
   *reinterpret_cast<uint2*>(out_row<T>(a, li, b, hd.h, row) + 4 * lane) = *reinterpret_cast<const uint2*>(o);
 }
-template <class T, int ROWS> inline cudaError_t launch_merge(const AttnArgs& a, int ranges, cudaStream_t s) {
-  constexpr int WPR = ROWS <= 8 ? MERGE_NT / 32 : 1;
-  const Heads<ROWS> heads(a.layer_count * a.c.batch, a.c.n_kv, a.c.group, a.n_new, ranges);
+template <class T, int ROWS, int WPR> inline cudaError_t launch_merge_by(const AttnArgs& a, int heads, cudaStream_t s) {
   const long long rows = (long long)a.n_new * a.c.group;
   const int most = (int)(rows < ROWS ? rows : ROWS), per = MERGE_NT / 32 / WPR;
-  return launch_dependent(k_paged_merge<T, ROWS, WPR>, dim3(heads.count(ranges), (most + per - 1) / per), MERGE_NT, 0, s, 1, a);
+  return launch_dependent(k_paged_merge<T, ROWS, WPR>, dim3(heads, (most + per - 1) / per), MERGE_NT, 0, s, 1, a);
+}
+template <class T, int ROWS> inline cudaError_t launch_merge(const AttnArgs& a, int ranges, cudaStream_t s) {
+  const Heads<ROWS> heads(a.layer_count * a.c.batch, a.c.n_kv, a.c.group, a.n_new, ranges);
+  const int n = heads.count(ranges), parts = heads.items < ranges ? ranges / heads.items : 1;   // (of an item, were all alike)
+  if (ROWS <= 8) return launch_merge_by<T, ROWS, MERGE_NT / 32>(a, n, s);
+  // Warps to a row: more where one would load parts several times in a row, as long as the GPU holds them all at once (1 sequence of 32768
+  // tokens, 32 rows: 37 us with one warp to a row, 20 with sixteen; 16 heads of 8000 tokens, 256 rows: 52 with one, 60 with four).
+  const long long room = 4ll * sm_count() * (MERGE_NT / 32) / n, rows = (long long)a.n_new * a.c.group, most = rows < ROWS ? rows : ROWS;
+  if (parts >= 28 && 16 * most <= room) return launch_merge_by<T, ROWS, 16>(a, n, s);
+  return parts >= 15 && 4 * most <= room ? launch_merge_by<T, ROWS, 4>(a, n, s) : launch_merge_by<T, ROWS, 1>(a, n, s);
 }
 
-// okq_paged_decode.cu: up to DECODE_ROWS rows, DECODE_PIPES pipelines per block.  An item's own costs in tiles: queries, the first tile's
-// latency and the output take about as long as one and a half.
+// okq_paged_decode.cu: DECODE_ROWS rows to an item, DECODE_PIPES pipelines per block.  An item's own costs in tiles: queries, the first
+// tile's latency and the output take about as long as one and a half.
 constexpr int DECODE_ROWS = 8, DECODE_PIPES = 3, DECODE_EXTRA = 1;
-cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int grid, int cluster, cudaStream_t s);   // cluster 0: ranges of the line, merge
+cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int blocks, int cluster, cudaStream_t s);   // cluster 0: ranges of the line, merge
 int decode_clusters(int size);   // clusters of so many blocks (at most eight) that run at once
-// okq_paged_prompt.cu: any number of rows, one pipeline per block.  An item of a single tile takes 8 to 10 us, a further tile 2 to 3.
+// okq_paged_prompt.cu: PROMPT_ROWS rows to an item, one pipeline per block.  An item of a single tile takes 8 to 10 us, a further tile 2 to 3.
 constexpr int PROMPT_ROWS = 256, PROMPT_EXTRA = 3;
 cudaError_t launch_paged_prompt(const AttnArgs& a, int dtype, int grid, cudaStream_t s);
 

@@ -1,5 +1,5 @@
-// Attention over the 8-bit paged cache for up to eight query rows per (layer, sequence, KV head): single tokens, and a few drafted
-// ones where the GQA group is small.
+// Attention over the 8-bit paged cache for few query rows per (layer, sequence, KV head): single tokens, a few drafted ones, and short
+// pieces of prompts.  An item has up to eight rows.
 //
 // All products are of 8-bit integers on tcgen05 (kind::i8), with the cache's codes as they lie in memory for one operand:
 //   scores   S[token][row] = K[token][channel] Q[row][channel]: A = a tile of 128 tokens (K-major), B = the queries as three signed
@@ -104,7 +104,7 @@ __device__ __forceinline__ void lane_sums(const float (&x)[R], float* to, int la
 }
 
 // Two of an item's rows, r0 and r0 + 1: limbs (swizzled) and scales.  One warp, four channels per lane.  `turns`: cosines and sines of
-// the item's queries, [query][64 pairs].
+// the item's queries, [query from the first on][64 pairs].
 template <class T>
 __device__ __forceinline__ void prepare_queries(const AttnArgs& a, const Cursor<R, EXTRA>& cur, int r0, const uint2 (&raw)[2], const float2* turns, int8_t* qbuf,
                                                 float* qscale, int lane) {
@@ -117,7 +117,7 @@ __device__ __forceinline__ void prepare_queries(const AttnArgs& a, const Cursor<
     const T* y = reinterpret_cast<const T*>(&raw[e]);
     float x[4] = {to_f(y[0]), to_f(y[1]), to_f(y[2]), to_f(y[3])};
     if (a.rope.freq) {
-      const float2* cs = turns + 64 * a.c.query_of(r) + pair0;
+      const float2* cs = turns + 64 * (a.c.query_of(R * cur.rt + r) - a.c.query_of(R * cur.rt)) + pair0;
 #pragma unroll
       for (int z = 0; z < 4; z++) {
         const float o = __shfl_sync(0xffffffffu, x[z], other);
@@ -193,14 +193,16 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
   Cuts cuts(0, 1);
   int v = 0, end = 0;            // this pipeline's range of the line, and the unit behind it
   Cursor<R, EXTRA> cur{};
-  const int unit = CLUSTER ? blockIdx.x / size : 0, rank = CLUSTER ? blockIdx.x - unit * size : 0;
-  if (CLUSTER) {
-    cur.pair = unit / c.n_kv;
-    cur.h = unit - cur.pair * c.n_kv;
+  int rank = 0;
+  if (CLUSTER) {   // (grid (size x row tiles, heads, pairs): a division on the way to the first tile is felt)
+    asm("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank));
+    asm("mov.u32 %0, %%clusterid.x;\n" : "=r"(cur.rt));
+    cur.h = blockIdx.y;
+    cur.pair = blockIdx.z;
     cur.li = work.layer_of(cur.pair);
     cur.b = cur.pair - cur.li * c.batch;
     work.lens(cur.li, cur.b, cur.len, cur.m);
-    cur.nt = cur.m ? work.tiles(cur.len, cur.m, 0) : 0;
+    cur.nt = cur.rt < work.row_tiles(cur.m) ? work.tiles(cur.len, cur.m, cur.rt) : 0;
     const Cuts share(cur.nt, G * size);
     cur.tile = share.start(g * size + rank);
     cur.left = share.size(g * size + rank);
@@ -211,7 +213,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     end = cuts.start(v) + cuts.size(v);
     cur = place<R, EXTRA, G>(sm.find, work, cuts, v, g);
   }
-  const int rows = cur.m * c.group;   // (CLUSTER: of the item)
+  const int rows = min(R, cur.m * c.group - R * cur.rt);   // (CLUSTER: of the item)
 
   if (role == SERVICE) {
     // ------------------------------------------------------------------ copies and products
@@ -327,7 +329,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     // ------------------------------------------------------------------ workers (after a timeout they run on, waits failing at once)
     const uint32_t lanes = (uint32_t)(32 * role) << 16;
     const int ch = 32 * role + lane;
-    float top[R], sum[R], qs[R], o[R];
+    float top[R], sum[R], o[R];   // (the rows' scales are read again with every tile: with them the state does not fit 128 registers)
     bool fresh = true, whole = cur.tile == 0, began = cur.tile != 0;   // the piece has its item's first tile; the item began in an earlier range
     if (CLUSTER) {
 #pragma unroll
@@ -335,25 +337,29 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     }
     if (!CLUSTER && !heads.by_item && tid == g * 128) a.heads[v].more = 0;
     for (int i = 0; cur.ok; i++) {
-      const int s = i % NS, b = i & 1, item0 = end - cur.left - cur.tile;   // (the item's first unit)
-      const int pair = cur.pair, li = cur.li, bq = cur.b, h = cur.h, tile = cur.tile, len = cur.len, m = cur.m, nt = cur.nt;
+      const int s = i % NS, b = i & 1;
+      // what is needed of this item when the cursor has gone on: its last tile's unit, its rows, and the token of the tile's first lane
+      // counted from the first that the first query does not see
+      const int li = cur.li, bq = cur.b, h = cur.h, rt = cur.rt, item_end = end - cur.left - cur.tile + cur.nt - 1;
+      const int rows = cur.m * c.group - R * rt, late = cur.tile * PT - (cur.len - cur.m + 1);
       if (fresh) {   // (the products of the item before are through: their sums have been read)
         // rows, and the turns of the item's queries (at most eight) in the place of the numerators
-        const int rows = cur.m * c.group;
+        const int row = R * rt + 2 * role;
         uint2 raw[2];
 #pragma unroll
         for (int e = 0; e < 2; e++) {
           raw[e] = make_uint2(0u, 0u);
-          if (2 * role + e < rows) raw[e] = *reinterpret_cast<const uint2*>(query_row<T>(a, cur.li, cur.b, cur.h, 2 * role + e) + 4 * lane);
+          if (2 * role + e < rows) raw[e] = *reinterpret_cast<const uint2*>(query_row<T>(a, li, bq, h, row + e) + 4 * lane);
         }
         float2* turns = reinterpret_cast<float2*>(pipe.p);
         if (a.rope.freq) {
           const size_t st = (size_t)c.batch * a.n_new;
+          const int q0 = c.query_of(R * rt), nq = c.query_of(R * rt + min(rows, R) - 1) - q0 + 1;
           const int pair = ch & 63;
           const double f = pair < a.rope.half ? a.rope.freq[pair] : 0.0;
-          const int32_t* pos = a.rope.positions + a.rope.axis(pair) * st + (size_t)cur.b * a.n_new;
+          const int32_t* pos = a.rope.positions + a.rope.axis(pair) * st + (size_t)bq * a.n_new + q0;
 #pragma unroll 1
-          for (int qi = ch >> 6; qi < cur.m; qi += 2) {
+          for (int qi = ch >> 6; qi < nq; qi += 2) {
             float2 y;
             turn((double)pos[qi] * f, y.x, y.y);
             turns[64 * qi + pair] = y;
@@ -365,7 +371,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         asm volatile("bar.sync %0, 128;\n" ::"r"(1 + g) : "memory");
         if (lane == 0) mbar_arrive(&sy.q_full);
 #pragma unroll
-        for (int r = 0; r < R; r++) { qs[r] = sy.qscale[r]; top[r] = -INFINITY; sum[r] = o[r] = 0.f; }
+        for (int r = 0; r < R; r++) { top[r] = -INFINITY; sum[r] = o[r] = 0.f; }
       }
       cur.next(work);
       const bool last = cur.ended || !cur.ok;
@@ -383,13 +389,12 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         tmem_ld8(tmem + S_COL + 16u + lanes, d2);
         tmem_wait_ld();
 #pragma unroll
-        for (int r = 0; r < R; r++) x[r] = fmaf((float)d2[r], 65536.f, (float)(d1[r] * 256 + d0[r])) * (qs[r] * ks);
+        for (int r = 0; r < R; r++) x[r] = fmaf((float)d2[r], 65536.f, (float)(d1[r] * 256 + d0[r])) * (sy.qscale[r] * ks);
       }
-      const int t = tile * PT + 32 * role + lane;
-      if (tile * PT + PT > len - m + 1) {   // some row does not see all of the tile
+      if (late + PT > 0) {   // some row may not see all of the tile
 #pragma unroll
         for (int r = 0; r < R; r++)
-          if (t >= len - m + 1 + c.query_of(r)) x[r] = -INFINITY;
+          if (late + 32 * role + lane >= c.query_of(R * rt + r)) x[r] = -INFINITY;
       }
       {
         float w[R];
@@ -459,13 +464,13 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         const bool ends = cur.ended, direct = whole && ends;
         float* slot = a.slots + (size_t)(2 * v + (began ? 0 : 1)) * SLOT;
         if (!began && (heads.by_item || !ends) && tid == g * 128)   // (the same thread as above)
-          a.heads[heads.at(v, c.n_kv, pair, h, 0)] = Head{ends ? 0 : cuts.range_of(item0 + nt - 1) - v, v, pair, h, 0, {}};
+          a.heads[heads.at(v, c.n_kv, li * c.batch + bq, h, rt)] = Head{ends ? 0 : cuts.range_of(item_end) - v, v, li * c.batch + bq, h, rt, {}};
 #pragma unroll
         for (int r = 0; r < R; r++) {
           float l = (sy.sum[0][r] + sy.sum[1][r]) + (sy.sum[2][r] + sy.sum[3][r]);
           if (sm.abort) l = NAN;
           if (direct) {
-            if (r < m * c.group) out_row<T>(a, li, bq, h, r)[ch] = from_f<T>(l == 0.f ? 0.f : o[r] / l);
+            if (r < rows) out_row<T>(a, li, bq, h, R * rt + r)[ch] = from_f<T>(l == 0.f ? 0.f : o[r] / l);
           } else {
             slot[r * D + ch] = o[r];
             if (ch == r) { slot[R * D + r] = top[r]; slot[R * D + R + r] = l; }
@@ -547,7 +552,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         l = fmaf(y[D + 1], f, l);
         o = fmaf(y[ch], f, o);
       }
-      out_row<T>(a, cur.li, cur.b, cur.h, r)[ch] = from_f<T>(l == 0.f ? 0.f : o / l);
+      out_row<T>(a, cur.li, cur.b, cur.h, R * cur.rt + r)[ch] = from_f<T>(l == 0.f ? 0.f : o / l);
     }
     __syncthreads();
   }
@@ -555,7 +560,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
   asm volatile("barrier.cluster.wait.aligned;\n" ::: "memory");   // no block ends while its parts are read
 }
 
-template <class T, bool CLUSTER> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map, int grid, int size, cudaStream_t s) {
+template <class T, bool CLUSTER> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map, dim3 grid, int size, cudaStream_t s) {
   static thread_local unsigned long long attr_mask = 0;
   int dev = 0;
   constexpr int SMEM = (int)sizeof(DecodeSmem) + 1024;
@@ -565,8 +570,8 @@ template <class T, bool CLUSTER> cudaError_t launch(const AttnArgs& a, const CUt
     if (e != cudaSuccess) return e;
     attr_done(attr_mask, dev);
   }
-  cudaError_t e = launch_dependent(k_paged_decode<T, CLUSTER>, dim3(grid), NT, SMEM, s, CLUSTER ? size : 1, map, a, size);
-  return e == cudaSuccess && !CLUSTER ? launch_merge<T, R>(a, G * grid, s) : e;
+  cudaError_t e = launch_dependent(k_paged_decode<T, CLUSTER>, grid, NT, SMEM, s, CLUSTER ? size : 1, map, a, size);
+  return e == cudaSuccess && !CLUSTER ? launch_merge<T, R>(a, G * (int)grid.x, s) : e;
 }
 
 }  // namespace
@@ -597,11 +602,14 @@ int decode_clusters(int size) {
   return known[size];
 }
 
-cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int grid, int cluster, cudaStream_t s) {
+cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int blocks, int cluster, cudaStream_t s) {
   CUtensorMap map;
   if (!codes_map(map, a.c, true)) return cudaErrorInvalidValue;
-  if (cluster > 0) return dtype == OKQ_FP16 ? launch<__half, true>(a, map, grid, cluster, s) : launch<__nv_bfloat16, true>(a, map, grid, cluster, s);
-  return dtype == OKQ_FP16 ? launch<__half, false>(a, map, grid, 1, s) : launch<__nv_bfloat16, false>(a, map, grid, 1, s);
+  if (cluster > 0) {
+    const dim3 grid((unsigned)cluster * (unsigned)((a.n_new * a.c.group + R - 1) / R), (unsigned)a.c.n_kv, (unsigned)(a.layer_count * a.c.batch));
+    return dtype == OKQ_FP16 ? launch<__half, true>(a, map, grid, cluster, s) : launch<__nv_bfloat16, true>(a, map, grid, cluster, s);
+  }
+  return dtype == OKQ_FP16 ? launch<__half, false>(a, map, dim3(blocks), 1, s) : launch<__nv_bfloat16, false>(a, map, dim3(blocks), 1, s);
 }
 
 }  // namespace okq

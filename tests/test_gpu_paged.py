@@ -135,11 +135,12 @@ def test_rope_gradient(sections, interleaved):
 
 # ------------------------------------------------------------------------------------------------ a cache and what it should hold
 class Model:
-    """A cache and every token appended to it, as the call was given it."""
+    """A cache and every token appended to it, as the call was given it.  `wide`: the table has room for 2^19 tokens of each sequence, so
+    that the rule of sizes does not take an item for a short one."""
 
-    def __init__(self, L, batch, H, Hq, max_pages, page, dtype, n_pages=None, seed=0):
+    def __init__(self, L, batch, H, Hq, max_pages, page, dtype, n_pages=None, seed=0, wide=False):
         n_pages = n_pages or batch * max_pages + 3
-        self.c = B.PagedCache(L, batch, H, Hq, n_pages, max_pages, page, dtype)
+        self.c = B.PagedCache(L, batch, H, Hq, n_pages, (1 << 19) // page if wide else max_pages, page, dtype)
         self.L, self.B, self.H, self.Hq, self.page, self.dtype = L, batch, H, Hq, page, dtype
         self.c.codes.random_(-127, 128)      # what is not written is not zero
         self.c.scales.normal_()
@@ -148,7 +149,7 @@ class Model:
         self.g = gen(seed + 100)
         # pages in an order of their own
         order = torch.randperm(n_pages, generator=self.g).int()[:batch * max_pages]
-        self.c.table.copy_(order.view(batch, max_pages))
+        self.c.table[:, :max_pages] = order.view(batch, max_pages).cuda()
         self.c.refs[order.long()] = 1
 
     def lens(self, l=0):
@@ -380,9 +381,11 @@ def test_attention_single_tokens(dtype, H, Hq, page):
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("H,Hq,page,n", [(1, 7, 64, 2), (2, 16, 32, 5), (4, 4, 128, 3), (3, 15, 256, 40), (2, 4, 64, 130), (1, 8, 32, 17), (1, 1, 32, 200)])
-def test_attention_several_queries(dtype, H, Hq, page, n):
-    m = Model(1, 5, H, Hq, max_pages=max(2, 1024 // page), page=page, dtype=dtype)
+def test_attention_several_queries(dtype, H, Hq, page, n, wide):
+    m = Model(1, 5, H, Hq, max_pages=max(2, 1024 // page), page=page, dtype=dtype, wide=wide)
+    assert not wide or n * Hq // H <= 16 or B.paged_plan(m.c, 1, n) == B.PLAN_PROMPT
     m.append(n, [n, max(1, n // 2), 1, 0, n - 1])
     m.attend(n)                                            # more queries than tokens: rows that see nothing
     m.append(420, [420, 7, 160, 0, 33])
@@ -398,10 +401,10 @@ def test_attention_long_context(n):
     m.attend(n)
 
 
-@pytest.mark.parametrize("n", [1, 40])
-def test_attention_scales_and_sinks(n):
+@pytest.mark.parametrize("n,wide", [(1, False), (40, False), (1, True), (40, True)])
+def test_attention_scales_and_sinks(n, wide):
     """Softmax scales of either sign and zero; one token that takes nearly all of the mass with next to no value; large scores."""
-    m = Model(1, 2, 2, 8, max_pages=8, page=64, dtype=F16)
+    m = Model(1, 2, 2, 8, max_pages=8, page=64, dtype=F16, wide=wide)
     k, v = randn(m.g, 1, 2, 2, 400, D), randn(m.g, 1, 2, 2, 400, D)
     k[:, 1, :, 0] = 0.5
     v[:, 1, :, 0] = 0
@@ -417,8 +420,8 @@ def test_attention_scales_and_sinks(n):
 
 
 def test_attention_infinite_and_lost_things():
-    for n in (1, 20):
-        m = Model(1, 4, 1, 2, max_pages=4, page=32, dtype=F16)
+    for n, wide in ((1, False), (20, False), (1, True), (20, True)):
+        m = Model(1, 4, 1, 2, max_pages=4, page=32, dtype=F16, wide=wide)
         k, v = randn(m.g, 1, 4, 1, 100, D), randn(m.g, 1, 4, 1, 100, D)
         k[0, 1, 0, 40, 3] = float("inf")         # second block of sequence 1
         v[0, 2, 0, 99, 3] = float("nan")         # last block of sequence 2
@@ -524,11 +527,13 @@ def check_random(c, q, out, q_len, poison):
         assert ((got - ref).abs() <= bound).all(), (b, T, m, ((got - ref).abs() / bound).max().item())
 
 
-# (layers, batch, KV heads, group, page, queries, longest): more items than ranges, items of one tile, row tiles of every kind (256 rows,
-# up to 128 and between) behind one another in a range, ranges that end inside items, sequences that are empty
+# (layers, batch, KV heads, group, page, queries, longest): more items than ranges, items of one tile, row tiles of every kind (eight rows
+# and fewer; 256, up to 128 and between) behind one another in a range, ranges that end inside items, sequences that are empty
 SCHEDULES = [(3, 64, 8, 4, 32, 1, 300), (1, 300, 4, 2, 64, 1, 130), (2, 1, 1, 8, 32, 1, 9000), (28, 9, 4, 7, 64, 1, 700), (1, 2, 8, 1, 256, 8, 40000),
              (1, 40, 4, 7, 32, 5, 400), (2, 33, 8, 4, 64, 40, 300), (1, 5, 2, 7, 128, 700, 1500), (1, 1, 1, 8, 64, 1000, 1000), (3, 17, 3, 5, 32, 130, 140),
-             (1, 200, 2, 8, 32, 20, 90), (1, 2, 1, 1, 64, 3000, 3500), (1, 3, 4, 8, 256, 33, 30000), (4, 50, 4, 1, 64, 300, 310)]
+             (1, 200, 2, 8, 32, 20, 90), (1, 2, 1, 1, 64, 3000, 3500), (1, 3, 4, 8, 256, 33, 30000), (4, 50, 4, 1, 64, 300, 310),
+             (1, 40, 4, 7, 32, 2, 400), (2, 9, 3, 5, 64, 4, 2000), (1, 1, 2, 1, 64, 13, 5000), (1, 2, 2, 7, 32, 9, 500), (1, 1, 4, 8, 64, 24, 900),
+             (28, 2, 4, 7, 64, 3, 700), (1, 1, 1, 3, 256, 8, 33000)]
 
 
 @pytest.mark.parametrize("shape", SCHEDULES, ids=str)
@@ -555,13 +560,16 @@ def test_attention_schedules(shape, dtype):
 
 
 def test_attention_plans():
-    """The rule of sizes: a cluster for few short items, even ranges for many or long ones, the prompt kernel from nine rows on."""
+    """The rule of sizes: a cluster for few short items of eight rows; even ranges for many or long ones, up to 16 rows, and 24 where not
+    all is read from memory again; the prompt kernel else."""
     def plan(L, batch, H, Hq, tokens, n):
         c = B.PagedCache(L, batch, H, Hq, 4, (tokens + 63) // 64, 64)
         return B.paged_plan(c, L, n)
     assert plan(1, 1, 1, 7, 2048, 1) == 8 and plan(1, 4, 4, 28, 4096, 1) in (4, 5, 6) and plan(1, 30, 4, 4, 130, 1) in (1, 2)
     assert plan(1, 1, 4, 28, 131072, 1) == plan(1, 16, 4, 32, 32768, 1) == plan(28, 8, 4, 28, 512, 1) == B.PLAN_LINE
-    assert plan(1, 1, 1, 7, 2048, 2) == plan(1, 1, 1, 8, 64, 2) == B.PLAN_PROMPT and plan(1, 1, 1, 1, 2048, 8) == 8
+    assert plan(1, 1, 1, 7, 2048, 2) == plan(1, 1, 1, 8, 64, 2) == plan(1, 1, 1, 1, 2048, 8) == 8 and plan(1, 1, 4, 32, 1000, 24) in (1, 2)
+    assert plan(1, 16, 4, 32, 32768, 2) == plan(1, 1, 4, 32, 131072, 3) == B.PLAN_LINE
+    assert plan(1, 16, 4, 32, 32768, 3) == plan(1, 1, 4, 32, 131072, 4) == plan(1, 1, 4, 28, 8192, 2048) == plan(1, 16, 4, 28, 12345, 5) == B.PLAN_PROMPT
 
 
 @pytest.mark.parametrize("batch,H,n,tokens", [(1, 1, 1, 2000), (30, 8, 1, 1500), (1, 2, 40, 2000), (2, 2, 300, 700)])
