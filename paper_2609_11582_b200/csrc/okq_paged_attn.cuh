@@ -336,13 +336,14 @@ template <class T, int ROWS> inline cudaError_t launch_merge(const AttnArgs& a, 
   return parts >= 15 && 4 * most <= room ? launch_merge_by<T, ROWS, 4>(a, n, s) : launch_merge_by<T, ROWS, 1>(a, n, s);
 }
 
-// okq_paged_decode.cu: DECODE_ROWS rows to an item, DECODE_PIPES pipelines per block.  An item's own costs in tiles: queries, the first
-// tile's latency and the output take about as long as one and a half.
-constexpr int DECODE_ROWS = 8, DECODE_PIPES = 3, DECODE_EXTRA = 1;
+// okq_paged_decode.cu: DECODE_ROWS rows to an item, DECODE_PIPES pipelines per block.  An item's own costs (queries, the first tile's
+// latency, the output) in tiles, as measured: 64 sequences x 8 heads of up to 1500 tokens, 24 rows, 93 us with 1, 75 with 2, 71 with 3.
+constexpr int DECODE_ROWS = 8, DECODE_PIPES = 3, DECODE_EXTRA = 3;
 cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int blocks, int cluster, cudaStream_t s);   // cluster 0: ranges of the line, merge
 int decode_clusters(int size);   // clusters of so many blocks (at most eight) that run at once
-// okq_paged_prompt.cu: PROMPT_ROWS rows to an item, one pipeline per block.  An item of a single tile takes 8 to 10 us, a further tile 2 to 3.
-constexpr int PROMPT_ROWS = 256, PROMPT_EXTRA = 3;
+// okq_paged_prompt.cu: PROMPT_ROWS rows to an item, one pipeline per block.  Own costs alike: 16 sequences x 4 heads of up to 12345 tokens,
+// 35 rows 62 us with 3, 58 with 4, 55 with 6, 56 with 8; 64 x 8 of up to 1500, 1024 rows, 555, 511, 462, 482.
+constexpr int PROMPT_ROWS = 256, PROMPT_EXTRA = 6;
 cudaError_t launch_paged_prompt(const AttnArgs& a, int dtype, int grid, cudaStream_t s);
 
 // the pool's codes as rows of 128 bytes, copied 32 at a time

@@ -422,54 +422,63 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
   } else if (warp >= W_CONV) {
     // ------------------------------------------------------------------ codes to fp16: eight lanes to a token, sixteen channels each
     // Two warps have the keys, two the values.
-    const int side = (warp - W_CONV) >> 1, who = (warp - W_CONV) & 1, ct = 32 * who + lane, j = ct & 7;
-    for (int x = 0, end_x = 0;; x++) {
-      if (x == end_x) {   // the next item's steps
-        if (!cur.ok) break;
+    // (of eight lanes four have the first 64 channels of token t and four the others of token t ^ 1, so that each store has all banks)
+    const int side = (warp - W_CONV) >> 1, who = (warp - W_CONV) & 1, j = lane & 7, tok = ((32 * who + lane) >> 3) ^ (j >> 2);
+    const uint32_t at = (uint32_t)((j >> 2) * KV_HALF + tok * 128), a0 = at + (((2 * (j & 3)) ^ tok) << 4), a1 = at + (((2 * (j & 3) + 1) ^ tok) << 4);
+    int end_x = 0;
+    auto there = [&](int x) {   // whether step x is the range's
+      if (x == end_x && cur.ok) {
         const int n = cur.piece();
         end_x += 2 * n;
         cur.skip(work, n);
       }
+      return x < end_x;
+    };
+    auto codes_of = [&](int x) { return sm.code[side][x >> 1 & 1] + ((x & 1) * PH + tok) * D + 16 * j; };
+    uint4 w[8], w_nx[8];
+    auto fetch = [&](int x, uint4 (&to)[8]) {
+      if (!(x & 1)) bar_wait(sm, &sm.code_full[side][x >> 1 & 1], (uint32_t)(x >> 2) & 1u);
+#pragma unroll
+      for (int z = 0; z < 8; z++) to[z] = *reinterpret_cast<const uint4*>(codes_of(x) + 8 * z * D);
+    };
+    bool more = there(0);
+    if (more) fetch(0, w);
+    for (int x = 0; more; x++) {
       const int i = x >> 1, half = x & 1, s = x % NR;
-      if (!half) {
-        if (side) bar_wait(sm, &sm.info_full[i & 3], (uint32_t)(i >> 2) & 1u);
-        bar_wait(sm, &sm.code_full[side][i & 1], (uint32_t)(i >> 1) & 1u);
-      }
-      const bool plain = !side || sm.info[i & 3].plain;
-      const int8_t* from = sm.code[side][i & 1] + (half * PH + (ct >> 3)) * D + 16 * j;
-      uint4 w[8];
-#pragma unroll
-      for (int z = 0; z < 8; z++) w[z] = *reinterpret_cast<const uint4*>(from + 8 * z * D);
+      more = there(x + 1);
+      if (more) fetch(x + 1, w_nx);
+      if (side && !half) bar_wait(sm, &sm.info_full[i & 3], (uint32_t)(i >> 2) & 1u);
       if (x >= NR) bar_wait(sm, side ? &sm.v_free[s] : &sm.k_free[s], (uint32_t)(x / NR - 1) & 1u);
-      unsigned char* to = (side ? sm.v[s][0] : sm.k[s][0]) + (j >> 2) * KV_HALF + (ct >> 3) * 128;
+      unsigned char* to = side ? sm.v[s][0] : sm.k[s][0];
+      if (!side || sm.info[i & 3].plain) {   // (no branch between the rows, so that their conversions overlap)
 #pragma unroll
-      for (int z = 0; z < 8; z++) {
-        const int t = 8 * z + (ct >> 3);
-        uint2 h[4] = {codes_to_half(w[z].x), codes_to_half(w[z].y), codes_to_half(w[z].z), codes_to_half(w[z].w)};
-        if (!plain) {
-          const float mul = sm.info[i & 3].mul[2 * half + (t >> 5)];
-          const __half2 m2 = __floats2half2_rn(mul, mul);
-#pragma unroll
-          for (int e = 0; e < 4; e++) {
-            __half2* y = reinterpret_cast<__half2*>(&h[e]);
-            y[0] = __hmul2(y[0], m2);
-            y[1] = __hmul2(y[1], m2);
-          }
+        for (int z = 0; z < 8; z++) {
+          const uint2 h[4] = {codes_to_half(w[z].x), codes_to_half(w[z].y), codes_to_half(w[z].z), codes_to_half(w[z].w)};
+          *reinterpret_cast<uint4*>(to + a0 + 1024 * z) = make_uint4(h[0].x, h[0].y, h[1].x, h[1].y);
+          *reinterpret_cast<uint4*>(to + a1 + 1024 * z) = make_uint4(h[2].x, h[2].y, h[3].x, h[3].y);
         }
-        // chunks 2 (j & 3) and the next of the row's 64 channels; the two halves' lanes in opposite order, for the banks' sake
-        unsigned char* row = to + 8 * z * 128;
-        const int a0 = (2 * (j & 3)) ^ (t & 7), a1 = (2 * (j & 3) + 1) ^ (t & 7);
-        const uint4 y0 = make_uint4(h[0].x, h[0].y, h[1].x, h[1].y), y1 = make_uint4(h[2].x, h[2].y, h[3].x, h[3].y);
-        *reinterpret_cast<uint4*>(row + (j < 4 ? a0 : a1) * 16) = j < 4 ? y0 : y1;
-        *reinterpret_cast<uint4*>(row + (j < 4 ? a1 : a0) * 16) = j < 4 ? y1 : y0;
+      } else {
+#pragma unroll 1
+        for (int z = 0; z < 8; z++) {
+          const uint4 x4 = *reinterpret_cast<const uint4*>(codes_of(x) + 8 * z * D);
+          const uint2 h[4] = {codes_to_half(x4.x), codes_to_half(x4.y), codes_to_half(x4.z), codes_to_half(x4.w)};
+          const float mul = sm.info[i & 3].mul[2 * half + (z >> 2)];
+          const __half2 m2 = __floats2half2_rn(mul, mul);
+          __half2 y[8];
+#pragma unroll
+          for (int e = 0; e < 8; e++) y[e] = __hmul2(reinterpret_cast<const __half2*>(h)[e], m2);
+          *reinterpret_cast<uint4*>(to + a0 + 1024 * z) = reinterpret_cast<const uint4*>(y)[0];
+          *reinterpret_cast<uint4*>(to + a1 + 1024 * z) = reinterpret_cast<const uint4*>(y)[1];
+        }
       }
       fence_async_smem();
       __syncwarp();
       if (lane == 0) {
-        __threadfence_block();
-        sm.done[side][who] = x + 1;
+        asm volatile("st.release.cta.shared.s32 [%0], %1;\n" ::"r"(smem_u32(const_cast<const int*>(&sm.done[side][who]))), "r"(x + 1) : "memory");
         if (half) mbar_arrive(&sm.code_free[side][i & 1]);
       }
+#pragma unroll
+      for (int z = 0; z < 8; z++) w[z] = w_nx[z];
     }
   } else {
     // ------------------------------------------------------------------ softmax: lane = row (after a timeout they run on, waits failing at once)
