@@ -294,35 +294,36 @@ __global__ void __launch_bounds__(NT) k_paged_advance(const PagedView c, int lay
   else if (m) c.seq_len[(size_t)l * c.batch + b] = len + m;
 }
 
+// Block: NT / 8 tokens of a (layer, sequence, head), eight threads to a token; 8-byte loads of codes so that a warp's stores are whole
+// lines.  Bound by memory.
 template <class T>
-__global__ void __launch_bounds__(NT) k_paged_read(const PagedView c, int layer, int begin, int n, T* k_out, T* v_out, long long items) {
+__global__ void __launch_bounds__(NT) k_paged_read(const PagedView c, int layer, int begin, int n, T* k_out, T* v_out, int chunks) {
   depend_wait();
-  const long long id = (long long)blockIdx.x * NT + threadIdx.x;
-  if (id >= items) return;
-  const int j = (int)(id & 7);                        // sixteen channels
-  long long u = id >> 3;
-  const int i = (int)(u % n);
-  u /= n;
-  const int h = (int)(u % c.n_kv);
-  u /= c.n_kv;
-  const int b = (int)(u % c.batch), li = (int)(u / c.batch), l = layer + li;
-  const int t = begin + i;
-  if (t >= c.held(l, b)) return;
+  const unsigned unit = blockIdx.x / (unsigned)chunks;
+  const unsigned pair = unit / (unsigned)c.n_kv, h = unit - pair * c.n_kv, li = pair / (unsigned)c.batch, b = pair - li * c.batch;
+  const int i = (int)(blockIdx.x - unit * chunks) * (NT / 8) + (threadIdx.x >> 3), j = threadIdx.x & 7, l = layer + (int)li, t = begin + i;
+  if (i >= n || t >= c.held(l, b)) return;
   const int page = c.page_of(b, t);
   if (page < 0) { set_status(c.status, OKQ_ERR_INVALID_ARG); return; }
+  uint2 w[2][2];
+  float scale[2];
 #pragma unroll
   for (int side = 0; side < 2; side++) {
     const size_t row = c.code_row(l, page, h, side) + (t & (c.page - 1));
-    const float scale = c.scales[row / PB];
-    const int4 w = *reinterpret_cast<const int4*>(c.codes + row * D + 16 * j);
-    const int8_t* q = reinterpret_cast<const int8_t*>(&w);
-    T* out = (side ? v_out : k_out) + (size_t)(id >> 3) * D + 16 * j;
+    scale[side] = c.scales[row / PB];
 #pragma unroll
-    for (int half = 0; half < 2; half++) {
+    for (int z = 0; z < 2; z++) w[side][z] = *reinterpret_cast<const uint2*>(c.codes + row * D + 64 * z + 8 * j);
+  }
+#pragma unroll
+  for (int side = 0; side < 2; side++) {
+    T* out = (side ? v_out : k_out) + ((size_t)unit * n + i) * D + 8 * j;
+#pragma unroll
+    for (int z = 0; z < 2; z++) {
+      const int8_t* q = reinterpret_cast<const int8_t*>(&w[side][z]);
       Vec8<T> y;
 #pragma unroll
-      for (int e = 0; e < 8; e++) y.v[e] = from_f<T>((float)q[8 * half + e] * scale);
-      *reinterpret_cast<Vec8<T>*>(out + 8 * half) = y;
+      for (int e = 0; e < 8; e++) y.v[e] = from_f<T>((float)q[e] * scale[side]);
+      *reinterpret_cast<Vec8<T>*>(out + 64 * z) = y;
     }
   }
 }
@@ -442,14 +443,15 @@ okq_status okq_paged_read(const okq_paged* cache, int32_t layer, int32_t layer_c
   if (!aligned16(k_out) || !aligned16(v_out)) return OKQ_ERR_ALIGNMENT;
   if (n == 0) return OKQ_OK;
   const PagedView c = paged_view(cache);
-  const long long items = (long long)layer_count * c.batch * c.n_kv * n * 8, grid = (items + NT - 1) / NT;
+  const int chunks = n / (NT / 8) + (n % (NT / 8) != 0);
+  const long long grid = (long long)layer_count * c.batch * c.n_kv * chunks;
   if (grid > 0x7fffffffll) return OKQ_ERR_UNSUPPORTED;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
   if (cache->dtype == OKQ_FP16)
-    e = launch_dependent(k_paged_read<__half>, dim3((unsigned)grid), NT, 0, s, 1, c, layer, begin, n, static_cast<__half*>(k_out), static_cast<__half*>(v_out), items);
+    e = launch_dependent(k_paged_read<__half>, dim3((unsigned)grid), NT, 0, s, 1, c, layer, begin, n, static_cast<__half*>(k_out), static_cast<__half*>(v_out), chunks);
   else
-    e = launch_dependent(k_paged_read<__nv_bfloat16>, dim3((unsigned)grid), NT, 0, s, 1, c, layer, begin, n, static_cast<__nv_bfloat16*>(k_out), static_cast<__nv_bfloat16*>(v_out), items);
+    e = launch_dependent(k_paged_read<__nv_bfloat16>, dim3((unsigned)grid), NT, 0, s, 1, c, layer, begin, n, static_cast<__nv_bfloat16*>(k_out), static_cast<__nv_bfloat16*>(v_out), chunks);
   return e != cudaSuccess ? failed(e) : launch_status();
 }
 
