@@ -506,7 +506,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
         int half = dual ? t : 0, tile = i;
         for (int y = 0; y < steps; y++) {
           const uint32_t p_at = s_at + 64u * (y & 1);
-          bar_wait(sm, &sm.info_full[tile & 3], (uint32_t)(tile >> 2) & 1u);
+          if (dual || !half) bar_wait(sm, &sm.info_full[tile & 3], (uint32_t)(tile >> 2) & 1u);
           const Info& info = sm.info[tile & 3];
           bar_wait(sm, &sm.s_full[t][y & 1], ph_s >> (y & 1) & 1u);
           ph_s ^= 1u << (y & 1);
