@@ -1,4 +1,4 @@
-// Attention over the 8-bit paged cache for more than eight query rows per (layer, sequence, KV head): prompts, pieces of prompts,
+// Attention over the 8-bit paged cache for many query rows per (layer, sequence, KV head): prompts, pieces of prompts,
 // drafted tokens.  Causal against the end of the sequence.
 //
 // Both products are fp16 on tcgen05 (kind::f16, fp32 accumulation in tensor memory):
@@ -14,12 +14,17 @@
 //
 // A block of threads has 256 rows, in two streams A and B of 128, and walks the tokens in steps of 64: a loader warp (32-token blocks
 // by page, two tiles of 128 tokens ahead), four warps that turn codes into fp16 (0x6400 | (code + 128) is 1024 + 128 + code; the rest is
-// one subtraction per two) in the layout of the products, to each stream an MMA warp (one for both is busy with waits and issue: 3.9
-// us a tile) and four softmax warps (lane = row).  A stream has
-// two places for scores, so that the next step's are there when a softmax ends.  Where an item has no more than 128 rows, both streams
-// have the same ones: A takes the first 64 tokens of every tile, B the others, and their sums are put together at the end.
+// one subtraction per two) in the layout of the products, to each stream an MMA warp (one for both was busy with waits and issue) and four
+// softmax warps (lane = row).  A stream has two places for scores, so that the next step's are there when a softmax ends.  Where an item
+// has no more than 128 rows (a dual item), both streams have the same ones: A takes the first 64 tokens of every tile, B the others, and
+// their sums are put together at the end.
 //
-// Bound by the exponentials (16 per cycle and SM: 2048 cycles for 256 x 128 scores) and the products (2048 cycles at fp16's rate).
+// At best bound by the exponentials (16 per cycle and SM: 2048 cycles for 256 x 128 scores) and the products (2048 cycles at fp16's
+// rate).  What it takes is about 5000 (2048 queries x 28 heads on 8192 tokens 282 us, 750 TFLOP/s of products): a softmax warp's own
+// chain of waits, tensor memory, maximum, exponentials and roundings, with two such warps on a scheduler and 128 registers to each.
+// Few rows (a dual item) are bound by the conversion, a step in 1500 cycles, a third of it waits and fences: 35 rows, 16 sequences x 4
+// heads of up to 12345 tokens 54 us (a converting warp to every other step, with half of those waits but a ring that is then too
+// short: 61).
 #include "okq_paged_attn.cuh"
 
 namespace okq {
@@ -421,7 +426,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     if (n_o > 0 && !mbar_drain(&sm.o_full[t], (uint32_t)(n_o - 1) & 1u)) sm.tmem_busy = 1;
   } else if (warp >= W_CONV) {
     // ------------------------------------------------------------------ codes to fp16: eight lanes to a token, sixteen channels each
-    // Two warps have the keys, two the values.
+    // Two warps have the keys, two the values; codes are loaded a step ahead.
     // (of eight lanes four have the first 64 channels of token t and four the others of token t ^ 1, so that each store has all banks)
     const int side = (warp - W_CONV) >> 1, who = (warp - W_CONV) & 1, j = lane & 7, tok = ((32 * who + lane) >> 3) ^ (j >> 2);
     const uint32_t at = (uint32_t)((j >> 2) * KV_HALF + tok * 128), a0 = at + (((2 * (j & 3)) ^ tok) << 4), a1 = at + (((2 * (j & 3) + 1) ^ tok) << 4);
