@@ -118,7 +118,9 @@ okq_status okq_paged_read(const okq_paged* cache, int32_t layer, int32_t layer_c
  *   sm_scale  softmax scale, normally 1/sqrt(128)
  *   out       device, of the cache's dtype, with strides of its own
  *   workspace device scratch of okq_paged_workspace_bytes(cache, layer_count, n_new); nothing in it is kept between calls
- * A sequence with a page missing below its length gives NaN and the status OKQ_ERR_INVALID_ARG.
+ * A sequence with a page missing below its length gives NaN and the status OKQ_ERR_INVALID_ARG.  OKQ_ERR_UNSUPPORTED (and a workspace
+ * of 0 bytes) where the work, were all sequences as long as their rows of the table, is 2^31 pieces of 128 tokens and 8 or 256 rows
+ * or more.
  */
 okq_status okq_paged_attention(const okq_paged* cache, int32_t layer, int32_t layer_count, const void* q, const int64_t q_strides[4],
                                int32_t n_new, const int32_t* q_len, const okq_rope* rope, float sm_scale, void* workspace,
