@@ -51,7 +51,8 @@ typedef struct okq_paged {
 /* Byte sizes of the seven buffers for the given shape fields, in the order of the struct. */
 okq_status okq_paged_sizes(const okq_paged* shape, size_t out_bytes[7]);
 
-/* Bytes of scratch that the calls below need at most for `layer_count` layers and n_new queries per sequence; 0 on a shape error. */
+/* Bytes of scratch that the calls below need at most for `layer_count` layers and n_new queries per sequence, or fewer of either; 0 on a
+ * shape error. */
 size_t okq_paged_workspace_bytes(const okq_paged* cache, int32_t layer_count, int32_t n_new);
 
 /*

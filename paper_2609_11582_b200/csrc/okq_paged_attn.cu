@@ -13,7 +13,7 @@ struct Plan {
   bool decode;
   int grid, ranges;         // blocks of the line of tiles, its parts
   int cluster;              // decode: blocks to a (layer, sequence, KV head), 0 where the line is cut evenly
-  size_t heads, bytes;      // of the workspace: heads, all
+  size_t heads, bytes;      // of the workspace: heads; what any plan for as many layers and queries or fewer takes
 };
 
 // Which kernel, for sequences as long as their rows of the table (lengths are the device's).  Measured in turn, us:
@@ -41,14 +41,17 @@ bool make_plan(const okq_paged* c, int layer_count, int n_new, Plan& p) {
       if (few <= decode_clusters(size) && (per_item + DECODE_PIPES * size - 1) / (DECODE_PIPES * size) <= other) p.cluster = size;
     if (p.cluster) p.decode = true;
   }
-  const int per = p.decode ? DECODE_ROWS : PROMPT_ROWS;
-  const double items = p.decode ? few : many;
-  if (items * (double)(per_item + (p.decode ? DECODE_EXTRA : PROMPT_EXTRA)) > 2147483647.0) return false;
-  const long long tiles = (long long)items * per_item;
-  p.grid = (int)(tiles < n ? tiles : n);
-  p.ranges = p.grid * (p.decode ? DECODE_PIPES : 1);
-  p.heads = (size_t)p.ranges * sizeof(Head);   // (the workspace is the line's, whichever it is)
-  p.bytes = p.heads + (size_t)2 * p.ranges * per * (D + 2) * sizeof(float);
+  // blocks, ranges and bytes of the line (the workspace is the line's, cluster or not)
+  auto line = [&](bool decode) {
+    const double items = decode ? few : many;
+    p.grid = (int)(items * (double)per_item < (double)n ? items * (double)per_item : (double)n);
+    p.ranges = p.grid * (decode ? DECODE_PIPES : 1);
+    p.heads = (size_t)p.ranges * sizeof(Head);
+    return p.heads + (size_t)2 * p.ranges * (decode ? DECODE_ROWS : PROMPT_ROWS) * (D + 2) * sizeof(float);
+  };
+  const size_t other = rows > 2 * DECODE_ROWS ? line(!p.decode) : 0, own = line(p.decode);
+  p.bytes = own > other ? own : other;
+  if ((p.decode ? few : many) * (double)(per_item + (p.decode ? DECODE_EXTRA : PROMPT_EXTRA)) > 2147483647.0) return false;
   return true;
 }
 

@@ -110,6 +110,15 @@ def test_other_refusals(L):
     assert L.okq_pages_compact(c, P16 + 2, P16, 1 << 20, None) == B.ERR_ALIGNMENT
 
 
+@pytest.mark.parametrize("shape", [dict(), dict(batch=8, n_kv_heads=4, n_q_heads=28, max_pages=64), dict(n_kv_heads=1, n_q_heads=1, max_pages=3000)])
+def test_scratch_serves_smaller_calls(L, shape):
+    """Sizes grow with layers and queries, whichever kernel takes a call."""
+    for layers in (1, 2):
+        sizes = [L.okq_paged_workspace_bytes(cache(**shape), layers, n) for n in range(0, 300)]
+        assert sizes[0] > 0 and all(a <= b for a, b in zip(sizes, sizes[1:]))
+        assert all(a <= L.okq_paged_workspace_bytes(cache(**shape), 2, n) for n, a in enumerate(sizes))
+
+
 def test_plan_and_debug_refusals(L):
     assert L.okq_debug_paged_plan(cache(), 1, 100) == B.PLAN_PROMPT and L.okq_debug_paged_plan(cache(), 1, 1) != 0
     for c, layers, n in ((cache(dtype=2), 1, 1), (cache(), 0, 1), (cache(), 3, 1), (cache(), 1, 0), (cache(), 1, 1 << 27)):
