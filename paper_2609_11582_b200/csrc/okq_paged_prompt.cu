@@ -116,6 +116,11 @@ __device__ __forceinline__ uint2 codes_to_half(uint32_t w) {
   return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
+// The warps of streams A and B that share a scheduler work out their numerators in turn (both have equally many steps).  Left alone they
+// fall into step, and each waits for the other's exponentials in that stretch and leaves the unit idle in the others.
+__device__ __forceinline__ void take_turn(int id) { asm volatile("bar.sync %0, 64;\n" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void pass_turn(int id) { asm volatile("bar.arrive %0, 64;\n" ::"r"(id) : "memory"); }
+
 // Wait of a warp until both converting warps have done step x, with the limit of every wait.
 __device__ __forceinline__ bool step_ready(PromptSmem& sm, const volatile int* done, int x) {
   const uint32_t at = smem_u32(const_cast<const int*>(done));
@@ -493,6 +498,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     int n_o = 0;
     bool whole = cur.tile == 0, began = cur.tile != 0;
     if (!heads.by_item && tid == 0) a.heads[v].more = 0;
+    if (t) pass_turn(2 + quarter);   // stream A begins
     for (int i = 0; cur.ok;) {
       const int n = cur.piece(), rows = cur.m * c.group - cur.rt * R, item0 = end - cur.left - cur.tile;   // (the item's first unit)
       const bool ends = cur.tile + n == cur.nt, dual = rows <= M;
@@ -544,7 +550,9 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
             }
           }
           const float ref = m == -INFINITY ? 0.f : m;
+          if (!dual) take_turn(2 + 4 * t + quarter);
           l = edge ? numerators<true>(x, p_at, info, 2 * half, back, ref, seen, l) : numerators<false>(x, p_at, info, 2 * half, back, ref, seen, l);
+          if (!dual) pass_turn(2 + 4 * (t ^ 1) + quarter);
           tmem_wait_st();
           before_sync();
           __syncwarp();
@@ -631,6 +639,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       i += n;
       cur.skip(work, n);
     }
+    if (!t) take_turn(2 + quarter);
   }
   before_sync();
   __syncthreads();
