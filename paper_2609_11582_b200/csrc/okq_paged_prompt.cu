@@ -199,6 +199,12 @@ __device__ __forceinline__ float prepare_queries(const AttnArgs& a, const Cursor
   return mine;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+
 // The lane's row of a step's scores, two blocks of 32 tokens, b0 the tile's number of the first; `seen`: last column that the row sees.
 template <bool EDGE>
 __device__ __forceinline__ float row_max(float (&x)[2][32], const Info& info, int b0, float back, int seen) {
@@ -212,8 +218,8 @@ __device__ __forceinline__ float row_max(float (&x)[2][32], const Info& info, in
     }
     float y[4] = {x[b][0], x[b][1], x[b][2], x[b][3]};
 #pragma unroll
-    for (int e = 4; e < 32; e++) y[e & 3] = fmaxf(y[e & 3], x[b][e]);
-    const float top = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+    for (int e = 4; e < 28; e += 2) y[(e >> 1) & 3] = max3(y[(e >> 1) & 3], x[b][e], x[b][e + 1]);
+    const float top = max3(max3(y[0], y[1], x[b][28]), max3(y[2], y[3], x[b][29]), fmaxf(x[b][30], x[b][31]));
     mx = fmaxf(mx, EDGE && top == -INFINITY ? top : top * (back * info.ks[b0 + b]));
   }
   return mx;
