@@ -20,10 +20,11 @@
 // their sums are put together at the end.
 //
 // At best bound by the exponentials (16 per cycle and SM: 2048 cycles for 256 x 128 scores) and the products (2048 cycles at fp16's
-// rate).  What it takes is about 5000 (2048 queries x 28 heads on 8192 tokens 282 us, 750 TFLOP/s of products): a softmax warp's own
-// chain of waits, tensor memory, maximum, exponentials and roundings, with two such warps on a scheduler and 128 registers to each.
+// rate).  What it takes is about 4200 (2048 queries x 28 heads on 8192 tokens 272 us, 775 TFLOP/s of products): a softmax warp's own
+// chain of waits, tensor memory, maximum, exponentials and roundings, with two such warps on a scheduler and 128 registers to each (the
+// maximum beside the exponentials, by last step's reference: 390 us, spills).
 // Few rows (a dual item) are bound by the conversion, a step in 1500 cycles, a third of it waits and fences: 35 rows, 16 sequences x 4
-// heads of up to 12345 tokens 54 us (a converting warp to every other step, with half of those waits but a ring that is then too
+// heads of up to 12345 tokens 53 us (a converting warp to every other step, with half of those waits but a ring that is then too
 // short: 61).
 #include "okq_paged_attn.cuh"
 
@@ -437,7 +438,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     if (n_o > 0 && !mbar_drain(&sm.o_full[t], (uint32_t)(n_o - 1) & 1u)) sm.tmem_busy = 1;
   } else if (warp >= W_CONV) {
     // ------------------------------------------------------------------ codes to fp16: eight lanes to a token, sixteen channels each
-    // Two warps have the keys, two the values; codes are loaded a step ahead.
+    // Two warps have the keys, two the values.  (Loads a step ahead: the moves between the registers cost a draft 5 %, a prompt gains 0.5.)
     // (of eight lanes four have the first 64 channels of token t and four the others of token t ^ 1, so that each store has all banks)
     const int side = (warp - W_CONV) >> 1, who = (warp - W_CONV) & 1, j = lane & 7, tok = ((32 * who + lane) >> 3) ^ (j >> 2);
     const uint32_t at = (uint32_t)((j >> 2) * KV_HALF + tok * 128), a0 = at + (((2 * (j & 3)) ^ tok) << 4), a1 = at + (((2 * (j & 3) + 1) ^ tok) << 4);
@@ -451,18 +452,15 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       return x < end_x;
     };
     auto codes_of = [&](int x) { return sm.code[side][x >> 1 & 1] + ((x & 1) * PH + tok) * D + 16 * j; };
-    uint4 w[8], w_nx[8];
+    uint4 w[8];
     auto fetch = [&](int x, uint4 (&to)[8]) {
       if (!(x & 1)) bar_wait(sm, &sm.code_full[side][x >> 1 & 1], (uint32_t)(x >> 2) & 1u);
 #pragma unroll
       for (int z = 0; z < 8; z++) to[z] = *reinterpret_cast<const uint4*>(codes_of(x) + 8 * z * D);
     };
-    bool more = there(0);
-    if (more) fetch(0, w);
-    for (int x = 0; more; x++) {
+    for (int x = 0; there(x); x++) {
       const int i = x >> 1, half = x & 1, s = x % NR;
-      more = there(x + 1);
-      if (more) fetch(x + 1, w_nx);
+      fetch(x, w);
       if (side && !half) bar_wait(sm, &sm.info_full[i & 3], (uint32_t)(i >> 2) & 1u);
       if (x >= NR) bar_wait(sm, side ? &sm.v_free[s] : &sm.k_free[s], (uint32_t)(x / NR - 1) & 1u);
       unsigned char* to = side ? sm.v[s][0] : sm.k[s][0];
@@ -493,8 +491,6 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
         asm volatile("st.release.cta.shared.s32 [%0], %1;\n" ::"r"(smem_u32(const_cast<const int*>(&sm.done[side][who]))), "r"(x + 1) : "memory");
         if (half) mbar_arrive(&sm.code_free[side][i & 1]);
       }
-#pragma unroll
-      for (int z = 0; z < 8; z++) w[z] = w_nx[z];
     }
   } else {
     // ------------------------------------------------------------------ softmax: lane = row (after a timeout they run on, waits failing at once)
