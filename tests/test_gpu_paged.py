@@ -1,4 +1,6 @@
 """The 8-bit paged cache and the rotary positions on the GPU against the oracle in 64 bits."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -480,6 +482,32 @@ def test_attention_graphs_share_a_workspace(n):
         m.compare(got[i], qs[i].cpu(), n, None, i, None, 0.0)
         B.paged_attention(m.c, i, 1, qs[i], ws, outs[i])
         assert torch.equal(outs[i], got[i])
+
+
+@pytest.mark.parametrize("n", [1, 64])
+def test_a_threads_first_call_may_be_a_captured_one(n):
+    """What the library asks the device about once per thread is asked in a capture here."""
+    m = Model(1, 2, 2, 14, max_pages=6, page=64, dtype=F16)
+    m.append(200, [200, 64])
+    q = randn(m.g, 1, 2, 14, n, D).cuda()
+    want, got = torch.zeros_like(q), torch.zeros_like(q)
+    ws = torch.empty(B.paged_workspace_bytes(m.c, 1, n), dtype=torch.uint8, device="cuda")
+    graph, failed = torch.cuda.CUDAGraph(), []
+
+    def capture():
+        try:
+            with torch.cuda.graph(graph):
+                B.paged_attention(m.c, 0, 1, q, ws, got)
+        except BaseException as e:   # noqa: BLE001
+            failed.append(e)
+    t = threading.Thread(target=capture)
+    t.start()
+    t.join()
+    assert not failed
+    graph.replay()
+    B.paged_attention(m.c, 0, 1, q, ws, want)
+    assert torch.equal(got, want)
+    m.compare(got, q.cpu(), n, None, 0, None, 0.0)
 
 
 def random_cache(g, L, batch, H, Hq, page, dtype, lens):
