@@ -5,9 +5,11 @@
 //   S[row][token] = Q[row][channel] K[token][channel]   the cache's codes are fp16 numbers as they are (|code| <= 127); queries are scaled
 //                                                       to a power of two per row, so that bf16 ones are fp16 numbers too
 //   O[row][channel] += P[row][token] V[token][channel]  P = 2^14 p w in fp16, in place of the scores in tensor memory, with
-//                                                       w = scale_v / (the largest one so far) of the token's block
+//                                                       w = scale_v / (the unit of O) of the token's block
 // and the scales of the blocks enter where they cost nothing: those of the keys in the factor of the exponent, those of the values as
-// log2(w) in its offset; the normaliser takes a block's sum divided by w.
+// log2(w) in its offset; the normaliser takes a block's sum divided by w.  The unit is the largest value scale of a tile, changed (and O
+// multiplied) where a tile's is twice as large, or less than 2^-4 of it: numerators keep their bits whatever was before.  A block with w
+// below 2^-4 has the power of two of it in its codes as fp16 numbers, where it is exact down to 2^-24.
 // The softmax' reference m is set 6 above a row's maximum and moves when the maximum passes it (log2 units): O is multiplied then,
 // by the row's own threads (3 above: every other step of a drifting sequence).  A numerator keeps fp16's 11 bits down to 2^-22 of the
 // largest.
@@ -41,15 +43,17 @@ constexpr int W_CONV = 8, W_MMA = 12, W_LOAD = 14;   // (an MMA warp to each str
 constexpr int NT = 15 * 32;
 constexpr uint32_t S_COL = 0, O_COL = 256;      // + 128 per stream, + 64 per place for scores; numerators lie on its first half
 constexpr size_t SLOT = (size_t)R * (D + 2);
-constexpr float P_SHIFT = 14.f, LEAD = 6.f, LEAST_W = 5.9604645e-8f;   // 2^-24
+constexpr float P_SHIFT = 14.f, LEAD = 6.f;
+constexpr float NEAR = 0.0625f;                 // w and units down to 2^-4 are left as they are
+constexpr float LEAST = 9.0949470e-13f;         // 2^-40: the unit stays above so much of the item's largest (O could overflow otherwise)
 
 struct Info {            // of a tile, by block
   float ks[4];           // key scales
-  float lw[4];           // log2 of w, and the shift
-  float iw[4];           // 2^-14 / w
-  float mul[4];          // what codes are multiplied by: 1, less where w is below 2^-24, 0 for scales of 0 and NaN
-  float vref;            // the largest value scale so far, up to a factor of 2
-  float fv;              // what the sums are multiplied by where it has changed, 1 otherwise
+  float mul[4];          // the part of w that codes are multiplied by: 1, a power of two below 2^-4, 0 for scales of 0 and NaN
+  float lw[4];           // log2 of the rest of w, and the shift
+  float iw[4];           // 2^-14 / the rest of w
+  float vref;            // the unit of the sums
+  float fv;              // what they are multiplied by where it has changed, 1 otherwise
   int lost;              // blocks whose value scale is NaN, a bit for each
   int plain;             // all of mul are 1
 };
@@ -323,7 +327,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       }
     };
     int armed[2] = {0, 0};
-    float vref = 0.f;
+    float vref = 0.f, vtop = 0.f;                // the unit of the sums, 0 while they are zeros; the item's largest
     bool out = a.withhold != 0;
     entries();
     scales();
@@ -357,17 +361,24 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
       big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
       float fv = 1.f;
-      if (first) vref = big > 0.f ? big : 1.f;
-      else if (big >= 2.f * vref) { fv = vref / big; vref = big; }
-      const float w = vs / vref, wu = fmaxf(w, LEAST_W);      // (fmaxf: NaN gives the least)
+      if (first) vref = vtop = 0.f;
+      if (big >= 2.f * vref || (big > 0.f && big < NEAR * vref)) {
+        vtop = fmaxf(vtop, big);
+        const float to = fmaxf(big, LEAST * vtop);
+        if (vref > 0.f) fv = vref / to;
+        vref = to;
+      }
       Info& info = sm.info[i & 3];
+      const bool none = !(vs > 0.f);               // (NaN too)
+      const float w = none ? 1.f : vs / vref, mul = w < NEAR ? __uint_as_float(max(__float_as_uint(w) & 0x7f800000u, 103u << 23)) : 1.f;   // 2^-24 at least
+      const float rest = fmaxf(w / mul, NEAR);
       if (lane < 4) {
         info.ks[lane] = ks;
-        info.lw[lane] = log2f(wu) + P_SHIFT;
-        info.iw[lane] = 1.f / (wu * 16384.f);
-        info.mul[lane] = vs != vs ? 0.f : w < LEAST_W ? w / LEAST_W : 1.f;
+        info.mul[lane] = none || w < NEAR * mul ? 0.f : mul;   // (values 2^-28 below the tile's largest are lost)
+        info.lw[lane] = log2f(rest) + P_SHIFT;
+        info.iw[lane] = 1.f / (rest * 16384.f);
       }
-      const unsigned lost = __ballot_sync(0xffffffffu, lane < 4 && vs != vs), small = __ballot_sync(0xffffffffu, lane < 4 && !(w >= LEAST_W));
+      const unsigned lost = __ballot_sync(0xffffffffu, lane < 4 && vs != vs), small = __ballot_sync(0xffffffffu, lane < 4 && (none || w < NEAR));
       if (lane == 0) { info.vref = vref; info.fv = fv; info.lost = (int)lost; info.plain = small == 0; }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.info_full[i & 3]);

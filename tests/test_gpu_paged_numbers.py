@@ -1,0 +1,140 @@
+"""The 8-bit paged cache's attention where a number could lose its bits: values of very different sizes.  Against softmax attention in 64
+bits, each kernel by its own bound."""
+import pytest
+import torch
+
+from paper_2609_11582_b200 import binding as B
+from tests.test_gpu_paged import BF16, BLOCK, D, F16, gen
+
+pytestmark = pytest.mark.gpu
+TILE = 128
+
+
+def kernel_bound(w, v, ref, amax, top, dtype, plan):
+    """What rows of an output may be off by; w [.., rows, tokens] their weights, v [.., tokens, 128] the tokens' values, amax [.., tokens] the largest
+    magnitude of a token's block (127 times its scale), top [.., rows] a row's largest |score|.
+    Scores carry three roundings of fp32 and the exponent one more, in a numerator and in the sum: 8 * 2^-24 |s|; exponentials, factors and
+    sums at most 32 * 2^-24.  Of that the weighted magnitudes sum w |v|.
+    Decode kernel: a tile's numerators, weight times scale, are whole multiples of 2^-30 of the largest of its 128 or less; half of that
+    times a code of 127 for each of 128 tokens: 2^-24 of the largest w * amax of the tile.
+    Prompt kernel: fp16, half a step is 2^-12, and twice that with the sums that round towards it; below fp16's normal numbers half a step of
+    2^-24, where the largest of a step's 64 numerators is 2^-4 at least: 64 * 2^-21 = 2^-15 of the largest w * amax of the step."""
+    mag = w @ v.abs()
+    step, part = (TILE // 2, 2.0 ** -15) if plan == B.PLAN_PROMPT else (TILE, 2.0 ** -24)
+    most = sum(x.amax(-1) for x in (w * amax[..., None, :]).split(step, -1))
+    err = (2.0 ** -24 * (8 * top[..., None] + 32) + (2.0 ** -11 if plan == B.PLAN_PROMPT else 0)) * mag + part * most[..., None]
+    return err + torch.finfo(dtype).eps / 2 * (ref.abs() + err) + (2.0 ** -25 if dtype == F16 else 1e-38)
+
+
+class Store:
+    """A cache of one layer that holds given keys and values [batch, H, tokens, 128] (fp32, on the GPU), quantised here."""
+
+    def __init__(self, k, v, Hq, wide, dtype=BF16, page=64, seed=0):
+        batch, H, T, _ = k.shape
+        self.T, self.H, self.Hq, self.dtype = T, H, Hq, dtype
+        width = (T + page - 1) // page
+        c = self.c = B.PagedCache(1, batch, H, Hq, batch * width + 2, (1 << 19) // page if wide else width, page, dtype)
+        table = torch.randperm(batch * width + 2, generator=gen(seed))[:batch * width].view(batch, width).cuda()
+        c.table[:, :width] = table.int()
+        c.seq_len.fill_(T)
+        x = torch.zeros(batch, H, 2, width * page, D, device="cuda")
+        x[:, :, 0, :T], x[:, :, 1, :T] = k, v
+        x = x.unflatten(3, (width, page // BLOCK, BLOCK))                       # [batch, H, 2, width, blocks, 32, 128]
+        scales = x.abs().amax((-1, -2)) / 127
+        codes = (x / torch.where(scales > 0, scales, 1.0)[..., None, None]).round().clamp(-127, 127)
+        c.codes[0, table] = codes.permute(0, 3, 1, 2, 4, 5, 6).flatten(4, 5).to(torch.int8)
+        c.scales[0, table] = scales.permute(0, 3, 1, 2, 4)
+        self.held = (codes.double() * scales.double()[..., None, None]).flatten(3, 5)[..., :T, :]
+        self.amax = (scales.double() * 127).repeat_interleave(BLOCK, -1).flatten(3, 4)[:, :, 1, :T]
+
+    def attend(self, q, sm_scale=None):
+        """One call, each row against its kernel's bound.  q [1, batch, Hq, n, 128]."""
+        n, G, scale = q.shape[3], self.Hq // self.H, D ** -0.5 if sm_scale is None else sm_scale
+        plan, q = B.paged_plan(self.c, 1, n), q.cuda()
+        out = torch.full_like(q, 7.0)
+        ws = torch.empty(B.paged_workspace_bytes(self.c, 1, n), dtype=torch.uint8, device="cuda")
+        B.paged_attention(self.c, 0, 1, q, ws, out, sm_scale=sm_scale)
+        late = torch.arange(self.T, device="cuda") > (self.T - n + torch.arange(n, device="cuda"))[:, None]
+        for b in range(q.shape[1]):
+            k, v = self.held[b, :, 0], self.held[b, :, 1]                       # [H, T, 128]
+            s = torch.einsum("hgnd,htd->hgnt", q[0, b].double().unflatten(0, (self.H, G)), k) * scale
+            top = s.masked_fill(late, 0.0).abs().amax(-1).flatten(1)
+            w = torch.softmax(s.masked_fill(late, -torch.inf), -1).nan_to_num(0.0).flatten(1, 2)
+            ref, got = w @ v, out[0, b].double().unflatten(0, (self.H, G)).flatten(1, 2)
+            limit = kernel_bound(w, v, ref, self.amax[b], top, self.dtype, plan)
+            assert ((got - ref).abs() <= limit).all(), (b, plan, ((got - ref).abs() / limit).max().item())
+        assert self.c.device_status() == 0
+        return plan
+
+
+# (queries, batch, KV heads, query heads, tokens, wide table), so that a range of tiles has several: the prompt kernel with two streams of rows, with
+# both streams on the same rows, and a few long items; the decode kernel's line, and its clusters
+PROMPT = [(150, 6, 8, 16, 2500, True), (20, 12, 8, 16, 2500, True), (5, 1, 2, 16, 60000, True)]
+LINE = [(1, 24, 8, 56, 2500, True), (3, 24, 8, 40, 2500, True)]
+CLUSTER = [(1, 1, 3, 21, 8000, False), (8, 1, 1, 2, 8000, False)]
+DECODE = LINE + CLUSTER
+ALL = PROMPT + DECODE
+
+
+def steered(n, batch, H, Hq, T, wide, seed=0, spread=1.0):
+    """Queries whose first channel is 16 in all rows, keys whose first channel is 0: a key with x there scores 1.414 x more."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    q, k, v = (torch.randn(*s, D, generator=g, device="cuda") for s in ((1, batch, Hq, n), (batch, H, T), (batch, H, T)))
+    q *= spread
+    q[..., 0], k[..., 0] = 16.0, 0.0
+    return q.to(BF16), k, v * 0.3
+
+
+def lift(natural):
+    return natural / (16.0 * D ** -0.5)
+
+
+def test_shapes_reach_their_kernels():
+    for shapes, want in ((PROMPT, lambda p: p == B.PLAN_PROMPT), (LINE, lambda p: p == B.PLAN_LINE), (CLUSTER, lambda p: p > 0)):
+        for n, batch, H, Hq, T, wide in shapes:
+            assert want(B.paged_plan(B.PagedCache(1, batch, H, Hq, 8, (1 << 13) if wide else (T + 63) // 64), 1, n)), (n, batch, H, Hq, T, wide)
+
+
+@pytest.mark.parametrize("size", [1e-4, 1e-6, 1e-9, 1e-20])
+@pytest.mark.parametrize("zeros", [128, 300, 1000])
+@pytest.mark.parametrize("shape", ALL, ids=str)
+def test_small_values_behind_zeros(shape, zeros, size):
+    """Tokens without any value first, as padding has it, then values far below 1."""
+    q, k, v = steered(*shape, seed=1)
+    v *= size
+    v[..., :zeros, :] = 0
+    Store(k, v, shape[3], shape[5]).attend(q)
+
+
+@pytest.mark.parametrize("size", [1e4, 1e9])
+@pytest.mark.parametrize("at", [0, 1280])
+@pytest.mark.parametrize("shape", ALL, ids=str)
+def test_large_values_without_weight(shape, at, size):
+    """A tile of huge values whose tokens nobody looks at, first or in the middle."""
+    q, k, v = steered(*shape, seed=2, spread=2.0)
+    v[..., at:at + 128, :] *= size
+    k[..., at:at + 128, 0] = lift(-90.0)
+    Store(k, v, shape[3], shape[5]).attend(q)
+
+
+@pytest.mark.parametrize("fall", [1])
+@pytest.mark.parametrize("shape", ALL, ids=str)
+def test_values_of_all_sizes(shape, fall):
+    """Values that fall, or rise, by 2^40 over the sequence, while the scores do the opposite."""
+    q, k, v = steered(*shape, seed=9)
+    t = torch.arange(shape[4], device="cuda") / shape[4]
+    v *= torch.exp2(-40.0 * fall * t)[:, None]
+    k[..., 0] = lift(40.0 * 0.6931) * fall * t
+    Store(k, v, shape[3], shape[5]).attend(q)
+
+
+@pytest.mark.parametrize("size", [2.0 ** -7, 2.0 ** -20])
+@pytest.mark.parametrize("shape", PROMPT, ids=str)
+def test_small_values_in_the_tiles_of_large_ones(shape, size):
+    """Every other block of 32 tokens has values far below its neighbours', and all of the weight."""
+    q, k, v = steered(*shape, seed=3, spread=2.0)
+    large = torch.arange(shape[4], device="cuda") // BLOCK % 2 == 0
+    v[..., ~large, :] *= size
+    k[..., large, 0] = lift(-90.0)
+    Store(k, v, shape[3], shape[5]).attend(q)
