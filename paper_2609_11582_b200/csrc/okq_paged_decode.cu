@@ -137,7 +137,7 @@ __device__ __forceinline__ void prepare_queries(const AttnArgs& a, const Cursor<
     // fixed point: 127 * 2^16 for the largest; numbers too small for a quotient (and infinities, NaN) have limbs of 0
     const float big = __uint_as_float(mx);
     const bool fine = mx < 0x7f800000u && big > 1e-30f;
-    const float f = fine ? __fdividef(127.f * 65536.f, big) : 0.f;   // (two units off at most, the same for all of the row's numbers)
+    const float f = fine ? __fdiv_rn(127.f * 65536.f, big) : 0.f;   // (__fdividef gives 0 for divisors above 2^126, which bf16 has)
     // signed digits to the base 256: with 128 added to each, the bytes of one sum
     uint32_t u[4];
 #pragma unroll

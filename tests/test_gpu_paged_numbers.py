@@ -1,5 +1,6 @@
-"""The 8-bit paged cache's attention where a number could lose its bits: values of very different sizes.  Against softmax attention in 64
-bits, each kernel by its own bound."""
+"""The 8-bit paged cache's attention where a number could lose its bits: values of very different sizes, queries at the end of their type's
+range.  Against softmax attention in 64 bits, each kernel by its own bound."""
+import numpy as np
 import pytest
 import torch
 
@@ -138,3 +139,12 @@ def test_small_values_in_the_tiles_of_large_ones(shape, size):
     v[..., ~large, :] *= size
     k[..., large, 0] = lift(-90.0)
     Store(k, v, shape[3], shape[5]).attend(q)
+
+
+@pytest.mark.parametrize("largest", [5e37, 1e38, 3e38, float(torch.finfo(BF16).max)])
+@pytest.mark.parametrize("shape", ALL, ids=str)
+def test_queries_at_the_end_of_their_range(shape, largest):
+    q, k, v = steered(*shape, seed=6)
+    q = (q.float() / q.float().abs().amax(-1, keepdim=True) * largest).to(BF16)
+    assert q.isfinite().all()
+    Store(k * 2.0 ** -60, v, shape[3], shape[5]).attend(q, sm_scale=float(np.float32(2.0 ** 61 / largest)))
