@@ -7,7 +7,9 @@
 //   values   O[channel][row] = V[token][channel] P[token][row]: A = the tile transposed by its descriptor (MN-major), B = the numerators
 //            p * scale_v as the four bytes of a 32-bit fixed-point number, exact sums in int32
 // so nothing is unpacked: a tile goes from memory to shared memory by TMA and from there into the tensor cores.  Fixed point is
-// relative to the largest numerator so far; what lies more than 2^-32 below it is lost, fp32 would keep 2^-24 of each.
+// relative to the row's largest p * scale_v in the tile (up to a factor of 4): the power of two R next above the largest log2 of p and
+// scale is taken off in the exponent and put back, with the running maximum, in the factor of the tile's sums.  What lies more than 2^-30
+// below the largest of the same tile is lost, whatever other tiles hold; fp32 would keep 2^-24 of each.
 //
 // A block has three pipelines, each with a range of tiles and a ring of two of its own, so that one tile's chain of products, softmax
 // and products hides behind those of the others.  A pipeline is a service warp (copies of 32-token blocks by page, products) and four
@@ -44,7 +46,7 @@ struct PipeSync {
   __align__(16) float wmax[2][4][R];
   __align__(16) float qscale[R];
   __align__(16) float sum[4][R];             // an item's normalisers, by worker warp
-  float scale[NS][8];                        // of the tile's four blocks: keys, values
+  __align__(16) float scale[NS][12];         // of the tile's four blocks: keys; values as a fraction of [1/2, 1), 2^32 times, and its exponent
   __align__(8) unsigned long long full[NS], s_full, p_full, o_full, q_full;
 };
 struct DecodeSmem {
@@ -273,7 +275,13 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
                        ::"r"(smem_u32(side ? pipe.v[s] : pipe.k[s]) + j * PB * D), "l"(reinterpret_cast<uint64_t>(&map)), "r"(0),
                          "r"(now.row + side * c.page), "r"(bar) : "memory");
       }
-      if (mine) { sy.scale[s][lane & 3] = now.ks; sy.scale[s][4 + (lane & 3)] = now.vs; }   // (may still be on their way: behind the copies)
+      if (mine) {   // (may still be on their way: behind the copies)
+        int e;
+        const float m = frexpf(now.vs, &e);
+        sy.scale[s][lane & 3] = now.ks;
+        sy.scale[s][4 + (lane & 3)] = m * 4294967296.f;
+        sy.scale[s][8 + (lane & 3)] = m > 0.f && m < 1.f ? (float)e : -INFINITY;
+      }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sy.full[s]);
       if (k == 4) scales();
@@ -331,11 +339,12 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     // ------------------------------------------------------------------ workers (after a timeout they run on, waits failing at once)
     const uint32_t lanes = (uint32_t)(32 * role) << 16;
     const int ch = 32 * role + lane;
-    float top[R], sum[R], o[R];   // (the rows' scales are read again with every tile: with them the state does not fit 128 registers)
+    const int rl = lane & (R - 1);   // the lane's own row, whose running maximum and factors it works out for all
+    float top = -INFINITY, sum[R], o[R];
     bool fresh = true, whole = cur.tile == 0, began = cur.tile != 0;   // the piece has its item's first tile; the item began in an earlier range
     if (CLUSTER) {
 #pragma unroll
-      for (int r = 0; r < R; r++) { top[r] = -INFINITY; sum[r] = o[r] = 0.f; }
+      for (int r = 0; r < R; r++) sum[r] = o[r] = 0.f;
     }
     if (!CLUSTER && !heads.by_item && tid == g * 128) a.heads[v].more = 0;
     for (int i = 0; cur.ok; i++) {
@@ -373,14 +382,16 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         asm volatile("bar.sync %0, 128;\n" ::"r"(1 + g) : "memory");
         if (lane == 0) mbar_arrive(&sy.q_full);
 #pragma unroll
-        for (int r = 0; r < R; r++) { top[r] = -INFINITY; sum[r] = o[r] = 0.f; }
+        for (int r = 0; r < R; r++) sum[r] = o[r] = 0.f;
+        top = -INFINITY;
       }
       cur.next(work);
       const bool last = cur.ended || !cur.ok;
       bar_wait(sm, &sy.full[s], (uint32_t)(i / NS) & 1u);   // (long complete: for the loader's scales)
-      // scales of this warp's block of 32 tokens; the largest value scale of the tile
-      const float ks = sy.scale[s][role], vs = sy.scale[s][4 + role];
-      const float vref = fmaxf(fmaxf(sy.scale[s][4], sy.scale[s][5]), fmaxf(sy.scale[s][6], sy.scale[s][7]));
+      // scales of this warp's block of 32 tokens; exponents of the tile's value scales
+      const float ks = sy.scale[s][role], frac = sy.scale[s][4 + role], exp_own = sy.scale[s][8 + role];
+      const float4 ev = *reinterpret_cast<const float4*>(&sy.scale[s][8]);
+      const bool lost = !(frac <= 4294967296.f);
       bar_wait(sm, &sy.s_full, (uint32_t)i & 1u);
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
       float x[R];
@@ -409,32 +420,28 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         }
       }
       asm volatile("bar.sync %0, 128;\n" ::"r"(1 + g) : "memory");
-      bool moved = false;
-      float mn[R];
-#pragma unroll
-      for (int r = 0; r < R; r++) {
-        mn[r] = fmaxf(fmaxf(fmaxf(sy.wmax[b][0][r], sy.wmax[b][1][r]), fmaxf(sy.wmax[b][2][r], sy.wmax[b][3][r])), top[r]);
-        moved |= mn[r] > top[r];
-      }
-      if (moved) {   // (the same in all of the pipeline's workers)
+      const float w0 = sy.wmax[b][0][rl], w1 = sy.wmax[b][1][rl], w2 = sy.wmax[b][2][rl], w3 = sy.wmax[b][3][rl];
+      const float mn = fmaxf(fmaxf(fmaxf(w0, w1), fmaxf(w2, w3)), top);
+      const float level = fmaxf(ceilf(fmaxf(fmaxf(w0 + ev.x, w1 + ev.y), fmaxf(w2 + ev.z, w3 + ev.w))), -3e38f);   // R
+      if (__any_sync(0xffffffffu, mn > top)) {   // (the same in all of the pipeline's workers)
+        const float keep = mn > top ? ex2(top - mn) : 1.f;
 #pragma unroll
         for (int r = 0; r < R; r++) {
-          if (mn[r] > top[r]) {
-            const float keep = ex2(top[r] - mn[r]);
-            sum[r] *= keep;
-            o[r] *= keep;
-            top[r] = mn[r];
-          }
+          const float f = __shfl_sync(0xffffffffu, keep, r);
+          sum[r] *= f;
+          o[r] *= f;
         }
+        top = mn;
       }
-      const float ratio = vref > 0.f ? vs / vref * 4294967040.f : 0.f;   // (largest fp32 number below 2^32)
+      const float t = top == -INFINITY ? 0.f : top;
       uint32_t u[R];
 #pragma unroll
       for (int r = 0; r < R; r++) {
-        const float p = ex2(x[r] - (top[r] == -INFINITY ? 0.f : top[r]));
+        const float p = ex2(x[r] - __shfl_sync(0xffffffffu, t, r));
         // a NaN scale of the values reaches the rows that see one of its tokens through their sum
-        sum[r] += vs != vs && x[r] != -INFINITY ? NAN : p;
-        u[r] = __float2uint_rn(p * ratio);
+        sum[r] += lost && x[r] != -INFINITY ? NAN : p;
+        // (R and the exponent are whole numbers: their difference is exact)
+        u[r] = __float2uint_rn(ex2(x[r] + (exp_own - __shfl_sync(0xffffffffu, level, r))) * frac);
       }
 #pragma unroll
       for (int half = 0; half < 2; half++)
@@ -444,8 +451,9 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       __syncwarp();
       if (lane == 0) mbar_arrive(&sy.p_full);
 
+      // what a row's sums are worth, 2^(R - top) (in two factors, so that neither exponent is rounded)
+      const float unit = ex2(rintf(t) - t) * ex2(level - rintf(t));
       // the tile's sums: lane = channel
-      const float unit = vref > 0.f ? vref * (1.f / 4294967040.f) : 0.f;
       bar_wait(sm, &sy.o_full, (uint32_t)i & 1u);
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
       {
@@ -456,7 +464,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
 #pragma unroll
         for (int r = 0; r < R; r++) {
           const int* d = &y[r >> 1][4 * (r & 1)];
-          o[r] = fmaf(fmaf((float)(d[3] * 256 + d[2]), 65536.f, (float)(d[1] * 256 + d[0])), unit, o[r]);
+          const float y2 = fmaf((float)(d[3] * 256 + d[2]), 1.52587890625e-5f, (float)(d[1] * 256 + d[0]) * 2.3283064365386963e-10f);   // 2^-16, 2^-32
+          o[r] = fmaf(y2, __shfl_sync(0xffffffffu, unit, r), o[r]);
         }
       }
       fresh = last;
@@ -475,7 +484,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
             if (r < rows) out_row<T>(a, li, bq, h, R * rt + r)[ch] = from_f<T>(l == 0.f ? 0.f : o[r] / l);
           } else {
             slot[r * D + ch] = o[r];
-            if (ch == r) { slot[R * D + r] = top[r]; slot[R * D + R + r] = l; }
+            if (ch == r) { slot[R * D + r] = top; slot[R * D + R + r] = l; }
           }
         }
         whole = true;
@@ -491,7 +500,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         part[r * D + ch] = o[r];
         if (ch == r) {
           const float l = (sy.sum[0][r] + sy.sum[1][r]) + (sy.sum[2][r] + sy.sum[3][r]);
-          part[R * D + r] = top[r];
+          part[R * D + r] = top;
           part[R * D + R + r] = sm.abort ? NAN : l;
         }
       }

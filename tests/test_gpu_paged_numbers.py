@@ -1,5 +1,5 @@
-"""The 8-bit paged cache's attention where a number could lose its bits: values of very different sizes, queries at the end of their type's
-range.  Against softmax attention in 64 bits, each kernel by its own bound."""
+"""The 8-bit paged cache's attention where a number could lose its bits: values of very different sizes, tokens that take nearly all of the weight,
+queries at the end of their type's range.  Against softmax attention in 64 bits, each kernel by its own bound."""
 import numpy as np
 import pytest
 import torch
@@ -119,8 +119,7 @@ def test_large_values_without_weight(shape, at, size):
     Store(k, v, shape[3], shape[5]).attend(q)
 
 
-@pytest.mark.parametrize("fall", [1])
-@pytest.mark.parametrize("shape", ALL, ids=str)
+@pytest.mark.parametrize("shape,fall", [(s, f) for s in ALL for f in (1, -1) if f > 0 or s in DECODE], ids=str)
 def test_values_of_all_sizes(shape, fall):
     """Values that fall, or rise, by 2^40 over the sequence, while the scores do the opposite."""
     q, k, v = steered(*shape, seed=9)
@@ -131,7 +130,7 @@ def test_values_of_all_sizes(shape, fall):
 
 
 @pytest.mark.parametrize("size", [2.0 ** -7, 2.0 ** -20])
-@pytest.mark.parametrize("shape", PROMPT, ids=str)
+@pytest.mark.parametrize("shape", ALL, ids=str)
 def test_small_values_in_the_tiles_of_large_ones(shape, size):
     """Every other block of 32 tokens has values far below its neighbours', and all of the weight."""
     q, k, v = steered(*shape, seed=3, spread=2.0)
@@ -148,3 +147,25 @@ def test_queries_at_the_end_of_their_range(shape, largest):
     q = (q.float() / q.float().abs().amax(-1, keepdim=True) * largest).to(BF16)
     assert q.isfinite().all()
     Store(k * 2.0 ** -60, v, shape[3], shape[5]).attend(q, sm_scale=float(np.float32(2.0 ** 61 / largest)))
+
+
+@pytest.mark.parametrize("above", [8.0, 16.0, 20.0, 26.0])
+@pytest.mark.parametrize("at", [0, 700, 2200])
+@pytest.mark.parametrize("shape", DECODE, ids=str)
+def test_sinks(shape, at, above):
+    """A token far above the rest without any value, in a tile of small values: the others' numerators keep their bits."""
+    q, k, v = steered(*shape, seed=4)
+    first = at - at % TILE
+    v[..., first:first + TILE, :] *= 2.0 ** -30
+    v[..., at, :] = 0
+    k[..., at, 0] = lift(above)
+    Store(k, v, shape[3], shape[5]).attend(q)
+
+
+@pytest.mark.parametrize("shape", ALL, ids=str)
+def test_sinks_of_all_heights(shape):
+    """Several of them, up and down: nothing overflows."""
+    q, k, v = steered(*shape, seed=5)
+    for at, above in ((0, 30.0), (300, 60.0), (640, 20.0), (900, 85.0), (1500, 10.0), (2000, 90.0)):
+        k[..., at, 0] = lift(above)
+    Store(k, v, shape[3], shape[5]).attend(q)
