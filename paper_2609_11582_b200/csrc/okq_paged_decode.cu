@@ -451,8 +451,12 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       __syncwarp();
       if (lane == 0) mbar_arrive(&sy.p_full);
 
-      // what a row's sums are worth, 2^(R - top) (in two factors, so that neither exponent is rounded)
-      const float unit = ex2(rintf(t) - t) * ex2(level - rintf(t));
+      // what a row's sums are worth, 2^(R - top) (in two factors, so that neither exponent is rounded), times 2^60 where that is a number in
+      // all rows: small weights of small values would be below fp32's range, and zeros
+      const float whole_t = rintf(t);
+      const bool large = __any_sync(0xffffffffu, level - whole_t > 60.f);
+      const float unit = ex2(whole_t - t) * ex2(large ? level - whole_t : level - whole_t + 60.f);
+      const float part_hi = large ? 1.52587890625e-5f : 1.3234889800848443e-23f, part_lo = large ? 2.3283064365386963e-10f : 2.0194839173657902e-28f;   // 2^-16, 2^-32, and those times 2^-60
       // the tile's sums: lane = channel
       bar_wait(sm, &sy.o_full, (uint32_t)i & 1u);
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
@@ -464,7 +468,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
 #pragma unroll
         for (int r = 0; r < R; r++) {
           const int* d = &y[r >> 1][4 * (r & 1)];
-          const float y2 = fmaf((float)(d[3] * 256 + d[2]), 1.52587890625e-5f, (float)(d[1] * 256 + d[0]) * 2.3283064365386963e-10f);   // 2^-16, 2^-32
+          const float y2 = fmaf((float)(d[3] * 256 + d[2]), part_hi, (float)(d[1] * 256 + d[0]) * part_lo);
           o[r] = fmaf(y2, __shfl_sync(0xffffffffu, unit, r), o[r]);
         }
       }

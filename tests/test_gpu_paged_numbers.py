@@ -169,3 +169,27 @@ def test_sinks_of_all_heights(shape):
     for at, above in ((0, 30.0), (300, 60.0), (640, 20.0), (900, 85.0), (1500, 10.0), (2000, 90.0)):
         k[..., at, 0] = lift(above)
     Store(k, v, shape[3], shape[5]).attend(q)
+
+
+@pytest.mark.parametrize("size", [1e-8, 1e-20, 1e-30])
+@pytest.mark.parametrize("above", [20.0, 40.0])
+@pytest.mark.parametrize("shape", DECODE, ids=str)
+def test_small_values_behind_sinks(shape, above, size):
+    """Both at once: sums that have grown large by the one, and are to be brought down by the other."""
+    q, k, v = steered(*shape, seed=10)
+    v *= size
+    v[..., :TILE, :] = 0
+    k[..., 5, 0] = lift(above)
+    Store(k, v, shape[3], shape[5]).attend(q)
+
+
+@pytest.mark.parametrize("rise", [0.0, 60.0, 110.0])
+@pytest.mark.parametrize("shape", DECODE, ids=str)
+def test_scores_fall_without_end(shape, rise):
+    """Scores that fall by 2^200 over the sequence, step by step, and values that rise: the first tokens have all of the weight, and the sums
+    of the last ones overflow nothing."""
+    q, k, v = steered(*shape, seed=11)
+    t = torch.arange(shape[4], device="cuda") / shape[4]
+    v *= torch.exp2(rise * t)[:, None]
+    k[..., 0] = lift(200.0 * 0.6931) * (1 - t)
+    Store(k, v, shape[3], shape[5]).attend(q)
