@@ -8,11 +8,13 @@
 //                                                       w = scale_v / (the unit of O) of the token's block
 // and the scales of the blocks enter where they cost nothing: those of the keys in the factor of the exponent, those of the values as
 // log2(w) in its offset; the normaliser takes a block's sum divided by w.  The unit is the largest value scale of a tile, changed (and O
-// multiplied) where a tile's is twice as large, or less than 2^-4 of it: numerators keep their bits whatever was before.  A block with w
-// below 2^-4 has the power of two of it in its codes as fp16 numbers, where it is exact down to 2^-24.
-// The softmax' reference m is set 6 above a row's maximum and moves when the maximum passes it (log2 units): O is multiplied then,
-// by the row's own threads (3 above: every other step of a drifting sequence).  A numerator keeps fp16's 11 bits down to 2^-22 of the
-// largest.
+// multiplied) where a tile's is twice as large, or less than 2^-2 of it: numerators keep their bits whatever was before.  A block with w
+// below 2^-2 has the power of two of it in its codes as fp16 numbers, where it is exact down to 2^-24.
+// The softmax' reference m is set 6 above a row's maximum and moves when a step's maximum passes it (log2 units): O is multiplied then,
+// by the row's own threads (3 above: every other step of a drifting sequence).  It moves down, too, to 6 above the maximum of a step that
+// lies 20 below it or more (14: three times as many multiplications where scores spread by 3, 306 us and not 284): sums in fp32 have
+// room for that, numerators in fp16 have not.  So the largest numerator of a step is 2^-8 or more, w included; 11 bits down to 2^-14, below
+// that rounded to 2^-24.
 //
 // A block of threads has 256 rows, in two streams A and B of 128, and walks the tokens in steps of 64: a loader warp (32-token blocks
 // by page, two tiles of 128 tokens ahead), four warps that turn codes into fp16 (0x6400 | (code + 128) is 1024 + 128 + code; the rest is
@@ -43,13 +45,16 @@ constexpr int W_CONV = 8, W_MMA = 12, W_LOAD = 14;   // (an MMA warp to each str
 constexpr int NT = 15 * 32;
 constexpr uint32_t S_COL = 0, O_COL = 256;      // + 128 per stream, + 64 per place for scores; numerators lie on its first half
 constexpr size_t SLOT = (size_t)R * (D + 2);
-constexpr float P_SHIFT = 14.f, LEAD = 6.f;
-constexpr float NEAR = 0.0625f;                 // w and units down to 2^-4 are left as they are
-constexpr float LEAST = 9.0949470e-13f;         // 2^-40: the unit stays above so much of the item's largest (O could overflow otherwise)
+constexpr float P_SHIFT = 14.f, LEAD = 6.f, DROP = 20.f;
+// The reference falls by 2^FALL at a time, while the normaliser is below 2^20: with the factor of the unit (LEAST), 127 * 2^15 and as many
+// tokens O stays below 2^126.  So weights of 2^-FALL of the largest, and smaller, may lose bits to it.
+constexpr float FALL = 64.f, MOST_L = 1048576.f;
+constexpr float NEAR = 0.25f;                   // w and units down to 2^-2 are left as they are
+constexpr float LEAST = 1.5258789e-5f;          // 2^-16: the unit stays above so much of the item's largest (O could overflow otherwise)
 
 struct Info {            // of a tile, by block
   float ks[4];           // key scales
-  float mul[4];          // the part of w that codes are multiplied by: 1, a power of two below 2^-4, 0 for scales of 0 and NaN
+  float mul[4];          // the part of w that codes are multiplied by: 1, a power of two below 2^-2, 0 for scales of 0 and NaN
   float lw[4];           // log2 of the rest of w, and the shift
   float iw[4];           // 2^-14 / the rest of w
   float vref;            // the unit of the sums
@@ -374,7 +379,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       const float rest = fmaxf(w / mul, NEAR);
       if (lane < 4) {
         info.ks[lane] = ks;
-        info.mul[lane] = none || w < NEAR * mul ? 0.f : mul;   // (values 2^-28 below the tile's largest are lost)
+        info.mul[lane] = none || w < NEAR * mul ? 0.f : mul;   // (values 2^-26 below the tile's largest are lost)
         info.lw[lane] = log2f(rest) + P_SHIFT;
         info.iw[lane] = 1.f / (rest * 16384.f);
       }
@@ -543,9 +548,10 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
           const float mx = edge ? row_max<true>(x, info, 2 * half, back, seen) : row_max<false>(x, info, 2 * half, back, seen);
           // a new reference: the row's sums so far are multiplied, once their last product is through
           const float fv = dual || !half ? info.fv : 1.f;
-          const bool passed = mx > m;
-          if (__any_sync(0xffffffffu, passed) || (fv != 1.f && y > 0)) {
-            const float mn = passed ? mx + LEAD : m, f = passed ? ex2(m - mn) : 1.f;   // (0 for the first)
+          const float below = m - mx;   // (-inf for the first; inf or NaN for steps that the row does not see)
+          if (__any_sync(0xffffffffu, fabsf(below - DROP / 2) > DROP / 2 && below < FALL + LEAD) || (fv != 1.f && y > 0)) {
+            const bool moves = below < 0.f || (below > DROP && below < FALL + LEAD && l < MOST_L);
+            const float mn = moves ? mx + LEAD : m, f = moves ? ex2(m - mn) : 1.f;   // (0 for the first)
             m = mn;
             l *= f;
             if (y > 0) {
@@ -604,10 +610,20 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       after_sync();
       const bool direct = whole && ends;
       float* slot = a.slots + (size_t)(2 * v + (began ? 0 : 1)) * SLOT;
-      float unit = vref * (1.f / 16384.f);
-      if (direct) unit = l == 0.f ? 0.f : unit / l;
-      f *= unit;
-      f_other *= unit;
+      // sums by the normaliser first, or by a power of two near it: where the reference has fallen both are large
+      float down = 1.f;
+      if (direct) {
+        down = l == 0.f ? 0.f : 1.f / l;
+      } else if (l >= MOST_L && l < INFINITY) {
+        const int e = (int)(__float_as_uint(l) >> 23) - 127;
+        down = __uint_as_float((uint32_t)(127 - e) << 23);
+        m += (float)e;
+        l *= down;
+      }
+      const float late = vref < 3.7252903e-9f ? vref : 1.f;   // (2^-28: the product of all three stays a normal number)
+      down *= (1.f / 16384.f) * (late == 1.f ? vref : 1.f);
+      f *= down;
+      f_other *= down;
       const bool there = row < rows;
       T* dst = there && direct ? out_row<T>(a, cur.li, cur.b, cur.h, cur.rt * R + row) : nullptr;
       // (a dual item's streams have 64 channels each)
@@ -627,6 +643,10 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
           for (int e = 0; e < 16; e++) x[e] = fmaf(y[e], f_other, x[e]);
         }
         if (!there) continue;
+        if (late != 1.f) {
+#pragma unroll
+          for (int e = 0; e < 16; e++) x[e] *= late;
+        }
         if (direct) {
 #pragma unroll
           for (int e = 0; e < 2; e++) {
