@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2609_11582_b200 import binding as B
-from tests.test_gpu_paged import BF16, BLOCK, D, F16, gen
+from tests.test_gpu_paged import BF16, BLOCK, D, F16, F32, gen, randn
 
 pytestmark = pytest.mark.gpu
 TILE = 128
@@ -194,3 +194,14 @@ def test_queries_at_the_end_of_their_range(shape, largest):
     q = (q.float() / q.float().abs().amax(-1, keepdim=True) * largest).to(BF16)
     assert q.isfinite().all()
     Store(k * 2.0 ** -60, v, shape[3], shape[5]).attend(q, sm_scale=float(np.float32(2.0 ** 61 / largest)))
+
+
+# Rows of several tiles of eight that the decode kernel takes (more than eight rows of a head, by its clusters or its line): here its own
+# bound holds, not the prompt kernel's.
+@pytest.mark.parametrize("H,Hq,n,tokens,wide", [(1, 1, 13, 2000, False), (1, 1, 13, 2000, True), (1, 7, 3, 900, False), (2, 8, 40, 500, False), (1, 8, 24, 900, False),
+                                                (4, 28, 2, 1300, True), (1, 8, 2, 1700, True), (1, 1, 16, 1000, True), (1, 3, 8, 3000, False), (1, 8, 100, 130, False)])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_many_rows_in_the_decode_kernel(H, Hq, n, tokens, wide, dtype):
+    g = gen(7)
+    k, v = randn(g, 1, H, tokens, D, dtype=F32).cuda(), randn(g, 1, H, tokens, D, dtype=F32).cuda()
+    assert Store(k, v, Hq, wide, dtype).attend(randn(g, 1, 1, Hq, n, D, dtype=dtype)) != B.PLAN_PROMPT
