@@ -64,8 +64,8 @@ size_t okq_paged_workspace_bytes(const okq_paged* cache, int32_t layer_count, in
  *                  (OKQ_ERR_INVALID_ARG where 3 sections[1] - 2 or 3 sections[2] - 1 is not a pair)
  *   freq       device double [pairs], radians per position
  *   positions  device int32 [3][batch][n]
- * Text alone: three equal positions.  The angle is taken and reduced in 64 bits, so that far positions are as
- * exact as near ones (sine and cosine to two units in their last place).
+ * Text alone: three equal positions.  The angle is taken and reduced in 64 bits: cosine and sine are off by 2^-22 + |angle| * 2^-51 at
+ * most (absolute), two units of fp32 up to 2^27 radians and 2^-20 more at 2^31.  |angle| < 2^51.
  */
 typedef struct okq_rope {
   int32_t sections[3];

@@ -77,7 +77,8 @@ struct RopeView {
 
 // cos and sin of an angle given in 64 bits: it is brought to a quarter of a turn around 0 there (fp32 would lose the fraction of a turn
 // from a few thousand positions on) and rounded to fp32 once, an error of 2^-25 of a quarter; sincospif adds its two units in the last
-// place.  Six operations of the fp64 pipe (with the series in 64 bits too one token of 8 sequences x 32 heads took 6.3 us, and not 4.3).
+// place.  The roundings in 64 bits are relative to the angle, 2^-51 of it at most: seen from 2^27 on, and in sines next to zero.
+// Six operations of the fp64 pipe (with the series in 64 bits too one token of 8 sequences x 32 heads took 6.3 us, and not 4.3).
 __device__ __forceinline__ void turn(double angle, float& c, float& s) {
   const double quarter = angle * 0.63661977236758134308;    // 2 / pi
   const double t = quarter + 6755399441055744.0;            // 1.5 * 2^52: rounds to an integer, whose low bits are t's

@@ -1,11 +1,13 @@
 """The 8-bit paged cache's attention where a number could lose its bits: values of very different sizes, tokens that take nearly all of the weight,
-queries at the end of their type's range.  Against softmax attention in 64 bits, each kernel by its own bound."""
+queries at the end of their type's range.  Against softmax attention in 64 bits, each kernel by its own bound.  Rotary positions near and
+far, by a bound that goes with the angle."""
 import numpy as np
 import pytest
 import torch
 
+from oracle import okq_paged_oracle as O
 from paper_2609_11582_b200 import binding as B
-from tests.test_gpu_paged import BF16, BLOCK, D, F16, F32, gen, randn
+from tests.test_gpu_paged import BF16, BLOCK, D, F16, F32, SECTIONS, f64, gen, randn
 
 pytestmark = pytest.mark.gpu
 TILE = 128
@@ -205,3 +207,31 @@ def test_many_rows_in_the_decode_kernel(H, Hq, n, tokens, wide, dtype):
     g = gen(7)
     k, v = randn(g, 1, H, tokens, D, dtype=F32).cuda(), randn(g, 1, H, tokens, D, dtype=F32).cuda()
     assert Store(k, v, Hq, wide, dtype).attend(randn(g, 1, 1, Hq, n, D, dtype=dtype)) != B.PLAN_PROMPT
+
+
+# ------------------------------------------------------------------------------------------------ rotary positions
+def turn_bound(x, ref, angle, half, dtype):
+    """Cosine and sine are off by 2^-22 + |angle| 2^-51 at most: two units of fp32 of sincospi (2^-23), the angle's fraction of a turn rounded to
+    fp32 (2^-25), its reduction in 64 bits (two roundings of 2^-53 and the constant's, relative to the angle).  The product and the sum
+    round once each (2^-24 of |a| + |b|), the result to its type."""
+    mag = np.abs(x)
+    inner = np.zeros_like(mag)
+    inner[..., :half] = inner[..., half:2 * half] = (mag[..., :half] + mag[..., half:2 * half]) * (2.0 ** -22 + 2.0 ** -23 + np.abs(angle) * 2.0 ** -51)
+    tiny = {F16: 2.0 ** -25, BF16: 0.0, F32: 0.0}[dtype]
+    return inner + (0 if dtype == F32 else torch.finfo(dtype).eps / 2 * (np.abs(ref) + inner)) + tiny
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("sections,interleaved", SECTIONS)
+def test_rope_error_by_position(dtype, sections, interleaved):
+    """From the nearest positions to the last ones, and where a sine is next to nothing (multiples of pi: 103993, 833719, 1146408)."""
+    half = sum(sections)
+    p = torch.tensor([0, 1, 2, 3, 22, 355, 710, 4095, 32767, 103993, 208341, 312689, 833719, 1146408, 16777217, 2 ** 30 + 1, 2 ** 31 - 1, -355, -2 ** 31 + 1])
+    pos = p.int().expand(3, 1, -1).contiguous()
+    x = randn(gen(8), 1, 4, len(p), D, dtype=dtype).cuda()
+    for freq in (B.rope_frequencies(1e6, half, "cpu"), torch.ones(half, dtype=torch.float64)):
+        out = torch.empty_like(x)
+        B.rope_apply(B.Rope(pos.cuda(), freq.cuda(), sections, interleaved), x, out)
+        ref = O.rope(f64(x), pos.numpy(), freq.numpy(), sections, interleaved)
+        angle = p.double().numpy()[:, None] * freq.numpy()[None]
+        assert (np.abs(f64(out) - ref) <= turn_bound(f64(x), ref, angle[None, None], half, dtype)).all()
