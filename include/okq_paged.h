@@ -12,8 +12,8 @@
  * quotients rounded to fp32, ties to even.  A block of zeros has scale 0 and codes 0.  A block with an infinity or NaN has a NaN scale:
  * its values are NaN, and so are outputs that see one of its tokens.  8.0078 bits per element.
  *
- * A block that is not full is quantised again from its raw tokens (kept in `raw`) with every append, so that after each call the
- * cache holds what one call with all of the tokens would have left, bit for bit.
+ * A block that is not full is quantised again from its raw tokens (kept in `raw`) with every append, so that after each call that
+ * brings a sequence tokens it holds what one call with all of them would have left, bit for bit.
  *
  * Pages.  A page has room for page_tokens tokens of one sequence in all layers and heads.  table[b][j] is the page with tokens
  * [j * page_tokens, (j + 1) * page_tokens) of sequence b, -1 where there is none; refs[p] counts the table entries that name page p, 0
@@ -97,8 +97,13 @@ okq_status okq_rope_apply(const okq_rope* rope, int32_t dtype, int32_t batch, in
  *   rope     null, or the rotation that the keys are given first (positions [3][batch][n_new], the same for all layers): the same
  *            numbers, bit for bit, as okq_rope_apply into a tensor of the cache's dtype and this call without it
  * The pages must be there (okq_pages_reserve): a sequence whose tokens would need a table entry that is missing, or that have no
- * room in its row, is left as it was, and the status word becomes OKQ_ERR_CAPACITY.  To take tokens back, seq_len may be lowered as
- * far as the start of the unfinished block, no further.
+ * room in its row, is left as it was, and the status word becomes OKQ_ERR_CAPACITY.
+ *
+ * Taking tokens back.  seq_len may be lowered as far as the start of the unfinished block (the last multiple of 32 not above it): the
+ * next append with a token quantises the block again without them; until then its codes keep the scale that they had a part in.
+ * It must not be lowered further: `raw` holds that block's tokens alone, an append would quantise those of another one, and nothing can tell.
+ * Drafted tokens that may be rejected across the end of a block are appended to a fork of the sequence (okq_pages_fork), which is released
+ * with them; the accepted ones are appended to the original.
  */
 okq_status okq_paged_append(const okq_paged* cache, int32_t layer, int32_t layer_count, const void* k, const int64_t k_strides[4],
                             const void* v, const int64_t v_strides[4], int32_t n_new, const int32_t* new_len,

@@ -1,13 +1,13 @@
 """The 8-bit paged cache's attention where a number could lose its bits: values of very different sizes, tokens that take nearly all of the weight,
 queries at the end of their type's range.  Against softmax attention in 64 bits, each kernel by its own bound.  Rotary positions near and
-far, by a bound that goes with the angle."""
+far, by a bound that goes with the angle.  Tokens taken back."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import okq_paged_oracle as O
 from paper_2609_11582_b200 import binding as B
-from tests.test_gpu_paged import BF16, BLOCK, D, F16, F32, SECTIONS, f64, gen, randn
+from tests.test_gpu_paged import BF16, BLOCK, D, F16, F32, SECTIONS, Model, f64, gen, randn
 
 pytestmark = pytest.mark.gpu
 TILE = 128
@@ -235,3 +235,51 @@ def test_rope_error_by_position(dtype, sections, interleaved):
         ref = O.rope(f64(x), pos.numpy(), freq.numpy(), sections, interleaved)
         angle = p.double().numpy()[:, None] * freq.numpy()[None]
         assert (np.abs(f64(out) - ref) <= turn_bound(f64(x), ref, angle[None, None], half, dtype)).all()
+
+
+# ------------------------------------------------------------------------------------------------ tokens taken back
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("held,draft,kept", [(62, 5, 1), (95, 7, 0), (31, 40, 3), (64, 5, 2), (50, 5, 4)])
+def test_drafts_on_a_fork(dtype, held, draft, kept):
+    """Drafted tokens across the end of a block, checked on a fork, given up with it, and the accepted ones appended to the original: the cache is
+    as if the others had never been there."""
+    m = Model(2, 3, 2, 6, max_pages=3, page=64, dtype=dtype, n_pages=12)
+    m.c.table.fill_(-1)
+    m.c.refs.zero_()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32).cuda()  # noqa: E731
+    ws = torch.empty(max(B.paged_workspace_bytes(m.c, 2, n) for n in (1, draft)), dtype=torch.uint8, device="cuda")
+    B.pages_reserve(m.c, i32(held, 0, 20))
+    m.append(held, [held, 0, 20])
+    k, v = (randn(m.g, 2, 3, 2, draft, D, dtype=dtype) for _ in range(2))
+    B.pages_fork(m.c, i32(0), i32(1), ws)
+    for l in range(2):
+        m.tok[l][1] = [list(t) for t in m.tok[l][0]]
+    B.pages_reserve(m.c, i32(0, held + draft, 0))
+    m.append(draft, [0, draft, 0], k=k, v=v)
+    m.check()
+    m.attend(draft, q_len=[0, draft, 0], workspace=ws)
+    B.pages_release(m.c, i32(1))
+    for l in range(2):
+        m.tok[l][1] = [[torch.zeros(0, D, dtype=dtype)] * 2 for _ in range(2)]
+    B.pages_reserve(m.c, i32(held + kept, 0, 0))
+    k[:, 0], v[:, 0] = k[:, 1], v[:, 1]
+    m.append(draft, [kept, 0, 0], k=k, v=v)
+    m.check()
+    m.attend(1, workspace=ws)
+    assert m.c.device_status() == 0
+
+
+def test_codes_after_a_take_back():
+    """Tokens of the unfinished block given back: its codes keep the scale of all of them until the next append, which leaves what the remaining
+    and the new ones alone would have."""
+    m = Model(1, 1, 1, 1, max_pages=2, page=32, dtype=BF16, seed=9)
+    k, v = randn(m.g, 1, 1, 1, 20, D, dtype=BF16), randn(m.g, 1, 1, 1, 20, D, dtype=BF16)
+    k[:, :, :, 12:] *= 8
+    m.append(20, k=k, v=v)
+    before = m.c.codes.clone(), m.c.scales.clone()
+    m.c.seq_len -= 8
+    m.tok[0][0][0] = [t[:12] for t in m.tok[0][0][0]]
+    B.paged_append(m.c, 0, 1, k[:, :, :, :1].cuda(), v[:, :, :, :1].cuda(), torch.zeros(1, dtype=torch.int32, device="cuda"))
+    assert torch.equal(m.c.codes, before[0]) and torch.equal(m.c.scales, before[1])   # (no new token: nothing is written)
+    m.append(1)
+    m.check()
