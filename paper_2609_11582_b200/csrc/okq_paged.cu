@@ -1,9 +1,10 @@
 // The 8-bit paged cache: argument checks, append (quantising whole blocks of 32 tokens and one head), read-back.
 //
-// Append.  A block of keys or values is 32 x 128 numbers with one scale, so its codes are known when all of its tokens are: one
-// thread block per (32-token block, head, sequence) reads the tokens that are there (those of an unfinished block from the raw copies, the
-// new ones from the caller's tensor), takes the maximum and writes codes, scale and, for the block that stays unfinished, the raw
-// copies.  Requantising the unfinished block with every append costs at most 16 KB of reads per head and makes the cache
+// Append.  A block of keys or values is 32 x 128 numbers with one scale, so its codes are known when all of its tokens are: 128 threads
+// read the tokens that are there (those of an unfinished block from the raw copies, the new ones from the caller's tensor), take the
+// maximum and write codes, scale and, for the block that stays unfinished, the raw copies.  A thread block has one side, keys or values,
+// of up to four consecutive blocks of a head; with up to 32 new tokens, the sides of a sequence's heads are dealt over a cluster.
+// Requantising the unfinished block with every append costs at most 16 KB of reads per head and makes the cache
 // independent of how its tokens were dealt over calls; keeping the codes and only lowering their scale would round twice.
 #include "okq_device.cuh"
 #include "okq_paged.cuh"

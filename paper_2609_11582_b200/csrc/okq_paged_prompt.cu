@@ -24,11 +24,11 @@
 // their sums are put together at the end.
 //
 // At best bound by the exponentials (16 per cycle and SM: 2048 cycles for 256 x 128 scores) and the products (2048 cycles at fp16's
-// rate).  What it takes is about 4200 (2048 queries x 28 heads on 8192 tokens 272 us, 775 TFLOP/s of products): a softmax warp's own
+// rate).  What it takes is about 4200 (2048 queries x 28 heads on 8192 tokens 285 us a call, 738 TFLOP/s of products): a softmax warp's own
 // chain of waits, tensor memory, maximum, exponentials and roundings, with two such warps on a scheduler and 128 registers to each (the
 // maximum beside the exponentials, by last step's reference: 390 us, spills).
 // Few rows (a dual item) are bound by the conversion, a step in 1500 cycles, a third of it waits and fences: 35 rows, 16 sequences x 4
-// heads of up to 12345 tokens 53 us (a converting warp to every other step, with half of those waits but a ring that is then too
+// heads of up to 12345 tokens 53 us a call (a converting warp to every other step, with half of those waits but a ring that is then too
 // short: 61).
 #include "okq_paged_attn.cuh"
 
