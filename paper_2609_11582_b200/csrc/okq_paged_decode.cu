@@ -8,7 +8,7 @@
 //            p * scale_v as the four bytes of a 32-bit fixed-point number, exact sums in int32
 // so nothing is unpacked: a tile goes from memory to shared memory by TMA and from there into the tensor cores.  Fixed point is
 // relative to the row's largest p * scale_v in the tile (up to a factor of 4): the power of two R next above the largest log2 of p and
-// scale is taken off in the exponent and put back, with the running maximum, in the factor of the tile's sums.  What lies more than 2^-30
+// scale is taken off in the exponent and put back in the factor of the tile's sums.  What lies more than 2^-30
 // below the largest of the same tile is lost, whatever other tiles hold; fp32 would keep 2^-24 of each.
 //
 // A block has three pipelines, each with a range of tiles and a ring of two of its own, so that one tile's chain of products, softmax
@@ -423,7 +423,6 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       asm volatile("bar.sync %0, 128;\n" ::"r"(1 + g) : "memory");
       const float w0 = sy.wmax[b][0][rl], w1 = sy.wmax[b][1][rl], w2 = sy.wmax[b][2][rl], w3 = sy.wmax[b][3][rl];
       const float mn = fmaxf(fmaxf(fmaxf(w0, w1), fmaxf(w2, w3)), top);
-      const float level = fmaxf(ceilf(fmaxf(fmaxf(w0 + ev.x, w1 + ev.y), fmaxf(w2 + ev.z, w3 + ev.w))), -3e38f);   // R
       if (__any_sync(0xffffffffu, mn > top)) {   // (the same in all of the pipeline's workers)
         const float keep = mn > top ? ex2(top - mn) : 1.f;
 #pragma unroll
@@ -434,15 +433,17 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         }
         top = mn;
       }
+      // R, below the running maximum (differences of scores are exact where their sums with exponents are not: scores may have no digits behind the point)
       const float t = top == -INFINITY ? 0.f : top;
+      const float level = fmaxf(ceilf(fmaxf(fmaxf((w0 - t) + ev.x, (w1 - t) + ev.y), fmaxf((w2 - t) + ev.z, (w3 - t) + ev.w))), -3e38f);
       uint32_t u[R];
 #pragma unroll
       for (int r = 0; r < R; r++) {
-        const float p = ex2(x[r] - __shfl_sync(0xffffffffu, t, r));
+        const float d = x[r] - __shfl_sync(0xffffffffu, t, r), p = ex2(d);
         // a NaN scale of the values reaches the rows that see one of its tokens through their sum
         sum[r] += lost && x[r] != -INFINITY ? NAN : p;
         // (R and the exponent are whole numbers: their difference is exact)
-        u[r] = __float2uint_rn(ex2(x[r] + (exp_own - __shfl_sync(0xffffffffu, level, r))) * frac);
+        u[r] = __float2uint_rn(ex2(d + (exp_own - __shfl_sync(0xffffffffu, level, r))) * frac);
       }
 #pragma unroll
       for (int half = 0; half < 2; half++)
@@ -452,11 +453,10 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       __syncwarp();
       if (lane == 0) mbar_arrive(&sy.p_full);
 
-      // what a row's sums are worth, 2^(R - top) (in two factors, so that neither exponent is rounded), times 2^60 where that is a number in
-      // all rows: small weights of small values would be below fp32's range, and zeros
-      const float whole_t = rintf(t);
-      const bool large = __any_sync(0xffffffffu, level - whole_t > 60.f);
-      const float unit = ex2(whole_t - t) * ex2(large ? level - whole_t : level - whole_t + 60.f);
+      // what a row's sums are worth, 2^R, times 2^60 where that is a number in all rows: small weights of small values would be below fp32's
+      // range, and zeros
+      const bool large = __any_sync(0xffffffffu, level > 60.f);
+      const float unit = ex2(large ? level : level + 60.f);
       const float part_hi = large ? 1.52587890625e-5f : 1.3234889800848443e-23f, part_lo = large ? 2.3283064365386963e-10f : 2.0194839173657902e-28f;   // 2^-16, 2^-32, and those times 2^-60
       // the tile's sums: lane = channel
       bar_wait(sm, &sy.o_full, (uint32_t)i & 1u);

@@ -189,6 +189,26 @@ def test_scores_fall_without_end(shape, rise):
     Store(k, v, shape[3], shape[5]).attend(q)
 
 
+@pytest.mark.parametrize("shape,score", [(s, x) for s in ALL for x in (1e3, 1e6, 2e7, 1e9, 1e12) if x < 1e9 or s in DECODE], ids=str)
+def test_scores_of_all_sizes(shape, score):
+    """One token whose score is so far above the others', which are 0, that the output is its value: scores beyond 2^24 have no digits behind the point.
+    The rounding of the value alone is left: its code times its scale in fp32 (three roundings and those of a sum of one), 2^-20 relative, or
+    the prompt kernel's numerator in fp16, 2^-11; then the output's."""
+    n, batch, H, Hq, T, wide = shape
+    q, k, v = steered(*shape, seed=12)
+    q[..., 1:], k[..., 1:] = 0.0, 0.0
+    at = T - n - 300
+    k[..., at, 0] = score / (16.0 * D ** -0.5)
+    v *= 0.01
+    s = Store(k, v, Hq, wide)
+    ws = torch.empty(B.paged_workspace_bytes(s.c, 1, n), dtype=torch.uint8, device="cuda")
+    out = torch.full_like(q, 7.0)
+    B.paged_attention(s.c, 0, 1, q, ws, out)
+    want = s.held[:, :, 1, at].repeat_interleave(Hq // H, 1)[:, :, None]
+    rel = 2.0 ** -11 if B.paged_plan(s.c, 1, n) == B.PLAN_PROMPT else 2.0 ** -20
+    assert ((out[0].double() - want).abs() <= (rel + torch.finfo(BF16).eps / 2 * (1 + rel)) * want.abs()).all()
+
+
 @pytest.mark.parametrize("largest", [5e37, 1e38, 3e38, float(torch.finfo(BF16).max)])
 @pytest.mark.parametrize("shape", ALL, ids=str)
 def test_queries_at_the_end_of_their_range(shape, largest):
