@@ -49,6 +49,7 @@ constexpr float P_SHIFT = 14.f, LEAD = 6.f, DROP = 20.f;
 // The reference falls by 2^FALL at a time, while the normaliser is below 2^20: with the factor of the unit (LEAST), 127 * 2^15 and as many
 // tokens O stays below 2^126.  So weights of 2^-FALL of the largest, and smaller, may lose bits to it.
 constexpr float FALL = 64.f, MOST_L = 1048576.f;
+constexpr float WIDE = 65536.f;                 // references beyond which a product's rounding shows
 constexpr float NEAR = 0.25f;                   // w and units down to 2^-2 are left as they are
 constexpr float LEAST = 1.5258789e-5f;          // 2^-16: the unit stays above so much of the item's largest (O could overflow otherwise)
 
@@ -234,6 +235,8 @@ __device__ __forceinline__ float row_max(float (&x)[2][32], const Info& info, in
   }
   return mx;
 }
+// EDGE also rounds a score once before the reference is taken off, as the maximum is: the difference is exact then, where scores are so
+// large that an unrounded one could lie far above it.  (Not by packed pairs: their product and sum were contracted to one rounding.)
 template <bool EDGE>
 __device__ __forceinline__ float numerators(const float (&x)[2][32], uint32_t s_at, const Info& info, int b0, float back, float ref, int seen, float l) {
 #pragma unroll
@@ -244,7 +247,9 @@ __device__ __forceinline__ float numerators(const float (&x)[2][32], uint32_t s_
     uint32_t u[16];
 #pragma unroll
     for (int e = 0; e < 16; e++) {
-      const float2 z = un2(fma2(f2(x[b][2 * e], x[b][2 * e + 1]), cb2, off2));
+      const float lw = info.lw[b0 + b];
+      const float2 z = EDGE ? make_float2(__fadd_rn(__fsub_rn(__fmul_rn(x[b][2 * e], cb), ref), lw), __fadd_rn(__fsub_rn(__fmul_rn(x[b][2 * e + 1], cb), ref), lw))
+                            : un2(fma2(f2(x[b][2 * e], x[b][2 * e + 1]), cb2, off2));
       float p0 = ex2(z.x), p1 = ex2(z.y);
       if (EDGE) {   // (-inf times a scale of zero is NaN)
         if (32 * b + 2 * e > seen) p0 = 0.f;
@@ -569,8 +574,9 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
             }
           }
           const float ref = m == -INFINITY ? 0.f : m;
+          const bool careful = edge || __any_sync(0xffffffffu, fabsf(ref) > WIDE);
           if (!dual) take_turn(2 + 4 * t + quarter);
-          l = edge ? numerators<true>(x, p_at, info, 2 * half, back, ref, seen, l) : numerators<false>(x, p_at, info, 2 * half, back, ref, seen, l);
+          l = careful ? numerators<true>(x, p_at, info, 2 * half, back, ref, seen, l) : numerators<false>(x, p_at, info, 2 * half, back, ref, seen, l);
           if (!dual) pass_turn(2 + 4 * (t ^ 1) + quarter);
           tmem_wait_st();
           before_sync();
@@ -616,9 +622,11 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
         down = l == 0.f ? 0.f : 1.f / l;
       } else if (l >= MOST_L && l < INFINITY) {
         const int e = (int)(__float_as_uint(l) >> 23) - 127;
-        down = __uint_as_float((uint32_t)(127 - e) << 23);
-        m += (float)e;
-        l *= down;
+        if (m + (float)e - m == (float)e) {
+          down = __uint_as_float((uint32_t)(127 - e) << 23);
+          m += (float)e;
+          l *= down;
+        }
       }
       const float late = vref < 3.7252903e-9f ? vref : 1.f;   // (2^-28: the product of all three stays a normal number)
       down *= (1.f / 16384.f) * (late == 1.f ? vref : 1.f);

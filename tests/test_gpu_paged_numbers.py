@@ -189,7 +189,8 @@ def test_scores_fall_without_end(shape, rise):
     Store(k, v, shape[3], shape[5]).attend(q)
 
 
-@pytest.mark.parametrize("shape,score", [(s, x) for s in ALL for x in (1e3, 1e6, 2e7, 1e9, 1e12) if x < 1e9 or s in DECODE], ids=str)
+@pytest.mark.parametrize("score", [1e3, 1e6, 2e7, 1e8, 1e9, 1e12])
+@pytest.mark.parametrize("shape", ALL, ids=str)
 def test_scores_of_all_sizes(shape, score):
     """One token whose score is so far above the others', which are 0, that the output is its value: scores beyond 2^24 have no digits behind the point.
     The rounding of the value alone is left: its code times its scale in fp32 (three roundings and those of a sum of one), 2^-20 relative, or
