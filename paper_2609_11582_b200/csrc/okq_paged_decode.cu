@@ -20,7 +20,7 @@
 // Bound by memory: 256 bytes per token and head; an SM's share of the copy rate is a tile in about 1400 cycles.  16 sequences of 32768
 // tokens x 4 heads (538 MB) take 95 us a call, 5.6 TB/s with the merge and both ends (93 in a graph); 1 sequence of 131072 tokens (134 MB,
 // partly in the second-level cache) 34; 1 head of 2048 tokens 7.2, which is latency: launch, table, copies, products, the cluster's merge.
-// (The running maxima in every thread and not in one lane per row: 98 us and not 95, 128 registers and not 126.)
+// (The running maxima in every thread and not in one lane per row: 98 us and not 95, 128 registers and not 127.)
 #include "okq_paged_attn.cuh"
 
 namespace okq {

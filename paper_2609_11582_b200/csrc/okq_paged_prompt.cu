@@ -5,16 +5,15 @@
 //   S[row][token] = Q[row][channel] K[token][channel]   the cache's codes are fp16 numbers as they are (|code| <= 127); queries are scaled
 //                                                       to a power of two per row, so that bf16 ones are fp16 numbers too
 //   O[row][channel] += P[row][token] V[token][channel]  P = 2^14 p w in fp16, in place of the scores in tensor memory, with
-//                                                       w = scale_v / (the unit of O) of the token's block
+//                                                       w the value scale of the token's block
 // and the scales of the blocks enter where they cost nothing: those of the keys in the factor of the exponent, those of the values as
-// log2(w) in its offset; the normaliser takes a block's sum divided by w.  The unit is the largest value scale of a tile, changed (and O
-// multiplied) where a tile's is twice as large, or less than 2^-2 of it: numerators keep their bits whatever was before.  A block with w
-// below 2^-2 has the power of two of it in its codes as fp16 numbers, where it is exact down to 2^-24.
-// The softmax' reference m is set 6 above a row's maximum and moves when a step's maximum passes it (log2 units): O is multiplied then,
-// by the row's own threads (3 above: every other step of a drifting sequence).  It moves down, too, to 6 above the maximum of a step that
-// lies 20 below it or more (14: three times as many multiplications where scores spread by 3, 306 us and not 284): sums in fp32 have
-// room for that, numerators in fp16 have not.  So the largest numerator of a step is 2^-8 or more, w included; 11 bits down to 2^-14, below
-// that rounded to 2^-24.
+// log2(w) in its offset; the normaliser takes a block's sum divided by w.
+// The reference m of the exponent is that of p w, row by row, not of p: fp16 numbers have room for what a row multiplies, whatever the
+// weights of tokens without value and the values of tokens that it does not see.  m is set 6 above a step's maximum and moves when one
+// passes it (log2 units): O is multiplied then, by the row's own threads (3 above: every other step of a drifting sequence).  It moves
+// down, too, to 6 above the maximum of a step that lies 20 below it or more (14: three times as many multiplications where scores spread
+// by 3, 306 us and not 284): sums in fp32 have room for that, numerators in fp16 have not.  So the largest numerator of a step is 2^-6 or
+// more; 11 bits down to 2^-14, below that rounded to 2^-24.
 //
 // A block of threads has 256 rows, in two streams A and B of 128, and walks the tokens in steps of 64: a loader warp (32-token blocks
 // by page, two tiles of 128 tokens ahead), four warps that turn codes into fp16 (0x6400 | (code + 128) is 1024 + 128 + code; the rest is
@@ -24,11 +23,11 @@
 // their sums are put together at the end.
 //
 // At best bound by the exponentials (16 per cycle and SM: 2048 cycles for 256 x 128 scores) and the products (2048 cycles at fp16's
-// rate).  What it takes is about 4200 (2048 queries x 28 heads on 8192 tokens 285 us a call, 738 TFLOP/s of products): a softmax warp's own
+// rate).  What it takes is about 4200 (2048 queries x 28 heads on 8192 tokens 286 us a call, 736 TFLOP/s of products): a softmax warp's own
 // chain of waits, tensor memory, maximum, exponentials and roundings, with two such warps on a scheduler and 128 registers to each (the
 // maximum beside the exponentials, by last step's reference: 390 us, spills).
 // Few rows (a dual item) are bound by the conversion, a step in 1500 cycles, a third of it waits and fences: 35 rows, 16 sequences x 4
-// heads of up to 12345 tokens 53 us a call (a converting warp to every other step, with half of those waits but a ring that is then too
+// heads of up to 12345 tokens 50 us a call (a converting warp to every other step, with half of those waits but a ring that is then too
 // short: 61).
 #include "okq_paged_attn.cuh"
 
@@ -46,22 +45,17 @@ constexpr int NT = 15 * 32;
 constexpr uint32_t S_COL = 0, O_COL = 256;      // + 128 per stream, + 64 per place for scores; numerators lie on its first half
 constexpr size_t SLOT = (size_t)R * (D + 2);
 constexpr float P_SHIFT = 14.f, LEAD = 6.f, DROP = 20.f;
-// The reference falls by 2^FALL at a time, while the normaliser is below 2^20: with the factor of the unit (LEAST), 127 * 2^15 and as many
-// tokens O stays below 2^126.  So weights of 2^-FALL of the largest, and smaller, may lose bits to it.
-constexpr float FALL = 64.f, MOST_L = 1048576.f;
+// The reference stays above 2^-FALL of the row's largest numerator: with 127 * 2^14 and 2^20 tokens O stays below 2^126.
+constexpr float FALL = 76.f;
 constexpr float WIDE = 65536.f;                 // references beyond which a product's rounding shows
-constexpr float NEAR = 0.25f;                   // w and units down to 2^-2 are left as they are
-constexpr float LEAST = 1.5258789e-5f;          // 2^-16: the unit stays above so much of the item's largest (O could overflow otherwise)
+constexpr float NO_VALUE = -112.f;              // log2(w) of blocks without a value: they move m where nothing else is near
+constexpr float LEAST_W = 1.9259299e-34f;       // 2^-112: scales below that count as 0 (the normaliser, tokens / w, is no number)
 
 struct Info {            // of a tile, by block
   float ks[4];           // key scales
-  float mul[4];          // the part of w that codes are multiplied by: 1, a power of two below 2^-2, 0 for scales of 0 and NaN
-  float lw[4];           // log2 of the rest of w, and the shift
-  float iw[4];           // 2^-14 / the rest of w
-  float vref;            // the unit of the sums
-  float fv;              // what they are multiplied by where it has changed, 1 otherwise
-  int lost;              // blocks whose value scale is NaN, a bit for each
-  int plain;             // all of mul are 1
+  float lw[4];           // log2 of w, and the shift
+  float iw[4];           // 2^-14 / w
+  int lost;              // blocks whose value scale is NaN, a bit for each; from bit 4 on those without a value
 };
 
 struct PromptSmem {
@@ -75,6 +69,7 @@ struct PromptSmem {
   // steps of keys, and values, that are in fp16, by converting warp: numbers and not phases, since a stream of a dual item looks at every
   // other step only and could take a phase for the one after the next
   __align__(8) volatile int done[2][2];
+  float peak[2 * M];                               // [stream][row] maximum of the numerators so far, LEAD below the highest reference
   FindSmem<1> find;
   uint32_t tmem_slot;
   long long limit;
@@ -217,6 +212,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // The lane's row of a step's scores, two blocks of 32 tokens, b0 the tile's number of the first; `seen`: last column that the row sees.
+// The largest log2 of p w, 2^P_SHIFT times.
 template <bool EDGE>
 __device__ __forceinline__ float row_max(float (&x)[2][32], const Info& info, int b0, float back, int seen) {
   float mx = -INFINITY;
@@ -231,25 +227,32 @@ __device__ __forceinline__ float row_max(float (&x)[2][32], const Info& info, in
 #pragma unroll
     for (int e = 4; e < 28; e += 2) y[(e >> 1) & 3] = max3(y[(e >> 1) & 3], x[b][e], x[b][e + 1]);
     const float top = max3(max3(y[0], y[1], x[b][28]), max3(y[2], y[3], x[b][29]), fmaxf(x[b][30], x[b][31]));
-    mx = fmaxf(mx, EDGE && top == -INFINITY ? top : top * (back * info.ks[b0 + b]));
+    mx = fmaxf(mx, EDGE && top == -INFINITY ? top : EDGE ? __fadd_rn(__fmul_rn(top, back * info.ks[b0 + b]), info.lw[b0 + b]) : fmaf(top, back * info.ks[b0 + b], info.lw[b0 + b]));
   }
   return mx;
 }
 // EDGE also rounds a score once before the reference is taken off, as the maximum is: the difference is exact then, where scores are so
-// large that an unrounded one could lie far above it.  (Not by packed pairs: their product and sum were contracted to one rounding.)
+// large that an unrounded one could lie far above it (not by packed pairs: their product and sum were contracted to one rounding).  Blocks
+// without a value count in the normaliser alone.
 template <bool EDGE>
 __device__ __forceinline__ float numerators(const float (&x)[2][32], uint32_t s_at, const Info& info, int b0, float back, float ref, int seen, float l) {
 #pragma unroll
   for (int b = 0; b < 2; b++) {
-    const float cb = back * info.ks[b0 + b], off = info.lw[b0 + b] - ref;
+    const bool none = EDGE && (info.lost >> (4 + b0 + b) & 1);
+    const float cb = back * info.ks[b0 + b], lw = none ? 0.f : info.lw[b0 + b], off = lw - ref;
     const F2 cb2 = f2(cb, cb), off2 = f2(off, off);
     F2 sum[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
     uint32_t u[16];
 #pragma unroll
     for (int e = 0; e < 16; e++) {
-      const float lw = info.lw[b0 + b];
-      const float2 z = EDGE ? make_float2(__fadd_rn(__fsub_rn(__fmul_rn(x[b][2 * e], cb), ref), lw), __fadd_rn(__fsub_rn(__fmul_rn(x[b][2 * e + 1], cb), ref), lw))
-                            : un2(fma2(f2(x[b][2 * e], x[b][2 * e + 1]), cb2, off2));
+      float2 z;
+      if (EDGE) {
+        const float most = none ? 127.f : P_SHIFT + 1.f;   // (lw may have no digit in the reference)
+        z = make_float2(__fadd_rn(__fsub_rn(__fmul_rn(x[b][2 * e], cb), ref), lw), __fadd_rn(__fsub_rn(__fmul_rn(x[b][2 * e + 1], cb), ref), lw));
+        z = make_float2(z.x > most ? most : z.x, z.y > most ? most : z.y);
+      } else {
+        z = un2(fma2(f2(x[b][2 * e], x[b][2 * e + 1]), cb2, off2));
+      }
       float p0 = ex2(z.x), p1 = ex2(z.y);
       if (EDGE) {   // (-inf times a scale of zero is NaN)
         if (32 * b + 2 * e > seen) p0 = 0.f;
@@ -257,7 +260,7 @@ __device__ __forceinline__ float numerators(const float (&x)[2][32], uint32_t s_
       }
       sum[e & 1] = add2(sum[e & 1], f2(p0, p1));
       const __half2 h = __floats2half2_rn(p0, p1);
-      u[e] = *reinterpret_cast<const uint32_t*>(&h);
+      u[e] = none ? 0u : *reinterpret_cast<const uint32_t*>(&h);
     }
     const float2 total = un2(add2(sum[0], sum[1]));
     l = fmaf(total.x + total.y, info.iw[b0 + b], l);
@@ -309,14 +312,13 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     Cursor<R, EXTRA> ahead = cur;
     int n_now = 0, n_nx = 0;
     int t_nx = 0, l_nx = 0, h_nx = 0, page_nx = -1;
-    bool in_nx = false, fresh_nx = false;
+    bool in_nx = false;
     int row_now = -1, row_nx = -1;               // -1: nothing to copy
     float ks_now = 0.f, vs_now = 0.f, ks_nx = 0.f, vs_nx = 0.f;
-    bool fresh_now = false;
     auto entries = [&] {
       int b = 0, len = 0;
       for (n_nx = 0; n_nx < 8 && ahead.ok; n_nx++) {
-        if (lane >> 2 == n_nx) { t_nx = ahead.tile * PT + PB * (lane & 3); len = ahead.len; l_nx = a.layer + ahead.li; b = ahead.b; h_nx = ahead.h; fresh_nx = ahead.tile == 0; }
+        if (lane >> 2 == n_nx) { t_nx = ahead.tile * PT + PB * (lane & 3); len = ahead.len; l_nx = a.layer + ahead.li; b = ahead.b; h_nx = ahead.h; }
         ahead.next(work);
       }
       in_nx = lane >> 2 < n_nx && t_nx < len;
@@ -337,7 +339,6 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       }
     };
     int armed[2] = {0, 0};
-    float vref = 0.f, vtop = 0.f;                // the unit of the sums, 0 while they are zeros; the item's largest
     bool out = a.withhold != 0;
     entries();
     scales();
@@ -345,7 +346,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       const int k = i & 7;
       if (k == 0) {
         n_now = n_nx;
-        row_now = row_nx; ks_now = ks_nx; vs_now = vs_nx; fresh_now = fresh_nx;
+        row_now = row_nx; ks_now = ks_nx; vs_now = vs_nx;
         entries();
       }
       if (k >= n_now) break;
@@ -366,30 +367,14 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       // what the other roles need to know of the tile (tile i - 4, whose place it takes, is through: the values of tile i - 2 are in fp16,
       // so those of tile i - 4 have been used)
       const float vs = __shfl_sync(0xffffffffu, vs_now, 4 * k + j), ks = __shfl_sync(0xffffffffu, ks_now, 4 * k + j);
-      const bool first = i == 0 || __shfl_sync(0xffffffffu, (int)fresh_now, 4 * k) != 0;
-      float big = vs != vs ? 0.f : vs;
-      big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
-      big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-      float fv = 1.f;
-      if (first) vref = vtop = 0.f;
-      if (big >= 2.f * vref || (big > 0.f && big < NEAR * vref)) {
-        vtop = fmaxf(vtop, big);
-        const float to = fmaxf(big, LEAST * vtop);
-        if (vref > 0.f) fv = vref / to;
-        vref = to;
-      }
       Info& info = sm.info[i & 3];
-      const bool none = !(vs > 0.f);               // (NaN too)
-      const float w = none ? 1.f : vs / vref, mul = w < NEAR ? __uint_as_float(max(__float_as_uint(w) & 0x7f800000u, 103u << 23)) : 1.f;   // 2^-24 at least
-      const float rest = fmaxf(w / mul, NEAR);
       if (lane < 4) {
         info.ks[lane] = ks;
-        info.mul[lane] = none || w < NEAR * mul ? 0.f : mul;   // (values 2^-26 below the tile's largest are lost)
-        info.lw[lane] = log2f(rest) + P_SHIFT;
-        info.iw[lane] = 1.f / (rest * 16384.f);
+        info.lw[lane] = (vs >= LEAST_W ? log2f(vs) : NO_VALUE) + P_SHIFT;
+        info.iw[lane] = vs >= LEAST_W ? 1.f / (vs * 16384.f) : 1.f;
       }
-      const unsigned lost = __ballot_sync(0xffffffffu, lane < 4 && vs != vs), small = __ballot_sync(0xffffffffu, lane < 4 && (none || w < NEAR));
-      if (lane == 0) { info.vref = vref; info.fv = fv; info.lost = (int)lost; info.plain = small == 0; }
+      const unsigned lost = __ballot_sync(0xffffffffu, lane < 4 && vs != vs), none = __ballot_sync(0xffffffffu, lane < 4 && !(vs >= LEAST_W));
+      if (lane == 0) info.lost = (int)(lost | none << 4);
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.info_full[i & 3]);
       if (k == 4) scales();
@@ -482,29 +467,13 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     for (int x = 0; there(x); x++) {
       const int i = x >> 1, half = x & 1, s = x % NR;
       fetch(x, w);
-      if (side && !half) bar_wait(sm, &sm.info_full[i & 3], (uint32_t)(i >> 2) & 1u);
       if (x >= NR) bar_wait(sm, side ? &sm.v_free[s] : &sm.k_free[s], (uint32_t)(x / NR - 1) & 1u);
       unsigned char* to = side ? sm.v[s][0] : sm.k[s][0];
-      if (!side || sm.info[i & 3].plain) {   // (no branch between the rows, so that their conversions overlap)
 #pragma unroll
-        for (int z = 0; z < 8; z++) {
-          const uint2 h[4] = {codes_to_half(w[z].x), codes_to_half(w[z].y), codes_to_half(w[z].z), codes_to_half(w[z].w)};
-          *reinterpret_cast<uint4*>(to + a0 + 1024 * z) = make_uint4(h[0].x, h[0].y, h[1].x, h[1].y);
-          *reinterpret_cast<uint4*>(to + a1 + 1024 * z) = make_uint4(h[2].x, h[2].y, h[3].x, h[3].y);
-        }
-      } else {
-#pragma unroll 1
-        for (int z = 0; z < 8; z++) {
-          const uint4 x4 = *reinterpret_cast<const uint4*>(codes_of(x) + 8 * z * D);
-          const uint2 h[4] = {codes_to_half(x4.x), codes_to_half(x4.y), codes_to_half(x4.z), codes_to_half(x4.w)};
-          const float mul = sm.info[i & 3].mul[2 * half + (z >> 2)];
-          const __half2 m2 = __floats2half2_rn(mul, mul);
-          __half2 y[8];
-#pragma unroll
-          for (int e = 0; e < 8; e++) y[e] = __hmul2(reinterpret_cast<const __half2*>(h)[e], m2);
-          *reinterpret_cast<uint4*>(to + a0 + 1024 * z) = reinterpret_cast<const uint4*>(y)[0];
-          *reinterpret_cast<uint4*>(to + a1 + 1024 * z) = reinterpret_cast<const uint4*>(y)[1];
-        }
+      for (int z = 0; z < 8; z++) {   // (no branch between the rows, so that their conversions overlap)
+        const uint2 h[4] = {codes_to_half(w[z].x), codes_to_half(w[z].y), codes_to_half(w[z].z), codes_to_half(w[z].w)};
+        *reinterpret_cast<uint4*>(to + a0 + 1024 * z) = make_uint4(h[0].x, h[0].y, h[1].x, h[1].y);
+        *reinterpret_cast<uint4*>(to + a1 + 1024 * z) = make_uint4(h[2].x, h[2].y, h[3].x, h[3].y);
       }
       fence_async_smem();
       __syncwarp();
@@ -534,10 +503,12 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.q_full[t]);
       float m = -INFINITY, l = 0.f;
+      sm.peak[M * t + 32 * quarter + lane] = -INFINITY;
       {
         // (what the loop keeps in registers besides 64 scores: as little as can be)
         int seen = cur.len - cur.m + c.query_of(cur.rt * R + row) - cur.tile * PT - (dual ? PH * t : 0);   // last column of the step that the row sees
         int half = dual ? t : 0, tile = i;
+        bool wide = false;
         for (int y = 0; y < steps; y++) {
           const uint32_t p_at = s_at + 64u * (y & 1);
           if (dual || !half) bar_wait(sm, &sm.info_full[tile & 3], (uint32_t)(tile >> 2) & 1u);
@@ -552,13 +523,18 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
           tmem_wait_ld();
           const float mx = edge ? row_max<true>(x, info, 2 * half, back, seen) : row_max<false>(x, info, 2 * half, back, seen);
           // a new reference: the row's sums so far are multiplied, once their last product is through
-          const float fv = dual || !half ? info.fv : 1.f;
           const float below = m - mx;   // (-inf for the first; inf or NaN for steps that the row does not see)
-          if (__any_sync(0xffffffffu, fabsf(below - DROP / 2) > DROP / 2 && below < FALL + LEAD) || (fv != 1.f && y > 0)) {
-            const bool moves = below < 0.f || (below > DROP && below < FALL + LEAD && l < MOST_L);
-            const float mn = moves ? mx + LEAD : m, f = moves ? ex2(m - mn) : 1.f;   // (0 for the first)
+          if (__any_sync(0xffffffffu, fabsf(below - (DROP / 2 - P_SHIFT)) > DROP / 2 && below < FALL)) {
+            float& peak = sm.peak[M * t + 32 * quarter + lane];
+            const bool up = below < -P_SHIFT;
+            if (l > 4e37f) l = 4e37f;   // (not infinite: weights of tokens without value, 2^100 above all others)
+            float mn = up || (below > DROP - P_SHIFT && below < FALL && peak - mx < FALL) ? mx + (LEAD - P_SHIFT) : m;
+            if (!up && !(l * ex2(m - mn) < 1e36f)) mn = m;
+            const float g = mn != m ? ex2(0.5f * (m - mn)) : 1.f, f = g * g;   // (0 for the first)
             m = mn;
-            l *= f;
+            if (up) peak = fmaxf(peak, mx);
+            wide = __any_sync(0xffffffffu, fabsf(m) > WIDE && m > -INFINITY);   // (scores so large that their products' rounding shows)
+            l = l * g * g;   // (in two steps: it may be as large as the square is small)
             if (y > 0) {
               bar_wait(sm, &sm.o_full[t], (uint32_t)(n_o + y - 1) & 1u);
               after_sync();
@@ -568,15 +544,14 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
                 tmem_ld16(o_at + 16u * b, o);
                 tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 16; e++) o[e] *= f * fv;
+                for (int e = 0; e < 16; e++) o[e] *= f;
                 tmem_st16(o_at + 16u * b, reinterpret_cast<const uint32_t(&)[16]>(o));
               }
             }
           }
           const float ref = m == -INFINITY ? 0.f : m;
-          const bool careful = edge || __any_sync(0xffffffffu, fabsf(ref) > WIDE);
           if (!dual) take_turn(2 + 4 * t + quarter);
-          l = careful ? numerators<true>(x, p_at, info, 2 * half, back, ref, seen, l) : numerators<false>(x, p_at, info, 2 * half, back, ref, seen, l);
+          l = edge || wide ? numerators<true>(x, p_at, info, 2 * half, back, ref, seen, l) : numerators<false>(x, p_at, info, 2 * half, back, ref, seen, l);
           if (!dual) pass_turn(2 + 4 * (t ^ 1) + quarter);
           tmem_wait_st();
           before_sync();
@@ -595,7 +570,6 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
           }
         }
       }
-      const float vref = sm.info[(i + n - 1) & 3].vref;   // (its place is not taken before this warp is at the next item)
       n_o += steps;
       bar_wait(sm, &sm.o_full[t], (uint32_t)(n_o - 1) & 1u);
       if (sm.abort) l = NAN;
@@ -608,30 +582,31 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
         asm volatile("bar.sync 1, 256;\n" ::: "memory");   // both streams' sums are complete
         const float2 y = stat[M * (t ^ 1) + r];
         const float mn = fmaxf(m, y.x), at = mn == -INFINITY ? 0.f : mn;
-        f = ex2(m - at);
-        f_other = ex2(y.x - at);
-        l = l * f + y.y * f_other;
+        const float g = ex2(0.5f * (m - at)), g_other = ex2(0.5f * (y.x - at));
+        f = g * g;
+        f_other = g_other * g_other;
+        l = l * g * g + y.y * g_other * g_other;
         m = mn;
       }
       after_sync();
       const bool direct = whole && ends;
       float* slot = a.slots + (size_t)(2 * v + (began ? 0 : 1)) * SLOT;
-      // sums by the normaliser first, or by a power of two near it: where the reference has fallen both are large
-      float down = 1.f;
+      // divided by the normaliser, or by a power of two near it: it is large where weight lies on tokens of little value
+      if (l > 4e37f) l = 4e37f;
+      float unit = 1.f, late = 1.f;
       if (direct) {
-        down = l == 0.f ? 0.f : 1.f / l;
-      } else if (l >= MOST_L && l < INFINITY) {
+        if (l > 1.2379400e27f) { unit = 1.1529215e18f; late = 8.6736174e-19f; }   // 2^90; 2^60 and back, so that the factor stays a normal number
+        unit = l == 0.f ? 0.f : unit / l;
+      } else if (l > 0.f && l < INFINITY) {
         const int e = (int)(__float_as_uint(l) >> 23) - 127;
         if (m + (float)e - m == (float)e) {
-          down = __uint_as_float((uint32_t)(127 - e) << 23);
+          const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+          unit *= down;
           m += (float)e;
           l *= down;
         }
       }
-      const float late = vref < 3.7252903e-9f ? vref : 1.f;   // (2^-28: the product of all three stays a normal number)
-      down *= (1.f / 16384.f) * (late == 1.f ? vref : 1.f);
-      f *= down;
-      f_other *= down;
+      unit *= 1.f / 16384.f;   // (not one factor with f: both may be small where the stream's sums are large)
       const bool there = row < rows;
       T* dst = there && direct ? out_row<T>(a, cur.li, cur.b, cur.h, cur.rt * R + row) : nullptr;
       // (a dual item's streams have 64 channels each)
@@ -641,16 +616,16 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
         float x[16];
         tmem_ld16(o_at + 16u * b, x);
         tmem_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 16; e++) x[e] *= f;
         if (dual) {
           float y[16];
           tmem_ld16(o_own + 128u * (t ^ 1) + 16u * b, y);
           tmem_wait_ld();
 #pragma unroll
-          for (int e = 0; e < 16; e++) x[e] = fmaf(y[e], f_other, x[e]);
+          for (int e = 0; e < 16; e++) x[e] = fmaf(y[e], f_other, x[e] * f);
         }
         if (!there) continue;
+#pragma unroll
+        for (int e = 0; e < 16; e++) x[e] *= unit;
         if (late != 1.f) {
 #pragma unroll
           for (int e = 0; e < 16; e++) x[e] *= late;

@@ -1,6 +1,8 @@
 """The 8-bit paged cache's attention where a number could lose its bits: values of very different sizes, tokens that take nearly all of the weight,
 queries at the end of their type's range.  Against softmax attention in 64 bits, each kernel by its own bound.  Rotary positions near and
 far, by a bound that goes with the angle.  Tokens taken back."""
+import random
+
 import numpy as np
 import pytest
 import torch
@@ -21,11 +23,14 @@ def kernel_bound(w, v, ref, amax, top, dtype, plan):
     Decode kernel: a tile's numerators, weight times scale, are whole multiples of 2^-30 of the largest of its 128 or less; half of that
     times a code of 127 for each of 128 tokens: 2^-24 of the largest w * amax of the tile.
     Prompt kernel: fp16, half a step is 2^-12, and twice that with the sums that round towards it; below fp16's normal numbers half a step of
-    2^-24, where the largest of a step's 64 numerators is 2^-8 at least: 64 * 2^-17 = 2^-11 of the largest w * amax of the step."""
+    2^-24, where the largest of a step's 64 numerators is 2^-6 at least: 64 * 2^-19 = 2^-13 of the largest w * amax of the step.  Numerators
+    that lie 2^-68 below the row's largest, all of its tokens.  Blocks with a scale below 2^-112 count as zeros, values up to 127 * 2^-112."""
     mag = w @ v.abs()
-    step, part = (TILE // 2, 2.0 ** -11) if plan == B.PLAN_PROMPT else (TILE, 2.0 ** -24)
-    most = sum(x.amax(-1) for x in (w * amax[..., None, :]).split(step, -1))
+    step, part = (TILE // 2, 2.0 ** -13) if plan == B.PLAN_PROMPT else (TILE, 2.0 ** -24)
+    most = [x.amax(-1) for x in (w * amax[..., None, :]).split(step, -1)]
+    most = sum(most) + (w.shape[-1] * 2.0 ** -68 / part * torch.stack(most).amax(0) if plan == B.PLAN_PROMPT else 0)
     err = (2.0 ** -24 * (8 * top[..., None] + 32) + (2.0 ** -11 if plan == B.PLAN_PROMPT else 0)) * mag + part * most[..., None]
+    err = err + (127 * 2.0 ** -112 if plan == B.PLAN_PROMPT else 0)
     return err + torch.finfo(dtype).eps / 2 * (ref.abs() + err) + (2.0 ** -25 if dtype == F16 else 1e-38)
 
 
@@ -208,6 +213,59 @@ def test_scores_of_all_sizes(shape, score):
     want = s.held[:, :, 1, at].repeat_interleave(Hq // H, 1)[:, :, None]
     rel = 2.0 ** -11 if B.paged_plan(s.c, 1, n) == B.PLAN_PROMPT else 2.0 ** -20
     assert ((out[0].double() - want).abs() <= (rel + torch.finfo(BF16).eps / 2 * (1 + rel)) * want.abs()).all()
+
+
+@pytest.mark.parametrize("fall", [4, 20, 60])
+@pytest.mark.parametrize("n,batch,H,Hq", [(150, 6, 2, 14), (128, 20, 4, 4), (26, 40, 2, 2), (700, 2, 2, 4)])
+def test_rows_that_see_small_values_only(n, batch, H, Hq, fall):
+    """Prompts whose values grow from block to block: early rows see none of the large ones, which lie in the same tile."""
+    q, k, v = steered(n, batch, H, Hq, n, True, seed=13)
+    v *= torch.exp2(fall * (torch.arange(n, device="cuda") // BLOCK % 4 - 2.0))[:, None]
+    Store(k, v, Hq, True).attend(q)
+
+
+@pytest.mark.parametrize("lifts,zero", [((0, 20, 40, 0, 20), (1, 2, 4)), ((0, 0, 40, 0, 20), (1, 2, 4)), ((0, 30, 0, 0, 0), (1,)), ((40, 0, 0, 0, 40), (0, 4)),
+                                        ((20, 20, 20, 0, 0), (0, 1, 2)), ((0, 20, 40, 0, 20), (2,))], ids=str)
+@pytest.mark.parametrize("n,batch,H,Hq", [(150, 6, 2, 14), (150, 20, 2, 2), (26, 40, 2, 2)])
+def test_blocks_without_value_and_all_of_the_weight(n, batch, H, Hq, lifts, zero):
+    q, k, v = steered(n, batch, H, Hq, 150, True, seed=14, spread=3.0)
+    block = torch.arange(150, device="cuda") // BLOCK
+    k[..., 0] = torch.tensor(lifts, device="cuda")[block] * lift(1.0)
+    for z in zero:
+        v[..., block == z, :] = 0
+    Store(k, v, Hq, True).attend(q)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_mixtures(seed):
+    """Forty calls each of random shapes: heads, groups, pages, queries, lengths, scores with a long tail, in steps, drifting or with a few dominant
+    tokens, blocks of values up to 2^30 apart on either side (2^6 in fp16), blocks and dominant tokens without value."""
+    rng = random.Random(seed)
+    for _ in range(40):
+        H, G, batch, n = rng.choice([1, 2, 4, 8]), rng.choice([1, 2, 5, 7, 8]), rng.choice([1, 1, 2, 6, 12]), rng.choice([1, 1, 2, 3, 5, 8, 20, 33, 70, 150, 300])
+        T, dtype, wide = max(n, rng.choice([1, 31, 33, 100, 128, 129, 700, 2500, 2501])), rng.choice([F16, BF16]), rng.random() < 0.5
+        q, k, v = steered(n, batch, H, H * G, T, wide, seed=rng.randrange(1 << 30), spread=rng.choice([0.3, 1.0, 3.0]))
+        g = torch.Generator(device="cuda")
+        g.manual_seed(rng.randrange(1 << 30))
+        uniform = lambda *s: torch.rand(*s, generator=g, device="cuda")  # noqa: E731
+        above, kind = lift(rng.choice([5.0, 15.0, 30.0, 40.0])), rng.choice(["even", "tail", "steps", "drift", "few"])
+        if kind == "tail":
+            k[..., 0] = above * uniform(batch, H, T) ** 8
+        elif kind == "steps":
+            k[..., 0] = above * (torch.arange(T, device="cuda") // rng.choice([32, 64, 100, 500]) % 3) / 2
+        elif kind == "drift":
+            k[..., 0] = (above / 30 * (uniform(batch, H, T) - 0.5) * 3.5).cumsum(-1)
+        elif kind == "few":
+            k[..., 0] = above * (uniform(batch, H, T) > 1 - 3 / T)
+        blocks = (T + BLOCK - 1) // BLOCK
+        spread = rng.choice([0, 0, 2, 6] if dtype == F16 else [0, 2, 10, 30])
+        by_token = lambda x: x.repeat_interleave(BLOCK, -1)[..., :T]  # noqa: E731
+        v *= by_token(torch.exp2((uniform(batch, H, blocks) * 2 - 1) * spread))[..., None]
+        if rng.random() < 0.3:
+            v[by_token(uniform(batch, H, blocks) < 0.3)] = 0
+        if rng.random() < 0.3:
+            v[k[..., 0] > k[..., 0].amax() - lift(3.0)] = 0
+        Store(k, v, H * G, wide, dtype, rng.choice([32, 64, 128, 256])).attend(q.to(dtype))
 
 
 @pytest.mark.parametrize("largest", [5e37, 1e38, 3e38, float(torch.finfo(BF16).max)])
