@@ -89,6 +89,36 @@ okq_status okq_rope_apply(const okq_rope* rope, int32_t dtype, int32_t batch, in
                           const okq_rope_tensor* k, int32_t inverse, void* stream);
 
 /*
+ * Norm of every head, then the rotation, in one pass: for a row x of 128 channels
+ *     y = R (weight * x * r),  r = (mean(x^2) + eps)^(-1/2)
+ * with R the rotation of okq_rope (none where `rope` is null); all of it in 32 bits, rounded to `dtype` once.  Rows whose squares have no
+ * sum in 32 bits are taken care of; a row with an infinity or NaN has NaN in those channels.
+ */
+typedef struct okq_norm_tensor {
+  const void* in;       /* element (b, h, i, c) at in[b*in_strides[0] + h*in_strides[1] + i*in_strides[2] + c], the others likewise */
+  const void* grad_out; /* okq_norm_rope_grad only: gradient of the result */
+  void* out;            /* the result; of okq_norm_rope_grad the gradient of `in` */
+  int64_t in_strides[3], grad_strides[3], out_strides[3]; /* in elements, multiples of 16 bytes */
+  const void* weight;   /* [128] of weight_dtype, the same for all heads; null: ones */
+  float* weight_grad;   /* okq_norm_rope_grad only: [128], overwritten; null: not wanted */
+  int32_t weight_dtype; /* OKQ_FP16, OKQ_BF16 or OKQ_FP32 */
+  int32_t heads;
+} okq_norm_tensor;
+
+/* q and, unless null, k (both of `dtype`, fp16, bf16 or fp32) in one launch.  1e-30 <= eps.  out == in with equal strides is allowed, any
+ * other overlap is not.  batch or n = 0 is a no-op. */
+okq_status okq_norm_rope_apply(const okq_rope* rope, float eps, int32_t dtype, int32_t batch, int32_t n, const okq_norm_tensor* q,
+                               const okq_norm_tensor* k, void* stream);
+
+/* The gradients of `in` and of the weights (sums over all rows in 32 bits, in an order that depends on the sizes alone) from `in`, as it
+ * was given to okq_norm_rope_apply, and the gradient of its result.  out == grad_out or out == in with equal strides is allowed.
+ * workspace: okq_norm_rope_workspace_bytes (0 on sizes that are refused); not needed without rows, where the weights' gradients are zeros,
+ * and where no weight_grad is wanted. */
+okq_status okq_norm_rope_grad(const okq_rope* rope, float eps, int32_t dtype, int32_t batch, int32_t n, const okq_norm_tensor* q,
+                              const okq_norm_tensor* k, void* workspace, size_t workspace_bytes, void* stream);
+size_t okq_norm_rope_workspace_bytes(int32_t batch, int32_t n, int32_t q_heads, int32_t k_heads);
+
+/*
  * Appends up to n_new tokens per sequence to layers [layer, layer + layer_count): new_len[b] of them (clamped to [0, n_new]), all
  * where new_len is null; rows behind are not read.
  *   k, v     device, of the cache's dtype, element (l, b, h, i, c) at k[l*ks[0] + b*ks[1] + h*ks[2] + i*ks[3] + c], l counted from

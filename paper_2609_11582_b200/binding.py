@@ -55,6 +55,11 @@ class okq_rope_tensor(C.Structure):
                 ("heads", C.c_int32)]
 
 
+class okq_norm_tensor(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("grad_out", C.c_void_p), ("out", C.c_void_p), ("in_strides", C.c_int64 * 3), ("grad_strides", C.c_int64 * 3),
+                ("out_strides", C.c_int64 * 3), ("weight", C.c_void_p), ("weight_grad", C.c_void_p), ("weight_dtype", C.c_int32), ("heads", C.c_int32)]
+
+
 class OkqError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -156,6 +161,12 @@ def lib():
         L.okq_paged_workspace_bytes.argtypes = [paged, i32, i32]
         L.okq_rope_apply.restype = C.c_int
         L.okq_rope_apply.argtypes = [ptr, i32, i32, i32, ptr, ptr, i32, ptr]
+        L.okq_norm_rope_apply.restype = C.c_int
+        L.okq_norm_rope_apply.argtypes = [ptr, C.c_float, i32, i32, i32, ptr, ptr, ptr]
+        L.okq_norm_rope_grad.restype = C.c_int
+        L.okq_norm_rope_grad.argtypes = [ptr, C.c_float, i32, i32, i32, ptr, ptr, ptr, C.c_size_t, ptr]
+        L.okq_norm_rope_workspace_bytes.restype = C.c_size_t
+        L.okq_norm_rope_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.okq_paged_append.restype = C.c_int
         L.okq_paged_append.argtypes = [paged, i32, i32, ptr, ptr, ptr, ptr, i32, ptr, ptr, ptr]
         L.okq_paged_read.restype = C.c_int
@@ -189,7 +200,8 @@ def exported_symbols():
             "okq_calib_moments", "okq_calib_rotation",
             "okq_ladder_codebook", "okq_ladder_quantize_keys", "okq_ladder_quantize_values",
             "okq_debug_ladder_timeout", "okq_ladder_decode_attention", "okq_turboquant_encode", "okq_turboquant_decode",
-            "okq_paged_sizes", "okq_paged_workspace_bytes", "okq_rope_apply", "okq_paged_append", "okq_paged_read",
+            "okq_paged_sizes", "okq_paged_workspace_bytes", "okq_rope_apply",
+            "okq_norm_rope_apply", "okq_norm_rope_grad", "okq_norm_rope_workspace_bytes", "okq_paged_append", "okq_paged_read",
             "okq_paged_attention", "okq_debug_paged_timeout", "okq_debug_paged_plan", "okq_pages_reserve", "okq_pages_fork", "okq_pages_release", "okq_pages_copy",
             "okq_pages_compact"]
 
@@ -504,6 +516,7 @@ DTYPE_CODES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
 _strides4 = struct.Struct("4q").pack                 # int64_t[4]
 _rope_struct = struct.Struct("4i2Q").pack            # okq_rope
 _rope_tensor_struct = struct.Struct("2Q6qi4x").pack  # okq_rope_tensor
+_norm_tensor_struct = struct.Struct("3Q9q2Q2i").pack  # okq_norm_tensor
 
 
 def _here(*tensors):
@@ -603,6 +616,52 @@ def rope_apply(rope: Rope, q, q_out, k=None, k_out=None, inverse=False, stream=N
     st = (_lib or lib()).okq_rope_apply(rope.ref, DTYPE_CODES[dtype], batch, n, q_ref, k_ref, 1 if inverse else 0, _stream(stream))
     if st != OK:
         raise OkqError(st, "okq_rope_apply")
+
+
+def _norm_tensor(x, up, out, weight, weight_grad, dtype, shape):
+    xs, os = x.stride(), out.stride()
+    us = xs if up is None else up.stride()
+    assert x.shape == out.shape == shape and x.dtype == out.dtype == dtype and xs[3] == os[3] == us[3] == 1
+    assert up is None or (up.shape == shape and up.dtype == dtype)
+    assert weight is None or (weight.numel() == HEAD_DIM and weight.is_contiguous())
+    assert weight_grad is None or (weight_grad.numel() == HEAD_DIM and weight_grad.is_contiguous() and weight_grad.dtype == torch.float32)
+    return _norm_tensor_struct(x.data_ptr(), 0 if up is None else up.data_ptr(), out.data_ptr(), xs[0], xs[1], xs[2], us[0], us[1], us[2], os[0], os[1], os[2],
+                               0 if weight is None else weight.data_ptr(), 0 if weight_grad is None else weight_grad.data_ptr(),
+                               2 if weight is None else DTYPE_CODES[weight.dtype], shape[1])
+
+
+def norm_rope_apply(rope, q, q_out, q_weight=None, k=None, k_out=None, k_weight=None, eps=1e-6, stream=None):
+    """Norm of every head of q and k, [batch, heads, n, 128] of fp16, bf16 or fp32 (last dim contiguous, any other strides), with its weight
+    ([128] of any of the three types, ones without it), then the rotation (none with rope=None), into q_out and k_out (which may be the
+    inputs)."""
+    _here(q, q_out, q_weight, k, k_out, k_weight, *((None, None) if rope is None else (rope.positions, rope.freq)))
+    batch, heads, n, _ = q.shape
+    dtype = q.dtype
+    q_ref = _norm_tensor(q, None, q_out, q_weight, None, dtype, (batch, heads, n, HEAD_DIM))
+    k_ref = None if k is None else _norm_tensor(k, None, k_out, k_weight, None, dtype, (batch, k.shape[1], n, HEAD_DIM))
+    st = (_lib or lib()).okq_norm_rope_apply(_rope_ref(rope, batch, n), eps, DTYPE_CODES[dtype], batch, n, q_ref, k_ref, _stream(stream))
+    if st != OK:
+        raise OkqError(st, "okq_norm_rope_apply")
+
+
+def norm_rope_workspace_bytes(batch: int, n: int, q_heads: int, k_heads: int = 0) -> int:
+    return lib().okq_norm_rope_workspace_bytes(batch, n, q_heads, k_heads)
+
+
+def norm_rope_grad(rope, q, q_up, q_grad, workspace=None, q_weight=None, q_weight_grad=None, k=None, k_up=None, k_grad=None, k_weight=None,
+                   k_weight_grad=None, eps=1e-6, stream=None):
+    """The gradients of norm_rope_apply's inputs into q_grad and k_grad (which may be q_up and k_up, the gradients of its results) and, where
+    q_weight_grad and k_weight_grad (float32 [128], overwritten) are given, those of its weights; q and k as they were before the norm."""
+    _here(q, q_up, q_grad, workspace, q_weight, q_weight_grad, k, k_up, k_grad, k_weight, k_weight_grad,
+          *((None, None) if rope is None else (rope.positions, rope.freq)))
+    batch, heads, n, _ = q.shape
+    dtype = q.dtype
+    q_ref = _norm_tensor(q, q_up, q_grad, q_weight, q_weight_grad, dtype, (batch, heads, n, HEAD_DIM))
+    k_ref = None if k is None else _norm_tensor(k, k_up, k_grad, k_weight, k_weight_grad, dtype, (batch, k.shape[1], n, HEAD_DIM))
+    st = (_lib or lib()).okq_norm_rope_grad(_rope_ref(rope, batch, n), eps, DTYPE_CODES[dtype], batch, n, q_ref, k_ref, _ptr(workspace),
+                                            0 if workspace is None else workspace.nbytes, _stream(stream))
+    if st != OK:
+        raise OkqError(st, "okq_norm_rope_grad")
 
 
 def _rows(cache, x, layer_count, heads, n):
