@@ -167,6 +167,37 @@ okq_status okq_paged_attention(const okq_paged* cache, int32_t layer, int32_t la
                                int32_t n_new, const int32_t* q_len, const okq_rope* rope, float sm_scale, void* workspace,
                                size_t workspace_bytes, void* out, const int64_t out_strides[4], void* stream);
 
+/*
+ * The same with a window: a query of token p sees token t <= p where p - t < window (at least 1: itself) or t < sinks.  Tokens are counted as
+ * the cache holds them, so that okq_pages_slide changes nothing.  Pages that no query of the call sees are not read, and need not be there.
+ * A window or sinks as long as a row of the table: okq_paged_attention, bit for bit.
+ */
+okq_status okq_paged_attention_window(const okq_paged* cache, int32_t layer, int32_t layer_count, const void* q, const int64_t q_strides[4],
+                                      int32_t n_new, const int32_t* q_len, const okq_rope* rope, float sm_scale, int32_t window, int32_t sinks,
+                                      void* workspace, size_t workspace_bytes, void* out, const int64_t out_strides[4], void* stream);
+
+/*
+ * The same for drafted tokens that form a tree.  The newest q_len[b] tokens of sequence b are its nodes, node j being token seq_len - q_len + j,
+ * and query i is node i's: it sees all tokens before the nodes, and node j where bit j mod 64 of seen[b][i][j / 64] is set (itself only if its own
+ * is; bits from q_len[b] on do not count).  A query that sees nothing gives zeros.
+ *   seen   device uint64 [batch][n_new][(n_new + 63) / 64], as okq_tree_ancestors makes it, or any other
+ * The nodes are appended like other tokens, in any order that puts parents first, with positions of their own in `rope`; to a fork, since
+ * they may be rejected.
+ */
+okq_status okq_paged_attention_tree(const okq_paged* cache, int32_t layer, int32_t layer_count, const void* q, const int64_t q_strides[4],
+                                    int32_t n_new, const int32_t* q_len, const okq_rope* rope, float sm_scale, const uint64_t* seen,
+                                    void* workspace, size_t workspace_bytes, void* out, const int64_t out_strides[4], void* stream);
+
+/* What the nodes of each sequence's tree see, from their parents: bits of a node's ancestors and its own, and how many ancestors it has.
+ *   parents  device int32 [batch][n_new]: a node before it, or -1 for one that follows the sequence itself.  Anything else: such a node counts
+ *            as one without a parent, and the cache's status becomes OKQ_ERR_INVALID_ARG
+ *   q_len    device int32 [batch] or null, nodes of each sequence (clamped to [0, n_new]); rows behind are left as they were
+ *   seen     device uint64 [batch][n_new][(n_new + 63) / 64]
+ *   depth    device int32 [batch][n_new], or null
+ * n_new at most 4096. */
+okq_status okq_tree_ancestors(const okq_paged* cache, const int32_t* parents, int32_t n_new, const int32_t* q_len, uint64_t* seen, int32_t* depth,
+                              void* stream);
+
 /* Testing aid for the bounded waits of okq_paged_attention, as okq_debug_bulk_timeout is for the 2-bit path's quantiser: nothing of a
  * sequence's codes is delivered and every wait is limited to `limit_clocks` SM clocks.  The kernel returns by itself, outputs of
  * sequences that hold tokens are NaN, the status word becomes OKQ_ERR_TIMEOUT. */
@@ -178,7 +209,8 @@ okq_status okq_debug_paged_timeout(const okq_paged* cache, int32_t layer, int32_
  * (layer, sequence, KV head); OKQ_PLAN_LINE: the decode kernel over even ranges, and the merge; OKQ_PLAN_PROMPT: the prompt kernel; 0:
  * refused.  Only sizes are looked at. */
 enum { OKQ_PLAN_LINE = -1, OKQ_PLAN_PROMPT = -2 };
-int32_t okq_debug_paged_plan(const okq_paged* cache, int32_t layer_count, int32_t n_new);
+int32_t okq_debug_paged_plan(const okq_paged* cache, int32_t layer_count, int32_t n_new);   /* and okq_paged_attention_tree */
+int32_t okq_debug_paged_plan_window(const okq_paged* cache, int32_t layer_count, int32_t n_new, int32_t window, int32_t sinks);
 
 /*
  * The pages.  All of it happens on the device, in stream order, without the host; free pages are handed out lowest index first, to
@@ -199,6 +231,13 @@ okq_status okq_pages_fork(const okq_paged* cache, const int32_t* src, const int3
 
 /* Sequences seqs[0 .. count) (device int32) give up their pages and become empty in all layers; naming one twice is naming it once. */
 okq_status okq_pages_release(const okq_paged* cache, const int32_t* seqs, int32_t count, void* stream);
+
+/* Gives back the pages that okq_paged_attention_window with this window and these sinks will not see again from any token that is still to
+ * come: of tokens [sinks, seq_len - window], seq_len that of the shortest layer, the whole pages leave each sequence's row, the entries
+ * behind them move down, and the lengths of all layers shrink by their tokens (multiples of page_tokens).  Keys stay as they were rotated:
+ * positions go on counting what was dropped.  To be called when the attention of the tokens appended so far is through in all layers.
+ * 1 <= window, 0 <= sinks.  dropped (device int32 [batch], may be null) receives the tokens that each sequence lost. */
+okq_status okq_pages_slide(const okq_paged* cache, int32_t window, int32_t sinks, int32_t* dropped, void* stream);
 
 /* Copies codes and scales of pages src[i] to pages dst[i] (device int32 [count]) in all layers; tables and counts stay.  A pair whose
  * destination is named by another pair, as source or destination, is skipped (OKQ_ERR_INVALID_ARG). */

@@ -177,6 +177,16 @@ def lib():
         L.okq_debug_paged_timeout.argtypes = [paged, i32, i32, ptr, ptr, i32, ptr, C.c_size_t, ptr, ptr, C.c_int64, ptr]
         L.okq_debug_paged_plan.restype = i32
         L.okq_debug_paged_plan.argtypes = [paged, i32, i32]
+        L.okq_paged_attention_window.restype = C.c_int
+        L.okq_paged_attention_window.argtypes = [paged, i32, i32, ptr, ptr, i32, ptr, ptr, C.c_float, i32, i32, ptr, C.c_size_t, ptr, ptr, ptr]
+        L.okq_paged_attention_tree.restype = C.c_int
+        L.okq_paged_attention_tree.argtypes = [paged, i32, i32, ptr, ptr, i32, ptr, ptr, C.c_float, ptr, ptr, C.c_size_t, ptr, ptr, ptr]
+        L.okq_tree_ancestors.restype = C.c_int
+        L.okq_tree_ancestors.argtypes = [paged, ptr, i32, ptr, ptr, ptr, ptr]
+        L.okq_debug_paged_plan_window.restype = i32
+        L.okq_debug_paged_plan_window.argtypes = [paged, i32, i32, i32, i32]
+        L.okq_pages_slide.restype = C.c_int
+        L.okq_pages_slide.argtypes = [paged, i32, i32, ptr, ptr]
         L.okq_pages_reserve.restype = C.c_int
         L.okq_pages_reserve.argtypes = [paged, ptr, ptr]
         L.okq_pages_fork.restype = C.c_int
@@ -203,7 +213,8 @@ def exported_symbols():
             "okq_paged_sizes", "okq_paged_workspace_bytes", "okq_rope_apply",
             "okq_norm_rope_apply", "okq_norm_rope_grad", "okq_norm_rope_workspace_bytes", "okq_paged_append", "okq_paged_read",
             "okq_paged_attention", "okq_debug_paged_timeout", "okq_debug_paged_plan", "okq_pages_reserve", "okq_pages_fork", "okq_pages_release", "okq_pages_copy",
-            "okq_pages_compact"]
+            "okq_pages_compact", "okq_pages_slide", "okq_paged_attention_window", "okq_paged_attention_tree", "okq_tree_ancestors",
+            "okq_debug_paged_plan_window"]
 
 
 def _ptr(t) -> int:
@@ -711,6 +722,50 @@ def paged_attention(cache: PagedCache, layer: int, layer_count: int, q, workspac
         raise OkqError(st, "okq_paged_attention")
 
 
+def paged_attention_window(cache: PagedCache, layer: int, layer_count: int, q, workspace, out, window: int, sinks: int = 0, q_len=None, rope=None,
+                           sm_scale=None, stream=None):
+    """paged_attention in which a query of token p sees token t <= p where p - t < window or t < sinks."""
+    _here(cache.codes, q, workspace, out, q_len, None if rope is None else rope.positions)
+    n = q.shape[3]
+    assert q_len is None or (q_len.dtype == torch.int32 and q_len.is_contiguous() and q_len.numel() == cache.batch)
+    st = (_lib or lib()).okq_paged_attention_window(
+        cache.ref, layer, layer_count, q.data_ptr(), _rows(cache, q, layer_count, cache.n_q_heads, n), n, _ptr(q_len), _rope_ref(rope, cache.batch, n),
+        HEAD_DIM ** -0.5 if sm_scale is None else sm_scale, window, sinks, _ptr(workspace), 0 if workspace is None else workspace.nbytes,
+        out.data_ptr(), _rows(cache, out, layer_count, cache.n_q_heads, n), _stream(stream))
+    if st != OK:
+        raise OkqError(st, "okq_paged_attention_window")
+
+
+def _seen(cache, seen, n):
+    assert seen.dtype in (torch.int64, torch.uint64) and seen.shape == (cache.batch, n, (n + 63) // 64) and seen.is_contiguous()
+    return seen.data_ptr()
+
+
+def paged_attention_tree(cache: PagedCache, layer: int, layer_count: int, q, workspace, out, seen, q_len=None, rope=None, sm_scale=None, stream=None):
+    """paged_attention of each sequence's newest n_new (q_len[b]) tokens as nodes of a tree: query i sees what was there before the nodes, and
+    node j where bit j % 64 of seen[b, i, j // 64] is set.  seen: int64 [batch, n_new, ceil(n_new / 64)], as tree_ancestors makes it."""
+    _here(cache.codes, q, workspace, out, seen, q_len, None if rope is None else rope.positions)
+    n = q.shape[3]
+    assert q_len is None or (q_len.dtype == torch.int32 and q_len.is_contiguous() and q_len.numel() == cache.batch)
+    st = (_lib or lib()).okq_paged_attention_tree(
+        cache.ref, layer, layer_count, q.data_ptr(), _rows(cache, q, layer_count, cache.n_q_heads, n), n, _ptr(q_len), _rope_ref(rope, cache.batch, n),
+        HEAD_DIM ** -0.5 if sm_scale is None else sm_scale, _seen(cache, seen, n), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
+        out.data_ptr(), _rows(cache, out, layer_count, cache.n_q_heads, n), _stream(stream))
+    if st != OK:
+        raise OkqError(st, "okq_paged_attention_tree")
+
+
+def tree_ancestors(cache: PagedCache, parents, seen, depth=None, q_len=None, stream=None):
+    """parents: int32 [batch, n_new], each a node before its own or -1.  Writes the bits of every node's ancestors and its own into seen
+    (int64 [batch, n_new, ceil(n_new / 64)]) and the number of its ancestors into depth (int32 [batch, n_new])."""
+    _here(cache.codes, parents, seen, depth, q_len)
+    n = parents.shape[1]
+    assert parents.shape[0] == cache.batch and (depth is None or (depth.shape == parents.shape and depth.dtype == torch.int32 and depth.is_contiguous()))
+    assert q_len is None or (q_len.dtype == torch.int32 and q_len.is_contiguous() and q_len.numel() == cache.batch)
+    _check((_lib or lib()).okq_tree_ancestors(cache.ref, _indices(parents), n, _ptr(q_len), _seen(cache, seen, n), _ptr(depth), _stream(stream)),
+           "okq_tree_ancestors")
+
+
 def debug_paged_timeout(cache: PagedCache, layer: int, layer_count: int, q, workspace, out, limit_clocks: int = 20_000_000, stream=None):
     """okq_debug_paged_timeout: paged_attention with nothing delivered and waits limited to `limit_clocks` SM clocks (testing aid)."""
     _here(cache.codes, q, workspace, out)
@@ -726,6 +781,11 @@ PLAN_LINE, PLAN_PROMPT = -1, -2
 def paged_plan(cache: PagedCache, layer_count: int, n_new: int = 1) -> int:
     """okq_debug_paged_plan: which kernel a paged_attention call would take."""
     return lib().okq_debug_paged_plan(cache.ref, layer_count, n_new)
+
+
+def paged_plan_window(cache: PagedCache, layer_count: int, n_new: int, window: int, sinks: int = 0) -> int:
+    """okq_debug_paged_plan_window: as paged_plan, for paged_attention_window."""
+    return lib().okq_debug_paged_plan_window(cache.ref, layer_count, n_new, window, sinks)
 
 
 def _indices(x, n=None):
@@ -750,6 +810,12 @@ def pages_release(cache: PagedCache, seqs, stream=None):
     """seqs: int32 [count]; the sequences become empty, pages that no other shares become free."""
     _here(cache.codes, seqs)
     _check(lib().okq_pages_release(cache.ref, _indices(seqs), seqs.numel(), _stream(stream)), "okq_pages_release")
+
+
+def pages_slide(cache: PagedCache, window: int, sinks: int = 0, dropped=None, stream=None):
+    """Gives back the pages that no coming token sees with this window and these sinks; dropped: int32 [batch], tokens that each sequence lost."""
+    _here(cache.codes, dropped)
+    _check((_lib or lib()).okq_pages_slide(cache.ref, window, sinks, 0 if dropped is None else _indices(dropped, cache.batch), _stream(stream)), "okq_pages_slide")
 
 
 def pages_copy(cache: PagedCache, src, dst, stream=None):

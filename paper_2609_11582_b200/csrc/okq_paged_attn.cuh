@@ -16,6 +16,10 @@ namespace okq {
 
 constexpr int PT = 128;   // tokens of a tile
 
+// Which of the tokens up to its own a query sees: all; the last `window` and the first `sinks`; those before the drafted tree and the nodes
+// that its bits name.  A template argument of the kernels, so that the first is what it would be without the others.
+enum Sight { CAUSAL, WINDOW, TREE };
+
 // Wait of a whole warp for one phase of an mbarrier: one look first, since most phases are complete when they are asked for and the
 // bounded wait's clock and abort flag cost a hundred cycles.
 template <class SM> __device__ __forceinline__ bool bar_wait(SM& sm, unsigned long long* bar, uint32_t parity) {
@@ -47,10 +51,21 @@ struct AttnArgs {
   int withhold;     // testing aid: the first tile of every range is never delivered, so that the waits for it run out
   struct Head* heads;   // [Heads::count]
   float* slots;         // [2 * ranges][ROWS * (128 + 2)]: sums, maxima, normalisers
+  int window, sinks;                    // WINDOW
+  const unsigned long long* seen;       // TREE: [batch][n_new][words]
+  int words;
 };
 
-// tiles that an item reads: those up to the last token that its last row sees
-template <int ROWS, int EXTRA> struct Work {
+// n lowest bits of 64
+__device__ __forceinline__ unsigned long long low_bits(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
+
+// Tiles that an item reads: those up to the last token that its last row sees, all of the sequence's for a tree (bits are in any order).  With
+// a window those between the sinks and the first token that its first row sees by the window are left out: an item's tiles are numbered
+// without them, `head` of them lie before the gap.
+struct Span {
+  int nt, head, gap;
+};
+template <int ROWS, int EXTRA, int SIGHT = CAUSAL> struct Work {
   int pairs, n_kv, group;
   const AttnArgs& a;
   __device__ __forceinline__ explicit Work(const AttnArgs& args) : pairs(args.layer_count * args.c.batch), n_kv(args.c.n_kv), group(args.c.group), a(args) {}
@@ -65,7 +80,20 @@ template <int ROWS, int EXTRA> struct Work {
     lens(li, pair - li * a.c.batch, len, m);
   }
   __device__ __forceinline__ int row_tiles(int m) const { return (m * group + ROWS - 1) / ROWS; }
+  // first token that the item's first row sees by the window (or a negative number)
+  __device__ __forceinline__ int window_from(int len, int m, int rt) const { return max(0, len - m + a.c.query_of(rt * ROWS)) - a.window + 1; }
+  __device__ __forceinline__ Span span(int len, int m, int rt) const {
+    const int last = a.c.query_of(min(m * group, (rt + 1) * ROWS) - 1), seen = SIGHT == TREE ? len : len - m + last + 1;
+    Span s{seen <= 0 ? 0 : (seen + PT - 1) / PT, 0, 0};
+    if (SIGHT == WINDOW && s.nt > 0) {
+      s.head = (min(a.sinks, seen) + PT - 1) / PT;
+      s.gap = max(0, max(0, window_from(len, m, rt)) / PT - s.head);
+      s.nt -= s.gap;
+    }
+    return s;
+  }
   __device__ __forceinline__ int tiles(int len, int m, int rt) const {
+    if (SIGHT != CAUSAL) return span(len, m, rt).nt;
     const int last = a.c.query_of(min(m * group, (rt + 1) * ROWS) - 1);   // query of the last row
     const int seen = len - m + last + 1;
     return seen <= 0 ? 0 : (seen + PT - 1) / PT;
@@ -79,29 +107,44 @@ template <int ROWS, int EXTRA> struct Work {
 };
 
 // A walk over the tiles of a range.
-template <int ROWS, int EXTRA> struct Cursor {
+template <int ROWS, int EXTRA, int SIGHT = CAUSAL> struct Cursor {
   int pair, h, rt, tile;     // item and tile inside it
   int li, b;                 // layer (of the call's) and sequence of the pair
   int len, m, nt;            // of the item: tokens, queries, tiles
+  int head, gap;             // WINDOW: Span's
   int left;                  // units of the range from this tile on
   bool ok, ended;            // there is a tile here; the tile before was its item's last
-  __device__ __forceinline__ void next_item(const Work<ROWS, EXTRA>& w) {
+  // number of the item's tile i among the sequence's
+  __device__ __forceinline__ int at(int i) const { return SIGHT == WINDOW && i >= head ? i + gap : i; }
+  __device__ __forceinline__ void measure(const Work<ROWS, EXTRA, SIGHT>& w) {
+    if (SIGHT != WINDOW) {
+      nt = w.tiles(len, m, rt);
+    } else {
+      const Span s = w.span(len, m, rt);
+      nt = s.nt;
+      head = s.head;
+      gap = s.gap;
+    }
+  }
+  __device__ __forceinline__ void next_item(const Work<ROWS, EXTRA, SIGHT>& w) {
     tile = 0;
     for (;;) {
-      if (++rt < w.row_tiles(m)) nt = w.tiles(len, m, rt);
-      else if (rt = 0, ++h < w.n_kv) nt = m ? w.tiles(len, m, 0) : 0;
-      else {
+      nt = 0;
+      if (++rt < w.row_tiles(m)) measure(w);
+      else if (rt = 0, ++h < w.n_kv) {
+        if (m) measure(w);
+      } else {
         h = 0;
         if (++pair >= w.pairs) { ok = false; return; }
         if (++b == w.a.c.batch) { b = 0; li++; }
         w.lens(li, b, len, m);
-        nt = m ? w.tiles(len, m, 0) : 0;
+        if (m) measure(w);
       }
       if (nt > 0) return;
     }
   }
   __device__ __forceinline__ int piece() const { return min(nt - tile, left); }   // tiles of the item in the range, from this one on
-  __device__ __forceinline__ void skip(const Work<ROWS, EXTRA>& w, int n) {       // no more than piece()
+  __device__ __forceinline__ void skip(const Work<ROWS, EXTRA, SIGHT>& w, int n) {       // no more than piece()
     tile += n;
     left -= n;
     ended = tile == nt;
@@ -109,7 +152,7 @@ template <int ROWS, int EXTRA> struct Cursor {
     ok = left > 0;
     if (ended && ok) next_item(w);
   }
-  __device__ __forceinline__ void next(const Work<ROWS, EXTRA>& w) { skip(w, 1); }
+  __device__ __forceinline__ void next(const Work<ROWS, EXTRA, SIGHT>& w) { skip(w, 1); }
 };
 
 // The line of `total` units in `ranges` parts, as even as they go: the first `extra` of them have one unit more.  With fewer units than
@@ -131,8 +174,8 @@ template <int G> struct FindSmem {
   int warp[32];
   int place[G][6];
 };
-template <int ROWS, int EXTRA, int NT, int G>
-__device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS, EXTRA>& w, int ranges, int v0, int step) {
+template <int ROWS, int EXTRA, int NT, int G, int SIGHT>
+__device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS, EXTRA, SIGHT>& w, int ranges, int v0, int step) {
   const int tid = threadIdx.x, lane = tid & 31, wp = tid >> 5;
   const int chunk = (w.pairs + NT - 1) / NT, p0 = min(w.pairs, tid * chunk), p1 = min(w.pairs, p0 + chunk);
   int len = 0, m = 0, per_head = 0, mine = 0;    // (of the last pair looked at: with no more pairs than threads, the only one)
@@ -181,16 +224,16 @@ __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS, EX
   return cuts;
 }
 // the first tile of range v = v0 + g * step
-template <int ROWS, int EXTRA, int G>
-__device__ __forceinline__ Cursor<ROWS, EXTRA> place(const FindSmem<G>& sm, const Work<ROWS, EXTRA>& w, const Cuts& cuts, int v, int g) {
-  Cursor<ROWS, EXTRA> c{};
+template <int ROWS, int EXTRA, int G, int SIGHT>
+__device__ __forceinline__ Cursor<ROWS, EXTRA, SIGHT> place(const FindSmem<G>& sm, const Work<ROWS, EXTRA, SIGHT>& w, const Cuts& cuts, int v, int g) {
+  Cursor<ROWS, EXTRA, SIGHT> c{};
   c.left = cuts.size(v);
   c.ok = c.left > 0;
   if (!c.ok) return c;
   c.pair = sm.place[g][0]; c.h = sm.place[g][1]; c.rt = sm.place[g][2]; c.tile = sm.place[g][3]; c.len = sm.place[g][4]; c.m = sm.place[g][5];
   c.li = w.layer_of(c.pair);
   c.b = c.pair - c.li * w.a.c.batch;
-  c.nt = w.tiles(c.len, c.m, c.rt);
+  c.measure(w);
   if (c.tile >= c.nt) {   // behind an item's last tile
     c.left -= c.nt + EXTRA - c.tile;
     c.ok = c.left > 0;
@@ -224,8 +267,8 @@ template <int ROWS> struct Heads {
 };
 
 // Zeros for the rows of items without tiles (queries that see nothing), and the heads of these items.  `who` of `n_who` warps.
-template <class T, int ROWS, int EXTRA>
-__device__ __forceinline__ void write_empty(const AttnArgs& a, const Work<ROWS, EXTRA>& w, const Heads<ROWS>& heads, int who, int n_who, int lane) {
+template <class T, int ROWS, int EXTRA, int SIGHT>
+__device__ __forceinline__ void write_empty(const AttnArgs& a, const Work<ROWS, EXTRA, SIGHT>& w, const Heads<ROWS>& heads, int who, int n_who, int lane) {
   for (int pair = who; pair < w.pairs; pair += n_who) {
     int len, m;
     const int li = w.layer_of(pair), b = pair - li * a.c.batch;
@@ -339,12 +382,12 @@ template <class T, int ROWS> inline cudaError_t launch_merge(const AttnArgs& a, 
 // okq_paged_decode.cu: DECODE_ROWS rows to an item, DECODE_PIPES pipelines per block.  An item's own costs (queries, the first tile's
 // latency, the output) in tiles, as measured: 64 sequences x 8 heads of up to 1500 tokens, 24 rows, 93 us with 1, 75 with 2, 71 with 3.
 constexpr int DECODE_ROWS = 8, DECODE_PIPES = 3, DECODE_EXTRA = 3;
-cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int blocks, int cluster, cudaStream_t s);   // cluster 0: ranges of the line, merge
+cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, Sight sight, int blocks, int cluster, cudaStream_t s);   // cluster 0: ranges of the line, merge
 int decode_clusters(int size);   // clusters of so many blocks (at most eight) that run at once
 // okq_paged_prompt.cu: PROMPT_ROWS rows to an item, one pipeline per block.  Own costs alike: 16 sequences x 4 heads of up to 12345 tokens,
 // 35 rows 62 us with 3, 58 with 4, 55 with 6, 56 with 8; 64 x 8 of up to 1500, 1024 rows, 555, 511, 462, 482.
 constexpr int PROMPT_ROWS = 256, PROMPT_EXTRA = 6;
-cudaError_t launch_paged_prompt(const AttnArgs& a, int dtype, int grid, cudaStream_t s);
+cudaError_t launch_paged_prompt(const AttnArgs& a, int dtype, Sight sight, int grid, cudaStream_t s);
 
 // the pool's codes as rows of 128 bytes, copied 32 at a time
 inline bool codes_map(CUtensorMap& map, const PagedView& c, bool swizzled) {

@@ -110,8 +110,8 @@ __device__ __forceinline__ void lane_sums(const float (&x)[R], float* to, int la
 
 // Two of an item's rows, r0 and r0 + 1: limbs (swizzled) and scales.  One warp, four channels per lane.  `turns`: cosines and sines of
 // the item's queries, [query from the first on][64 pairs].
-template <class T>
-__device__ __forceinline__ void prepare_queries(const AttnArgs& a, const Cursor<R, EXTRA>& cur, int r0, const uint2 (&raw)[2], const float2* turns, int8_t* qbuf,
+template <class T, class Cur>
+__device__ __forceinline__ void prepare_queries(const AttnArgs& a, const Cur& cur, int r0, const uint2 (&raw)[2], const float2* turns, int8_t* qbuf,
                                                 float* qscale, int lane) {
   const int step = a.rope.half >> 2;   // lanes from a channel to its partner
   const bool turned = a.rope.freq && lane < 2 * step, low = lane < step;
@@ -159,7 +159,7 @@ __device__ __forceinline__ void prepare_queries(const AttnArgs& a, const Cursor<
 
 // CLUSTER: every (layer, sequence, KV head) has a cluster of `size` blocks, whose pipelines share its tiles evenly, and its parts are put
 // together in the cluster's shared memory: one launch.  Otherwise pipelines have even ranges of the whole line and k_paged_merge follows.
-template <class T, bool CLUSTER>
+template <class T, bool CLUSTER, int SIGHT>
 __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ CUtensorMap map, const AttnArgs a, int size) {
   extern __shared__ unsigned char raw_smem[];
   DecodeSmem& sm = *reinterpret_cast<DecodeSmem*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~(uintptr_t)1023);
@@ -193,11 +193,11 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
   depend_wait();
 
   const PagedView& c = a.c;
-  const Work<R, EXTRA> work(a);
+  const Work<R, EXTRA, SIGHT> work(a);
   const Heads<R> heads(work.pairs, c.n_kv, c.group, a.n_new, G * gridDim.x);
   Cuts cuts(0, 1);
   int v = 0, end = 0;            // this pipeline's range of the line, and the unit behind it
-  Cursor<R, EXTRA> cur{};
+  Cursor<R, EXTRA, SIGHT> cur{};
   int rank = 0;
   if (CLUSTER) {   // (grid (size x row tiles, heads, pairs): a division on the way to the first tile is felt)
     asm("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank));
@@ -207,16 +207,16 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     cur.li = work.layer_of(cur.pair);
     cur.b = cur.pair - cur.li * c.batch;
     work.lens(cur.li, cur.b, cur.len, cur.m);
-    cur.nt = cur.rt < work.row_tiles(cur.m) ? work.tiles(cur.len, cur.m, cur.rt) : 0;
+    if (cur.rt < work.row_tiles(cur.m)) cur.measure(work);   // (else none)
     const Cuts share(cur.nt, G * size);
     cur.tile = share.start(g * size + rank);
     cur.left = share.size(g * size + rank);
     cur.ok = cur.left > 0;
   } else {
-    cuts = find_places<R, EXTRA, NT, G>(sm.find, work, G * gridDim.x, blockIdx.x, gridDim.x);
+    cuts = find_places<R, EXTRA, NT, G, SIGHT>(sm.find, work, G * gridDim.x, blockIdx.x, gridDim.x);
     v = blockIdx.x + g * gridDim.x;
     end = cuts.start(v) + cuts.size(v);
-    cur = place<R, EXTRA, G>(sm.find, work, cuts, v, g);
+    cur = place<R, EXTRA, G, SIGHT>(sm.find, work, cuts, v, g);
   }
   const int rows = min(R, cur.m * c.group - R * cur.rt);   // (CLUSTER: of the item)
 
@@ -227,18 +227,22 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
     constexpr uint32_t id_o = shape | (1u << 7) | (1u << 15) | (1u << 16);                     // A signed, B unsigned, both MN-major
     // Blocks of the tiles to come, eight tiles at a time, a lane for each block: entries of the page table when the batch before
     // begins, their scales halfway through it, so that neither load is waited for.
-    Cursor<R, EXTRA> ahead = cur;      // first tile that has not been looked up
+    Cursor<R, EXTRA, SIGHT> ahead = cur;      // first tile that has not been looked up
     int n_now = 0, n_nx = 0;           // tiles of a batch
     int t_nx = 0, l_nx = 0, h_nx = 0, page_nx = -1;
     bool in_nx = false;
     Block now{-1, 0.f, 0.f}, nxt{-1, 0.f, 0.f};
     auto entries = [&] {
-      int b = 0, len = 0;
+      int b = 0, len = 0, from = 0;
       for (n_nx = 0; n_nx < 8 && ahead.ok; n_nx++) {
-        if (lane >> 2 == n_nx) { t_nx = ahead.tile * PT + PB * (lane & 3); len = ahead.len; l_nx = a.layer + ahead.li; b = ahead.b; h_nx = ahead.h; }
+        if (lane >> 2 == n_nx) {
+          t_nx = ahead.at(ahead.tile) * PT + PB * (lane & 3); len = ahead.len; l_nx = a.layer + ahead.li; b = ahead.b; h_nx = ahead.h;
+          if (SIGHT == WINDOW) from = work.window_from(len, ahead.m, ahead.rt);
+        }
         ahead.next(work);
       }
       in_nx = lane >> 2 < n_nx && t_nx < len;
+      if (SIGHT == WINDOW) in_nx = in_nx && (t_nx < a.sinks || t_nx + PB > from);   // (blocks that no row sees may have no page)
       if (in_nx) {
         const int j = t_nx >> c.page_shift;
         page_nx = __ldcg(&c.table[(size_t)b * c.max_pages + j]);   // (held() keeps j inside the row)
@@ -353,7 +357,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       // what is needed of this item when the cursor has gone on: its last tile's unit, its rows, and the token of the tile's first lane
       // counted from the first that the first query does not see
       const int li = cur.li, bq = cur.b, h = cur.h, rt = cur.rt, item_end = end - cur.left - cur.tile + cur.nt - 1;
-      const int rows = cur.m * c.group - R * rt, late = cur.tile * PT - (cur.len - cur.m + 1);
+      const int rows = cur.m * c.group - R * rt, late = cur.at(cur.tile) * PT - (cur.len - cur.m + 1);
       if (fresh) {   // (the products of the item before are through: their sums have been read)
         // rows, and the turns of the item's queries (at most eight) in the place of the numerators
         const int row = R * rt + 2 * role;
@@ -386,6 +390,34 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
         for (int r = 0; r < R; r++) sum[r] = o[r] = 0.f;
         top = -INFINITY;
       }
+      // the rows that see the lane's token, a bit each
+      unsigned sees = 0xffu;
+      if (SIGHT == WINDOW) {
+        const int base = cur.len - cur.m, t0 = late + base + 1, own = t0 + 32 * role + lane;
+        const int q0 = c.query_of(R * rt), q1 = c.query_of(R * rt + min(rows, R) - 1);
+        if (t0 + PT - 1 > base + q0 || (t0 + PT > a.sinks && t0 <= base + q1 - a.window)) {   // some row may not see all of the tile
+          sees = 0;
+#pragma unroll
+          for (int r = 0; r < R; r++) {
+            const int p = base + c.query_of(R * rt + r);
+            if (own <= p && (own < a.sinks || p - own < a.window)) sees |= 1u << r;
+          }
+        }
+      }
+      if (SIGHT == TREE && late + PT > -1) {   // the tile has nodes, or ends behind the sequence
+        const int node = late + 1 + 32 * role + lane;
+        if (node >= 0) {
+          sees = 0;
+          if (node < cur.m) {
+            unsigned long long bits[R];
+#pragma unroll
+            for (int r = 0; r < R; r++)
+              bits[r] = r < rows ? __ldcg(a.seen + ((size_t)bq * a.n_new + c.query_of(R * rt + r)) * a.words + (node >> 6)) : 0ull;
+#pragma unroll
+            for (int r = 0; r < R; r++) sees |= (unsigned)(bits[r] >> (node & 63) & 1ull) << r;
+          }
+        }
+      }
       cur.next(work);
       const bool last = cur.ended || !cur.ok;
       bar_wait(sm, &sy.full[s], (uint32_t)(i / NS) & 1u);   // (long complete: for the loader's scales)
@@ -405,7 +437,11 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
 #pragma unroll
         for (int r = 0; r < R; r++) x[r] = fmaf((float)d2[r], 65536.f, (float)(d1[r] * 256 + d0[r])) * (sy.qscale[r] * ks);
       }
-      if (late + PT > 0) {   // some row may not see all of the tile
+      if (SIGHT != CAUSAL) {
+#pragma unroll
+        for (int r = 0; r < R; r++)
+          if (!(sees >> r & 1u)) x[r] = -INFINITY;
+      } else if (late + PT > 0) {   // some row may not see all of the tile
 #pragma unroll
         for (int r = 0; r < R; r++)
           if (late + 32 * role + lane >= c.query_of(R * rt + r)) x[r] = -INFINITY;
@@ -576,18 +612,26 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
   asm volatile("barrier.cluster.wait.aligned;\n" ::: "memory");   // no block ends while its parts are read
 }
 
-template <class T, bool CLUSTER> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map, dim3 grid, int size, cudaStream_t s) {
+template <class T, bool CLUSTER, int SIGHT> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map, dim3 grid, int size, cudaStream_t s) {
   static thread_local unsigned long long attr_mask = 0;
   int dev = 0;
   constexpr int SMEM = (int)sizeof(DecodeSmem) + 1024;
   static_assert(SMEM <= 227 * 1024, "shared memory of one block");
   if (attr_needed(attr_mask, dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(k_paged_decode<T, CLUSTER>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(k_paged_decode<T, CLUSTER, SIGHT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
     if (e != cudaSuccess) return e;
     attr_done(attr_mask, dev);
   }
-  cudaError_t e = launch_dependent(k_paged_decode<T, CLUSTER>, grid, NT, SMEM, s, CLUSTER ? size : 1, map, a, size);
+  cudaError_t e = launch_dependent(k_paged_decode<T, CLUSTER, SIGHT>, grid, NT, SMEM, s, CLUSTER ? size : 1, map, a, size);
   return e == cudaSuccess && !CLUSTER ? launch_merge<T, R>(a, G * (int)grid.x, s) : e;
+}
+
+template <int SIGHT> cudaError_t launch_sight(const AttnArgs& a, const CUtensorMap& map, int dtype, int blocks, int cluster, cudaStream_t s) {
+  if (cluster > 0) {
+    const dim3 grid((unsigned)cluster * (unsigned)((a.n_new * a.c.group + R - 1) / R), (unsigned)a.c.n_kv, (unsigned)(a.layer_count * a.c.batch));
+    return dtype == OKQ_FP16 ? launch<__half, true, SIGHT>(a, map, grid, cluster, s) : launch<__nv_bfloat16, true, SIGHT>(a, map, grid, cluster, s);
+  }
+  return dtype == OKQ_FP16 ? launch<__half, false, SIGHT>(a, map, dim3(blocks), 1, s) : launch<__nv_bfloat16, false, SIGHT>(a, map, dim3(blocks), 1, s);
 }
 
 }  // namespace
@@ -609,8 +653,8 @@ int decode_clusters(int size) {
       cfg.attrs = at;
       cfg.numAttrs = 1;
       known[k] = 0;
-      if (cudaFuncSetAttribute(k_paged_decode<__half, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes) != cudaSuccess ||
-          cudaOccupancyMaxActiveClusters(&known[k], k_paged_decode<__half, true>, &cfg) != cudaSuccess)
+      if (cudaFuncSetAttribute(k_paged_decode<__half, true, CAUSAL>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes) != cudaSuccess ||
+          cudaOccupancyMaxActiveClusters(&known[k], k_paged_decode<__half, true, CAUSAL>, &cfg) != cudaSuccess)
         (void)cudaGetLastError();
     }
     known_dev = dev;
@@ -618,14 +662,12 @@ int decode_clusters(int size) {
   return known[size];
 }
 
-cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, int blocks, int cluster, cudaStream_t s) {
+cudaError_t launch_paged_decode(const AttnArgs& a, int dtype, Sight sight, int blocks, int cluster, cudaStream_t s) {
   CUtensorMap map;
   if (!codes_map(map, a.c, true)) return cudaErrorInvalidValue;
-  if (cluster > 0) {
-    const dim3 grid((unsigned)cluster * (unsigned)((a.n_new * a.c.group + R - 1) / R), (unsigned)a.c.n_kv, (unsigned)(a.layer_count * a.c.batch));
-    return dtype == OKQ_FP16 ? launch<__half, true>(a, map, grid, cluster, s) : launch<__nv_bfloat16, true>(a, map, grid, cluster, s);
-  }
-  return dtype == OKQ_FP16 ? launch<__half, false>(a, map, dim3(blocks), 1, s) : launch<__nv_bfloat16, false>(a, map, dim3(blocks), 1, s);
+  if (sight == WINDOW) return launch_sight<WINDOW>(a, map, dtype, blocks, cluster, s);
+  if (sight == TREE) return launch_sight<TREE>(a, map, dtype, blocks, cluster, s);
+  return launch_sight<CAUSAL>(a, map, dtype, blocks, cluster, s);
 }
 
 }  // namespace okq

@@ -148,8 +148,8 @@ __device__ __forceinline__ bool step_ready(PromptSmem& sm, const volatile int* d
 
 // The 32 rows of a warp in a row tile: rotated, scaled by a power of two, swizzled; returns the factor of the exponent that undoes the
 // scaling for the lane's own row (times the softmax scale, whose sign goes to the queries).  Eight lanes to a row, sixteen channels each.
-template <class T>
-__device__ __forceinline__ float prepare_queries(const AttnArgs& a, const Cursor<R, EXTRA>& cur, int row0, unsigned char* q, bool store, int lane) {
+template <class T, class Cur>
+__device__ __forceinline__ float prepare_queries(const AttnArgs& a, const Cur& cur, int row0, unsigned char* q, bool store, int lane) {
   const PagedView& c = a.c;
   const int rows = cur.m * c.group;
   const int j = lane & 7, nc = a.rope.half >> 3;
@@ -211,17 +211,55 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return y;
 }
 
-// The lane's row of a step's scores, two blocks of 32 tokens, b0 the tile's number of the first; `seen`: last column that the row sees.
+// Columns of a step that a row sees: up to one of them, or a bit for each.
+struct UpTo {
+  int last;
+  __device__ __forceinline__ bool sees(int col) const { return col <= last; }
+  __device__ __forceinline__ bool none_of(int block) const { return 32 * block > last; }
+  __device__ __forceinline__ bool all() const { return last >= PH - 1; }
+};
+struct Bits {
+  uint32_t half[2];
+  __device__ __forceinline__ Bits(unsigned long long b) : half{(uint32_t)b, (uint32_t)(b >> 32)} {}
+  __device__ __forceinline__ bool sees(int col) const { return half[col >> 5] >> (col & 31) & 1u; }
+  __device__ __forceinline__ bool none_of(int block) const { return half[block] == 0u; }
+  __device__ __forceinline__ bool all() const { return (half[0] & half[1]) == 0xffffffffu; }
+};
+
+// Of the step whose first token is t0.  `own`: the row's token; of a tree: the first node's.
+template <int SIGHT>
+__device__ __forceinline__ unsigned long long sight_bits(const AttnArgs& a, int t0, int own, const unsigned long long* row_bits, int len) {
+  if (SIGHT == WINDOW) {
+    const int last = own - t0, first = last - a.window + 1, sinks = a.sinks - t0;
+    if (last >= PH - 1 && (first <= 0 || sinks >= PH)) return ~0ull;
+    return low_bits(last + 1) & (~low_bits(first) | low_bits(sinks));
+  }
+  const int first = own - t0;
+  if (first >= PH) return ~0ull;
+  unsigned long long nodes = 0;
+  if (row_bits) {
+    if (first >= 0) {
+      nodes = __ldcg(row_bits) << first;
+    } else {
+      const int w = -first >> 6, s = -first & 63;
+      if (w < a.words) nodes = __ldcg(row_bits + w) >> s;
+      if (s && w + 1 < a.words) nodes |= __ldcg(row_bits + w + 1) << (64 - s);
+    }
+  }
+  return (low_bits(first) | nodes) & low_bits(len - t0);
+}
+
+// The lane's row of a step's scores, two blocks of 32 tokens, b0 the tile's number of the first; `seen`: the columns that the row sees.
 // The largest log2 of p w, 2^P_SHIFT times.
-template <bool EDGE>
-__device__ __forceinline__ float row_max(float (&x)[2][32], const Info& info, int b0, float back, int seen) {
+template <bool EDGE, class Seen>
+__device__ __forceinline__ float row_max(float (&x)[2][32], const Info& info, int b0, float back, const Seen& seen) {
   float mx = -INFINITY;
 #pragma unroll
   for (int b = 0; b < 2; b++) {
     if (EDGE) {
 #pragma unroll
       for (int e = 0; e < 32; e++)
-        if (32 * b + e > seen) x[b][e] = -INFINITY;
+        if (!seen.sees(32 * b + e)) x[b][e] = -INFINITY;
     }
     float y[4] = {x[b][0], x[b][1], x[b][2], x[b][3]};
 #pragma unroll
@@ -234,8 +272,8 @@ __device__ __forceinline__ float row_max(float (&x)[2][32], const Info& info, in
 // EDGE also rounds a score once before the reference is taken off, as the maximum is: the difference is exact then, where scores are so
 // large that an unrounded one could lie far above it (not by packed pairs: their product and sum were contracted to one rounding).  Blocks
 // without a value count in the normaliser alone.
-template <bool EDGE>
-__device__ __forceinline__ float numerators(const float (&x)[2][32], uint32_t s_at, const Info& info, int b0, float back, float ref, int seen, float l) {
+template <bool EDGE, class Seen>
+__device__ __forceinline__ float numerators(const float (&x)[2][32], uint32_t s_at, const Info& info, int b0, float back, float ref, const Seen& seen, float l) {
 #pragma unroll
   for (int b = 0; b < 2; b++) {
     const bool none = EDGE && (info.lost >> (4 + b0 + b) & 1);
@@ -255,8 +293,8 @@ __device__ __forceinline__ float numerators(const float (&x)[2][32], uint32_t s_
       }
       float p0 = ex2(z.x), p1 = ex2(z.y);
       if (EDGE) {   // (-inf times a scale of zero is NaN)
-        if (32 * b + 2 * e > seen) p0 = 0.f;
-        if (32 * b + 2 * e + 1 > seen) p1 = 0.f;
+        if (!seen.sees(32 * b + 2 * e)) p0 = 0.f;
+        if (!seen.sees(32 * b + 2 * e + 1)) p1 = 0.f;
       }
       sum[e & 1] = add2(sum[e & 1], f2(p0, p1));
       const __half2 h = __floats2half2_rn(p0, p1);
@@ -264,13 +302,13 @@ __device__ __forceinline__ float numerators(const float (&x)[2][32], uint32_t s_
     }
     const float2 total = un2(add2(sum[0], sum[1]));
     l = fmaf(total.x + total.y, info.iw[b0 + b], l);
-    if (EDGE && (info.lost >> (b0 + b) & 1) && 32 * b <= seen) l = NAN;
+    if (EDGE && (info.lost >> (b0 + b) & 1) && !seen.none_of(b)) l = NAN;
     tmem_st16(s_at + 16u * b, u);
   }
   return l;
 }
 
-template <class T>
+template <class T, int SIGHT>
 __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ CUtensorMap map, const AttnArgs a) {
   extern __shared__ unsigned char raw_smem[];
   PromptSmem& sm = *reinterpret_cast<PromptSmem*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~(uintptr_t)1023);
@@ -300,28 +338,32 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
   depend_wait();
 
   const PagedView& c = a.c;
-  const Work<R, EXTRA> work(a);
+  const Work<R, EXTRA, SIGHT> work(a);
   const int v = blockIdx.x;                     // this block's range
-  const Cuts cuts = find_places<R, EXTRA, NT, 1>(sm.find, work, gridDim.x, v, 0);
+  const Cuts cuts = find_places<R, EXTRA, NT, 1, SIGHT>(sm.find, work, gridDim.x, v, 0);
   const int end = cuts.start(v) + cuts.size(v); // the unit behind it
   const Heads<R> heads(work.pairs, c.n_kv, c.group, a.n_new, gridDim.x);
-  Cursor<R, EXTRA> cur = place<R, EXTRA, 1>(sm.find, work, cuts, v, 0);
+  Cursor<R, EXTRA, SIGHT> cur = place<R, EXTRA, 1, SIGHT>(sm.find, work, cuts, v, 0);
 
   if (warp == W_LOAD) {
     // ------------------------------------------------------------------ loader: blocks of the tiles to come, as in the decode kernel
-    Cursor<R, EXTRA> ahead = cur;
+    Cursor<R, EXTRA, SIGHT> ahead = cur;
     int n_now = 0, n_nx = 0;
     int t_nx = 0, l_nx = 0, h_nx = 0, page_nx = -1;
     bool in_nx = false;
     int row_now = -1, row_nx = -1;               // -1: nothing to copy
     float ks_now = 0.f, vs_now = 0.f, ks_nx = 0.f, vs_nx = 0.f;
     auto entries = [&] {
-      int b = 0, len = 0;
+      int b = 0, len = 0, from = 0;
       for (n_nx = 0; n_nx < 8 && ahead.ok; n_nx++) {
-        if (lane >> 2 == n_nx) { t_nx = ahead.tile * PT + PB * (lane & 3); len = ahead.len; l_nx = a.layer + ahead.li; b = ahead.b; h_nx = ahead.h; }
+        if (lane >> 2 == n_nx) {
+          t_nx = ahead.at(ahead.tile) * PT + PB * (lane & 3); len = ahead.len; l_nx = a.layer + ahead.li; b = ahead.b; h_nx = ahead.h;
+          if (SIGHT == WINDOW) from = work.window_from(len, ahead.m, ahead.rt);
+        }
         ahead.next(work);
       }
       in_nx = lane >> 2 < n_nx && t_nx < len;
+      if (SIGHT == WINDOW) in_nx = in_nx && (t_nx < a.sinks || t_nx + PB > from);   // (blocks that no row sees may have no page)
       if (in_nx) page_nx = __ldcg(&c.table[(size_t)b * c.max_pages + (t_nx >> c.page_shift)]);
     };
     auto scales = [&] {
@@ -507,21 +549,28 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       {
         // (what the loop keeps in registers besides 64 scores: as little as can be)
         int seen = cur.len - cur.m + c.query_of(cur.rt * R + row) - cur.tile * PT - (dual ? PH * t : 0);   // last column of the step that the row sees
+        const unsigned long long* row_bits = nullptr;
+        if (SIGHT == TREE && row < rows) row_bits = a.seen + ((size_t)cur.b * a.n_new + c.query_of(cur.rt * R + row)) * a.words;
+        if (SIGHT == WINDOW) seen = cur.len - cur.m + c.query_of(cur.rt * R + row);   // (the row's token)
         int half = dual ? t : 0, tile = i;
         bool wide = false;
         for (int y = 0; y < steps; y++) {
           const uint32_t p_at = s_at + 64u * (y & 1);
           if (dual || !half) bar_wait(sm, &sm.info_full[tile & 3], (uint32_t)(tile >> 2) & 1u);
           const Info& info = sm.info[tile & 3];
+          const auto sight = [&] {
+            if constexpr (SIGHT == CAUSAL) return UpTo{seen};
+            else return Bits(sight_bits<SIGHT>(a, cur.at(cur.tile + tile - i) * PT + PH * half, SIGHT == TREE ? cur.len - cur.m : seen, row_bits, cur.len));
+          }();
           bar_wait(sm, &sm.s_full[t][y & 1], ph_s >> (y & 1) & 1u);
           ph_s ^= 1u << (y & 1);
           after_sync();
           float x[2][32];
           tmem_ld32(p_at, x[0]);
           tmem_ld32(p_at + 32u, x[1]);
-          const bool edge = __any_sync(0xffffffffu, seen < PH - 1) || info.lost;
+          const bool edge = __any_sync(0xffffffffu, !sight.all()) || info.lost;
           tmem_wait_ld();
-          const float mx = edge ? row_max<true>(x, info, 2 * half, back, seen) : row_max<false>(x, info, 2 * half, back, seen);
+          const float mx = edge ? row_max<true>(x, info, 2 * half, back, sight) : row_max<false>(x, info, 2 * half, back, sight);
           // a new reference: the row's sums so far are multiplied, once their last product is through
           const float below = m - mx;   // (-inf for the first; inf or NaN for steps that the row does not see)
           if (__any_sync(0xffffffffu, fabsf(below - (DROP / 2 - P_SHIFT)) > DROP / 2 && below < FALL)) {
@@ -551,7 +600,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
           }
           const float ref = m == -INFINITY ? 0.f : m;
           if (!dual) take_turn(2 + 4 * t + quarter);
-          l = edge || wide ? numerators<true>(x, p_at, info, 2 * half, back, ref, seen, l) : numerators<false>(x, p_at, info, 2 * half, back, ref, seen, l);
+          l = edge || wide ? numerators<true>(x, p_at, info, 2 * half, back, ref, sight, l) : numerators<false>(x, p_at, info, 2 * half, back, ref, sight, l);
           if (!dual) pass_turn(2 + 4 * (t ^ 1) + quarter);
           tmem_wait_st();
           before_sync();
@@ -562,11 +611,11 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
           if (lane == 0) mbar_arrive(&sm.p_full[t][y & 1]);
           if (dual) {
             tile++;
-            seen -= PT;
+            if (SIGHT == CAUSAL) seen -= PT;
           } else {
             tile += half;
             half ^= 1;
-            seen -= PH;
+            if (SIGHT == CAUSAL) seen -= PH;
           }
         }
       }
@@ -663,26 +712,32 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
   if (warp == 0 && !sm.tmem_busy) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
 }
 
-template <class T> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map, int grid, cudaStream_t s) {
+template <class T, int SIGHT> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map, int grid, cudaStream_t s) {
   static thread_local unsigned long long attr_mask = 0;
   int dev = 0;
   constexpr int SMEM = (int)sizeof(PromptSmem) + 1024;
   static_assert(SMEM <= 227 * 1024, "shared memory of one block");
   if (attr_needed(attr_mask, dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(k_paged_prompt<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(k_paged_prompt<T, SIGHT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
     if (e != cudaSuccess) return e;
     attr_done(attr_mask, dev);
   }
-  cudaError_t e = launch_dependent(k_paged_prompt<T>, dim3(grid), NT, SMEM, s, 1, map, a);
+  cudaError_t e = launch_dependent(k_paged_prompt<T, SIGHT>, dim3(grid), NT, SMEM, s, 1, map, a);
   return e == cudaSuccess ? launch_merge<T, R>(a, grid, s) : e;
+}
+
+template <int SIGHT> cudaError_t launch_sight(const AttnArgs& a, const CUtensorMap& map, int dtype, int grid, cudaStream_t s) {
+  return dtype == OKQ_FP16 ? launch<__half, SIGHT>(a, map, grid, s) : launch<__nv_bfloat16, SIGHT>(a, map, grid, s);
 }
 
 }  // namespace
 
-cudaError_t launch_paged_prompt(const AttnArgs& a, int dtype, int grid, cudaStream_t s) {
+cudaError_t launch_paged_prompt(const AttnArgs& a, int dtype, Sight sight, int grid, cudaStream_t s) {
   CUtensorMap map;
   if (!codes_map(map, a.c, false)) return cudaErrorInvalidValue;
-  return dtype == OKQ_FP16 ? launch<__half>(a, map, grid, s) : launch<__nv_bfloat16>(a, map, grid, s);
+  if (sight == WINDOW) return launch_sight<WINDOW>(a, map, dtype, grid, s);
+  if (sight == TREE) return launch_sight<TREE>(a, map, dtype, grid, s);
+  return launch_sight<CAUSAL>(a, map, dtype, grid, s);
 }
 
 }  // namespace okq

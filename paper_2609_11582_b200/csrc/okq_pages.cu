@@ -321,6 +321,55 @@ __global__ void __launch_bounds__(CT) k_pages_release(const PagedView c, const i
   for (int l = threadIdx.x; l < c.n_layers; l += CT) c.seq_len[(size_t)l * c.batch + b] = 0;
 }
 
+// takes a table's entry out of the count of its page
+__device__ __forceinline__ void give_up(const PagedView& c, int p) {
+  if (p < 0) return;
+  if (p >= c.n_pages) { set_status(c.status, OKQ_ERR_INVALID_ARG); return; }
+  if (atomicSub(&c.refs[p], 1) <= 0) {                                     // counts that do not match the tables
+    atomicAdd(&c.refs[p], 1);
+    set_status(c.status, OKQ_ERR_INVALID_ARG);
+  }
+}
+
+// One block per sequence: its entries [first, first + gone) are given up, those behind them move down, 4 * CT at a time (a thread's reads
+// are through before any entry that they come from is overwritten: entries move towards the front, a barrier between a chunk's reads
+// and its writes).
+__global__ void __launch_bounds__(CT) k_pages_slide(const PagedView c, int window, int sinks, int32_t* dropped) {
+  __shared__ int least[CT / 32];
+  depend_wait();
+  const int b = blockIdx.x, tid = threadIdx.x;
+  int len = c.room();
+  for (int l = tid; l < c.n_layers; l += CT) len = min(len, c.held(l, b));
+  len = __reduce_min_sync(0xffffffffu, len);
+  if ((tid & 31) == 0) least[tid >> 5] = len;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < CT / 32; i++) len = min(len, least[i]);
+  const int first = (int)(((long long)sinks + c.page - 1) >> c.page_shift);
+  const int gone = max(0, (max(0, len - window + 1) >> c.page_shift) - first);
+  if (dropped && tid == 0) dropped[b] = gone << c.page_shift;
+  if (gone == 0) return;
+  int32_t* row = c.table + (size_t)b * c.max_pages;
+  for (int j = first + tid; j < first + gone; j += CT) give_up(c, __ldcg(&row[j]));
+  __syncthreads();
+  for (int j0 = first; j0 < c.max_pages; j0 += PER * CT) {
+    int e[PER];
+#pragma unroll
+    for (int i = 0; i < PER; i++) {
+      const int j = j0 + i * CT + tid;
+      e[i] = j < c.max_pages - gone ? __ldcg(&row[j + gone]) : -1;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; i++) {
+      const int j = j0 + i * CT + tid;
+      if (j < c.max_pages) row[j] = e[i];
+    }
+    __syncthreads();
+  }
+  for (int l = tid; l < c.n_layers; l += CT) c.seq_len[(size_t)l * c.batch + b] = c.held(l, b) - (gone << c.page_shift);
+}
+
 // grid (pairs, layers, parts)
 __global__ void __launch_bounds__(CT) k_pages_copy(const PagedView c, const int32_t* src, const int32_t* dst, int count) {
   depend_wait();
@@ -458,6 +507,16 @@ okq_status okq_pages_release(const okq_paged* cache, const int32_t* seqs, int32_
   if (reinterpret_cast<uintptr_t>(seqs) & 3) return OKQ_ERR_ALIGNMENT;
   if (count == 0) return OKQ_OK;
   const cudaError_t e = launch_dependent(k_pages_release, dim3(count), CT, 0, static_cast<cudaStream_t>(stream), 1, paged_view(cache), seqs);
+  return e != cudaSuccess ? failed(e) : launch_status();
+}
+
+okq_status okq_pages_slide(const okq_paged* cache, int32_t window, int32_t sinks, int32_t* dropped, void* stream) {
+  using namespace okq;
+  const okq_status st = check_paged(cache, true);
+  if (st != OKQ_OK) return st;
+  if (window <= 0 || sinks < 0) return OKQ_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(dropped) & 3) return OKQ_ERR_ALIGNMENT;
+  const cudaError_t e = launch_dependent(k_pages_slide, dim3(cache->batch), CT, 0, static_cast<cudaStream_t>(stream), 1, paged_view(cache), window, sinks, dropped);
   return e != cudaSuccess ? failed(e) : launch_status();
 }
 
