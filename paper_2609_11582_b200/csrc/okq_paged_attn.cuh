@@ -54,6 +54,7 @@ struct AttnArgs {
   int window, sinks;                    // WINDOW
   const unsigned long long* seen;       // TREE: [batch][n_new][words]
   int words;
+  int whole;                            // not CAUSAL: ranges are cut between items only, so that there are no parts
 };
 
 // n lowest bits of 64
@@ -143,13 +144,15 @@ template <int ROWS, int EXTRA, int SIGHT = CAUSAL> struct Cursor {
       if (nt > 0) return;
     }
   }
-  __device__ __forceinline__ int piece() const { return min(nt - tile, left); }   // tiles of the item in the range, from this one on
+  __device__ __forceinline__ int piece(const Work<ROWS, EXTRA, SIGHT>& w) const {   // tiles of the item in the range, from this one on
+    return SIGHT != CAUSAL && w.a.whole ? nt - tile : min(nt - tile, left);
+  }
   __device__ __forceinline__ void skip(const Work<ROWS, EXTRA, SIGHT>& w, int n) {       // no more than piece()
     tile += n;
     left -= n;
     ended = tile == nt;
     if (ended) left -= EXTRA;
-    ok = left > 0;
+    ok = left > 0 || (SIGHT != CAUSAL && w.a.whole && !ended);
     if (ended && ok) next_item(w);
   }
   __device__ __forceinline__ void next(const Work<ROWS, EXTRA, SIGHT>& w) { skip(w, 1); }
@@ -234,7 +237,7 @@ __device__ __forceinline__ Cursor<ROWS, EXTRA, SIGHT> place(const FindSmem<G>& s
   c.li = w.layer_of(c.pair);
   c.b = c.pair - c.li * w.a.c.batch;
   c.measure(w);
-  if (c.tile >= c.nt) {   // behind an item's last tile
+  if (c.tile >= c.nt || (SIGHT != CAUSAL && w.a.whole && c.tile > 0)) {   // behind an item's last tile, or where the range before goes on
     c.left -= c.nt + EXTRA - c.tile;
     c.ok = c.left > 0;
     if (c.ok) c.next_item(w);
@@ -287,11 +290,11 @@ __device__ __forceinline__ void write_empty(const AttnArgs& a, const Work<ROWS, 
 
 constexpr int MERGE_NT = 512;
 
-// Block (x, y): rows of the item of head x, if it is in parts.  WPR warps to a row, of which each has every WPR-th part, a lane four
-// channels.  Bound by latency: a few megabytes of parts at most; all of a part is loaded at once, seven parts in flight.
-template <class T, int ROWS, int WPR>
+// Block (x, y): row y of the item of head x, if it is in parts, each warp has every sixteenth part, a lane four channels.  Bound by latency:
+// a few megabytes of parts at most; all of a part is loaded at once, seven parts in flight.  (Of the decode kernel's parts.)
+template <class T, int ROWS>
 __global__ void __launch_bounds__(MERGE_NT) k_paged_merge(const AttnArgs a) {
-  constexpr int WARPS = MERGE_NT / 32;
+  constexpr int WARPS = MERGE_NT / 32, WPR = WARPS;
   __shared__ float4 sums[WARPS][32];
   __shared__ float2 stat[WARPS];
   depend_wait();
@@ -363,22 +366,6 @@ __global__ void __launch_bounds__(MERGE_NT) k_paged_merge(const AttnArgs a) {
             from_f<T>(l == 0.f ? 0.f : acc.w / l)};
   *reinterpret_cast<uint2*>(out_row<T>(a, li, b, hd.h, row) + 4 * lane) = *reinterpret_cast<const uint2*>(o);
 }
-template <class T, int ROWS, int WPR> inline cudaError_t launch_merge_by(const AttnArgs& a, int heads, cudaStream_t s) {
-  const long long rows = (long long)a.n_new * a.c.group;
-  const int most = (int)(rows < ROWS ? rows : ROWS), per = MERGE_NT / 32 / WPR;
-  return launch_dependent(k_paged_merge<T, ROWS, WPR>, dim3(heads, (most + per - 1) / per), MERGE_NT, 0, s, 1, a);
-}
-template <class T, int ROWS> inline cudaError_t launch_merge(const AttnArgs& a, int ranges, cudaStream_t s) {
-  const Heads<ROWS> heads(a.layer_count * a.c.batch, a.c.n_kv, a.c.group, a.n_new, ranges);
-  const int n = heads.count(ranges), parts = heads.items < ranges ? ranges / heads.items : 1;   // (of an item, were all alike)
-  if (ROWS <= 8) return launch_merge_by<T, ROWS, MERGE_NT / 32>(a, n, s);
-  // Warps to a row: more where one would load parts several times in a row, as long as the GPU holds them all at once (1 sequence of 32768
-  // tokens, 32 rows: 37 us with one warp to a row, 20 with sixteen; 16 heads of 8000 tokens, 256 rows: 52 with one, 60 with four).
-  const long long room = 4ll * sm_count() * (MERGE_NT / 32) / n, rows = (long long)a.n_new * a.c.group, most = rows < ROWS ? rows : ROWS;
-  if (parts >= 28 && 16 * most <= room) return launch_merge_by<T, ROWS, 16>(a, n, s);
-  return parts >= 15 && 4 * most <= room ? launch_merge_by<T, ROWS, 4>(a, n, s) : launch_merge_by<T, ROWS, 1>(a, n, s);
-}
-
 // okq_paged_decode.cu: DECODE_ROWS rows to an item, DECODE_PIPES pipelines per block.  An item's own costs (queries, the first tile's
 // latency, the output) in tiles, as measured: 64 sequences x 8 heads of up to 1500 tokens, 24 rows, 93 us with 1, 75 with 2, 71 with 3.
 constexpr int DECODE_ROWS = 8, DECODE_PIPES = 3, DECODE_EXTRA = 3;
@@ -387,6 +374,7 @@ int decode_clusters(int size);   // clusters of so many blocks (at most eight) t
 // okq_paged_prompt.cu: PROMPT_ROWS rows to an item, one pipeline per block.  Own costs alike: 16 sequences x 4 heads of up to 12345 tokens,
 // 35 rows 62 us with 3, 58 with 4, 55 with 6, 56 with 8; 64 x 8 of up to 1500, 1024 rows, 555, 511, 462, 482.
 constexpr int PROMPT_ROWS = 256, PROMPT_EXTRA = 6;
+constexpr double PROMPT_ITEM = 4.0, PROMPT_MERGE = 8.0;   // an item's own costs, and those of a merge with its parts, in tiles
 cudaError_t launch_paged_prompt(const AttnArgs& a, int dtype, Sight sight, int grid, cudaStream_t s);
 
 // the pool's codes as rows of 128 bytes, copied 32 at a time

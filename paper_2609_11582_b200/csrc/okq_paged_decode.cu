@@ -623,7 +623,10 @@ template <class T, bool CLUSTER, int SIGHT> cudaError_t launch(const AttnArgs& a
     attr_done(attr_mask, dev);
   }
   cudaError_t e = launch_dependent(k_paged_decode<T, CLUSTER, SIGHT>, grid, NT, SMEM, s, CLUSTER ? size : 1, map, a, size);
-  return e == cudaSuccess && !CLUSTER ? launch_merge<T, R>(a, G * (int)grid.x, s) : e;
+  if (e != cudaSuccess || CLUSTER) return e;
+  const int ranges = G * (int)grid.x, rows = a.n_new * a.c.group;
+  const Heads<R> heads(a.layer_count * a.c.batch, a.c.n_kv, a.c.group, a.n_new, ranges);
+  return launch_dependent(k_paged_merge<T, R>, dim3(heads.count(ranges), rows < R ? rows : R), MERGE_NT, 0, s, 1, a);
 }
 
 template <int SIGHT> cudaError_t launch_sight(const AttnArgs& a, const CUtensorMap& map, int dtype, int blocks, int cluster, cudaStream_t s) {

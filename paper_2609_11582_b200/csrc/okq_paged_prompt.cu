@@ -70,6 +70,7 @@ struct PromptSmem {
   // other step only and could take a phase for the one after the next
   __align__(8) volatile int done[2][2];
   float peak[2 * M];                               // [stream][row] maximum of the numerators so far, LEAD below the highest reference
+  signed char row_exp[M];                          // of a dual item's rows, from stream A for B
   FindSmem<1> find;
   uint32_t tmem_slot;
   long long limit;
@@ -146,60 +147,90 @@ __device__ __forceinline__ bool step_ready(PromptSmem& sm, const volatile int* d
   return __all_sync(0xffffffffu, ok);
 }
 
-// The 32 rows of a warp in a row tile: rotated, scaled by a power of two, swizzled; returns the factor of the exponent that undoes the
-// scaling for the lane's own row (times the softmax scale, whose sign goes to the queries).  Eight lanes to a row, sixteen channels each.
+// A warp's 32 rows of a row tile, eight lanes to a row and sixteen channels each.  Their numbers are copied, as they are, into the places that
+// the fp16 ones will have (both have 16 bits); a lane copies what it will turn itself, so that its own wait is enough.  All of it is in
+// flight at once, behind the end of the item before (loaded into registers two rows at a time the queries took 11000 to 17000 cycles of an
+// item's 40000).
+struct QueryPlace {
+  int c0, c1;      // first channels of both eights
+  bool turns;
+  __device__ __forceinline__ QueryPlace(const RopeView& rope, int lane) {
+    const int j = lane & 7, nc = rope.half >> 3;
+    turns = rope.freq && j < nc;
+    c0 = !rope.freq || j < nc ? 8 * j : 2 * rope.half + 16 * (j - nc);
+    c1 = !rope.freq ? c0 + 64 : j < nc ? c0 + rope.half : c0 + 8;
+  }
+  // of row r of the stream
+  __device__ __forceinline__ unsigned char* at(unsigned char* q, int r, int ch) const { return q + (ch >> 6) * Q_HALF + r * 128 + ((((ch & 63) >> 3) ^ (r & 7)) << 4); }
+};
 template <class T, class Cur>
-__device__ __forceinline__ float prepare_queries(const AttnArgs& a, const Cur& cur, int row0, unsigned char* q, bool store, int lane) {
-  const PagedView& c = a.c;
-  const int rows = cur.m * c.group;
-  const int j = lane & 7, nc = a.rope.half >> 3;
-  const bool turns = a.rope.freq && j < nc;
-  const int c0 = !a.rope.freq || j < nc ? 8 * j : 2 * a.rope.half + 16 * (j - nc);
-  const int c1 = !a.rope.freq ? c0 + 64 : j < nc ? c0 + a.rope.half : c0 + 8;
-  float mine = 0.f;
-#pragma unroll 2
-  for (int it = 0; it < 8; it++) {
-    const int rl = 4 * it + (lane >> 3), row = cur.rt * R + row0 + rl;    // row inside the warp, of the item's queries
-    Vec8<T> x[2] = {};
-    if (row < rows) {
-      const T* src = query_row<T>(a, cur.li, cur.b, cur.h, row);
-      x[0] = *reinterpret_cast<const Vec8<T>*>(src + c0);
-      x[1] = *reinterpret_cast<const Vec8<T>*>(src + c1);
-      if (turns) {
-        float cs[8], sn[8];
-        turns8(a.rope, a.rope.positions + (size_t)cur.b * a.n_new + c.query_of(row), (size_t)c.batch * a.n_new, c0, cs, sn);
+__device__ __forceinline__ void fetch_queries(const AttnArgs& a, const Cur& cur, int row0, unsigned char* q, int lane) {
+  const QueryPlace pl(a.rope, lane);
+  const int rows = cur.m * a.c.group;
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-          float u = to_f(x[0].v[e]), w = to_f(x[1].v[e]);
-          rotate_pair(u, w, cs[e], sn[e]);
-          x[0].v[e] = from_f<T>(u);
-          x[1].v[e] = from_f<T>(w);
-        }
+  for (int it = 0; it < 8; it++) {
+    const int rl = 4 * it + (lane >> 3), row = cur.rt * R + row0 + rl, r = (row0 & (M - 1)) + rl;
+    const int bytes = row < rows ? 16 : 0;   // (zeros for rows that the item does not have)
+    const T* src = query_row<T>(a, cur.li, cur.b, cur.h, bytes ? row : 0);
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(smem_u32(pl.at(q, r, pl.c0))), "l"(src + pl.c0), "r"(bytes) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(smem_u32(pl.at(q, r, pl.c1))), "l"(src + pl.c1), "r"(bytes) : "memory");
+  }
+}
+
+// The rows that fetch_queries copied: rotated, scaled by a power of two, whose exponent is returned for the lane's own row (the softmax
+// scale's sign goes to the queries).
+constexpr int ROW_ZERO = -128, ROW_NAN = 127;   // rows that are zeros here; with an infinity or NaN
+// the factor of the exponent that undoes the scaling, times the softmax scale
+__device__ __forceinline__ float back_of(int e2, float scale2) {
+  return e2 == ROW_NAN ? NAN : e2 == ROW_ZERO ? 0.f : __uint_as_float((uint32_t)(127 + e2) << 23) * fabsf(scale2);
+}
+template <class T, class Cur>
+__device__ __forceinline__ int prepare_queries(const AttnArgs& a, const Cur& cur, int row0, unsigned char* q, int lane) {
+  const PagedView& c = a.c;
+  const QueryPlace pl(a.rope, lane);
+  const int rows = cur.m * c.group;
+  int mine = ROW_ZERO;
+  asm volatile("cp.async.wait_all;\n" ::: "memory");
+#pragma unroll 1
+  for (int it = 0; it < 8; it++) {
+    if (cur.rt * R + row0 + 4 * it >= rows) break;   // (the same in all lanes)
+    const int rl = 4 * it + (lane >> 3), row = cur.rt * R + row0 + rl, r = (row0 & (M - 1)) + rl;    // row inside the warp, of the item's queries, of the stream
+    Vec8<T> x[2] = {*reinterpret_cast<const Vec8<T>*>(pl.at(q, r, pl.c0)), *reinterpret_cast<const Vec8<T>*>(pl.at(q, r, pl.c1))};
+    if (pl.turns && row < rows) {
+      float cs[8], sn[8];
+      turns8(a.rope, a.rope.positions + (size_t)cur.b * a.n_new + c.query_of(row), (size_t)c.batch * a.n_new, pl.c0, cs, sn);
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        float u = to_f(x[0].v[e]), w = to_f(x[1].v[e]);
+        rotate_pair(u, w, cs[e], sn[e]);
+        x[0].v[e] = from_f<T>(u);
+        x[1].v[e] = from_f<T>(w);
       }
     }
-    unsigned mx = 0;
+    // the largest magnitude, of two numbers at a time: without the sign they are in the order of their bits
+    const uint32_t* bits = reinterpret_cast<const uint32_t*>(x);
+    uint32_t top2 = bits[0] & 0x7fff7fffu;
 #pragma unroll
-    for (int e = 0; e < 16; e++) mx = max(mx, __float_as_uint(to_f(x[e >> 3].v[e & 7])) & 0x7fffffffu);
+    for (int e = 1; e < 8; e++) top2 = __vmaxu2(top2, bits[e] & 0x7fff7fffu);
 #pragma unroll
-    for (int d = 4; d >= 1; d >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+    for (int d = 4; d >= 1; d >>= 1) top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, d));
+    const unsigned short top1 = (unsigned short)max(top2 & 0xffffu, top2 >> 16);
+    const unsigned mx = __float_as_uint(to_f(*reinterpret_cast<const T*>(&top1)));
     // 2^-e brings the largest magnitude to [1, 2) (4 at the end of the range); rows too small for that, and those with an infinity or NaN, are zeros here
     const int e2 = min((int)(mx >> 23) - 127, 126);
     const bool fine = mx < 0x7f800000u && e2 > -100;
     const float up = fine ? __uint_as_float((uint32_t)(127 - e2) << 23) * (a.scale2 < 0.f ? -1.f : 1.f) : 0.f;
-    const float back = mx >= 0x7f800000u ? NAN : fine ? __uint_as_float((uint32_t)(127 + e2) << 23) * fabsf(a.scale2) : 0.f;
 #pragma unroll
     for (int z = 0; z < 2; z++) {
-      const int ch = z ? c1 : c0;
-      __half2 y[4];
+      uint32_t y[4];
 #pragma unroll
       for (int e = 0; e < 4; e++) {
-        const float u = to_f(x[z].v[2 * e]), w = to_f(x[z].v[2 * e + 1]);
-        y[e] = __floats2half2_rn(fine ? u * up : 0.f, fine ? w * up : 0.f);
+        const __half2 h = __floats2half2_rn(to_f(x[z].v[2 * e]) * up, to_f(x[z].v[2 * e + 1]) * up);
+        y[e] = fine ? *reinterpret_cast<const uint32_t*>(&h) : 0u;
       }
-      const int r = (row0 & (M - 1)) + rl;
-      if (store) *reinterpret_cast<uint4*>(q + (ch >> 6) * Q_HALF + r * 128 + ((((ch & 63) >> 3) ^ (r & 7)) << 4)) = *reinterpret_cast<const uint4*>(y);
+      *reinterpret_cast<uint4*>(pl.at(q, r, z ? pl.c1 : pl.c0)) = make_uint4(y[0], y[1], y[2], y[3]);
     }
-    const float got = __shfl_sync(0xffffffffu, back, 8 * (lane & 3));    // rows 4 it .. 4 it + 3 are in lanes 0, 8, 16, 24
+    const int got = __shfl_sync(0xffffffffu, mx >= 0x7f800000u ? ROW_NAN : fine ? e2 : ROW_ZERO, 8 * (lane & 3));    // rows 4 it .. 4 it + 3 are in lanes 0, 8, 16, 24
     if (lane >> 2 == it) mine = got;
   }
   return mine;
@@ -213,17 +244,20 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 
 // Columns of a step that a row sees: up to one of them, or a bit for each.
 struct UpTo {
+  static constexpr bool all_ways = true;   // steps that some row does not see all of take the long way
   int last;
   __device__ __forceinline__ bool sees(int col) const { return col <= last; }
   __device__ __forceinline__ bool none_of(int block) const { return 32 * block > last; }
   __device__ __forceinline__ bool all() const { return last >= PH - 1; }
 };
 struct Bits {
+  static constexpr bool all_ways = false;
   uint32_t half[2];
   __device__ __forceinline__ Bits(unsigned long long b) : half{(uint32_t)b, (uint32_t)(b >> 32)} {}
   __device__ __forceinline__ bool sees(int col) const { return half[col >> 5] >> (col & 31) & 1u; }
   __device__ __forceinline__ bool none_of(int block) const { return half[block] == 0u; }
   __device__ __forceinline__ bool all() const { return (half[0] & half[1]) == 0xffffffffu; }
+  __device__ __forceinline__ bool none() const { return (half[0] | half[1]) == 0u; }
 };
 
 // Of the step whose first token is t0.  `own`: the row's token; of a tree: the first node's.
@@ -249,23 +283,36 @@ __device__ __forceinline__ unsigned long long sight_bits(const AttnArgs& a, int 
   return (low_bits(first) | nodes) & low_bits(len - t0);
 }
 
+// The factor of a block's scores.  Where -inf stands in the columns that a row does not see: one that makes no NaN of it (a zero is none for
+// scores that are finite; a NaN is kept where the row sees any of the block).
+template <class Seen> __device__ __forceinline__ float factor_of(const Info& info, int b0, int b, float back, const Seen& seen) {
+  const float cb = back * info.ks[b0 + b];
+  if (Seen::all_ways) return cb;
+  return seen.none_of(b) ? 1.f : cb == 0.f ? 1e-38f : cb;
+}
+
+template <class Seen> __device__ __forceinline__ void mask(float (&x)[2][32], const Seen& seen) {
+#pragma unroll
+  for (int b = 0; b < 2; b++) {
+#pragma unroll
+    for (int e = 0; e < 32; e++)
+      if (!seen.sees(32 * b + e)) x[b][e] = -INFINITY;
+  }
+}
+
 // The lane's row of a step's scores, two blocks of 32 tokens, b0 the tile's number of the first; `seen`: the columns that the row sees.
 // The largest log2 of p w, 2^P_SHIFT times.
 template <bool EDGE, class Seen>
 __device__ __forceinline__ float row_max(float (&x)[2][32], const Info& info, int b0, float back, const Seen& seen) {
   float mx = -INFINITY;
+  if (EDGE) mask(x, seen);
 #pragma unroll
   for (int b = 0; b < 2; b++) {
-    if (EDGE) {
-#pragma unroll
-      for (int e = 0; e < 32; e++)
-        if (!seen.sees(32 * b + e)) x[b][e] = -INFINITY;
-    }
     float y[4] = {x[b][0], x[b][1], x[b][2], x[b][3]};
 #pragma unroll
     for (int e = 4; e < 28; e += 2) y[(e >> 1) & 3] = max3(y[(e >> 1) & 3], x[b][e], x[b][e + 1]);
     const float top = max3(max3(y[0], y[1], x[b][28]), max3(y[2], y[3], x[b][29]), fmaxf(x[b][30], x[b][31]));
-    mx = fmaxf(mx, EDGE && top == -INFINITY ? top : EDGE ? __fadd_rn(__fmul_rn(top, back * info.ks[b0 + b]), info.lw[b0 + b]) : fmaf(top, back * info.ks[b0 + b], info.lw[b0 + b]));
+    mx = fmaxf(mx, EDGE && top == -INFINITY ? top : EDGE ? __fadd_rn(__fmul_rn(top, back * info.ks[b0 + b]), info.lw[b0 + b]) : fmaf(top, factor_of(info, b0, b, back, seen), info.lw[b0 + b]));
   }
   return mx;
 }
@@ -277,7 +324,7 @@ __device__ __forceinline__ float numerators(const float (&x)[2][32], uint32_t s_
 #pragma unroll
   for (int b = 0; b < 2; b++) {
     const bool none = EDGE && (info.lost >> (4 + b0 + b) & 1);
-    const float cb = back * info.ks[b0 + b], lw = none ? 0.f : info.lw[b0 + b], off = lw - ref;
+    const float cb = EDGE ? back * info.ks[b0 + b] : factor_of(info, b0, b, back, seen), lw = none ? 0.f : info.lw[b0 + b], off = lw - ref;
     const F2 cb2 = f2(cb, cb), off2 = f2(off, off);
     F2 sum[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
     uint32_t u[16];
@@ -368,7 +415,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     };
     auto scales = [&] {
       row_nx = -1;
-      ks_nx = vs_nx = 0.f;
+      ks_nx = 0.f;
+      vs_nx = SIGHT == CAUSAL ? 0.f : 1.f;   // (of a block that nobody sees: one that needs no care)
       if (!in_nx) return;
       if ((unsigned)page_nx >= (unsigned)c.n_pages) {
         ks_nx = vs_nx = NAN;
@@ -454,7 +502,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     };
     for (int i = 0; cur.ok && go;) {
       const bool dual = cur.m * c.group - cur.rt * R <= M;        // both streams have the same rows
-      const int n = cur.piece(), steps = dual ? n : 2 * n;
+      const int n = cur.piece(work), steps = dual ? n : 2 * n;
       const int x0 = 2 * i + (dual ? t : 0), dx = dual ? 2 : 1;   // step y is step x0 + dx y of the range
       const uint64_t ad = make_desc_sw128(smem_u32(sm.q[dual ? 0 : t][0]));
       go = bar_wait(sm, &sm.q_full[t], (uint32_t)(items++) & 1u);
@@ -493,7 +541,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     int end_x = 0;
     auto there = [&](int x) {   // whether step x is the range's
       if (x == end_x && cur.ok) {
-        const int n = cur.piece();
+        const int n = cur.piece(work);
         end_x += 2 * n;
         cur.skip(work, n);
       }
@@ -533,15 +581,25 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     bool whole = cur.tile == 0, began = cur.tile != 0;
     if (!heads.by_item && tid == 0) a.heads[v].more = 0;
     if (t) pass_turn(2 + quarter);   // stream A begins
+    bool fetched = false;            // the item's queries are on their way
     for (int i = 0; cur.ok;) {
-      const int n = cur.piece(), rows = cur.m * c.group - cur.rt * R, item0 = end - cur.left - cur.tile;   // (the item's first unit)
+      const int n = cur.piece(work), rows = cur.m * c.group - cur.rt * R, item0 = end - cur.left - cur.tile;   // (the item's first unit)
       const bool ends = cur.tile + n == cur.nt, dual = rows <= M;
       const int row0 = (dual ? 0 : M * t) + 32 * quarter, row = row0 + lane, steps = dual ? n : 2 * n;
       // (the stream's own products of the item before are through)
-      // (stream B of a dual item takes its rows' factors only: its place holds the item's statistics in the end)
-      const float back = prepare_queries<T>(a, cur, row0, sm.q[t][0], !dual || t == 0, lane);
-      fence_async_smem();
-      if (dual) asm volatile("bar.sync 1, 256;\n" ::: "memory");   // stream A's queries are B's too
+      // (stream B of a dual item takes its rows' factors from A: its place holds the item's statistics in the end)
+      int row_exp = ROW_ZERO;
+      if (!dual || t == 0) {
+        if (!fetched) fetch_queries<T>(a, cur, row0, sm.q[t][0], lane);
+        row_exp = prepare_queries<T>(a, cur, row0, sm.q[t][0], lane);
+        if (dual) sm.row_exp[row] = (signed char)row_exp;
+        fence_async_smem();
+      }
+      if (dual) {
+        asm volatile("bar.sync 1, 256;\n" ::: "memory");   // stream A's queries are B's too
+        row_exp = sm.row_exp[row];
+      }
+      const float back = back_of(row_exp, a.scale2);
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.q_full[t]);
       float m = -INFINITY, l = 0.f;
@@ -568,8 +626,11 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
           float x[2][32];
           tmem_ld32(p_at, x[0]);
           tmem_ld32(p_at + 32u, x[1]);
-          const bool edge = __any_sync(0xffffffffu, !sight.all()) || info.lost;
+          // (of a window and a tree many steps are masked, and their scores are set to -inf for the short way; it is the code's size that
+          // counts: a masked copy of the short way took 4000 cycles a step)
+          const bool masked = __any_sync(0xffffffffu, !sight.all()), edge = info.lost || (SIGHT == CAUSAL && masked);
           tmem_wait_ld();
+          if (SIGHT != CAUSAL && masked) mask(x, sight);
           const float mx = edge ? row_max<true>(x, info, 2 * half, back, sight) : row_max<false>(x, info, 2 * half, back, sight);
           // a new reference: the row's sums so far are multiplied, once their last product is through
           const float below = m - mx;   // (-inf for the first; inf or NaN for steps that the row does not see)
@@ -620,6 +681,15 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
         }
       }
       n_o += steps;
+      // The next item's queries, from here on: this stream's scores are through, and those of a dual item when both streams meet.
+      auto next = cur;
+      next.skip(work, n);
+      auto fetch_next = [&] {
+        const bool next_dual = next.m * c.group - next.rt * R <= M;
+        fetched = next.ok && (t == 0 || !next_dual);
+        if (fetched) fetch_queries<T>(a, next, (next_dual ? 0 : M * t) + 32 * quarter, sm.q[t][0], lane);
+      };
+      if (!dual) fetch_next();
       bar_wait(sm, &sm.o_full[t], (uint32_t)(n_o - 1) & 1u);
       if (sm.abort) l = NAN;
       float f = 1.f, f_other = 0.f;
@@ -629,6 +699,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
         stat[M * t + r] = make_float2(m, l);
         before_sync();
         asm volatile("bar.sync 1, 256;\n" ::: "memory");   // both streams' sums are complete
+        if (t == 0) fetch_next();
         const float2 y = stat[M * (t ^ 1) + r];
         const float mn = fmaxf(m, y.x), at = mn == -INFINITY ? 0.f : mn;
         const float g = ex2(0.5f * (m - at)), g_other = ex2(0.5f * (y.x - at));
@@ -689,20 +760,22 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
           }
         } else {
 #pragma unroll
-          for (int e = 0; e < 4; e++)
-            *reinterpret_cast<float4*>(slot + (size_t)row * D + 16 * b + 4 * e) = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+          for (int e = 0; e < 16; e++) slot[(16 * b + e) * R + row] = x[e];
         }
       }
       before_sync();
       if (there && !direct && (!dual || t == 0)) { slot[(size_t)R * D + row] = m; slot[(size_t)R * D + R + row] = l; }
-      if (dual) asm volatile("bar.sync 1, 256;\n" ::: "memory");   // the next item's products may replace the sums
+      if (dual) {
+        asm volatile("bar.sync 1, 256;\n" ::: "memory");   // the next item's products may replace the sums, and its queries the statistics
+        if (t == 1) fetch_next();
+      }
       if (!began && (heads.by_item || !ends) && tid == 0)
         a.heads[heads.at(v, c.n_kv, cur.pair, cur.h, cur.rt)] =
             Head{ends ? 0 : cuts.range_of(item0 + cur.nt - 1) - v, v, cur.pair, cur.h, cur.rt, {}};
       whole = true;
       began = false;
       i += n;
-      cur.skip(work, n);
+      cur = next;
     }
     if (!t) take_turn(2 + quarter);
   }
@@ -710,6 +783,108 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
   __syncthreads();
   if (tid == 0 && sm.abort) set_status(c.status, OKQ_ERR_TIMEOUT);
   if (warp == 0 && !sm.tmem_busy) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
+}
+
+// Parts put together, in order.  A part has its sums channel by channel, R rows each, as the lanes that hold rows write and read whole lines of
+// them (row by row the stores took 8000 cycles of a piece's 90000, and this kernel 23 us of 135 for 2048 queries x 28 heads with a window).
+// A warp has 32 rows and eight channels, WPR warps have every WPR-th part each; unit u of a block's 16 / WPR is rows u / 16, channels u % 16.
+template <class T, int WPR>
+__global__ void __launch_bounds__(MERGE_NT, 2) k_prompt_merge(const AttnArgs a) {
+  constexpr int WARPS = MERGE_NT / 32;
+  __shared__ float sums[WPR > 1 ? WARPS : 1][8][32];
+  __shared__ float2 stat[WPR > 1 ? WARPS : 1][32];
+  depend_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, unit = blockIdx.y * (WARPS / WPR) + warp / WPR, first = warp % WPR;
+  const int r = 32 * (unit >> 4) + lane, ch = 8 * (unit & 15);
+  const int4 h0 = __ldcg(reinterpret_cast<const int4*>(&a.heads[blockIdx.x]));
+  const Head hd{h0.x, h0.y, h0.z, h0.w, __ldcg(&a.heads[blockIdx.x].rt), {}};
+  if (hd.more == 0) return;
+  const int n = hd.more + 1, row = hd.rt * R + r;
+  auto slot = [&](int k) { return a.slots + (size_t)(2 * (hd.v + k) + (k == 0)) * SLOT; };
+  const Work<R, 0> w(a);
+  int len, m;
+  const int li = w.layer_of(hd.pair), b = hd.pair - li * a.c.batch;
+  w.lens(li, b, len, m);
+  const bool there = row < m * w.group;
+  float acc[8] = {}, top = -INFINITY, l = 0.f;
+  if (there) {
+    for (int k0 = first; k0 < n; k0 += 7 * WPR) {
+      float tk[7], lk[7];
+      float mn = top;
+#pragma unroll
+      for (int e = 0; e < 7; e++) {
+        const int k = k0 + e * WPR;
+        const float* s = slot(k) + R * D + r;
+        tk[e] = k < n ? __ldcg(s) : -INFINITY;
+        lk[e] = k < n ? __ldcg(s + R) : 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 7; e++) mn = fmaxf(mn, tk[e]);
+      const float ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(top - ref);
+      l *= f0;
+#pragma unroll
+      for (int z = 0; z < 8; z++) acc[z] *= f0;
+      top = mn;
+#pragma unroll
+      for (int e0 = 0; e0 < 7; e0 += 2) {   // two parts in flight (four: 64 registers do not hold them, and more leave one block to an SM)
+        float x[2][8];
+#pragma unroll
+        for (int e = e0; e < min(7, e0 + 2); e++) {
+          const int k = k0 + e * WPR;
+          const float* s = slot(k) + (size_t)ch * R + r;
+#pragma unroll
+          for (int z = 0; z < 8; z++) x[e - e0][z] = k < n ? __ldcg(s + z * R) : 0.f;
+        }
+#pragma unroll
+        for (int e = e0; e < min(7, e0 + 2); e++) {
+          const float f = ex2(tk[e] - ref);   // (0 where there is none)
+          l = fmaf(lk[e], f, l);
+#pragma unroll
+          for (int z = 0; z < 8; z++) acc[z] = fmaf(x[e - e0][z], f, acc[z]);
+        }
+      }
+    }
+  }
+  if (WPR > 1) {
+#pragma unroll
+    for (int z = 0; z < 8; z++) sums[warp][z][lane] = acc[z];
+    stat[warp][lane] = make_float2(top, l);
+    __syncthreads();
+    if (first != 0) return;
+    float mn = top;
+#pragma unroll
+    for (int i = 1; i < WPR; i++) mn = fmaxf(mn, stat[warp + i][lane].x);
+    const float ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(top - ref);
+    l *= f0;
+#pragma unroll
+    for (int z = 0; z < 8; z++) acc[z] *= f0;
+#pragma unroll
+    for (int i = 1; i < WPR; i++) {
+      const float2 y = stat[warp + i][lane];
+      const float f = ex2(y.x - ref);
+      l = fmaf(y.y, f, l);
+#pragma unroll
+      for (int z = 0; z < 8; z++) acc[z] = fmaf(sums[warp + i][z][lane], f, acc[z]);
+    }
+  }
+  if (!there) return;
+  Vec8<T> o;
+#pragma unroll
+  for (int z = 0; z < 8; z++) o.v[z] = from_f<T>(l == 0.f ? 0.f : acc[z] / l);
+  *reinterpret_cast<Vec8<T>*>(out_row<T>(a, li, b, hd.h, row) + ch) = o;
+}
+template <class T, int WPR> cudaError_t launch_merge_by(const AttnArgs& a, int heads, int rows, cudaStream_t s) {
+  const int units = (rows + 31) / 32 * 16, per = MERGE_NT / 32 / WPR;
+  return launch_dependent(k_prompt_merge<T, WPR>, dim3(heads, (units + per - 1) / per), MERGE_NT, 0, s, 1, a);
+}
+template <class T> cudaError_t launch_merge(const AttnArgs& a, int ranges, cudaStream_t s) {
+  const Heads<R> heads(a.layer_count * a.c.batch, a.c.n_kv, a.c.group, a.n_new, ranges);
+  const int n = heads.count(ranges), parts = heads.items < ranges ? ranges / heads.items : 1;   // (of an item, were all alike)
+  // Warps to a row: more where one would load parts several times in a row, as long as the GPU holds them all at once (1 sequence of 32768
+  // tokens, 32 rows: 37 us with one warp to a row, 20 with sixteen; 16 heads of 8000 tokens, 256 rows: 52 with one, 60 with four).
+  const long long room = 4ll * sm_count() * (MERGE_NT / 32) / n, rows = (long long)a.n_new * a.c.group, most = rows < R ? rows : R;
+  if (parts >= 28 && 16 * most <= room) return launch_merge_by<T, 16>(a, n, (int)most, s);
+  return parts >= 15 && 4 * most <= room ? launch_merge_by<T, 4>(a, n, (int)most, s) : launch_merge_by<T, 1>(a, n, (int)most, s);
 }
 
 template <class T, int SIGHT> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map, int grid, cudaStream_t s) {
@@ -723,7 +898,7 @@ template <class T, int SIGHT> cudaError_t launch(const AttnArgs& a, const CUtens
     attr_done(attr_mask, dev);
   }
   cudaError_t e = launch_dependent(k_paged_prompt<T, SIGHT>, dim3(grid), NT, SMEM, s, 1, map, a);
-  return e == cudaSuccess ? launch_merge<T, R>(a, grid, s) : e;
+  return e == cudaSuccess && !a.whole ? launch_merge<T>(a, grid, s) : e;
 }
 
 template <int SIGHT> cudaError_t launch_sight(const AttnArgs& a, const CUtensorMap& map, int dtype, int grid, cudaStream_t s) {
