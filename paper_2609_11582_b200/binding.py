@@ -629,28 +629,50 @@ def rope_apply(rope: Rope, q, q_out, k=None, k_out=None, inverse=False, stream=N
         raise OkqError(st, "okq_rope_apply")
 
 
-def _norm_tensor(x, up, out, weight, weight_grad, dtype, shape):
-    xs, os = x.stride(), out.stride()
-    us = xs if up is None else up.stride()
-    assert x.shape == out.shape == shape and x.dtype == out.dtype == dtype and xs[3] == os[3] == us[3] == 1
-    assert up is None or (up.shape == shape and up.dtype == dtype)
-    assert weight is None or (weight.numel() == HEAD_DIM and weight.is_contiguous())
-    assert weight_grad is None or (weight_grad.numel() == HEAD_DIM and weight_grad.is_contiguous() and weight_grad.dtype == torch.float32)
-    return _norm_tensor_struct(x.data_ptr(), 0 if up is None else up.data_ptr(), out.data_ptr(), xs[0], xs[1], xs[2], us[0], us[1], us[2], os[0], os[1], os[2],
-                               0 if weight is None else weight.data_ptr(), 0 if weight_grad is None else weight_grad.data_ptr(),
-                               2 if weight is None else DTYPE_CODES[weight.dtype], shape[1])
+def _norm_tensor(x, up, out, weight, weight_grad, shape):
+    """okq_norm_tensor of one side; checks what the C call cannot see."""
+    dtype, (x0, x1, x2, x3), (o0, o1, o2, o3) = x.dtype, x.stride(), out.stride()
+    assert out.shape == shape and out.dtype == dtype and x3 == 1 and o3 == 1 and shape[3] == HEAD_DIM
+    up_ptr, u0, u1, u2 = 0, 0, 0, 0
+    if up is not None:
+        up_ptr, (u0, u1, u2, u3) = up.data_ptr(), up.stride()
+        assert up.shape == shape and up.dtype == dtype and u3 == 1
+    weight_ptr = grad_ptr = 0
+    code = 2
+    if weight is not None:
+        weight_ptr, code = weight.data_ptr(), DTYPE_CODES[weight.dtype]
+        assert weight.numel() == HEAD_DIM and weight.is_contiguous()
+    if weight_grad is not None:
+        grad_ptr = weight_grad.data_ptr()
+        assert weight_grad.numel() == HEAD_DIM and weight_grad.is_contiguous() and weight_grad.dtype == torch.float32
+    return _norm_tensor_struct(x.data_ptr(), up_ptr, out.data_ptr(), x0, x1, x2, u0, u1, u2, o0, o1, o2, weight_ptr, grad_ptr, code, shape[1])
+
+
+def _norm_sides(rope, q, k):
+    """(batch, n, shapes of q and k, the rotation's struct)"""
+    shape = q.shape
+    batch, n = shape[0], shape[2]
+    k_shape = None
+    if k is not None:
+        k_shape = k.shape
+        assert k_shape[0] == batch and k_shape[2] == n and k.dtype == q.dtype
+    if rope is None:
+        return batch, n, shape, k_shape, None
+    assert rope.batch == batch and rope.n == n, "positions are [3, batch, n] of the call's own tokens"
+    return batch, n, shape, k_shape, rope.ref
 
 
 def norm_rope_apply(rope, q, q_out, q_weight=None, k=None, k_out=None, k_weight=None, eps=1e-6, stream=None):
     """Norm of every head of q and k, [batch, heads, n, 128] of fp16, bf16 or fp32 (last dim contiguous, any other strides), with its weight
     ([128] of any of the three types, ones without it), then the rotation (none with rope=None), into q_out and k_out (which may be the
     inputs)."""
-    _here(q, q_out, q_weight, k, k_out, k_weight, *((None, None) if rope is None else (rope.positions, rope.freq)))
-    batch, heads, n, _ = q.shape
-    dtype = q.dtype
-    q_ref = _norm_tensor(q, None, q_out, q_weight, None, dtype, (batch, heads, n, HEAD_DIM))
-    k_ref = None if k is None else _norm_tensor(k, None, k_out, k_weight, None, dtype, (batch, k.shape[1], n, HEAD_DIM))
-    st = (_lib or lib()).okq_norm_rope_apply(_rope_ref(rope, batch, n), eps, DTYPE_CODES[dtype], batch, n, q_ref, k_ref, _stream(stream))
+    if rope is None:
+        _here(q, q_out, q_weight, k, k_out, k_weight)
+    else:
+        _here(q, q_out, q_weight, k, k_out, k_weight, rope.positions)
+    batch, n, shape, k_shape, ref = _norm_sides(rope, q, k)
+    st = (_lib or lib()).okq_norm_rope_apply(ref, eps, DTYPE_CODES[q.dtype], batch, n, _norm_tensor(q, None, q_out, q_weight, None, shape),
+                                             None if k is None else _norm_tensor(k, None, k_out, k_weight, None, k_shape), _stream(stream))
     if st != OK:
         raise OkqError(st, "okq_norm_rope_apply")
 
@@ -663,13 +685,10 @@ def norm_rope_grad(rope, q, q_up, q_grad, workspace=None, q_weight=None, q_weigh
                    k_weight_grad=None, eps=1e-6, stream=None):
     """The gradients of norm_rope_apply's inputs into q_grad and k_grad (which may be q_up and k_up, the gradients of its results) and, where
     q_weight_grad and k_weight_grad (float32 [128], overwritten) are given, those of its weights; q and k as they were before the norm."""
-    _here(q, q_up, q_grad, workspace, q_weight, q_weight_grad, k, k_up, k_grad, k_weight, k_weight_grad,
-          *((None, None) if rope is None else (rope.positions, rope.freq)))
-    batch, heads, n, _ = q.shape
-    dtype = q.dtype
-    q_ref = _norm_tensor(q, q_up, q_grad, q_weight, q_weight_grad, dtype, (batch, heads, n, HEAD_DIM))
-    k_ref = None if k is None else _norm_tensor(k, k_up, k_grad, k_weight, k_weight_grad, dtype, (batch, k.shape[1], n, HEAD_DIM))
-    st = (_lib or lib()).okq_norm_rope_grad(_rope_ref(rope, batch, n), eps, DTYPE_CODES[dtype], batch, n, q_ref, k_ref, _ptr(workspace),
+    _here(q, q_up, q_grad, workspace, q_weight, q_weight_grad, k, k_up, k_grad, k_weight, k_weight_grad, None if rope is None else rope.positions)
+    batch, n, shape, k_shape, ref = _norm_sides(rope, q, k)
+    st = (_lib or lib()).okq_norm_rope_grad(ref, eps, DTYPE_CODES[q.dtype], batch, n, _norm_tensor(q, q_up, q_grad, q_weight, q_weight_grad, shape),
+                                            None if k is None else _norm_tensor(k, k_up, k_grad, k_weight, k_weight_grad, k_shape), _ptr(workspace),
                                             0 if workspace is None else workspace.nbytes, _stream(stream))
     if st != OK:
         raise OkqError(st, "okq_norm_rope_grad")

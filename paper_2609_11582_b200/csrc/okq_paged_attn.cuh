@@ -171,6 +171,37 @@ struct Cuts {
   }
 };
 
+// Units of a head's row tiles before tile `rt` that begin no later than `offset`, found by a warp, 32 row tiles at a time; all lanes get the
+// same answer.  (With one thread and 56 row tiles finding the first tile took 10000 to 23000 cycles of a block's 170000.)
+template <int ROWS, int EXTRA, int SIGHT>
+__device__ __forceinline__ int warp_units(const Work<ROWS, EXTRA, SIGHT>& w, int len, int m, int lane) {   // of the whole head
+  int s = 0;
+  for (int rt = lane; rt < w.row_tiles(m); rt += 32) s += w.units(w.tiles(len, m, rt));
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+  return s;
+}
+template <int ROWS, int EXTRA, int SIGHT>
+__device__ __forceinline__ void warp_row_tile(const Work<ROWS, EXTRA, SIGHT>& w, int len, int m, int offset, int lane, int& rt, int& tile) {
+  for (int rt0 = 0, at = 0;; rt0 += 32) {
+    int u = rt0 + lane < w.row_tiles(m) ? w.units(w.tiles(len, m, rt0 + lane)) : 0, end = u;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, end, d);
+      if (lane >= d) end += y;
+    }
+    const unsigned behind = __ballot_sync(0xffffffffu, offset < at + end);   // row tiles that end behind the unit
+    if (behind) {
+      const int l = __ffs(behind) - 1;
+      rt = rt0 + l;
+      tile = offset - (at + __shfl_sync(0xffffffffu, end - u, l));
+      return;
+    }
+    at += __shfl_sync(0xffffffffu, end, 31);
+    if (rt0 + 32 >= w.row_tiles(m)) { rt = tile = 0; return; }   // (cannot be: the unit is the head's)
+  }
+}
+
 // All threads of a block find the line's length and where the first units of the block's ranges v0, v0 + step, .. lie.  Threads hold
 // consecutive pairs.
 template <int G> struct FindSmem {
@@ -182,10 +213,22 @@ __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS, EX
   const int tid = threadIdx.x, lane = tid & 31, wp = tid >> 5;
   const int chunk = (w.pairs + NT - 1) / NT, p0 = min(w.pairs, tid * chunk), p1 = min(w.pairs, p0 + chunk);
   int len = 0, m = 0, per_head = 0, mine = 0;    // (of the last pair looked at: with no more pairs than threads, the only one)
-  for (int p = p0; p < p1; p++) {
-    w.lens(p, len, m);
-    per_head = w.head_units(len, m);
-    mine += per_head * w.n_kv;
+  // whether a warp goes through its pairs' row tiles together
+  const int row_tiles = w.row_tiles(w.a.n_new), pairs_here = min(32, max(0, w.pairs - 32 * wp));
+  const bool together = ROWS > 8 && chunk == 1 && pairs_here * ((row_tiles + 31) / 32) < row_tiles;
+  if (together) {
+    if (p0 < p1) w.lens(p0, len, m);
+    for (int l = 0; l < pairs_here; l++) {
+      const int s = warp_units(w, __shfl_sync(0xffffffffu, len, l), __shfl_sync(0xffffffffu, m, l), lane);
+      if (lane == l) per_head = s;
+    }
+    mine = per_head * w.n_kv;
+  } else {
+    for (int p = p0; p < p1; p++) {
+      w.lens(p, len, m);
+      per_head = w.head_units(len, m);
+      mine += per_head * w.n_kv;
+    }
   }
   int v = mine;
 #pragma unroll
@@ -203,7 +246,21 @@ __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS, EX
     total += x;
   }
   const Cuts cuts(total, ranges);
-  if (mine > 0) {
+  if (together) {
+#pragma unroll
+    for (int g = 0; g < G; g++) {
+      const int target = cuts.start(v0 + g * step);
+      const unsigned owner = __ballot_sync(0xffffffffu, mine > 0 && target >= before && target < before + mine);
+      if (owner == 0) continue;
+      const int l = __ffs(owner) - 1, heads = __shfl_sync(0xffffffffu, per_head, l), offset = target - __shfl_sync(0xffffffffu, before, l);
+      const int h = offset / heads, len_l = __shfl_sync(0xffffffffu, len, l), m_l = __shfl_sync(0xffffffffu, m, l);
+      int rt, tile;
+      warp_row_tile(w, len_l, m_l, offset - h * heads, lane, rt, tile);
+      if (lane == l) {
+        sm.place[g][0] = p0; sm.place[g][1] = h; sm.place[g][2] = rt; sm.place[g][3] = tile; sm.place[g][4] = len; sm.place[g][5] = m;
+      }
+    }
+  } else if (mine > 0) {
 #pragma unroll
     for (int g = 0; g < G; g++) {
       const int target = cuts.start(v0 + g * step);

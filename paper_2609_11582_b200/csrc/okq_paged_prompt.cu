@@ -788,8 +788,9 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
 // Parts put together, in order.  A part has its sums channel by channel, R rows each, as the lanes that hold rows write and read whole lines of
 // them (row by row the stores took 8000 cycles of a piece's 90000, and this kernel 23 us of 135 for 2048 queries x 28 heads with a window).
 // A warp has 32 rows and eight channels, WPR warps have every WPR-th part each; unit u of a block's 16 / WPR is rows u / 16, channels u % 16.
-template <class T, int WPR>
-__global__ void __launch_bounds__(MERGE_NT, 2) k_prompt_merge(const AttnArgs a) {
+// FLIGHT parts are loaded at once: two, so that two blocks fit an SM, or seven where there are no more blocks than SMs.
+template <class T, int WPR, int FLIGHT>
+__global__ void __launch_bounds__(MERGE_NT, FLIGHT > 2 ? 1 : 2) k_prompt_merge(const AttnArgs a) {
   constexpr int WARPS = MERGE_NT / 32;
   __shared__ float sums[WPR > 1 ? WARPS : 1][8][32];
   __shared__ float2 stat[WPR > 1 ? WARPS : 1][32];
@@ -826,17 +827,17 @@ __global__ void __launch_bounds__(MERGE_NT, 2) k_prompt_merge(const AttnArgs a) 
       for (int z = 0; z < 8; z++) acc[z] *= f0;
       top = mn;
 #pragma unroll
-      for (int e0 = 0; e0 < 7; e0 += 2) {   // two parts in flight (four: 64 registers do not hold them, and more leave one block to an SM)
-        float x[2][8];
+      for (int e0 = 0; e0 < 7; e0 += FLIGHT) {
+        float x[FLIGHT][8];
 #pragma unroll
-        for (int e = e0; e < min(7, e0 + 2); e++) {
+        for (int e = e0; e < min(7, e0 + FLIGHT); e++) {
           const int k = k0 + e * WPR;
           const float* s = slot(k) + (size_t)ch * R + r;
 #pragma unroll
           for (int z = 0; z < 8; z++) x[e - e0][z] = k < n ? __ldcg(s + z * R) : 0.f;
         }
 #pragma unroll
-        for (int e = e0; e < min(7, e0 + 2); e++) {
+        for (int e = e0; e < min(7, e0 + FLIGHT); e++) {
           const float f = ex2(tk[e] - ref);   // (0 where there is none)
           l = fmaf(lk[e], f, l);
 #pragma unroll
@@ -873,18 +874,20 @@ __global__ void __launch_bounds__(MERGE_NT, 2) k_prompt_merge(const AttnArgs a) 
   for (int z = 0; z < 8; z++) o.v[z] = from_f<T>(l == 0.f ? 0.f : acc[z] / l);
   *reinterpret_cast<Vec8<T>*>(out_row<T>(a, li, b, hd.h, row) + ch) = o;
 }
-template <class T, int WPR> cudaError_t launch_merge_by(const AttnArgs& a, int heads, int rows, cudaStream_t s) {
+template <class T, int WPR, int FLIGHT> cudaError_t launch_merge_by(const AttnArgs& a, int heads, int rows, cudaStream_t s) {
   const int units = (rows + 31) / 32 * 16, per = MERGE_NT / 32 / WPR;
-  return launch_dependent(k_prompt_merge<T, WPR>, dim3(heads, (units + per - 1) / per), MERGE_NT, 0, s, 1, a);
+  return launch_dependent(k_prompt_merge<T, WPR, FLIGHT>, dim3(heads, (units + per - 1) / per), MERGE_NT, 0, s, 1, a);
 }
 template <class T> cudaError_t launch_merge(const AttnArgs& a, int ranges, cudaStream_t s) {
   const Heads<R> heads(a.layer_count * a.c.batch, a.c.n_kv, a.c.group, a.n_new, ranges);
   const int n = heads.count(ranges), parts = heads.items < ranges ? ranges / heads.items : 1;   // (of an item, were all alike)
-  // Warps to a row: more where one would load parts several times in a row, as long as the GPU holds them all at once (1 sequence of 32768
-  // tokens, 32 rows: 37 us with one warp to a row, 20 with sixteen; 16 heads of 8000 tokens, 256 rows: 52 with one, 60 with four).
-  const long long room = 4ll * sm_count() * (MERGE_NT / 32) / n, rows = (long long)a.n_new * a.c.group, most = rows < R ? rows : R;
-  if (parts >= 28 && 16 * most <= room) return launch_merge_by<T, 16>(a, n, (int)most, s);
-  return parts >= 15 && 4 * most <= room ? launch_merge_by<T, 4>(a, n, (int)most, s) : launch_merge_by<T, 1>(a, n, (int)most, s);
+  const long long rows = (long long)a.n_new * a.c.group, most = rows < R ? rows : R, blocks = n * ((most + 31) / 32), sms = sm_count();
+  // Warps to a row: more where one would load parts several times in a row, as long as the GPU holds them all at once.  A call in us with one,
+  // four, sixteen: 1 x 4 heads of 32768 tokens, 64 rows (37 parts, 8 blocks with one) 49, 41, 37; 16 heads of 4096, 112 rows (9 parts, 64
+  // blocks) 37, 33, 39; 16 heads of 8000, 256 rows (9 parts, 128 blocks) 51, 53, 66.
+  if (parts >= 16 && 16 * blocks <= sms) return launch_merge_by<T, 16, 2>(a, n, (int)most, s);
+  if (parts >= 4 && 4 * blocks <= 2 * sms) return launch_merge_by<T, 4, 2>(a, n, (int)most, s);
+  return blocks <= sms ? launch_merge_by<T, 1, 7>(a, n, (int)most, s) : launch_merge_by<T, 1, 2>(a, n, (int)most, s);
 }
 
 template <class T, int SIGHT> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map, int grid, cudaStream_t s) {
