@@ -39,7 +39,6 @@ constexpr int R = PROMPT_ROWS, EXTRA = PROMPT_EXTRA, M = 128;         // rows of
 constexpr int PH = PT / 2;                      // tokens of a step
 constexpr int SIDE = PT * D;                    // bytes of a tile's keys or values as codes
 constexpr int Q_HALF = M * 128, KV_HALF = PH * 128;   // 64 channels in fp16, of a stream's queries and of a step's keys or values
-constexpr int NR = 3;                           // ring of steps' keys, and values, in fp16
 constexpr int W_CONV = 8, W_MMA = 12, W_LOAD = 14;   // (an MMA warp to each stream)
 constexpr int NT = 15 * 32;
 constexpr uint32_t S_COL = 0, O_COL = 256;      // + 128 per stream, + 64 per place for scores; numerators lie on its first half
@@ -58,8 +57,10 @@ struct Info {            // of a tile, by block
   int lost;              // blocks whose value scale is NaN, a bit for each; from bit 4 on those without a value
 };
 
-struct PromptSmem {
-  __align__(1024) unsigned char q[2][2][Q_HALF];   // [stream][channels / 64]
+// NARROW: a call with no more than 128 rows to a head, whose items are all dual: no queries for stream B, and a longer ring in their place.
+template <bool NARROW> struct PromptSmem {
+  static constexpr int NR = NARROW ? 4 : 3;        // ring of steps' keys, and values, in fp16
+  __align__(1024) unsigned char q[NARROW ? 1 : 2][2][Q_HALF];   // [stream][channels / 64]
   __align__(1024) unsigned char k[NR][2][KV_HALF];
   __align__(1024) unsigned char v[NR][2][KV_HALF];
   __align__(1024) int8_t code[2][2][SIDE];         // [keys, values][tile mod 2]
@@ -70,7 +71,7 @@ struct PromptSmem {
   // other step only and could take a phase for the one after the next
   __align__(8) volatile int done[2][2];
   float peak[2 * M];                               // [stream][row] maximum of the numerators so far, LEAD below the highest reference
-  signed char row_exp[M];                          // of a dual item's rows, from stream A for B
+  signed char row_exp[2 * M];                      // of the item's rows
   FindSmem<1> find;
   uint32_t tmem_slot;
   long long limit;
@@ -108,6 +109,14 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&r)[16]) {
                : "=f"(r[0]),"=f"(r[1]),"=f"(r[2]),"=f"(r[3]),"=f"(r[4]),"=f"(r[5]),"=f"(r[6]),"=f"(r[7]),"=f"(r[8]),"=f"(r[9]),"=f"(r[10]),"=f"(r[11]),"=f"(r[12]),"=f"(r[13]),"=f"(r[14]),"=f"(r[15])
                : "r"(taddr) : "memory");
 }
+__device__ __forceinline__ void tmem_st2(uint32_t taddr, float a, float b) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};\n" ::"r"(taddr), "f"(a), "f"(b) : "memory");
+}
+__device__ __forceinline__ float2 tmem_ld2(uint32_t taddr) {
+  float2 r;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0, %1}, [%2];\ntcgen05.wait::ld.sync.aligned;\n" : "=f"(r.x), "=f"(r.y) : "r"(taddr) : "memory");
+  return r;
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory"); }
@@ -129,7 +138,7 @@ __device__ __forceinline__ void take_turn(int id) { asm volatile("bar.sync %0, 6
 __device__ __forceinline__ void pass_turn(int id) { asm volatile("bar.arrive %0, 64;\n" ::"r"(id) : "memory"); }
 
 // Wait of a warp until both converting warps have done step x, with the limit of every wait.
-__device__ __forceinline__ bool step_ready(PromptSmem& sm, const volatile int* done, int x) {
+template <class SM> __device__ __forceinline__ bool step_ready(SM& sm, const volatile int* done, int x) {
   const uint32_t at = smem_u32(const_cast<const int*>(done));
   const long long t0 = clock64();
   bool ok = true;
@@ -147,7 +156,7 @@ __device__ __forceinline__ bool step_ready(PromptSmem& sm, const volatile int* d
   return __all_sync(0xffffffffu, ok);
 }
 
-// A warp's 32 rows of a row tile, eight lanes to a row and sixteen channels each.  Their numbers are copied, as they are, into the places that
+// A warp's rows of a row tile, four times ROUNDS from row0 on, eight lanes to a row and sixteen channels each.  Their numbers are copied, as they are, into the places that
 // the fp16 ones will have (both have 16 bits); a lane copies what it will turn itself, so that its own wait is enough.  All of it is in
 // flight at once, behind the end of the item before (loaded into registers two rows at a time the queries took 11000 to 17000 cycles of an
 // item's 40000).
@@ -163,12 +172,12 @@ struct QueryPlace {
   // of row r of the stream
   __device__ __forceinline__ unsigned char* at(unsigned char* q, int r, int ch) const { return q + (ch >> 6) * Q_HALF + r * 128 + ((((ch & 63) >> 3) ^ (r & 7)) << 4); }
 };
-template <class T, class Cur>
+template <class T, int ROUNDS, class Cur>
 __device__ __forceinline__ void fetch_queries(const AttnArgs& a, const Cur& cur, int row0, unsigned char* q, int lane) {
   const QueryPlace pl(a.rope, lane);
   const int rows = cur.m * a.c.group;
-#pragma unroll
-  for (int it = 0; it < 8; it++) {
+#pragma unroll 2
+  for (int it = 0; it < ROUNDS; it++) {
     const int rl = 4 * it + (lane >> 3), row = cur.rt * R + row0 + rl, r = (row0 & (M - 1)) + rl;
     const int bytes = row < rows ? 16 : 0;   // (zeros for rows that the item does not have)
     const T* src = query_row<T>(a, cur.li, cur.b, cur.h, bytes ? row : 0);
@@ -177,22 +186,23 @@ __device__ __forceinline__ void fetch_queries(const AttnArgs& a, const Cur& cur,
   }
 }
 
-// The rows that fetch_queries copied: rotated, scaled by a power of two, whose exponent is returned for the lane's own row (the softmax
-// scale's sign goes to the queries).
+// The rows that fetch_queries copied: rotated, scaled by a power of two, whose exponents go to row_exp (the softmax scale's sign goes to the
+// queries).
 constexpr int ROW_ZERO = -128, ROW_NAN = 127;   // rows that are zeros here; with an infinity or NaN
 // the factor of the exponent that undoes the scaling, times the softmax scale
 __device__ __forceinline__ float back_of(int e2, float scale2) {
   return e2 == ROW_NAN ? NAN : e2 == ROW_ZERO ? 0.f : __uint_as_float((uint32_t)(127 + e2) << 23) * fabsf(scale2);
 }
-template <class T, class Cur>
-__device__ __forceinline__ int prepare_queries(const AttnArgs& a, const Cur& cur, int row0, unsigned char* q, int lane) {
+template <class T, int ROUNDS, class Cur>
+__device__ __forceinline__ void prepare_queries(const AttnArgs& a, const Cur& cur, int row0, unsigned char* q, signed char* row_exp, int lane) {
   const PagedView& c = a.c;
   const QueryPlace pl(a.rope, lane);
   const int rows = cur.m * c.group;
-  int mine = ROW_ZERO;
+  if (lane < 4 * ROUNDS) row_exp[row0 + lane] = (signed char)ROW_ZERO;
+  __syncwarp();
   asm volatile("cp.async.wait_all;\n" ::: "memory");
 #pragma unroll 1
-  for (int it = 0; it < 8; it++) {
+  for (int it = 0; it < ROUNDS; it++) {
     if (cur.rt * R + row0 + 4 * it >= rows) break;   // (the same in all lanes)
     const int rl = 4 * it + (lane >> 3), row = cur.rt * R + row0 + rl, r = (row0 & (M - 1)) + rl;    // row inside the warp, of the item's queries, of the stream
     Vec8<T> x[2] = {*reinterpret_cast<const Vec8<T>*>(pl.at(q, r, pl.c0)), *reinterpret_cast<const Vec8<T>*>(pl.at(q, r, pl.c1))};
@@ -230,10 +240,8 @@ __device__ __forceinline__ int prepare_queries(const AttnArgs& a, const Cur& cur
       }
       *reinterpret_cast<uint4*>(pl.at(q, r, z ? pl.c1 : pl.c0)) = make_uint4(y[0], y[1], y[2], y[3]);
     }
-    const int got = __shfl_sync(0xffffffffu, mx >= 0x7f800000u ? ROW_NAN : fine ? e2 : ROW_ZERO, 8 * (lane & 3));    // rows 4 it .. 4 it + 3 are in lanes 0, 8, 16, 24
-    if (lane >> 2 == it) mine = got;
+    if ((lane & 7) == 0) row_exp[row0 + rl] = (signed char)(mx >= 0x7f800000u ? ROW_NAN : fine ? e2 : ROW_ZERO);
   }
-  return mine;
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -355,10 +363,13 @@ __device__ __forceinline__ float numerators(const float (&x)[2][32], uint32_t s_
   return l;
 }
 
-template <class T, int SIGHT>
+// NARROW: all items are dual, and the code for the others is left out.
+template <class T, int SIGHT, bool NARROW>
 __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ CUtensorMap map, const AttnArgs a) {
   extern __shared__ unsigned char raw_smem[];
-  PromptSmem& sm = *reinterpret_cast<PromptSmem*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~(uintptr_t)1023);
+  using Smem = PromptSmem<NARROW>;
+  constexpr int NR = Smem::NR;
+  Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~(uintptr_t)1023);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     auto init = [](unsigned long long* b, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(smem_u32(b)), "r"(count)); };
@@ -501,10 +512,10 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       ph_s ^= 1u << place;
     };
     for (int i = 0; cur.ok && go;) {
-      const bool dual = cur.m * c.group - cur.rt * R <= M;        // both streams have the same rows
+      const bool dual = NARROW || cur.m * c.group - cur.rt * R <= M;        // both streams have the same rows
       const int n = cur.piece(work), steps = dual ? n : 2 * n;
       const int x0 = 2 * i + (dual ? t : 0), dx = dual ? 2 : 1;   // step y is step x0 + dx y of the range
-      const uint64_t ad = make_desc_sw128(smem_u32(sm.q[dual ? 0 : t][0]));
+      const uint64_t ad = make_desc_sw128(smem_u32(sm.q[NARROW || dual ? 0 : t][0]));
       go = bar_wait(sm, &sm.q_full[t], (uint32_t)(items++) & 1u);
       for (int y = 0; y < min(2, steps); y++) score(x0 + dx * y, y, ad, dual);
       for (int y = 0; y < steps && go; y++) {
@@ -580,26 +591,25 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
     int n_o = 0;
     bool whole = cur.tile == 0, began = cur.tile != 0;
     if (!heads.by_item && tid == 0) a.heads[v].more = 0;
-    if (t) pass_turn(2 + quarter);   // stream A begins
-    bool fetched = false;            // the item's queries are on their way
+    if (!NARROW && t) pass_turn(2 + quarter);   // stream A begins
+    bool first_item = true;
     for (int i = 0; cur.ok;) {
       const int n = cur.piece(work), rows = cur.m * c.group - cur.rt * R, item0 = end - cur.left - cur.tile;   // (the item's first unit)
-      const bool ends = cur.tile + n == cur.nt, dual = rows <= M;
+      const bool ends = cur.tile + n == cur.nt, dual = NARROW || rows <= M;
       const int row0 = (dual ? 0 : M * t) + 32 * quarter, row = row0 + lane, steps = dual ? n : 2 * n;
       // (the stream's own products of the item before are through)
-      // (stream B of a dual item takes its rows' factors from A: its place holds the item's statistics in the end)
-      int row_exp = ROW_ZERO;
-      if (!dual || t == 0) {
-        if (!fetched) fetch_queries<T>(a, cur, row0, sm.q[t][0], lane);
-        row_exp = prepare_queries<T>(a, cur, row0, sm.q[t][0], lane);
-        if (dual) sm.row_exp[row] = (signed char)row_exp;
+      // A dual item's queries lie in A's place and are prepared by A, or, where all items are dual, by both.
+      constexpr int ROUNDS = NARROW ? 4 : 8;
+      if (NARROW || !dual || t == 0) {
+        const int first = NARROW ? 32 * quarter + 16 * t : row0;
+        unsigned char* place = sm.q[NARROW || dual ? 0 : t][0];
+        if (first_item) fetch_queries<T, ROUNDS>(a, cur, first, place, lane);
+        prepare_queries<T, ROUNDS>(a, cur, first, place, sm.row_exp, lane);
         fence_async_smem();
       }
-      if (dual) {
-        asm volatile("bar.sync 1, 256;\n" ::: "memory");   // stream A's queries are B's too
-        row_exp = sm.row_exp[row];
-      }
-      const float back = back_of(row_exp, a.scale2);
+      if (dual) asm volatile("bar.sync 1, 256;\n" ::: "memory");
+      __syncwarp();
+      const float back = back_of(sm.row_exp[row], a.scale2);
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.q_full[t]);
       float m = -INFINITY, l = 0.f;
@@ -685,22 +695,25 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       auto next = cur;
       next.skip(work, n);
       auto fetch_next = [&] {
-        const bool next_dual = next.m * c.group - next.rt * R <= M;
-        fetched = next.ok && (t == 0 || !next_dual);
-        if (fetched) fetch_queries<T>(a, next, (next_dual ? 0 : M * t) + 32 * quarter, sm.q[t][0], lane);
+        const bool next_dual = NARROW || next.m * c.group - next.rt * R <= M;
+        if (next.ok && (NARROW || t == 0 || !next_dual))
+          fetch_queries<T, ROUNDS>(a, next, NARROW ? 32 * quarter + 16 * t : (next_dual ? 0 : M * t) + 32 * quarter, sm.q[NARROW || next_dual ? 0 : t][0], lane);
       };
+      first_item = false;
       if (!dual) fetch_next();
       bar_wait(sm, &sm.o_full[t], (uint32_t)(n_o - 1) & 1u);
       if (sm.abort) l = NAN;
       float f = 1.f, f_other = 0.f;
       if (dual) {
-        const int r = 32 * quarter + lane;
-        float2* stat = reinterpret_cast<float2*>(sm.q[1][0]);
-        stat[M * t + r] = make_float2(m, l);
+        // statistics in the place of the first scores
+        const uint32_t stat = tmem + S_COL + lanes;
+        tmem_st2(stat + 128u * t, m, l);
+        tmem_wait_st();
         before_sync();
         asm volatile("bar.sync 1, 256;\n" ::: "memory");   // both streams' sums are complete
-        if (t == 0) fetch_next();
-        const float2 y = stat[M * (t ^ 1) + r];
+        after_sync();
+        fetch_next();
+        const float2 y = tmem_ld2(stat + 128u * (t ^ 1));
         const float mn = fmaxf(m, y.x), at = mn == -INFINITY ? 0.f : mn;
         const float g = ex2(0.5f * (m - at)), g_other = ex2(0.5f * (y.x - at));
         f = g * g;
@@ -765,10 +778,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       }
       before_sync();
       if (there && !direct && (!dual || t == 0)) { slot[(size_t)R * D + row] = m; slot[(size_t)R * D + R + row] = l; }
-      if (dual) {
-        asm volatile("bar.sync 1, 256;\n" ::: "memory");   // the next item's products may replace the sums, and its queries the statistics
-        if (t == 1) fetch_next();
-      }
+      if (dual) asm volatile("bar.sync 1, 256;\n" ::: "memory");   // the next item's products may replace the sums and statistics
       if (!began && (heads.by_item || !ends) && tid == 0)
         a.heads[heads.at(v, c.n_kv, cur.pair, cur.h, cur.rt)] =
             Head{ends ? 0 : cuts.range_of(item0 + cur.nt - 1) - v, v, cur.pair, cur.h, cur.rt, {}};
@@ -777,7 +787,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
       i += n;
       cur = next;
     }
-    if (!t) take_turn(2 + quarter);
+    if (!NARROW && !t) take_turn(2 + quarter);
   }
   before_sync();
   __syncthreads();
@@ -890,22 +900,24 @@ template <class T> cudaError_t launch_merge(const AttnArgs& a, int ranges, cudaS
   return blocks <= sms ? launch_merge_by<T, 1, 7>(a, n, (int)most, s) : launch_merge_by<T, 1, 2>(a, n, (int)most, s);
 }
 
-template <class T, int SIGHT> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map, int grid, cudaStream_t s) {
+template <class T, int SIGHT, bool NARROW> cudaError_t launch(const AttnArgs& a, const CUtensorMap& map, int grid, cudaStream_t s) {
   static thread_local unsigned long long attr_mask = 0;
   int dev = 0;
-  constexpr int SMEM = (int)sizeof(PromptSmem) + 1024;
+  constexpr int SMEM = (int)sizeof(PromptSmem<NARROW>) + 1024;
   static_assert(SMEM <= 227 * 1024, "shared memory of one block");
   if (attr_needed(attr_mask, dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(k_paged_prompt<T, SIGHT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(k_paged_prompt<T, SIGHT, NARROW>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
     if (e != cudaSuccess) return e;
     attr_done(attr_mask, dev);
   }
-  cudaError_t e = launch_dependent(k_paged_prompt<T, SIGHT>, dim3(grid), NT, SMEM, s, 1, map, a);
+  cudaError_t e = launch_dependent(k_paged_prompt<T, SIGHT, NARROW>, dim3(grid), NT, SMEM, s, 1, map, a);
   return e == cudaSuccess && !a.whole ? launch_merge<T>(a, grid, s) : e;
 }
 
 template <int SIGHT> cudaError_t launch_sight(const AttnArgs& a, const CUtensorMap& map, int dtype, int grid, cudaStream_t s) {
-  return dtype == OKQ_FP16 ? launch<__half, SIGHT>(a, map, grid, s) : launch<__nv_bfloat16, SIGHT>(a, map, grid, s);
+  if ((long long)a.n_new * a.c.group <= M)
+    return dtype == OKQ_FP16 ? launch<__half, SIGHT, true>(a, map, grid, s) : launch<__nv_bfloat16, SIGHT, true>(a, map, grid, s);
+  return dtype == OKQ_FP16 ? launch<__half, SIGHT, false>(a, map, grid, s) : launch<__nv_bfloat16, SIGHT, false>(a, map, grid, s);
 }
 
 }  // namespace
