@@ -593,12 +593,13 @@ class Rope:
     """Rotary positions of one call: positions int32 [3, batch, n], freq float64 [pairs] (contiguous, on the device; kept alive here)."""
 
     def __init__(self, positions, freq, sections, interleaved=False):
-        assert positions.dtype == torch.int32 and positions.dim() == 3 and positions.shape[0] == 3 and positions.is_contiguous()
+        axes, self.batch, self.n = positions.shape
+        assert positions.dtype == torch.int32 and axes == 3 and positions.is_contiguous()
         assert freq.dtype == torch.float64 and freq.numel() == sum(sections) and freq.is_contiguous()
-        if freq.device != positions.device:
+        index = freq.get_device()
+        if index != positions.get_device() or (index < 0 and freq.device != positions.device):
             raise ValueError(f"positions on {positions.device}, freq on {freq.device}")
         self.positions, self.freq = positions, freq
-        self.batch, self.n = positions.shape[1], positions.shape[2]
         self.ref = _rope_struct(*sections, 1 if interleaved else 0, freq.data_ptr(), positions.data_ptr())
 
 

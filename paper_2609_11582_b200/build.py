@@ -29,7 +29,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     flags = list(FLAGS)
     if verbose:
         flags += ["-Xptxas", "-v"]
-    cmd = [nvcc, *flags, "-rdc=false", "-shared", "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES] + ["-lcudart"]
+    cmd = [nvcc, *flags, "-t", "0", "-rdc=false", "-shared", "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES] + ["-lcudart"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if verbose or r.returncode != 0:
         sys.stderr.write(r.stdout + r.stderr)

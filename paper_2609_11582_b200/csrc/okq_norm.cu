@@ -212,14 +212,14 @@ __device__ __forceinline__ float normalise(F2 (&x)[8], float eps, bool& scaled) 
   float s = dot(x, x);
   scaled = s > 1e37f;
   if (__any_sync(0xffffffffu, scaled)) {
-    const float f = scaled ? SMALL : 1.f;   // eps is nothing beside such rows
+    const float f = scaled ? SMALL : 1.f;
 #pragma unroll
     for (int e = 0; e < 8; e++) x[e] = mul2(x[e], f2(f, f));
     const float z = dot(x, x);
     if (scaled) s = z;
   }
-  float r;   // (of a normal number: eps is one, and rows beside which it is not are far above)
-  asm("rsqrt.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(fmaf(s, 1.f / D, scaled ? 0.f : eps)));
+  float r;   // (of a normal number: eps is one, and where it is made smaller the rest is not below 2^-70; two units in the last place)
+  asm("rsqrt.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(fmaf(s, 1.f / D, scaled ? eps * SMALL * SMALL : eps)));
 #pragma unroll
   for (int e = 0; e < 8; e++) x[e] = mul2(x[e], f2(r, r));
   return r;
@@ -557,6 +557,7 @@ okq_status okq_norm_rope_grad(const okq_rope* rope, float eps, int32_t dtype, in
   if ((st = make_rope(rope, r)) != OKQ_OK) return st;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool sums = x[0].weight_grad || x[1].weight_grad;
+  if (((long long)batch * n + TOKENS - 1) / TOKENS > 0x7fffffffll) return OKQ_ERR_UNSUPPORTED;
   if (batch == 0 || n == 0 || x[0].heads + x[1].heads == 0) {   // no rows: sums of nothing
     const cudaError_t e = sums ? launch_dependent(k_norm_weight_grad, dim3(D / 8, 2), 256, 0, s, 1, nullptr, 0, x[0].weight_grad, x[1].weight_grad) : cudaSuccess;
     return e != cudaSuccess ? failed(e) : OKQ_OK;

@@ -188,6 +188,20 @@ def test_rows_at_the_ends_of_the_range(dtype):
     assert torch.isnan(row[5]) and (row[:5] == 0).all() and (row[6:] == 0).all() and torch.isnan(out[0, 0, 8]).all() and torch.isnan(dw).any()
 
 
+def test_an_eps_beside_large_rows():
+    """Rows whose squares have no sum in fp32, and an eps of their size."""
+    g = gen(9)
+    x, up = randn(g, 1, 1, 5, D, dtype=F32) * 2e18, randn(g, 1, 1, 5, D, dtype=F32)
+    w, eps = weight(g, F32, 1.0), 1e37
+    out, dx = torch.empty_like(x).cuda(), torch.empty_like(x).cuda()
+    B.norm_rope_apply(None, x.cuda(), out, w, eps=eps)
+    B.norm_rope_grad(None, x.cuda(), up.cuda(), dx, None, w, eps=eps)
+    ref, y = N.norm_rope(f64(x), f64(w), np.float64(np.float32(eps)))
+    assert (np.abs(f64(out) - ref) <= apply_bound(ref, y, F32, None)).all()
+    gx, _, u = N.norm_rope_grad(f64(x), f64(w), f64(up), np.float64(np.float32(eps)))
+    assert (np.abs(f64(dx) - gx) <= grad_bounds(f64(x), f64(w), f64(up), u, gx, F32, eps, None, 64)[0]).all()
+
+
 def test_gradient_agrees_with_differences():
     """The call's gradients against central differences of the formula in 64 bits (h = 1e-5: 1e-8 of the sum).  Roundings of fp32, 2^-18 of the
     products' magnitudes at most by the bound of the numbers."""

@@ -308,6 +308,47 @@ def test_graphs_share_a_workspace(n):
     assert m.c.seq_len[0].tolist() == [T - 64 * S.slide(T, 64, 100, 5)[1] for T in (450, 214, 1)] == [450 - 64 * 4, 214, 1] and m.c.device_status() == 0
 
 
+# ------------------------------------------------------------------------------------------------ few rows in the prompt kernel
+# (layers, batch, KV heads, group, queries, longest): up to 128 rows to a head; items of one tile, and such that are cut
+NARROW = [(1, 40, 4, 7, 5, 400), (18, 28, 8, 4, 9, 12), (1, 3, 2, 8, 16, 9000), (1, 1, 1, 8, 4, 60000), (2, 33, 4, 7, 18, 1500)]
+
+
+@pytest.mark.parametrize("shape", NARROW, ids=str)
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_up_to_128_rows(shape, dtype):
+    L, batch, H, G, n, longest = shape
+    g = gen(longest + n)
+    for ragged in (False, True):
+        lens = lengths(g, batch, longest, ragged)
+        q_len = None if not ragged else torch.randint(-1, n + 2, (batch,), generator=g).tolist()
+        c = random_cache(g, L, batch, H, H * G, 64, dtype, lens)
+        q, ws = randn(g, L, batch, H * G, n, D, dtype=dtype).cuda(), scratch(c, L, n)
+        plan = B.paged_plan(c, L, n)
+        assert ragged or plan == B.PLAN_PROMPT
+        out = torch.full_like(q, 5.0)
+        B.paged_attention(c, 0, L, q, ws, out, None if q_len is None else i32(q_len))
+        assert c.device_status() == 0
+        check(c, q, out, q_len, 5.0, plan, lambda b, T, m: S.window_mask(T, m, 1 << 30, 0))
+
+
+@pytest.mark.parametrize("batch,H,n,tokens", [(40, 4, 5, 1000), (3, 2, 16, 9000)])
+def test_waits_are_bounded_with_few_rows(batch, H, n, tokens):
+    """As for the other kernels: with nothing delivered every role's wait runs out, and the device goes on."""
+    g = gen(11)
+    c = random_cache(g, 1, batch, H, 7 * H, 64, F16, [tokens] * batch)
+    assert B.paged_plan(c, 1, n) == B.PLAN_PROMPT
+    q = randn(g, 1, batch, 7 * H, n, D).cuda()
+    out, ws = torch.zeros_like(q), scratch(c, 1, n)
+    B.debug_paged_timeout(c, 0, 1, q, ws, out, limit_clocks=2_000_000)
+    torch.cuda.synchronize()
+    assert c.device_status() == B.ERR_TIMEOUT and torch.isnan(out).all()
+    c.status.zero_()
+    out.fill_(5.0)
+    B.paged_attention(c, 0, 1, q, ws, out)
+    check(c, q, out, None, 5.0, B.PLAN_PROMPT, lambda b, T, m: S.window_mask(T, m, 1 << 30, 0))
+    assert c.device_status() == 0
+
+
 # ------------------------------------------------------------------------------------------------ pages that slide
 @pytest.mark.parametrize("page,max_pages,batch", [(32, 9, 40), (64, 40, 7), (32, 3001, 5), (256, 3, 300)])
 def test_slide_against_lists(page, max_pages, batch):
