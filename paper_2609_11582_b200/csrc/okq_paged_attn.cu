@@ -14,7 +14,6 @@ struct Plan {
   bool decode;
   int grid, ranges;         // blocks of the line of tiles, its parts
   int cluster;              // decode: blocks to a (layer, sequence, KV head), 0 where the line is cut evenly
-  bool whole;               // prompt: the line is cut between items
   size_t heads, bytes;      // of the workspace: heads; what any plan for as many layers and queries or fewer takes
 };
 
@@ -53,11 +52,6 @@ bool make_plan(const okq_paged* c, int layer_count, int n_new, int window, int s
       if (few <= decode_clusters(size) && (per_few + DECODE_PIPES * size - 1) / (DECODE_PIPES * size) <= other) p.cluster = size;
     if (p.cluster) p.decode = true;
   }
-  // A window's or a tree's line cut between items: ranges have whole ones and there is nothing to merge, but in the last round of items blocks
-  // may be idle.  That, in tiles, against the merge and what its parts cost (us, whole items and even ranges: 224 items of 6 tiles 70, 80;
-  // of 14 tiles 125, 125; of 25 tiles 186, 172; 180 items of 19 tiles 141, 121; 240 items of 7 tiles 72, 82).
-  const double rounds = many / (double)n, idle = (double)(long long)(rounds + 0.999999) - rounds;
-  p.whole = !p.decode && rounds > 1.0 && idle * (double)(per_many + PROMPT_ITEM) <= PROMPT_MERGE;
   // blocks, ranges and bytes of the line (the workspace is the line's, cluster or not)
   auto line = [&](bool decode) {
     const double tiles = decode ? few * (double)per_few : many * (double)per_many;
@@ -112,9 +106,8 @@ static okq_status attention(const okq_paged* cache, int32_t layer, int32_t layer
   AttnArgs a{paged_view(cache), {q, {qs[0], qs[1], qs[2], qs[3]}}, {out, {os[0], os[1], os[2], os[3]}}, q_len, r, layer, layer_count, n_new,
              sm_scale * 1.44269504088896340736f, limit, withhold, static_cast<Head*>(workspace),
              reinterpret_cast<float*>(static_cast<char*>(workspace) + p.heads), sight.window, sight.sinks,
-             reinterpret_cast<const unsigned long long*>(sight.seen), (n_new + 63) / 64, 0};
+             reinterpret_cast<const unsigned long long*>(sight.seen), (n_new + 63) / 64};
   const Sight how = sight.window ? WINDOW : sight.seen ? TREE : CAUSAL;
-  a.whole = how != CAUSAL && p.whole;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = p.decode ? launch_paged_decode(a, cache->dtype, how, p.grid, p.cluster, s) : launch_paged_prompt(a, cache->dtype, how, p.grid, s);
   if (e != cudaSuccess) {

@@ -54,7 +54,6 @@ struct AttnArgs {
   int window, sinks;                    // WINDOW
   const unsigned long long* seen;       // TREE: [batch][n_new][words]
   int words;
-  int whole;                            // not CAUSAL: ranges are cut between items only, so that there are no parts
 };
 
 // n lowest bits of 64
@@ -68,6 +67,7 @@ struct Span {
 };
 template <int ROWS, int EXTRA, int SIGHT = CAUSAL> struct Work {
   int pairs, n_kv, group;
+  bool whole = false;   // ranges are cut between items only, so that there are no parts (find_places)
   const AttnArgs& a;
   __device__ __forceinline__ explicit Work(const AttnArgs& args) : pairs(args.layer_count * args.c.batch), n_kv(args.c.n_kv), group(args.c.group), a(args) {}
   __device__ __forceinline__ void lens(int li, int b, int& len, int& m) const {   // tokens held, queries
@@ -107,6 +107,10 @@ template <int ROWS, int EXTRA, int SIGHT = CAUSAL> struct Work {
   }
 };
 
+// Whether the line may be cut between items only: where many rows are put together by a merge that costs several tiles, and where the causal
+// kernels' results would not change with it.
+template <int ROWS, int SIGHT> constexpr bool CAN_BE_WHOLE = ROWS > 8 && SIGHT != CAUSAL;
+
 // A walk over the tiles of a range.
 template <int ROWS, int EXTRA, int SIGHT = CAUSAL> struct Cursor {
   int pair, h, rt, tile;     // item and tile inside it
@@ -145,14 +149,14 @@ template <int ROWS, int EXTRA, int SIGHT = CAUSAL> struct Cursor {
     }
   }
   __device__ __forceinline__ int piece(const Work<ROWS, EXTRA, SIGHT>& w) const {   // tiles of the item in the range, from this one on
-    return SIGHT != CAUSAL && w.a.whole ? nt - tile : min(nt - tile, left);
+    return CAN_BE_WHOLE<ROWS, SIGHT> && w.whole ? nt - tile : min(nt - tile, left);
   }
   __device__ __forceinline__ void skip(const Work<ROWS, EXTRA, SIGHT>& w, int n) {       // no more than piece()
     tile += n;
     left -= n;
     ended = tile == nt;
     if (ended) left -= EXTRA;
-    ok = left > 0 || (SIGHT != CAUSAL && w.a.whole && !ended);
+    ok = left > 0 || (CAN_BE_WHOLE<ROWS, SIGHT> && w.whole && !ended);
     if (ended && ok) next_item(w);
   }
   __device__ __forceinline__ void next(const Work<ROWS, EXTRA, SIGHT>& w) { skip(w, 1); }
@@ -162,6 +166,7 @@ template <int ROWS, int EXTRA, int SIGHT = CAUSAL> struct Cursor {
 // ranges the last ranges have none.  (Numbers of units have 32 bits: the caller sees to it.)
 struct Cuts {
   int total, each, extra;
+  bool whole = false;
   __device__ __forceinline__ Cuts(int t, int ranges) : total(t), each(t / ranges), extra(t - each * ranges) {}
   __device__ __forceinline__ int start(int v) const { return v * each + min(v, extra); }
   __device__ __forceinline__ int size(int v) const { return each + (v < extra); }
@@ -204,12 +209,14 @@ __device__ __forceinline__ void warp_row_tile(const Work<ROWS, EXTRA, SIGHT>& w,
 
 // All threads of a block find the line's length and where the first units of the block's ranges v0, v0 + step, .. lie.  Threads hold
 // consecutive pairs.
+constexpr float WHOLE_GAIN = 8.f;   // what a merge and its parts cost, in units
 template <int G> struct FindSmem {
-  int warp[32];
+  int warp[16], items[16], most[16];   // of a warp's pairs: units, items, the largest item's units (the latter two: CAN_BE_WHOLE)
   int place[G][6];
 };
 template <int ROWS, int EXTRA, int NT, int G, int SIGHT>
 __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS, EXTRA, SIGHT>& w, int ranges, int v0, int step) {
+  static_assert(NT <= 512, "a place for each warp");
   const int tid = threadIdx.x, lane = tid & 31, wp = tid >> 5;
   const int chunk = (w.pairs + NT - 1) / NT, p0 = min(w.pairs, tid * chunk), p1 = min(w.pairs, p0 + chunk);
   int len = 0, m = 0, per_head = 0, mine = 0;    // (of the last pair looked at: with no more pairs than threads, the only one)
@@ -237,6 +244,18 @@ __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS, EX
     if (lane >= d) v += y;
   }
   if (lane == 31) sm.warp[wp] = v;
+  if (CAN_BE_WHOLE<ROWS, SIGHT>) {
+    int items = 0, most = 0;
+    for (int p = p0; p < p1; p++) {
+      if (chunk > 1) w.lens(p, len, m);
+      const int n = w.row_tiles(m);
+      items += n * w.n_kv;
+      if (n > 0) most = max(most, max(w.units(w.tiles(len, m, 0)), w.units(w.tiles(len, m, n - 1))));   // (those between are hardly longer)
+    }
+    items = __reduce_add_sync(0xffffffffu, items);
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) { sm.items[wp] = items; sm.most[wp] = most; }
+  }
   __syncthreads();
   int before = v - mine, total = 0;
 #pragma unroll
@@ -245,7 +264,20 @@ __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS, EX
     if (i < wp) before += x;
     total += x;
   }
-  const Cuts cuts(total, ranges);
+  Cuts cuts(total, ranges);
+  if (CAN_BE_WHOLE<ROWS, SIGHT>) {
+    // Whole items, as many rounds of the largest as it takes, against even parts and their merge, in units (us, whole items and even parts,
+    // windows of long sequences: 224 items of 6 tiles 67, 74; of 14 tiles 121, 119; 240 items of 7 tiles 74, 80; 180 of 19 tiles 141, 119;
+    // 240 ragged ones of up to 12 tiles 92, 74).
+    int items = 0, most = 0;
+#pragma unroll
+    for (int i = 0; i < NT / 32; i++) {
+      items += sm.items[i];
+      most = max(most, sm.most[i]);
+    }
+    const int rounds = (items + ranges - 1) / ranges;
+    cuts.whole = rounds > 1 && (float)rounds * (float)most <= (float)total / (float)ranges + WHOLE_GAIN;
+  }
   if (together) {
 #pragma unroll
     for (int g = 0; g < G; g++) {
@@ -294,7 +326,7 @@ __device__ __forceinline__ Cursor<ROWS, EXTRA, SIGHT> place(const FindSmem<G>& s
   c.li = w.layer_of(c.pair);
   c.b = c.pair - c.li * w.a.c.batch;
   c.measure(w);
-  if (c.tile >= c.nt || (SIGHT != CAUSAL && w.a.whole && c.tile > 0)) {   // behind an item's last tile, or where the range before goes on
+  if (c.tile >= c.nt || (CAN_BE_WHOLE<ROWS, SIGHT> && w.whole && c.tile > 0)) {   // behind an item's last tile, or where the range before goes on
     c.left -= c.nt + EXTRA - c.tile;
     c.ok = c.left > 0;
     if (c.ok) c.next_item(w);
@@ -431,7 +463,6 @@ int decode_clusters(int size);   // clusters of so many blocks (at most eight) t
 // okq_paged_prompt.cu: PROMPT_ROWS rows to an item, one pipeline per block.  Own costs alike: 16 sequences x 4 heads of up to 12345 tokens,
 // 35 rows 62 us with 3, 58 with 4, 55 with 6, 56 with 8; 64 x 8 of up to 1500, 1024 rows, 555, 511, 462, 482.
 constexpr int PROMPT_ROWS = 256, PROMPT_EXTRA = 6;
-constexpr double PROMPT_ITEM = 4.0, PROMPT_MERGE = 8.0;   // an item's own costs, and those of a merge with its parts, in tiles
 cudaError_t launch_paged_prompt(const AttnArgs& a, int dtype, Sight sight, int grid, cudaStream_t s);
 
 // the pool's codes as rows of 128 bytes, copied 32 at a time

@@ -396,9 +396,10 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
   depend_wait();
 
   const PagedView& c = a.c;
-  const Work<R, EXTRA, SIGHT> work(a);
+  Work<R, EXTRA, SIGHT> work(a);
   const int v = blockIdx.x;                     // this block's range
   const Cuts cuts = find_places<R, EXTRA, NT, 1, SIGHT>(sm.find, work, gridDim.x, v, 0);
+  work.whole = cuts.whole;
   const int end = cuts.start(v) + cuts.size(v); // the unit behind it
   const Heads<R> heads(work.pairs, c.n_kv, c.group, a.n_new, gridDim.x);
   Cursor<R, EXTRA, SIGHT> cur = place<R, EXTRA, 1, SIGHT>(sm.find, work, cuts, v, 0);
@@ -911,7 +912,7 @@ template <class T, int SIGHT, bool NARROW> cudaError_t launch(const AttnArgs& a,
     attr_done(attr_mask, dev);
   }
   cudaError_t e = launch_dependent(k_paged_prompt<T, SIGHT, NARROW>, dim3(grid), NT, SMEM, s, 1, map, a);
-  return e == cudaSuccess && !a.whole ? launch_merge<T>(a, grid, s) : e;
+  return e == cudaSuccess ? launch_merge<T>(a, grid, s) : e;
 }
 
 template <int SIGHT> cudaError_t launch_sight(const AttnArgs& a, const CUtensorMap& map, int dtype, int grid, cudaStream_t s) {
