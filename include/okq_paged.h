@@ -1,6 +1,6 @@
 /*
- * okq_paged - an 8-bit KV cache in pages, next to the 2-bit cache of okq.h: rotary positions with three axes, append,
- * attention for prompts and single tokens, and the pages' bookkeeping.  Plain C ABI with the conventions of okq.h: every tensor
+ * okq_paged - an 8-bit KV cache in pages, next to the 2-bit cache of okq.h: rotary positions with three axes, alone or behind a norm of
+ * every head, append, attention for prompts and single tokens, with a window, and for trees of drafted tokens, and the pages' bookkeeping.  Plain C ABI with the conventions of okq.h: every tensor
  * argument is a DEVICE pointer owned by the caller and aligned to 16 bytes; structs, `strides` and `sections` are HOST memory,
  * read before the call returns; calls are asynchronous on `stream` and allocate nothing; errors that the host can see are returned
  * before anything is launched, errors only the device can see go to the cache's sticky status word.

@@ -1,5 +1,7 @@
 // Attention over the 8-bit paged cache for few query rows per (layer, sequence, KV head): single tokens, a few drafted ones, and short
-// pieces of prompts.  An item has up to eight rows.
+// pieces of prompts.  An item has up to eight rows.  With a window the tiles between the sinks and the window are left out, and of the
+// others the blocks that no row sees; where some row does not see a tile's token, its score is -inf (of a tree: by the bits, loaded while
+// the products are waited for).
 //
 // All products are of 8-bit integers on tcgen05 (kind::i8), with the cache's codes as they lie in memory for one operand:
 //   scores   S[token][row] = K[token][channel] Q[row][channel]: A = a tile of 128 tokens (K-major), B = the queries as three signed
@@ -20,6 +22,7 @@
 // Bound by memory: 256 bytes per token and head; an SM's share of the copy rate is a tile in about 1400 cycles.  16 sequences of 32768
 // tokens x 4 heads (538 MB) take 95 us a call, 5.6 TB/s with the merge and both ends (93 in a graph); 1 sequence of 131072 tokens (134 MB,
 // partly in the second-level cache) 34; 1 head of 2048 tokens 7.2, which is latency: launch, table, copies, products, the cluster's merge.
+// 16 sequences x 4 heads with a window of 4096 and 64 sinks (68 MB, 2 blocks to each head) 21 us, 10 of them latency at both ends.
 // (The running maxima in every thread and not in one lane per row: 98 us and not 95, 128 registers and not 127.)
 #include "okq_paged_attn.cuh"
 

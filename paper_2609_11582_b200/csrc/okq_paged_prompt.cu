@@ -1,5 +1,5 @@
 // Attention over the 8-bit paged cache for many query rows per (layer, sequence, KV head): prompts, pieces of prompts,
-// drafted tokens.  Causal against the end of the sequence.
+// drafted tokens.  Causal against the end of the sequence, with a window and sinks, or by the bits of a tree of drafted tokens.
 //
 // Both products are fp16 on tcgen05 (kind::f16, fp32 accumulation in tensor memory):
 //   S[row][token] = Q[row][channel] K[token][channel]   the cache's codes are fp16 numbers as they are (|code| <= 127); queries are scaled
@@ -22,13 +22,21 @@
 // has no more than 128 rows (a dual item), both streams have the same ones: A takes the first 64 tokens of every tile, B the others, and
 // their sums are put together at the end.
 //
+// What a row sees of a step is one number where the kernel is causal, and 64 bits otherwise, worked out while the products are waited for.
+// Steps that some row does not see all of have -inf put in and go the same way as the others: of a window or a tree such steps are a large
+// part, and a copy of the loop for them took 4000 to 5000 cycles a step for its code's size, where this takes 2600 to 2900.  (The causal
+// kernel keeps its copy, which rounds otherwise, for the step or two at the end.)
+//
 // At best bound by the exponentials (16 per cycle and SM: 2048 cycles for 256 x 128 scores) and the products (2048 cycles at fp16's
-// rate).  What it takes is about 4200 (2048 queries x 28 heads on 8192 tokens 286 us a call, 736 TFLOP/s of products): a softmax warp's own
+// rate).  What it takes is about 4200 (2048 queries x 28 heads on 8192 tokens 260 us a call, 810 TFLOP/s of products): a softmax warp's own
 // chain of waits, tensor memory, maximum, exponentials and roundings, with two such warps on a scheduler and 128 registers to each (the
-// maximum beside the exponentials, by last step's reference: 390 us, spills).
-// Few rows (a dual item) are bound by the conversion, a step in 1500 cycles, a third of it waits and fences: 35 rows, 16 sequences x 4
-// heads of up to 12345 tokens 50 us a call (a converting warp to every other step, with half of those waits but a ring that is then too
-// short: 61).
+// maximum beside the exponentials, by last step's reference: 390 us, spills).  A multiplication of O is another 1000 cycles in its step.
+// A window's items are short, and their ends show: of 85000 cycles of 256 rows with a window of 1400 (26 steps) the queries take 5000, the
+// first scores 2500, the last products and the output 7000; 2048 queries x 28 heads 109 us.  Queries are copied to their place as they are
+// while the item before ends (loaded there and then they took 11000 to 17000 cycles).
+// Few rows (a dual item) are bound by the conversion, a step in 1500 to 1700 cycles, a third of it waits and fences: 35 rows, 16 sequences x 4
+// heads of up to 12345 tokens 47 us a call (a converting warp to every other step, with half of those waits but a ring that is then too
+// short: 61).  Calls whose items are all dual have a kernel of their own (NARROW).
 #include "okq_paged_attn.cuh"
 
 namespace okq {
