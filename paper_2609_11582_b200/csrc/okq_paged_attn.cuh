@@ -67,7 +67,12 @@ struct Span {
 };
 template <int ROWS, int EXTRA, int SIGHT = CAUSAL> struct Work {
   int pairs, n_kv, group;
-  bool whole = false;   // ranges are cut between items only, so that there are no parts (find_places)
+  uint32_t whole_at = 0;   // CAN_BE_WHOLE: place in shared memory of FindSmem's `whole`
+  __device__ __forceinline__ bool whole() const {
+    int x;
+    asm volatile("ld.shared.s32 %0, [%1];\n" : "=r"(x) : "r"(whole_at) : "memory");
+    return x != 0;
+  }
   const AttnArgs& a;
   __device__ __forceinline__ explicit Work(const AttnArgs& args) : pairs(args.layer_count * args.c.batch), n_kv(args.c.n_kv), group(args.c.group), a(args) {}
   __device__ __forceinline__ void lens(int li, int b, int& len, int& m) const {   // tokens held, queries
@@ -149,14 +154,14 @@ template <int ROWS, int EXTRA, int SIGHT = CAUSAL> struct Cursor {
     }
   }
   __device__ __forceinline__ int piece(const Work<ROWS, EXTRA, SIGHT>& w) const {   // tiles of the item in the range, from this one on
-    return CAN_BE_WHOLE<ROWS, SIGHT> && w.whole ? nt - tile : min(nt - tile, left);
+    return CAN_BE_WHOLE<ROWS, SIGHT> && w.whole() ? nt - tile : min(nt - tile, left);
   }
   __device__ __forceinline__ void skip(const Work<ROWS, EXTRA, SIGHT>& w, int n) {       // no more than piece()
     tile += n;
     left -= n;
     ended = tile == nt;
     if (ended) left -= EXTRA;
-    ok = left > 0 || (CAN_BE_WHOLE<ROWS, SIGHT> && w.whole && !ended);
+    ok = left > 0 || (CAN_BE_WHOLE<ROWS, SIGHT> && w.whole() && !ended);
     if (ended && ok) next_item(w);
   }
   __device__ __forceinline__ void next(const Work<ROWS, EXTRA, SIGHT>& w) { skip(w, 1); }
@@ -166,7 +171,6 @@ template <int ROWS, int EXTRA, int SIGHT = CAUSAL> struct Cursor {
 // ranges the last ranges have none.  (Numbers of units have 32 bits: the caller sees to it.)
 struct Cuts {
   int total, each, extra;
-  bool whole = false;
   __device__ __forceinline__ Cuts(int t, int ranges) : total(t), each(t / ranges), extra(t - each * ranges) {}
   __device__ __forceinline__ int start(int v) const { return v * each + min(v, extra); }
   __device__ __forceinline__ int size(int v) const { return each + (v < extra); }
@@ -212,6 +216,7 @@ __device__ __forceinline__ void warp_row_tile(const Work<ROWS, EXTRA, SIGHT>& w,
 constexpr float WHOLE_GAIN = 8.f;   // what a merge and its parts cost, in units
 template <int G> struct FindSmem {
   int warp[16], items[16], most[16];   // of a warp's pairs: units, items, the largest item's units (the latter two: CAN_BE_WHOLE)
+  int whole;
   int place[G][6];
 };
 template <int ROWS, int EXTRA, int NT, int G, int SIGHT>
@@ -264,7 +269,7 @@ __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS, EX
     if (i < wp) before += x;
     total += x;
   }
-  Cuts cuts(total, ranges);
+  const Cuts cuts(total, ranges);
   if (CAN_BE_WHOLE<ROWS, SIGHT>) {
     // Whole items, as many rounds of the largest as it takes, against even parts and their merge, in units (us, whole items and even parts,
     // windows of long sequences: 224 items of 6 tiles 67, 74; of 14 tiles 121, 119; 240 items of 7 tiles 74, 80; 180 of 19 tiles 141, 119;
@@ -276,7 +281,7 @@ __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS, EX
       most = max(most, sm.most[i]);
     }
     const int rounds = (items + ranges - 1) / ranges;
-    cuts.whole = rounds > 1 && (float)rounds * (float)most <= (float)total / (float)ranges + WHOLE_GAIN;
+    sm.whole = rounds > 1 && (float)rounds * (float)most <= (float)total / (float)ranges + WHOLE_GAIN;
   }
   if (together) {
 #pragma unroll
@@ -326,7 +331,7 @@ __device__ __forceinline__ Cursor<ROWS, EXTRA, SIGHT> place(const FindSmem<G>& s
   c.li = w.layer_of(c.pair);
   c.b = c.pair - c.li * w.a.c.batch;
   c.measure(w);
-  if (c.tile >= c.nt || (CAN_BE_WHOLE<ROWS, SIGHT> && w.whole && c.tile > 0)) {   // behind an item's last tile, or where the range before goes on
+  if (c.tile >= c.nt || (CAN_BE_WHOLE<ROWS, SIGHT> && w.whole() && c.tile > 0)) {   // behind an item's last tile, or where the range before goes on
     c.left -= c.nt + EXTRA - c.tile;
     c.ok = c.left > 0;
     if (c.ok) c.next_item(w);

@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
   Work<R, EXTRA, SIGHT> work(a);
   const int v = blockIdx.x;                     // this block's range
   const Cuts cuts = find_places<R, EXTRA, NT, 1, SIGHT>(sm.find, work, gridDim.x, v, 0);
-  work.whole = cuts.whole;
+  work.whole_at = smem_u32(&sm.find.whole);
   const int end = cuts.start(v) + cuts.size(v); // the unit behind it
   const Heads<R> heads(work.pairs, c.n_kv, c.group, a.n_new, gridDim.x);
   Cursor<R, EXTRA, SIGHT> cur = place<R, EXTRA, 1, SIGHT>(sm.find, work, cuts, v, 0);
