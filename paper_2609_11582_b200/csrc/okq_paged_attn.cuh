@@ -382,12 +382,17 @@ __device__ __forceinline__ void write_empty(const AttnArgs& a, const Work<ROWS, 
   }
 }
 
+// A sum that falls so far below a new maximum that 2^d leaves fp32's normal numbers (the row's largest weight may lie on a token without
+// value) is multiplied by 2^-100 first, and its maximum raised by as much.
+constexpr float FALL = -120.f, LATE_BITS = 100.f, LATE = 7.888609e-31f;
+__device__ __forceinline__ bool falls(float top, float ref) { return top - ref < FALL && top != -INFINITY; }
+
 constexpr int MERGE_NT = 512;
 
 // Block (x, y): row y of the item of head x, if it is in parts, each warp has every sixteenth part, a lane four channels.  Bound by latency:
 // a few megabytes of parts at most; all of a part is loaded at once, seven parts in flight.  (Of the decode kernel's parts.)
 template <class T, int ROWS>
-__global__ void __launch_bounds__(MERGE_NT) k_paged_merge(const AttnArgs a) {
+__global__ void __launch_bounds__(MERGE_NT, 2) k_paged_merge(const AttnArgs a) {
   constexpr int WARPS = MERGE_NT / 32, WPR = WARPS;
   __shared__ float4 sums[WARPS][32];
   __shared__ float2 stat[WARPS];
@@ -423,13 +428,16 @@ __global__ void __launch_bounds__(MERGE_NT) k_paged_merge(const AttnArgs a) {
       float mn = top;
 #pragma unroll
       for (int e = 0; e < 7; e++) mn = fmaxf(mn, tk[e]);
-      const float ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(top - ref);
+      const float ref = mn == -INFINITY ? 0.f : mn;
+      if (falls(top, ref)) { top += LATE_BITS; l *= LATE; acc.x *= LATE; acc.y *= LATE; acc.z *= LATE; acc.w *= LATE; }
+      const float f0 = ex2(top - ref);
       l *= f0;
       acc.x *= f0; acc.y *= f0; acc.z *= f0; acc.w *= f0;
       top = mn;
 #pragma unroll
       for (int e = 0; e < 7; e++) {
         if (k0 + e * WPR >= n) continue;
+        if (falls(tk[e], ref)) { tk[e] += LATE_BITS; lk[e] *= LATE; x[e].x *= LATE; x[e].y *= LATE; x[e].z *= LATE; x[e].w *= LATE; }   // (the same in the whole warp)
         const float f = ex2(tk[e] - ref);
         l = fmaf(lk[e], f, l);
         acc.x = fmaf(x[e].x, f, acc.x); acc.y = fmaf(x[e].y, f, acc.y); acc.z = fmaf(x[e].z, f, acc.z); acc.w = fmaf(x[e].w, f, acc.w);
@@ -444,14 +452,18 @@ __global__ void __launch_bounds__(MERGE_NT) k_paged_merge(const AttnArgs a) {
     float mn = top;
 #pragma unroll
     for (int i = 1; i < WPR; i++) mn = fmaxf(mn, stat[warp + i].x);
-    const float ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(top - ref);
+    const float ref = mn == -INFINITY ? 0.f : mn;
+    if (falls(top, ref)) { top += LATE_BITS; l *= LATE; acc.x *= LATE; acc.y *= LATE; acc.z *= LATE; acc.w *= LATE; }
+    const float f0 = ex2(top - ref);
     l *= f0;
     acc.x *= f0; acc.y *= f0; acc.z *= f0; acc.w *= f0;
 #pragma unroll
     for (int i = 1; i < WPR; i++) {
-      const float f = ex2(stat[warp + i].x - ref);
-      const float4 x = sums[warp + i][lane];
-      l = fmaf(stat[warp + i].y, f, l);
+      float2 st = stat[warp + i];
+      float4 x = sums[warp + i][lane];
+      if (falls(st.x, ref)) { st.x += LATE_BITS; st.y *= LATE; x.x *= LATE; x.y *= LATE; x.z *= LATE; x.w *= LATE; }
+      const float f = ex2(st.x - ref);
+      l = fmaf(st.y, f, l);
       acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y); acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);
     }
   }

@@ -463,7 +463,18 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       const float w0 = sy.wmax[b][0][rl], w1 = sy.wmax[b][1][rl], w2 = sy.wmax[b][2][rl], w3 = sy.wmax[b][3][rl];
       const float mn = fmaxf(fmaxf(fmaxf(w0, w1), fmaxf(w2, w3)), top);
       if (__any_sync(0xffffffffu, mn > top)) {   // (the same in all of the pipeline's workers)
-        const float keep = mn > top ? ex2(top - mn) : 1.f;
+        float d = mn > top ? top - mn : 0.f;
+        const bool far = falls(d, 0.f);
+        if (__any_sync(0xffffffffu, far)) {
+          d += far ? LATE_BITS : 0.f;
+#pragma unroll
+          for (int r = 0; r < R; r++) {
+            const float f = __shfl_sync(0xffffffffu, far ? LATE : 1.f, r);
+            sum[r] *= f;
+            o[r] *= f;
+          }
+        }
+        const float keep = ex2(d);
 #pragma unroll
         for (int r = 0; r < R; r++) {
           const float f = __shfl_sync(0xffffffffu, keep, r);
@@ -583,6 +594,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
       const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
       for (int k = 0; k < MOST_CLUSTER; k++) {
+        if (falls(t[k], ref)) { t[k] += LATE_BITS; l[k] *= LATE; o[k] *= LATE; }
         const float f = ex2(t[k] - ref);
         ls = fmaf(l[k], f, ls);
         os = fmaf(o[k], f, os);
@@ -603,9 +615,9 @@ __global__ void __launch_bounds__(NT, 1) k_paged_decode(const __grid_constant__ 
 #pragma unroll
       for (int g2 = 0; g2 < G; g2++) {
         const float* y = reinterpret_cast<const float*>(sm.pipe[g2].p);
-        const float f = ex2(y[D] - top);
-        l = fmaf(y[D + 1], f, l);
-        o = fmaf(y[ch], f, o);
+        const float late = falls(y[D], top) ? LATE : 1.f, f = ex2(y[D] - top + (late == LATE ? LATE_BITS : 0.f));
+        l = fmaf(y[D + 1] * late, f, l);
+        o = fmaf(y[ch] * late, f, o);
       }
       out_row<T>(a, cur.li, cur.b, cur.h, R * cur.rt + r)[ch] = from_f<T>(l == 0.f ? 0.f : o / l);
     }

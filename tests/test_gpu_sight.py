@@ -1,6 +1,7 @@
 """Attention with a window and for trees of drafted tokens over the 8-bit paged cache, and sliding pages, on the GPU against the oracle in
 64 bits."""
 import random
+import threading
 
 import numpy as np
 import pytest
@@ -12,7 +13,7 @@ from oracle import okq_sight_oracle as S
 from paper_2609_11582_b200 import binding as B
 from tests.test_gpu_norm import apply_bound
 from tests.test_gpu_paged import BF16, BLOCK, D, F16, Model, f64, gen, positions, randn, random_cache
-from tests.test_gpu_paged_numbers import kernel_bound
+from tests.test_gpu_paged_numbers import Store, kernel_bound, lift, steered
 
 pytestmark = pytest.mark.gpu
 i32 = lambda x: torch.tensor(x, dtype=torch.int32).cuda()  # noqa: E731
@@ -306,6 +307,96 @@ def test_graphs_share_a_workspace(n):
             assert torch.equal(outs[i], got[i])
         graphs[2].replay()
     assert m.c.seq_len[0].tolist() == [T - 64 * S.slide(T, 64, 100, 5)[1] for T in (450, 214, 1)] == [450 - 64 * 4, 214, 1] and m.c.device_status() == 0
+
+
+@pytest.mark.parametrize("n", [1, 5, 64])
+def test_a_threads_first_call_may_be_a_captured_one(n):
+    m = Model(1, 2, 2, 14, max_pages=6, page=64, dtype=F16)
+    m.append(200, [200, 64])
+    q, ws = randn(m.g, 1, 2, 14, n, D).cuda(), scratch(m.c, 1, n)
+    seen = torch.tensor([to_words([1 << i for i in range(n)], n)] * 2).cuda()
+    want, got, graph, failed = [torch.zeros_like(q) for _ in range(2)], [torch.zeros_like(q) for _ in range(2)], torch.cuda.CUDAGraph(), []
+
+    def both(o):
+        B.paged_attention_window(m.c, 0, 1, q, ws, o[0], 70, 2)
+        B.paged_attention_tree(m.c, 0, 1, q, ws, o[1], seen)
+
+    def capture():
+        try:
+            with torch.cuda.graph(graph):
+                both(got)
+        except BaseException as e:   # noqa: BLE001
+            failed.append(e)
+    t = threading.Thread(target=capture)
+    t.start()
+    t.join()
+    assert not failed
+    graph.replay()
+    both(want)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_calls_at_once_on_two_streams():
+    """Two sequences' worth of calls next to one another, each with its own workspace, give what they give alone."""
+    g = gen(31)
+    jobs = []
+    for n, window in ((1, 300), (5, 200), (70, 450), (3, None), (40, None)):
+        c = random_cache(g, 1, 3, 2, 14, 64, BF16, [2000, 900, 64])
+        q = randn(g, 1, 3, 14, n, D, dtype=BF16).cuda()
+        seen = torch.tensor([to_words([1 << i | i for i in range(n)], n)] * 3).cuda()
+        jobs.append((c, q, n, window, seen, [scratch(c, 1, n) for _ in range(2)], [torch.zeros_like(q) for _ in range(3)]))
+
+    def call(job, which, out, stream=None):
+        c, q, n, window, seen, ws, outs = job
+        if window:
+            B.paged_attention_window(c, 0, 1, q, ws[which], outs[out], window, 4, stream=stream)
+        else:
+            B.paged_attention_tree(c, 0, 1, q, ws[which], outs[out], seen, stream=stream)
+    for job in jobs:
+        call(job, 0, 0)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        for k in range(len(jobs)):
+            call(jobs[k], 0, 1, streams[0])
+            call(jobs[-1 - k], 1, 2, streams[1])
+    torch.cuda.synchronize()
+    for job in jobs:
+        assert torch.equal(job[6][0], job[6][1]) and torch.equal(job[6][0], job[6][2]) and job[0].device_status() == 0
+
+
+# ------------------------------------------------------------------------------------------------ values of very different sizes
+@pytest.mark.parametrize("seed", range(6))
+def test_numbers_behind_masks(seed):
+    """Windows and any bits over keys and values with zeros, values from 1e-20 to 1e9 and tokens that take all of the weight, in stretches that
+    masks cut: each row by its kernel's own bound."""
+    rng = random.Random(seed)
+    for shape in ((150, 2, 4, 8, 2500, True), (16, 2, 2, 16, 3000 + seed, True), (1, 24, 8, 56, 2500, True), (3, 24, 8, 40, 2500, True), (8, 1, 1, 2, 8000, False)):
+        n, batch, H, Hq, T, wide = shape
+        q, k, v = steered(*shape, seed=seed, spread=rng.choice([0.5, 1.0, 3.0, 8.0]))
+        for _ in range(rng.randint(1, 4)):
+            a = rng.randrange(T)
+            b = min(T, a + rng.choice([1, 32, 128, 300, 1000]))
+            what = rng.choice(["size", "zeros", "lift", "sink"])
+            if what == "size":
+                v[..., a:b, :] *= 10.0 ** rng.choice([-20, -9, -6, -4, 4, 9])
+            elif what == "zeros":
+                v[..., a:b, :] = 0
+            elif what == "lift":
+                k[..., a:b, 0] = lift(rng.choice([-90.0, -30.0, 20.0, 60.0, 300.0]))
+            else:
+                k[..., a, 0] = lift(rng.choice([30.0, 100.0]))
+                v[..., a, :] = 0
+        c = Store(k, v, Hq, wide, seed=seed).c
+        q, ws = q.cuda(), scratch(c, 1, n)
+        window, sinks = max(1, int(T ** rng.random())), rng.choice([0, 1, 4, 100, 700])
+        sets = [[rng.getrandbits(64 * ((n + 63) // 64)) for _ in range(n)] for _ in range(batch)]
+        out = torch.full_like(q, 5.0)
+        B.paged_attention_window(c, 0, 1, q, ws, out, window, sinks)
+        check(c, q, out, None, 5.0, B.paged_plan_window(c, 1, n, window, sinks), lambda b, T, m: S.window_mask(T, m, window, sinks))
+        B.paged_attention_tree(c, 0, 1, q, ws, out, torch.tensor([to_words(x, n) for x in sets]).cuda())
+        check(c, q, out, None, 5.0, B.paged_plan(c, 1, n), lambda b, T, m: S.tree_mask(T, m, sets[b]))
+        assert c.device_status() == 0
 
 
 # ------------------------------------------------------------------------------------------------ few rows in the prompt kernel
