@@ -1,4 +1,6 @@
 """Normed heads with rotary positions, and their gradients, on the GPU against the oracle in 64 bits."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -265,3 +267,55 @@ def test_other_stream_and_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, out))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_keys_alone_and_queries_alone(dtype):
+    """A side without heads; its weight's gradient is zeros.  The other side's numbers are those of a call with both."""
+    g = gen(8)
+    rope = B.Rope(positions(g, 2, 21, "near").cuda(), B.rope_frequencies(1e6, 64), (24, 20, 20), True)
+    q, k, qu, ku = (tensor(g, 2, h, 21, dtype, True) for h in (5, 3, 5, 3))
+    wq, wk = weight(g, dtype), weight(g, dtype)
+    ws = torch.empty(B.norm_rope_workspace_bytes(2, 21, 5, 3), dtype=torch.uint8, device="cuda")
+    both, alone = [torch.empty_like(x) for x in (q, k, q, k)], [torch.empty_like(x) for x in (q, k, q, k)]
+    none = torch.empty(2, 0, 21, D, dtype=dtype, device="cuda")
+    sums = torch.full((2, D), 7.0, device="cuda")
+    B.norm_rope_apply(rope, q, both[0], wq, k, both[1], wk)
+    B.norm_rope_grad(rope, q, qu, both[2], ws, wq, sums[0], k, ku, both[3], wk, sums[1])
+    B.norm_rope_apply(rope, none, none, wq, k, alone[1], wk)
+    B.norm_rope_apply(rope, q, alone[0], wq)
+    sums[0] = 7.0
+    B.norm_rope_grad(rope, none, none, none, ws, wq, sums[0], k, ku, alone[3], wk)
+    assert (sums[0] == 0).all()
+    B.norm_rope_grad(rope, q, qu, alone[2], ws, wq)
+    assert all(torch.equal(a, b) for a, b in zip(both, alone))
+
+
+def test_a_threads_first_call_may_be_a_captured_one():
+    """What the library asks the device about once per thread is asked in a capture here; two graphs share a workspace."""
+    g = gen(10)
+    q, up = tensor(g, 2, 6, 33, BF16, True), tensor(g, 2, 6, 33, BF16, True)
+    w, ws = weight(g, BF16), torch.empty(B.norm_rope_workspace_bytes(2, 33, 6), dtype=torch.uint8, device="cuda")
+    make = lambda: [torch.empty_like(q), torch.empty_like(q), torch.empty(D, device="cuda")]  # noqa: E731
+    want, got, graphs, failed = make(), [make(), make()], [torch.cuda.CUDAGraph() for _ in range(2)], []
+
+    def both(o):
+        B.norm_rope_apply(None, q, o[0], w)
+        B.norm_rope_grad(None, q, up, o[1], ws, w, o[2])
+
+    def capture():
+        try:
+            for o, graph in zip(got, graphs):
+                with torch.cuda.graph(graph):
+                    both(o)
+        except BaseException as e:   # noqa: BLE001
+            failed.append(e)
+    t = threading.Thread(target=capture)
+    t.start()
+    t.join()
+    assert not failed
+    for graph in graphs:
+        ws.fill_(0xff)
+        graph.replay()
+    both(want)
+    assert all(torch.equal(a, b) for o in got for a, b in zip(o, want))
