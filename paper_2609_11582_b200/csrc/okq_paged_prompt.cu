@@ -14,6 +14,9 @@
 // down, too, to 6 above the maximum of a step that lies 20 below it or more (14: three times as many multiplications where scores spread
 // by 3, 306 us and not 284): sums in fp32 have room for that, numerators in fp16 have not.  So the largest numerator of a step is 2^-6 or
 // more; 11 bits down to 2^-14, below that rounded to 2^-24.
+// With a window and for a tree a numerator is two fp16 numbers, the rounded one and what is left, each multiplied with the same values: 22
+// bits.  (The causal call has one: its results are what they were.)  The products are not what it costs: without the second ones 2 %; the
+// numbers are, 128 instructions of a softmax warp's step: 2048 queries x 28 heads with a window of 1400 110 -> 123 us.
 //
 // A block of threads has 256 rows, in two streams A and B of 128, and walks the tokens in steps of 64: a loader warp (32-token blocks
 // by page, two tiles of 128 tokens ahead), four warps that turn codes into fp16 (0x6400 | (code + 128) is 1024 + 128 + code; the rest is
@@ -49,7 +52,8 @@ constexpr int SIDE = PT * D;                    // bytes of a tile's keys or val
 constexpr int Q_HALF = M * 128, KV_HALF = PH * 128;   // 64 channels in fp16, of a stream's queries and of a step's keys or values
 constexpr int W_CONV = 8, W_MMA = 12, W_LOAD = 14;   // (an MMA warp to each stream)
 constexpr int NT = 15 * 32;
-constexpr uint32_t S_COL = 0, O_COL = 256;      // + 128 per stream, + 64 per place for scores; numerators lie on its first half
+constexpr uint32_t S_COL = 0, O_COL = 256;      // + 128 per stream, + 64 per place for scores; numerators lie on its first half,
+constexpr uint32_t REST = 32;                   // of a window and a tree what their rounding left on the second
 constexpr size_t SLOT = (size_t)R * (D + 2);
 constexpr float P_SHIFT = 14.f, LEAD = 6.f, DROP = 20.f;
 // The reference stays above 2^-FALL of the row's largest numerator: with 127 * 2^14 and 2^20 tokens O stays below 2^126.
@@ -273,7 +277,6 @@ struct Bits {
   __device__ __forceinline__ bool sees(int col) const { return half[col >> 5] >> (col & 31) & 1u; }
   __device__ __forceinline__ bool none_of(int block) const { return half[block] == 0u; }
   __device__ __forceinline__ bool all() const { return (half[0] & half[1]) == 0xffffffffu; }
-  __device__ __forceinline__ bool none() const { return (half[0] | half[1]) == 0u; }
 };
 
 // Of the step whose first token is t0.  `own`: the row's token; of a tree: the first node's.
@@ -335,8 +338,9 @@ __device__ __forceinline__ float row_max(float (&x)[2][32], const Info& info, in
 // EDGE also rounds a score once before the reference is taken off, as the maximum is: the difference is exact then, where scores are so
 // large that an unrounded one could lie far above it (not by packed pairs: their product and sum were contracted to one rounding).  Blocks
 // without a value count in the normaliser alone.
+// Of a window and a tree the numerators stay in x, for store_numerators.
 template <bool EDGE, class Seen>
-__device__ __forceinline__ float numerators(const float (&x)[2][32], uint32_t s_at, const Info& info, int b0, float back, float ref, const Seen& seen, float l) {
+__device__ __forceinline__ float numerators(float (&x)[2][32], uint32_t s_at, const Info& info, int b0, float back, float ref, const Seen& seen, float l) {
 #pragma unroll
   for (int b = 0; b < 2; b++) {
     const bool none = EDGE && (info.lost >> (4 + b0 + b) & 1);
@@ -360,15 +364,41 @@ __device__ __forceinline__ float numerators(const float (&x)[2][32], uint32_t s_
         if (!seen.sees(32 * b + 2 * e + 1)) p1 = 0.f;
       }
       sum[e & 1] = add2(sum[e & 1], f2(p0, p1));
-      const __half2 h = __floats2half2_rn(p0, p1);
-      u[e] = none ? 0u : *reinterpret_cast<const uint32_t*>(&h);
+      if (Seen::all_ways) {
+        const __half2 h = __floats2half2_rn(p0, p1);
+        u[e] = none ? 0u : *reinterpret_cast<const uint32_t*>(&h);
+      } else {
+        x[b][2 * e] = none ? 0.f : p0;
+        x[b][2 * e + 1] = none ? 0.f : p1;
+      }
     }
     const float2 total = un2(add2(sum[0], sum[1]));
     l = fmaf(total.x + total.y, info.iw[b0 + b], l);
     if (EDGE && (info.lost >> (b0 + b) & 1) && !seen.none_of(b)) l = NAN;
-    tmem_st16(s_at + 16u * b, u);
+    if (Seen::all_ways) tmem_st16(s_at + 16u * b, u);
   }
   return l;
+}
+// Numerators as two fp16 numbers, the rounded one and what the rounding left (exact in fp32; a multiply-add that takes fp16 numbers as they
+// are: with the upper bits cut out and taken off, 2048 queries with a window of 1400 128 us and not 123).
+__device__ __forceinline__ void store_numerators(const float (&x)[2][32], uint32_t s_at) {
+#pragma unroll
+  for (int b = 0; b < 2; b++) {
+    uint32_t u[16], rest[16];
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+      const float p0 = x[b][2 * e], p1 = x[b][2 * e + 1];
+      const __half2 h = __floats2half2_rn(p0, p1);
+      u[e] = *reinterpret_cast<const uint32_t*>(&h);
+      float r0, r1;   // p - h
+      asm("{\n\t.reg .b16 a, b, minus;\n\tmov.b32 {a, b}, %2;\n\tmov.b16 minus, 0xbc00;\n\tfma.rn.f32.f16 %0, a, minus, %3;\n\tfma.rn.f32.f16 %1, b, minus, %4;\n\t}\n"
+          : "=f"(r0), "=f"(r1) : "r"(u[e]), "f"(p0), "f"(p1));
+      const __half2 g = __floats2half2_rn(r0, r1);
+      rest[e] = *reinterpret_cast<const uint32_t*>(&g);
+    }
+    tmem_st16(s_at + 16u * b, u);
+    tmem_st16(s_at + REST + 16u * b, rest);
+  }
 }
 
 // NARROW: all items are dual, and the code for the others is left out.
@@ -535,8 +565,8 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
           after_sync();
           const uint64_t bd = make_desc_mn(smem_u32(sm.v[s][0]));
 #pragma unroll
-          for (int k = 0; k < 4; k++)   // 16 tokens further
-            mma_ts(o_at, s_at + 64u * place + 8u * k, bd + (uint64_t)(k * 2048 >> 4), id_o, y > 0 || k != 0);
+          for (int k = 0; k < (SIGHT == CAUSAL ? 4 : 8); k++)   // 16 tokens further; then what the rounding left
+            mma_ts(o_at, s_at + 64u * place + 8u * k, bd + (uint64_t)((k & 3) * 2048 >> 4), id_o, y > 0 || k != 0);
           commit(&sm.o_full[t]);
           commit(&sm.v_free[s]);
           if (dual) commit(&sm.v_free[s]);
@@ -682,6 +712,7 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
           if (!dual) take_turn(2 + 4 * t + quarter);
           l = edge || wide ? numerators<true>(x, p_at, info, 2 * half, back, ref, sight, l) : numerators<false>(x, p_at, info, 2 * half, back, ref, sight, l);
           if (!dual) pass_turn(2 + 4 * (t ^ 1) + quarter);
+          if (SIGHT != CAUSAL) store_numerators(x, p_at);
           tmem_wait_st();
           before_sync();
           __syncwarp();
