@@ -157,8 +157,8 @@ okq_status okq_paged_read(const okq_paged* cache, int32_t layer, int32_t layer_c
  * Numbers.  Scores, maxima, sums and normalisers have 32 bits.  With few rows (queries x group) to a head, queries are in fixed point, 2^-24 of
  * their row's largest channel, and numerators (weight x value scale) too, 2^-30 of the largest among the 128 tokens of a tile.  With many,
  * queries are fp16 numbers after a power of two, and numerators fp16: 11 bits (two such numbers, 22 bits, with a window and for a tree), and
- * not less than 2^-18 of the largest among 64 tokens; those 2^-68 below the row's largest, and weights 2^-100 below a token's without value,
- * may be lost, and values below 2e-32 count as zeros.
+ * not less than 2^-18 of the largest among 64 tokens; those 2^-68 below the row's largest, and what adds less than 2e-32 to an output, may be
+ * lost.
  * Query rows without a magnitude above 1e-30 count as zeros.
  * A sequence with a page missing below its length gives NaN and the status OKQ_ERR_INVALID_ARG.  OKQ_ERR_UNSUPPORTED (and a workspace
  * of 0 bytes) where the work, were all sequences as long as their rows of the table, is 2^31 pieces of 128 tokens and 8 or 256 rows

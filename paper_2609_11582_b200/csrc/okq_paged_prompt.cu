@@ -835,7 +835,15 @@ __global__ void __launch_bounds__(NT, 1) k_paged_prompt(const __grid_constant__ 
   if (warp == 0 && !sm.tmem_busy) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
 }
 
-// Parts put together, in order.  A part has its sums channel by channel, R rows each, as the lanes that hold rows write and read whole lines of
+__device__ __forceinline__ void late(float& top, float& l, float (&x)[8]) {
+  top += LATE_BITS;
+  l *= LATE;
+#pragma unroll
+  for (int z = 0; z < 8; z++) x[z] *= LATE;
+}
+// Parts put together, in order.  A part's reference may lie 2^76 below its largest numerator, and its sums above as much: factors go down to
+// 2^-226, in two steps where one would leave fp32's normal numbers (calls with 9 to 37 parts to a row 0.2 to 1.1 us longer for it; a look
+// at all parts before the one at each was no shorter).  A part has its sums channel by channel, R rows each, as the lanes that hold rows write and read whole lines of
 // them (row by row the stores took 8000 cycles of a piece's 90000, and this kernel 23 us of 135 for 2048 queries x 28 heads with a window).
 // A warp has 32 rows and eight channels, WPR warps have every WPR-th part each; unit u of a block's 16 / WPR is rows u / 16, channels u % 16.
 // FLIGHT parts are loaded at once: two, so that two blocks fit an SM, or seven where there are no more blocks than SMs.
@@ -871,7 +879,9 @@ __global__ void __launch_bounds__(MERGE_NT, FLIGHT > 2 ? 1 : 2) k_prompt_merge(c
       }
 #pragma unroll
       for (int e = 0; e < 7; e++) mn = fmaxf(mn, tk[e]);
-      const float ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(top - ref);
+      const float ref = mn == -INFINITY ? 0.f : mn;
+      if (falls(top, ref)) late(top, l, acc);
+      const float f0 = ex2(top - ref);
       l *= f0;
 #pragma unroll
       for (int z = 0; z < 8; z++) acc[z] *= f0;
@@ -888,6 +898,7 @@ __global__ void __launch_bounds__(MERGE_NT, FLIGHT > 2 ? 1 : 2) k_prompt_merge(c
         }
 #pragma unroll
         for (int e = e0; e < min(7, e0 + FLIGHT); e++) {
+          if (falls(tk[e], ref)) late(tk[e], lk[e], x[e - e0]);
           const float f = ex2(tk[e] - ref);   // (0 where there is none)
           l = fmaf(lk[e], f, l);
 #pragma unroll
@@ -905,17 +916,23 @@ __global__ void __launch_bounds__(MERGE_NT, FLIGHT > 2 ? 1 : 2) k_prompt_merge(c
     float mn = top;
 #pragma unroll
     for (int i = 1; i < WPR; i++) mn = fmaxf(mn, stat[warp + i][lane].x);
-    const float ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(top - ref);
+    const float ref = mn == -INFINITY ? 0.f : mn;
+    if (falls(top, ref)) late(top, l, acc);
+    const float f0 = ex2(top - ref);
     l *= f0;
 #pragma unroll
     for (int z = 0; z < 8; z++) acc[z] *= f0;
 #pragma unroll
     for (int i = 1; i < WPR; i++) {
-      const float2 y = stat[warp + i][lane];
+      float2 y = stat[warp + i][lane];
+      float x[8];
+#pragma unroll
+      for (int z = 0; z < 8; z++) x[z] = sums[warp + i][z][lane];
+      if (falls(y.x, ref)) late(y.x, y.y, x);
       const float f = ex2(y.x - ref);
       l = fmaf(y.y, f, l);
 #pragma unroll
-      for (int z = 0; z < 8; z++) acc[z] = fmaf(sums[warp + i][z][lane], f, acc[z]);
+      for (int z = 0; z < 8; z++) acc[z] = fmaf(x[z], f, acc[z]);
     }
   }
   if (!there) return;

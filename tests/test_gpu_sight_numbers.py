@@ -8,6 +8,8 @@ import torch
 from oracle import okq_sight_oracle as S
 from paper_2609_11582_b200 import binding as B
 from tests.test_gpu_paged import D, F16, gen, randn, random_cache
+from tests import test_gpu_sight as sight
+from tests.test_gpu_paged_numbers import PROMPT, Store, kernel_bound, lift, steered
 from tests.test_gpu_sight import held, scratch, to_words
 
 pytestmark = pytest.mark.gpu
@@ -54,3 +56,32 @@ def test_numerators_of_many_rows_keep_their_bits(n, G, spread):
             limit = err + 2.0 ** -11 * (ref.abs() + err) + 2.0 ** -25
             got = out[0, b].double().unflatten(0, (-1, G)).flatten(1, 2)
             assert ((got - ref).abs() <= limit).all(), (b, ((got - ref).abs() / limit).max().item())
+
+
+@pytest.mark.parametrize("shape", PROMPT, ids=str)
+@pytest.mark.parametrize("main", [35.0, 45.0])
+def test_weights_behind_tokens_without_value(shape, main):
+    """A token without value that takes all of the weight, tokens e^(main - 95) of it, and others far below these: what the second ones bring
+    is the output, whatever reference the parts of a row end with.  The kernel's bound with all tokens of that size."""
+    n, batch, H, Hq, T, wide = shape
+    q, k, v = steered(*shape, seed=4)
+    k[..., 10::256, 0] = lift(main)
+    v[..., 600:1000, :] = 0
+    k[..., 700, 0] = lift(95.0)
+    store, rng = Store(k, v, Hq, wide, seed=4), random.Random(n)
+    assert store.attend(q) == B.PLAN_PROMPT
+    c, q = store.c, q.cuda()
+    sets = [[rng.getrandbits(64 * ((n + 63) // 64)) for _ in range(n)] for _ in range(batch)]
+    for out, mask in both_calls(c, q, T - 300, 800, sets):
+        for b in range(batch):
+            w, x, ref, amax, top = reference(c, q, b, mask(b))
+            got = out[0, b].double().unflatten(0, (-1, Hq // H)).flatten(1, 2)
+            limit = kernel_bound(w, x, ref, amax, top, q.dtype, B.PLAN_PROMPT)
+            assert (ref.abs().amax(-1) > 100 * limit.amin(-1)).all()            # (it says something)
+            assert ((got - ref).abs() <= limit).all(), (b, ((got - ref).abs() / limit).max().item())
+    assert c.device_status() == 0
+
+
+@pytest.mark.parametrize("seed", [65, 100])
+def test_numbers_behind_masks_of_other_seeds(seed):
+    sight.test_numbers_behind_masks(seed)
