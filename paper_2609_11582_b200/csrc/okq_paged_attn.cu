@@ -101,8 +101,10 @@ static okq_status attention(const okq_paged* cache, int32_t layer, int32_t layer
   if ((st = make_rope(rope, r)) != OKQ_OK) return st;
   if (n_new == 0) return OKQ_OK;
   Plan p;
-  if (!make_plan(cache, layer_count, n_new, sight.window, sight.sinks, p)) return OKQ_ERR_UNSUPPORTED;
-  if (!workspace || workspace_bytes < okq_paged_workspace_bytes(cache, layer_count, n_new)) return OKQ_ERR_WORKSPACE;
+  // (with a window there may be a plan for rows that no scratch is known for)
+  const size_t need = okq_paged_workspace_bytes(cache, layer_count, n_new);
+  if (need == 0 || !make_plan(cache, layer_count, n_new, sight.window, sight.sinks, p)) return OKQ_ERR_UNSUPPORTED;
+  if (!workspace || workspace_bytes < need) return OKQ_ERR_WORKSPACE;
   AttnArgs a{paged_view(cache), {q, {qs[0], qs[1], qs[2], qs[3]}}, {out, {os[0], os[1], os[2], os[3]}}, q_len, r, layer, layer_count, n_new,
              sm_scale * 1.44269504088896340736f, limit, withhold, static_cast<Head*>(workspace),
              reinterpret_cast<float*>(static_cast<char*>(workspace) + p.heads), sight.window, sight.sinks,
@@ -155,7 +157,8 @@ okq_status okq_debug_paged_timeout(const okq_paged* cache, int32_t layer, int32_
 
 static int32_t plan_of(const okq_paged* cache, int32_t layer_count, int32_t n_new, const AttnSight& sight) {
   okq::Plan p;
-  if (layer_count <= 0 || layer_count > cache->n_layers || n_new <= 0 || !okq::make_plan(cache, layer_count, n_new, sight.window, sight.sinks, p)) return 0;
+  if (layer_count <= 0 || layer_count > cache->n_layers || n_new <= 0 || okq_paged_workspace_bytes(cache, layer_count, n_new) == 0 ||
+      !okq::make_plan(cache, layer_count, n_new, sight.window, sight.sinks, p)) return 0;
   return p.decode ? (p.cluster ? p.cluster : OKQ_PLAN_LINE) : OKQ_PLAN_PROMPT;
 }
 
