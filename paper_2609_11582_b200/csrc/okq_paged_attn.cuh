@@ -391,13 +391,33 @@ constexpr int MERGE_NT = 512;
 
 // Block (x, y): row y of the item of head x, if it is in parts, each warp has every sixteenth part, a lane four channels.  Bound by latency:
 // a few megabytes of parts at most; all of a part is loaded at once, seven parts in flight.  (Of the decode kernel's parts.)
+// Parts far below the maximum are looked for once and added by a loop of their own: with a branch at each part in the common one, 64
+// sequences x 8 heads of 1500 tokens took 58.4 us and not 57.2.
+struct MergeSum {
+  float top, l;
+  float4 x;
+  __device__ __forceinline__ void times(float f) {
+    l *= f;
+    x.x *= f; x.y *= f; x.z *= f; x.w *= f;
+  }
+  __device__ __forceinline__ void late(float ref) {
+    if (!falls(top, ref)) return;
+    top += LATE_BITS;
+    times(LATE);
+  }
+  __device__ __forceinline__ void add(const MergeSum& y, float ref) {
+    const float f = ex2(y.top - ref);
+    l = fmaf(y.l, f, l);
+    x.x = fmaf(y.x.x, f, x.x); x.y = fmaf(y.x.y, f, x.y); x.z = fmaf(y.x.z, f, x.z); x.w = fmaf(y.x.w, f, x.w);
+  }
+};
 template <class T, int ROWS>
 __global__ void __launch_bounds__(MERGE_NT, 2) k_paged_merge(const AttnArgs a) {
-  constexpr int WARPS = MERGE_NT / 32, WPR = WARPS;
+  constexpr int WARPS = MERGE_NT / 32;
   __shared__ float4 sums[WARPS][32];
   __shared__ float2 stat[WARPS];
   depend_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = blockIdx.y * (WARPS / WPR) + warp / WPR, first = warp % WPR;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = blockIdx.y;
   const int4 h0 = __ldcg(reinterpret_cast<const int4*>(&a.heads[blockIdx.x]));
   const Head hd{h0.x, h0.y, h0.z, h0.w, __ldcg(&a.heads[blockIdx.x].rt), {}};
   if (hd.more == 0) return;
@@ -408,68 +428,64 @@ __global__ void __launch_bounds__(MERGE_NT, 2) k_paged_merge(const AttnArgs a) {
   int len, m;
   const int li = w.layer_of(hd.pair), b = hd.pair - li * a.c.batch;
   w.lens(li, b, len, m);
-  const bool there = row < m * w.group;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  float top = -INFINITY, l = 0.f;
-  if (there) {
-    for (int k0 = first; k0 < n; k0 += 7 * WPR) {
-      float4 x[7];
-      float tk[7], lk[7];
+  if (row >= m * w.group) return;
+  MergeSum acc{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+  // to the maximum `mn` of acc and of what is added next
+  auto raise = [&](float mn, float ref) {
+    acc.late(ref);
+    acc.times(ex2(acc.top - ref));
+    acc.top = mn;
+  };
+  for (int k0 = warp; k0 < n; k0 += 7 * WARPS) {
+    MergeSum y[7];
 #pragma unroll
-      for (int e = 0; e < 7; e++) {
-        const int k = k0 + e * WPR;
-        tk[e] = -INFINITY;
-        if (k >= n) continue;
-        const float* s = slot(k);
-        x[e] = __ldcg(reinterpret_cast<const float4*>(s + (size_t)r * D) + lane);
-        tk[e] = __ldcg(s + ROWS * D + r);
-        lk[e] = __ldcg(s + ROWS * D + ROWS + r);
-      }
-      float mn = top;
-#pragma unroll
-      for (int e = 0; e < 7; e++) mn = fmaxf(mn, tk[e]);
-      const float ref = mn == -INFINITY ? 0.f : mn;
-      if (falls(top, ref)) { top += LATE_BITS; l *= LATE; acc.x *= LATE; acc.y *= LATE; acc.z *= LATE; acc.w *= LATE; }
-      const float f0 = ex2(top - ref);
-      l *= f0;
-      acc.x *= f0; acc.y *= f0; acc.z *= f0; acc.w *= f0;
-      top = mn;
-#pragma unroll
-      for (int e = 0; e < 7; e++) {
-        if (k0 + e * WPR >= n) continue;
-        if (falls(tk[e], ref)) { tk[e] += LATE_BITS; lk[e] *= LATE; x[e].x *= LATE; x[e].y *= LATE; x[e].z *= LATE; x[e].w *= LATE; }   // (the same in the whole warp)
-        const float f = ex2(tk[e] - ref);
-        l = fmaf(lk[e], f, l);
-        acc.x = fmaf(x[e].x, f, acc.x); acc.y = fmaf(x[e].y, f, acc.y); acc.z = fmaf(x[e].z, f, acc.z); acc.w = fmaf(x[e].w, f, acc.w);
-      }
+    for (int e = 0; e < 7; e++) {
+      const int k = k0 + e * WARPS;
+      y[e].top = -INFINITY;
+      if (k >= n) continue;
+      const float* s = slot(k);
+      y[e].x = __ldcg(reinterpret_cast<const float4*>(s + (size_t)r * D) + lane);
+      y[e].top = __ldcg(s + ROWS * D + r);
+      y[e].l = __ldcg(s + ROWS * D + ROWS + r);
     }
-  }
-  if (WPR > 1) {
-    sums[warp][lane] = acc;
-    if (lane == 0) stat[warp] = make_float2(top, l);
-    __syncthreads();
-    if (first != 0) return;
-    float mn = top;
+    float mn = acc.top;
 #pragma unroll
-    for (int i = 1; i < WPR; i++) mn = fmaxf(mn, stat[warp + i].x);
+    for (int e = 0; e < 7; e++) mn = fmaxf(mn, y[e].top);
     const float ref = mn == -INFINITY ? 0.f : mn;
-    if (falls(top, ref)) { top += LATE_BITS; l *= LATE; acc.x *= LATE; acc.y *= LATE; acc.z *= LATE; acc.w *= LATE; }
-    const float f0 = ex2(top - ref);
-    l *= f0;
-    acc.x *= f0; acc.y *= f0; acc.z *= f0; acc.w *= f0;
+    if (n > WARPS) {   // (else the warp has one part at most, and that is the maximum)
 #pragma unroll
-    for (int i = 1; i < WPR; i++) {
-      float2 st = stat[warp + i];
-      float4 x = sums[warp + i][lane];
-      if (falls(st.x, ref)) { st.x += LATE_BITS; st.y *= LATE; x.x *= LATE; x.y *= LATE; x.z *= LATE; x.w *= LATE; }
-      const float f = ex2(st.x - ref);
-      l = fmaf(st.y, f, l);
-      acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y); acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);
+      for (int e = 0; e < 7; e++) y[e].late(ref);
     }
+    raise(mn, ref);
+#pragma unroll
+    for (int e = 0; e < 7; e++)
+      if (k0 + e * WARPS < n) acc.add(y[e], ref);
   }
-  if (!there) return;
-  T o[4] = {from_f<T>(l == 0.f ? 0.f : acc.x / l), from_f<T>(l == 0.f ? 0.f : acc.y / l), from_f<T>(l == 0.f ? 0.f : acc.z / l),
-            from_f<T>(l == 0.f ? 0.f : acc.w / l)};
+  sums[warp][lane] = acc.x;
+  if (lane == 0) stat[warp] = make_float2(acc.top, acc.l);
+  __syncthreads();
+  if (warp != 0) return;
+  float mn = acc.top;
+#pragma unroll
+  for (int i = 1; i < WARPS; i++) mn = fmaxf(mn, stat[i].x);
+  const float ref = mn == -INFINITY ? 0.f : mn;
+  const bool far = __any_sync(0xffffffffu, falls(stat[lane % WARPS].x, ref));
+  raise(mn, ref);
+  auto part = [&](int i) { return MergeSum{stat[i].x, stat[i].y, sums[i][lane]}; };
+  if (far) {
+#pragma unroll 1
+    for (int i = 1; i < WARPS; i++) {
+      MergeSum y = part(i);
+      y.late(ref);
+      acc.add(y, ref);
+    }
+  } else {
+#pragma unroll
+    for (int i = 1; i < WARPS; i++) acc.add(part(i), ref);
+  }
+  const float l = acc.l;
+  T o[4] = {from_f<T>(l == 0.f ? 0.f : acc.x.x / l), from_f<T>(l == 0.f ? 0.f : acc.x.y / l), from_f<T>(l == 0.f ? 0.f : acc.x.z / l),
+            from_f<T>(l == 0.f ? 0.f : acc.x.w / l)};
   *reinterpret_cast<uint2*>(out_row<T>(a, li, b, hd.h, row) + 4 * lane) = *reinterpret_cast<const uint2*>(o);
 }
 // okq_paged_decode.cu: DECODE_ROWS rows to an item, DECODE_PIPES pipelines per block.  An item's own costs (queries, the first tile's
