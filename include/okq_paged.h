@@ -207,6 +207,11 @@ okq_status okq_debug_paged_timeout(const okq_paged* cache, int32_t layer, int32_
                                    int32_t n_new, void* workspace, size_t workspace_bytes, void* out, const int64_t out_strides[4],
                                    int64_t limit_clocks, void* stream);
 
+/* The same for okq_paged_attention_window (window > 0, seen null) and okq_paged_attention_tree (window 0, seen as there). */
+okq_status okq_debug_paged_timeout_sight(const okq_paged* cache, int32_t layer, int32_t layer_count, const void* q, const int64_t q_strides[4],
+                                         int32_t n_new, int32_t window, int32_t sinks, const uint64_t* seen, void* workspace,
+                                         size_t workspace_bytes, void* out, const int64_t out_strides[4], int64_t limit_clocks, void* stream);
+
 /* How okq_paged_attention would take a call; for tests of the rules.  Positive: the decode kernel with a cluster of so many blocks per
  * (layer, sequence, KV head); OKQ_PLAN_LINE: the decode kernel over even ranges, and the merge; OKQ_PLAN_PROMPT: the prompt kernel; 0:
  * refused.  Only sizes are looked at. */

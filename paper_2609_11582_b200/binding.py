@@ -175,6 +175,8 @@ def lib():
         L.okq_paged_attention.argtypes = [paged, i32, i32, ptr, ptr, i32, ptr, ptr, C.c_float, ptr, C.c_size_t, ptr, ptr, ptr]
         L.okq_debug_paged_timeout.restype = C.c_int
         L.okq_debug_paged_timeout.argtypes = [paged, i32, i32, ptr, ptr, i32, ptr, C.c_size_t, ptr, ptr, C.c_int64, ptr]
+        L.okq_debug_paged_timeout_sight.restype = C.c_int
+        L.okq_debug_paged_timeout_sight.argtypes = [paged, i32, i32, ptr, ptr, i32, i32, i32, ptr, ptr, C.c_size_t, ptr, ptr, C.c_int64, ptr]
         L.okq_debug_paged_plan.restype = i32
         L.okq_debug_paged_plan.argtypes = [paged, i32, i32]
         L.okq_paged_attention_window.restype = C.c_int
@@ -214,7 +216,7 @@ def exported_symbols():
             "okq_norm_rope_apply", "okq_norm_rope_grad", "okq_norm_rope_workspace_bytes", "okq_paged_append", "okq_paged_read",
             "okq_paged_attention", "okq_debug_paged_timeout", "okq_debug_paged_plan", "okq_pages_reserve", "okq_pages_fork", "okq_pages_release", "okq_pages_copy",
             "okq_pages_compact", "okq_pages_slide", "okq_paged_attention_window", "okq_paged_attention_tree", "okq_tree_ancestors",
-            "okq_debug_paged_plan_window"]
+            "okq_debug_paged_plan_window", "okq_debug_paged_timeout_sight"]
 
 
 def _ptr(t) -> int:
@@ -796,6 +798,18 @@ def debug_paged_timeout(cache: PagedCache, layer: int, layer_count: int, q, work
 
 
 PLAN_LINE, PLAN_PROMPT = -1, -2
+
+
+def debug_paged_timeout_sight(cache: PagedCache, layer: int, layer_count: int, q, workspace, out, window: int = 0, sinks: int = 0, seen=None,
+                              limit_clocks: int = 20_000_000, stream=None):
+    """okq_debug_paged_timeout_sight: the same for paged_attention_window or, with `seen`, paged_attention_tree (testing aid)."""
+    _here(cache.codes, q, workspace, out, seen)
+    n = q.shape[3]
+    _check(lib().okq_debug_paged_timeout_sight(cache.ref, layer, layer_count, q.data_ptr(), _rows(cache, q, layer_count, cache.n_q_heads, n), n,
+                                               window, sinks, 0 if seen is None else _seen(cache, seen, n), _ptr(workspace),
+                                               0 if workspace is None else workspace.nbytes, out.data_ptr(),
+                                               _rows(cache, out, layer_count, cache.n_q_heads, n), limit_clocks, _stream(stream)),
+           "okq_debug_paged_timeout_sight")
 
 
 def paged_plan(cache: PagedCache, layer_count: int, n_new: int = 1) -> int:

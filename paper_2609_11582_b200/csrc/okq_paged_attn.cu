@@ -155,6 +155,15 @@ okq_status okq_debug_paged_timeout(const okq_paged* cache, int32_t layer, int32_
   return attention(cache, layer, layer_count, q, qs, n_new, nullptr, nullptr, 0.08838834764831845f, workspace, workspace_bytes, out, os, {}, limit_clocks, 1, stream);
 }
 
+okq_status okq_debug_paged_timeout_sight(const okq_paged* cache, int32_t layer, int32_t layer_count, const void* q, const int64_t qs[4], int32_t n_new,
+                                         int32_t window, int32_t sinks, const uint64_t* seen, void* workspace, size_t workspace_bytes, void* out,
+                                         const int64_t os[4], int64_t limit_clocks, void* stream) {
+  if (!cache || limit_clocks <= 0 || window < 0 || sinks < 0 || (window > 0) == (seen != nullptr)) return OKQ_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(seen) & 7) return OKQ_ERR_ALIGNMENT;
+  return attention(cache, layer, layer_count, q, qs, n_new, nullptr, nullptr, 0.08838834764831845f, workspace, workspace_bytes, out, os,
+                   seen ? AttnSight{0, 0, seen} : window_of(cache, window, sinks), limit_clocks, 1, stream);
+}
+
 static int32_t plan_of(const okq_paged* cache, int32_t layer_count, int32_t n_new, const AttnSight& sight) {
   okq::Plan p;
   if (layer_count <= 0 || layer_count > cache->n_layers || n_new <= 0 || okq_paged_workspace_bytes(cache, layer_count, n_new) == 0 ||

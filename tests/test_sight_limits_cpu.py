@@ -3,7 +3,7 @@ import pytest
 
 from paper_2609_11582_b200 import binding as B
 from paper_2609_11582_b200 import build as build_mod
-from tests.test_paged_cpu import cache
+from tests.test_paged_cpu import P16, S4, cache
 from tests.test_sight_cpu import tree, window
 
 LONG = dict(n_layers=64, batch=512, n_kv_heads=8, n_q_heads=64, max_pages=32768, n_pages=4096)
@@ -31,3 +31,11 @@ def test_rows_beyond_what_scratch_is_known_for(L, n, sight):
     need = L.okq_paged_workspace_bytes(c, 1, n)
     assert need > 0 and L.okq_debug_paged_plan_window(c, 1, n, w, s) != 0
     assert window(L, c, count=1, n=n, window=w, sinks=s, ws_bytes=need - 1) == B.ERR_WORKSPACE
+
+
+def test_refusals_of_the_testing_aid(L):
+    c = cache()
+    go = lambda window=0, sinks=0, seen=0, limit=1000, c=c: L.okq_debug_paged_timeout_sight(c, 0, 1, P16, S4, 1, window, sinks, seen, P16, 1 << 30, P16, S4,  # noqa: E731
+                                                                                            limit, None)
+    assert go() == go(window=-1) == go(window=5, sinks=-1) == go(window=5, seen=P16) == go(window=5, limit=0) == go(window=5, c=None) == B.ERR_INVALID_ARG
+    assert go(seen=P16 + 4) == B.ERR_ALIGNMENT
