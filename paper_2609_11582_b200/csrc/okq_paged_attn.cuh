@@ -67,7 +67,7 @@ struct Span {
 };
 template <int ROWS, int EXTRA, int SIGHT = CAUSAL> struct Work {
   int pairs, n_kv, group;
-  uint32_t whole_at = 0;   // CAN_BE_WHOLE: place in shared memory of FindSmem's `whole`
+  uint32_t whole_at = 0;   // CAN_BE_WHOLE: place in shared memory of FindWhole's `whole`
   __device__ __forceinline__ bool whole() const {
     int x;
     asm volatile("ld.shared.s32 %0, [%1];\n" : "=r"(x) : "r"(whole_at) : "memory");
@@ -215,12 +215,15 @@ __device__ __forceinline__ void warp_row_tile(const Work<ROWS, EXTRA, SIGHT>& w,
 // consecutive pairs.
 constexpr float WHOLE_GAIN = 8.f;   // what a merge and its parts cost, in units
 template <int G> struct FindSmem {
-  int warp[16], items[16], most[16];   // of a warp's pairs: units, items, the largest item's units (the latter two: CAN_BE_WHOLE)
-  int whole;
+  int warp[16];   // units of a warp's pairs
   int place[G][6];
 };
-template <int ROWS, int EXTRA, int NT, int G, int SIGHT>
-__device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS, EXTRA, SIGHT>& w, int ranges, int v0, int step) {
+struct FindWhole : FindSmem<1> {     // CAN_BE_WHOLE
+  int items[16], most[16];   // of a warp's pairs: items, the largest item's units
+  int whole;
+};
+template <int ROWS, int EXTRA, int NT, int G, int SIGHT, class Smem>
+__device__ __forceinline__ Cuts find_places(Smem& sm, const Work<ROWS, EXTRA, SIGHT>& w, int ranges, int v0, int step) {
   static_assert(NT <= 512, "a place for each warp");
   const int tid = threadIdx.x, lane = tid & 31, wp = tid >> 5;
   const int chunk = (w.pairs + NT - 1) / NT, p0 = min(w.pairs, tid * chunk), p1 = min(w.pairs, p0 + chunk);
@@ -249,7 +252,7 @@ __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS, EX
     if (lane >= d) v += y;
   }
   if (lane == 31) sm.warp[wp] = v;
-  if (CAN_BE_WHOLE<ROWS, SIGHT>) {
+  if constexpr (CAN_BE_WHOLE<ROWS, SIGHT>) {
     int items = 0, most = 0;
     for (int p = p0; p < p1; p++) {
       if (chunk > 1) w.lens(p, len, m);
@@ -270,10 +273,11 @@ __device__ __forceinline__ Cuts find_places(FindSmem<G>& sm, const Work<ROWS, EX
     total += x;
   }
   const Cuts cuts(total, ranges);
-  if (CAN_BE_WHOLE<ROWS, SIGHT>) {
+  if constexpr (CAN_BE_WHOLE<ROWS, SIGHT>) {
     // Whole items, as many rounds of the largest as it takes, against even parts and their merge, in units (us, whole items and even parts,
     // windows of long sequences: 224 items of 6 tiles 67, 74; of 14 tiles 121, 119; 240 items of 7 tiles 74, 80; 180 of 19 tiles 141, 119;
-    // 240 ragged ones of up to 12 tiles 92, 74).
+    // 240 ragged ones of up to 12 tiles 92, 74).  It is an estimate, good for items that are alike: a range takes the items that begin in it, its
+    // share and up to one item more.
     int items = 0, most = 0;
 #pragma unroll
     for (int i = 0; i < NT / 32; i++) {

@@ -84,7 +84,7 @@ template <bool NARROW> struct PromptSmem {
   __align__(8) volatile int done[2][2];
   float peak[2 * M];                               // [stream][row] maximum of the numerators so far, LEAD below the highest reference
   signed char row_exp[2 * M];                      // of the item's rows
-  FindSmem<1> find;
+  FindWhole find;
   uint32_t tmem_slot;
   long long limit;
   volatile int abort;
