@@ -689,6 +689,7 @@ def norm_rope_grad(rope, q, q_up, q_grad, workspace=None, q_weight=None, q_weigh
     """The gradients of norm_rope_apply's inputs into q_grad and k_grad (which may be q_up and k_up, the gradients of its results) and, where
     q_weight_grad and k_weight_grad (float32 [128], overwritten) are given, those of its weights; q and k as they were before the norm."""
     _here(q, q_up, q_grad, workspace, q_weight, q_weight_grad, k, k_up, k_grad, k_weight, k_weight_grad, None if rope is None else rope.positions)
+    assert k is not None or (k_up is None and k_grad is None and k_weight_grad is None), "gradients of keys that were not given"
     batch, n, shape, k_shape, ref = _norm_sides(rope, q, k)
     st = (_lib or lib()).okq_norm_rope_grad(ref, eps, DTYPE_CODES[q.dtype], batch, n, _norm_tensor(q, q_up, q_grad, q_weight, q_weight_grad, shape),
                                             None if k is None else _norm_tensor(k, k_up, k_grad, k_weight, k_weight_grad, k_shape), _ptr(workspace),

@@ -88,3 +88,10 @@ def test_no_scale_and_queries_without_a_number(batch, n):
         else:
             assert torch.isnan(out[0, 0, 3, i]).all() and torch.isnan(out[0, 1, 4, i]).all() and torch.isfinite(out[0, 0, :3, i]).all()
     assert c.device_status() == 0
+
+
+def test_gradients_of_keys_that_are_not_there_are_refused():
+    q, sums = torch.ones(1, 2, 3, D, dtype=F16, device="cuda"), torch.zeros(D, device="cuda")
+    ws = torch.empty(B.norm_rope_workspace_bytes(1, 3, 2), dtype=torch.uint8, device="cuda")
+    with pytest.raises(AssertionError):
+        B.norm_rope_grad(None, q, q, torch.empty_like(q), ws, None, None, k_weight_grad=sums)
