@@ -31,7 +31,7 @@ extern "C" {
 
 #define OKQ_FP16 0
 #define OKQ_BF16 1
-#define OKQ_FP32 2 /* okq_rope_apply only */
+#define OKQ_FP32 2 /* okq_rope_apply and the normed heads only */
 
 typedef struct okq_paged {
   int32_t n_layers, batch, n_kv_heads, n_q_heads; /* GQA group n_q_heads / n_kv_heads: an integer <= 8; head_dim is 128 */
@@ -92,7 +92,8 @@ okq_status okq_rope_apply(const okq_rope* rope, int32_t dtype, int32_t batch, in
  * Norm of every head, then the rotation, in one pass: for a row x of 128 channels
  *     y = R (weight * x * r),  r = (mean(x^2) + eps)^(-1/2)
  * with R the rotation of okq_rope (none where `rope` is null); all of it in 32 bits, rounded to `dtype` once.  Rows whose squares have no
- * sum in 32 bits are taken care of; a row with an infinity or NaN has NaN in those channels.
+ * sum in 32 bits are taken care of.  A NaN makes its whole row NaN; an infinity its own channel, and the one that it is turned with, and zeros of
+ * the others.
  */
 typedef struct okq_norm_tensor {
   const void* in;       /* element (b, h, i, c) at in[b*in_strides[0] + h*in_strides[1] + i*in_strides[2] + c], the others likewise */
@@ -242,7 +243,8 @@ okq_status okq_pages_release(const okq_paged* cache, const int32_t* seqs, int32_
 /* Gives back the pages that okq_paged_attention_window with this window and these sinks will not see again from any token that is still to
  * come: of tokens [sinks, seq_len - window], seq_len that of the shortest layer, the whole pages leave each sequence's row, the entries
  * behind them move down, and the lengths of all layers shrink by their tokens (multiples of page_tokens).  Keys stay as they were rotated:
- * positions go on counting what was dropped.  To be called when the attention of the tokens appended so far is through in all layers.
+ * positions go on counting what was dropped.  To be called when the attention of the tokens appended so far is through in all layers, and none of
+ * them will be taken back: the tokens before them, come again, would see further back than these.
  * 1 <= window, 0 <= sinks.  dropped (device int32 [batch], may be null) receives the tokens that each sequence lost. */
 okq_status okq_pages_slide(const okq_paged* cache, int32_t window, int32_t sinks, int32_t* dropped, void* stream);
 

@@ -9,8 +9,10 @@
 // have a row, sixteen channels each, which hold both channels of each pair they turn; its sums take three exchanges.  A token's cosines and sines
 // are worked out once for all of its heads, and all blocks have equal parts of the line of tokens and heads; rows come by copies into
 // shared memory two steps ahead, each thread its own.
-// Times (copy rate of 6.55 TB/s: floor): 32767 tokens x 36 heads in bf16 113 us (92); 8191 in fp32 54 (46); gradients of 12285 tokens x 36 heads
-// in bf16 63 (52), of 8191 in fp32 90 (69); 8 tokens 4.5.  Measured and left: rows by loads into registers, one step ahead 131 (the gradients of
+// Times, ten calls in a graph (copy rate of 6.55 TB/s: floor): 32767 tokens x 36 heads in bf16 116 us (92); 8191 in fp32 56 (46); gradients
+// of 12285 tokens x 36 heads in bf16 65 (52), of 8191 in fp32 85 (69), 5 of each the sums of the weights; 8 tokens 4.3.  Few heads: 65536 tokens x 8
+// heads 50 to 54 (41), the gradients 78 to 82 (62): the copies begin anew with each side of a tile, its likely cause.  Measured and left, each beside the kernel of
+// its time: rows by loads into registers, one step ahead 131 (the gradients of
 // 12285 tokens), queries' and keys' rows on blocks of their own, each with its own cosines 96; copies five steps ahead 92, three 70;
 // five blocks to an SM forwards (spills) 119; a thread's heads as grid rows, cosines three times per token 154.
 #include "okq_device.cuh"
@@ -22,7 +24,7 @@ namespace okq {
 namespace {
 
 constexpr int NT = 128, TOKENS = NT / 8;
-// Blocks that run at once on an SM, by registers (122 and 128) and shared memory.
+// Blocks that run at once on an SM, by registers (124 and 128) and shared memory.
 constexpr int APPLY_PER_SM = 4;
 template <class T> constexpr int GRAD_PER_SM = sizeof(T) == 4 ? 3 : 4;
 constexpr int GRAD_BLOCKS = 1024;   // of the backward pass at most, and what the scratch is for
@@ -218,7 +220,7 @@ __device__ __forceinline__ float normalise(F2 (&x)[8], float eps, bool& scaled) 
     const float z = dot(x, x);
     if (scaled) s = z;
   }
-  float r;   // (of a normal number: eps is one, and where it is made smaller the rest is not below 2^-70; two units in the last place)
+  float r;   // (of a normal number: eps is one, and where it is made smaller the rest is not below 2^-77; two units in the last place)
   asm("rsqrt.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(fmaf(s, 1.f / D, scaled ? eps * SMALL * SMALL : eps)));
 #pragma unroll
   for (int e = 0; e < 8; e++) x[e] = mul2(x[e], f2(r, r));

@@ -15,8 +15,8 @@
 // by 3, 306 us and not 284): sums in fp32 have room for that, numerators in fp16 have not.  So the largest numerator of a step is 2^-6 or
 // more; 11 bits down to 2^-14, below that rounded to 2^-24.
 // With a window and for a tree a numerator is two fp16 numbers, the rounded one and what is left, each multiplied with the same values: 22
-// bits.  (The causal call has one: its results are what they were.)  The products are not what it costs: without the second ones 2 %; the
-// numbers are, 128 instructions of a softmax warp's step: 2048 queries x 28 heads with a window of 1400 110 -> 123 us.
+// bits.  (The causal call has one: its results are what they were.)  The second products cost 1 %; the second numbers, some 100 instructions
+// of a softmax warp's step, 11: 2048 queries x 28 heads with a window of 1400 110 -> 123 us.
 //
 // A block of threads has 256 rows, in two streams A and B of 128, and walks the tokens in steps of 64: a loader warp (32-token blocks
 // by page, two tiles of 128 tokens ahead), four warps that turn codes into fp16 (0x6400 | (code + 128) is 1024 + 128 + code; the rest is
@@ -27,18 +27,19 @@
 //
 // What a row sees of a step is one number where the kernel is causal, and 64 bits otherwise, worked out while the products are waited for.
 // Steps that some row does not see all of have -inf put in and go the same way as the others: of a window or a tree such steps are a large
-// part, and a copy of the loop for them took 4000 to 5000 cycles a step for its code's size, where this takes 2600 to 2900.  (The causal
+// part, and a copy of the loop for them took 4000 to 5000 cycles a step for its code's size, where this took 2600 to 2900.  (The causal
 // kernel keeps its copy, which rounds otherwise, for the step or two at the end.)
 //
 // At best bound by the exponentials (16 per cycle and SM: 2048 cycles for 256 x 128 scores) and the products (2048 cycles at fp16's
 // rate).  What it takes is about 4200 (2048 queries x 28 heads on 8192 tokens 260 us a call, 810 TFLOP/s of products): a softmax warp's own
 // chain of waits, tensor memory, maximum, exponentials and roundings, with two such warps on a scheduler and 128 registers to each (the
 // maximum beside the exponentials, by last step's reference: 390 us, spills).  A multiplication of O is another 1000 cycles in its step.
-// A window's items are short, and their ends show: of 85000 cycles of 256 rows with a window of 1400 (26 steps) the queries take 5000, the
-// first scores 2500, the last products and the output 7000; 2048 queries x 28 heads 109 us.  Queries are copied to their place as they are
+// A window's items are short, and their ends show: of 93000 cycles of 256 rows with a window of 1400 (26 steps) the queries take 5000, the
+// first scores 2500, the last products and the output 7000; 2048 queries x 28 heads 123 us.  (Cycles as counted with one number to a
+// numerator, here and below, and 300 more for a step.)  Queries are copied to their place as they are
 // while the item before ends (loaded there and then they took 11000 to 17000 cycles).
 // Few rows (a dual item) are bound by the conversion, a step in 1500 to 1700 cycles, a third of it waits and fences: 35 rows, 16 sequences x 4
-// heads of up to 12345 tokens 47 us a call (a converting warp to every other step, with half of those waits but a ring that is then too
+// heads of up to 12345 tokens 47 us a causal call (a converting warp to every other step, with half of those waits but a ring that is then too
 // short: 61).  Calls whose items are all dual have a kernel of their own (NARROW).
 #include "okq_paged_attn.cuh"
 
