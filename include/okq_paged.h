@@ -172,8 +172,8 @@ okq_status okq_paged_attention(const okq_paged* cache, int32_t layer, int32_t la
 /*
  * The same with a window: a query of token p sees token t <= p where p - t < window (at least 1: itself) or t < sinks.  Tokens are counted as
  * the cache holds them, so that okq_pages_slide changes nothing.  Pages that no query of the call sees are not read, and need not be there.
- * A window or sinks as long as a row of the table: okq_paged_attention, bit for bit.  OKQ_ERR_UNSUPPORTED where that gives it, however short
- * the window is.
+ * A window or sinks as long as a row of the table: okq_paged_attention, bit for bit (its numerators of 11 bits included).  OKQ_ERR_UNSUPPORTED
+ * where that gives it, however short the window is.
  */
 okq_status okq_paged_attention_window(const okq_paged* cache, int32_t layer, int32_t layer_count, const void* q, const int64_t q_strides[4],
                                       int32_t n_new, const int32_t* q_len, const okq_rope* rope, float sm_scale, int32_t window, int32_t sinks,
